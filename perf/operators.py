@@ -1,0 +1,589 @@
+"""The serving operators, case by case: prompt attention, block tables, the 8-bit cache's store and the attention
+that reads it.
+
+A model's prompt goes through causal attention (prompt_attention), its keys and values, whole or compacted, are
+given blocks of the cache (block_tables) and stored there in 8 bits (cache_store), and every token after that
+attends over the cached blocks (cache_attention).  A cell is one sequence's key/value head; cells keep different
+numbers of entries, so each has a row of the block table of its own.
+
+The plain forms are elementary torch operations in 32 bits; `own` makes the library's calls.  Lengths come from the
+case, values and the blocks' places from the seed.  Inputs follow the recipes of the library's workloads: standard
+normal rows, four key channels scaled by 8, per-head temperatures.
+"""
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+BF16, F32 = "bf16", "f32"
+E4M3_MAX = 448.0
+
+
+# ---------------------------------------------------------------------------
+# the cases
+# ---------------------------------------------------------------------------
+def listed():
+    return [
+        # a handful of short chat turns in one batch: the smallest prompt call, where latency counts
+        dict(name="prompt_short", kind="prompt", dtype=BF16, heads=32, kv_heads=8, d=128, seqs=8, lo=1, hi=48, mix=1,
+             prefix=0, causal=True, temps=False),
+        # a packed batch of prompts of all lengths, some of them later chunks of a longer prompt
+        dict(name="prompt_packed", kind="prompt", dtype=BF16, heads=32, kv_heads=8, d=128, seqs=16, lo=65, hi=4096,
+             mix=2, prefix=1777, causal=True, temps=True),
+        # one long document
+        dict(name="prompt_long", kind="prompt", dtype=BF16, heads=32, kv_heads=8, d=128, seqs=1, lo=16384, hi=16384,
+             mix=3, prefix=0, causal=True, temps=False),
+        # float32 rows of an encoder: every key visible, 80-wide heads, groups of three, sizes that no tile divides
+        dict(name="prompt_f32", kind="prompt", dtype=F32, heads=6, kv_heads=2, d=80, seqs=5, lo=33, hi=1999, mix=4,
+             prefix=0, causal=False, temps=False),
+        # one proposed token for every cell of 32 layers, 8 heads, 8 sequences, then taken back
+        dict(name="tables_step", kind="tables", cells=2048, block=64, add=1, lo=1, hi=4096, mix=5),
+        # 256 compacted cells get their blocks and slots, and give them back when the request ends
+        dict(name="tables_prompt", kind="tables", cells=256, block=64, add=0, lo=3000, hi=30000, mix=6),
+        # one token of 64 sequences, 8 heads, appended to part-filled blocks
+        dict(name="store_step", kind="store", dtype=BF16, cells=512, d=128, block=64, add=1, lo=0, hi=400, mix=7),
+        # the compacted keys and values of 256 cells, a tenth of 131,072 positions on average
+        dict(name="store_prompt", kind="store", dtype=BF16, cells=256, d=128, block=64, add=0, lo=3000, hi=30000,
+             mix=8),
+        # one sequence, 8 heads, a tenth of 4096 positions kept: the smallest decoding call
+        dict(name="decode_one", kind="decode", dtype=BF16, seqs=1, kv_heads=8, group=4, tokens=1, d=128, block=64,
+             lo=200, hi=800, mix=9, temps=False),
+        # 64 sequences, a tenth of 32,768 positions kept on average, as unevenly as a shared threshold keeps them
+        dict(name="decode_batch", kind="decode", dtype=BF16, seqs=64, kv_heads=8, group=4, tokens=1, d=128, block=64,
+             lo=800, hi=10000, mix=10, temps=True),
+        # 8 sequences, nothing evicted from 131,072 positions
+        dict(name="decode_long", kind="decode", dtype=BF16, seqs=8, kv_heads=8, group=4, tokens=1, d=128, block=128,
+             lo=131000, hi=131072, mix=11, temps=False),
+        # four drafted tokens to be verified at once, float32 rows, 80-wide heads, blocks of 16
+        dict(name="decode_draft", kind="decode", dtype=F32, seqs=12, kv_heads=5, group=3, tokens=4, d=80, block=16,
+             lo=4, hi=6000, mix=12, temps=True),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["prompt", "prompt", "prompt", "decode", "decode", "decode", "store", "tables"])
+    c = dict(kind=kind, mix=rng.randrange(1 << 20))
+    if kind == "prompt":
+        c["dtype"] = rng.choice([BF16, BF16, BF16, F32])
+        c["d"] = rng.choice([64, 80, 128, 128, 128])
+        c["kv_heads"] = rng.choice([1, 2, 8])
+        c["heads"] = c["kv_heads"] * rng.choice([1, 3, 4, 4, 8])
+        c["hi"] = _log(rng, 1, 12000 if c["dtype"] == BF16 else 2500)
+        c["lo"] = rng.randint(1, c["hi"])
+        c["prefix"] = rng.choice([0, 0, _log(rng, 1, 4000)])
+        c["causal"] = rng.random() < 0.8
+        # at most half the (padded) scores of the longest listed prompt, whose causal half is computed
+        room = 16 * 16384.0 ** 2 * (1.0 if c["dtype"] == BF16 else 1 / 32)
+        c["seqs"] = max(1, min(_log(rng, 1, 40), int(room / (c["heads"] * c["hi"] * (c["hi"] + c["prefix"])))))
+        c["temps"] = rng.random() < 0.5
+    elif kind == "decode":
+        c["dtype"] = rng.choice([BF16, BF16, BF16, F32])
+        c["d"] = rng.choice([64, 80, 128, 128, 128])
+        c["kv_heads"] = rng.choice([1, 4, 8, 8])
+        c["group"] = rng.choice([1, 3, 4, 4, 8])
+        c["tokens"] = rng.choice([1, 1, 1, _log(rng, 2, 8)])
+        c["block"] = rng.choice([16, 32, 64, 64, 128])
+        c["hi"] = _log(rng, 1, 120000)
+        c["lo"] = rng.randint(1, c["hi"])
+        c["seqs"] = max(1, min(_log(rng, 1, 128), int(8.0e6 / (c["hi"] * c["kv_heads"]))))
+        c["temps"] = rng.random() < 0.5
+    elif kind == "store":
+        c["dtype"] = rng.choice([BF16, BF16, F32])
+        c["d"] = rng.choice([64, 80, 128, 128, 128])
+        c["block"] = rng.choice([16, 32, 64, 64, 128])
+        c["add"] = rng.choice([0, 1, rng.randint(1, 200)])
+        c["lo"], c["hi"] = (0, _log(rng, 1, 600)) if c["add"] else (1, _log(rng, 2, 20000))
+        c["cells"] = max(1, min(_log(rng, 4, 1024), int(2.0e6 / (c["hi"] + c["add"]))))
+    else:
+        c["block"] = rng.choice([16, 32, 64, 64, 128])
+        c["add"] = rng.choice([0, 1, 1, rng.randint(2, 200)])
+        c["lo"] = 1
+        c["hi"] = _log(rng, 2, 20000)
+        c["cells"] = max(1, min(_log(rng, 4, 5000), int(4.0e6 / (c["hi"] + c["add"]))))
+    return c
+
+
+def _lengths(case, count):
+    """`count` lengths between lo and hi, spread over their logarithm; the longest is hi."""
+    r = random.Random(case["mix"])
+    lo, hi = case["lo"], case["hi"]
+    got = [lo - 1 + _log(r, 1, hi - lo + 1) for _ in range(count)]
+    got[r.randrange(count)] = hi
+    return got
+
+
+# ---------------------------------------------------------------------------
+# inputs
+# ---------------------------------------------------------------------------
+def _device():
+    return "cuda" if torch.cuda.is_available() else "cpu"
+
+
+def _type(case):
+    return torch.bfloat16 if case["dtype"] == BF16 else torch.float32
+
+
+def _gen(seed):
+    return torch.Generator(device=_device()).manual_seed(seed)
+
+
+def _randn(gen, *shape):
+    return torch.randn(*shape, generator=gen, device=_device(), dtype=torch.float32)
+
+
+def _keys(gen, *shape):
+    """Standard normal rows with four channels scaled by 8."""
+    k = _randn(gen, *shape)
+    k[..., torch.randperm(shape[-1], generator=gen, device=_device())[:4]] *= 8.0
+    return k
+
+
+def _offsets(lengths):
+    return torch.tensor(np.concatenate([[0], np.cumsum(lengths)]), dtype=torch.int64, device=_device())
+
+
+def _scale(case, gen, heads):
+    if not case["temps"]:
+        return None
+    t = 0.5 + 1.5 * torch.rand(heads, generator=gen, device=_device(), dtype=torch.float32)
+    return 1.0 / (math.sqrt(case["d"]) * t)
+
+
+def _prompt_lengths(case):
+    """Query and key lengths; with a prefix, every third sequence is a later chunk: its keys go back further."""
+    q = _lengths(case, case["seqs"])
+    return q, [n + (case["prefix"] if i % 3 == 1 else 0) for i, n in enumerate(q)]
+
+
+def _prepare_prompt(case, seed):
+    gen, dt = _gen(seed), _type(case)
+    H, Hkv, d = case["heads"], case["kv_heads"], case["d"]
+    lq, lk = _prompt_lengths(case)
+    if lq == lk:  # one projection's output: queries, keys and values of a token side by side
+        qkv = torch.empty(sum(lq), H + 2 * Hkv, d, dtype=dt, device=_device())
+        q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+        q.copy_(_randn(gen, sum(lq), H, d))
+        k.copy_(_keys(gen, sum(lq), Hkv, d))
+        v.copy_(_randn(gen, sum(lq), Hkv, d))
+    else:
+        q = _randn(gen, sum(lq), H, d).to(dt)
+        k, v = _keys(gen, sum(lk), Hkv, d).to(dt), _randn(gen, sum(lk), Hkv, d).to(dt)
+    return dict(q=q, k=k, v=v, cu_q=_offsets(lq), cu_k=_offsets(lk), scale=_scale(case, gen, Hkv),
+                max_q=max(lq), max_k=max(lk))
+
+
+def _pool(case, gen, blocks_of):
+    """A block table for cells of so many blocks each, their places in the pool in no order."""
+    C, total = len(blocks_of), sum(blocks_of)
+    n_blocks = total + 1 + total // 8
+    places = torch.randperm(n_blocks, generator=gen, device=_device()).to(torch.int32)
+    width = max(1, max(blocks_of))
+    n = torch.tensor(blocks_of, device=_device())
+    at = torch.cumsum(n, 0) - n
+    j = torch.arange(width, device=_device())
+    table = torch.where(j < n[:, None], places[(at[:, None] + j).clamp_(max=n_blocks - 1)], -1)
+    return table.to(torch.int32).contiguous(), places[total:].contiguous(), n_blocks
+
+
+def _blocks(n, size):
+    return -(-n // size)
+
+
+def _prepare_tables(case, seed):
+    gen, bs = _gen(seed), case["block"]
+    lens = _lengths(case, case["cells"])
+    # add = 0: whole requests come and go; otherwise cells of these lengths grow by `add` tokens
+    old, new = ([0] * len(lens), lens) if not case["add"] else (lens, [n + case["add"] for n in lens])
+    table, free, n_blocks = _pool(case, gen, [_blocks(n, bs) for n in new])
+    held = torch.tensor([_blocks(n, bs) for n in old], device=_device())
+    gone = torch.arange(table.shape[1], device=_device()) >= held[:, None]
+    free = torch.cat([free, table[gone & (table >= 0)]])
+    table.masked_fill_(gone, -1)
+    free_list = torch.full((n_blocks,), -1, dtype=torch.int32, device=_device())
+    free_list[:free.numel()] = free
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device=_device())  # noqa: E731
+    return dict(old=ints(old), new=ints(new), table=table, free_list=free_list, n_free=ints([free.numel()]),
+                n_slots=sum(new) - sum(old))
+
+
+def _buffers(case, n_blocks):
+    """The cache's buffers, as the library lays them out: rows of d values padded with zeros to 32, 64, 96, 128, ..."""
+    dp = next(x for x in (32, 64, 96, 128, 192, 256) if x >= case["d"])
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8, device=_device())  # noqa: E731
+    return u8(n_blocks, case["block"], dp), u8(n_blocks, dp, case["block"]), u8(n_blocks), u8(n_blocks)
+
+
+def _fill(case, gen, cache):
+    """Blocks that were filled before: every code, and exponents as keys and values of unit size get them."""
+    k, v, k_exp, v_exp = cache
+    d = case["d"]
+    for codes, exps, at in ((k, k_exp, 2), (v, v_exp, 1)):
+        x = _randn(gen, *codes.shape).mul_(100.0).clamp_(-E4M3_MAX, E4M3_MAX)
+        x.narrow(at, d, codes.shape[at] - d).zero_()
+        codes.copy_(x.to(torch.float8_e4m3fn).view(torch.uint8))
+        exps.copy_(torch.randint(119, 122, exps.shape, generator=gen, device=_device(), dtype=torch.uint8))
+
+
+def _prepare_store(case, seed):
+    gen, dt, bs, d = _gen(seed), _type(case), case["block"], case["d"]
+    lens = _lengths(case, case["cells"])
+    old = lens if case["add"] else [0] * len(lens)
+    add = [case["add"]] * len(lens) if case["add"] else lens
+    table, _, n_blocks = _pool(case, gen, [_blocks(a + b, bs) for a, b in zip(old, add)])
+    cache = _buffers(case, n_blocks)
+    if case["add"]:
+        _fill(case, gen, cache)
+    offsets = _offsets(add)
+    n = sum(add)
+    i = torch.arange(n, device=_device())
+    c = torch.searchsorted(offsets, i, right=True) - 1
+    pos = torch.tensor(old, device=_device())[c] + i - offsets[c]
+    slots = table[c, pos // bs].to(torch.int64) * bs + pos % bs
+    k = _keys(gen, n, d).to(dt)
+    return dict(cache=cache, k=k, v=_randn(gen, n, d).to(dt), offsets=offsets, slots=slots, block=bs)
+
+
+def _prepare_decode(case, seed):
+    gen, dt, bs = _gen(seed), _type(case), case["block"]
+    lens = _lengths(case, case["seqs"] * case["kv_heads"])
+    table, _, n_blocks = _pool(case, gen, [_blocks(n, bs) for n in lens])
+    cache = _buffers(case, n_blocks)
+    _fill(case, gen, cache)
+    q = _randn(gen, case["seqs"], case["tokens"], case["kv_heads"] * case["group"], case["d"]).to(dt)
+    return dict(cache=cache, q=q, table=table, lens=torch.tensor(lens, dtype=torch.int32, device=_device()),
+                scale=_scale(case, gen, case["kv_heads"]), kv_heads=case["kv_heads"])
+
+
+def prepare(case, seed):
+    s = {"prompt": _prepare_prompt, "tables": _prepare_tables, "store": _prepare_store,
+         "decode": _prepare_decode}[case["kind"]](case, seed)
+    return dict(s, case=case)
+
+
+# ---------------------------------------------------------------------------
+# the plain forms
+# ---------------------------------------------------------------------------
+def _softmax_v(z, v):
+    """Weighted values and log-sum-exp of masked scores z [..., rows, keys]; a row of no keys gives 0 and -inf."""
+    m = z.amax(-1, keepdim=True).clamp_(min=torch.finfo(z.dtype).min)
+    p = z.sub_(m).exp_()
+    s = p.sum(-1, keepdim=True)
+    o = torch.matmul(p, v) / torch.where(s > 0, s, 1)
+    return o, (m + s.log()).squeeze(-1)
+
+
+def _plain_prompt(s):
+    c, q, k, v = s["case"], s["q"], s["k"], s["v"]
+    H, Hkv, d, dev = c["heads"], c["kv_heads"], c["d"], q.device
+    cu_q, cu_k, Lq, Lk = s["cu_q"], s["cu_k"], s["max_q"], s["max_k"]
+    nq, nk = (cu_q[1:] - cu_q[:-1])[:, None], (cu_k[1:] - cu_k[:-1])[:, None]
+    i, j = torch.arange(Lq, device=dev), torch.arange(Lk, device=dev)
+    at_q = (cu_q[:-1, None] + i).clamp_(max=q.shape[0] - 1)
+    at_k = (cu_k[:-1, None] + j).clamp_(max=k.shape[0] - 1)
+    # [sequences][kv heads][group x positions][d]
+    Q = q[at_q].float().unflatten(2, (Hkv, -1)).permute(0, 2, 3, 1, 4).flatten(2, 3)
+    K = k[at_k].float().permute(0, 2, 3, 1).contiguous()
+    V = v[at_k].float().permute(0, 2, 1, 3).contiguous()
+    scale = s["scale"] if s["scale"] is not None else torch.full((Hkv,), 1.0 / math.sqrt(d), device=dev)
+    z = torch.matmul(Q * scale[:, None, None], K).unflatten(2, (-1, Lq))
+    hidden = (j >= nk)[:, None, :].expand(-1, Lq, -1)
+    if c["causal"]:
+        hidden = hidden | (j > (i + nk - nq)[:, :, None])
+    z.masked_fill_(hidden[:, None, None], -math.inf)
+    o, lse = _softmax_v(z.flatten(2, 3), V)
+    # back to packed rows
+    t = torch.arange(q.shape[0], device=dev)
+    b = torch.searchsorted(cu_q, t, right=True) - 1
+    p = t - cu_q[b]
+    o = o.unflatten(2, (-1, Lq)).permute(0, 3, 1, 2, 4)[b, p].flatten(1, 2)
+    lse = lse.unflatten(2, (-1, Lq)).permute(0, 3, 1, 2)[b, p].flatten(1, 2)
+    return dict(o=o.to(q.dtype), lse=lse)
+
+
+def _plain_tables_step(old, new, table, free_list, n_free, bs, n_slots):
+    dev, W = table.device, table.shape[1]
+    o, n = old.long(), new.long()
+    had, want = -(-o // bs), -(-n // bs)
+    want = torch.where(want > W, had, want)
+    # blocks given back, the last one lowest on the stack
+    back = (had - want).clamp(min=0)
+    j = torch.arange(W, device=dev)
+    out = (j >= want[:, None]) & (j < had[:, None])
+    rank = (torch.cumsum(back, 0) - back)[:, None] + j - want[:, None]
+    total = back.sum()
+    spare = free_list.numel()
+    stack = torch.cat([free_list, free_list.new_zeros(1)])
+    stack[torch.where(out, n_free + total - 1 - rank, spare)] = table
+    # blocks taken, in the cells' order, as far as they go
+    need = (want - had).clamp(min=0)
+    upto = torch.cumsum(need, 0)
+    top = n_free + total
+    granted = (upto <= top) & (-(-n // bs) <= W)
+    take = granted[:, None] & (j >= had[:, None]) & (j < want[:, None])
+    k = (upto - need)[:, None] + j - had[:, None]
+    table.copy_(torch.where(take, stack[(top - 1 - k).clamp(0, spare - 1)], torch.where(out, -1, table)))
+    free_list.copy_(stack[:spare])
+    n_free.copy_(top - torch.where(granted, need, 0).sum())
+    # a slot for every token that came
+    add = (n - o).clamp(min=0)
+    ends = torch.cumsum(add, 0)
+    offsets = torch.cat([ends.new_zeros(1), ends])
+    i = torch.arange(n_slots, device=dev)
+    c = torch.searchsorted(offsets, i, right=True).sub_(1).clamp_(max=o.numel() - 1)
+    pos = o[c] + i - offsets[c]
+    slots = torch.where(granted[c], table[c, (pos // bs).clamp(max=W - 1)].long() * bs + pos % bs, -1)
+    lens = torch.where(granted, n, o).to(torch.int32)
+    return dict(slots=slots, offsets=offsets, lens=lens, refused=(~granted).sum().to(torch.int32).view(1))
+
+
+def _plain_tables(s):
+    c = s["case"]
+    a = (s["table"], s["free_list"], s["n_free"], c["block"])
+    up = _plain_tables_step(s["old"], s["new"], *a, s["n_slots"])
+    down = _plain_tables_step(up["lens"], s["old"], *a, 0)
+    return dict(up=up, down=down, table=s["table"], free_list=s["free_list"], n_free=s["n_free"])
+
+
+def _two_to(e):
+    """2^(127 - e) of an exponent byte e in 1 .. 253, in float32."""
+    return ((254 - e.to(torch.int32)) << 23).view(torch.float32)
+
+
+def _plain_store_rows(x, codes, exps, b, off, first, part, transposed):
+    """One of the two halves: x [n][d] into the blocks b at offsets off; part: rows that open a part-filled block."""
+    d, n_blocks = x.shape[1], exps.numel()
+    x = x.float()
+    amax = torch.where(x.isfinite(), x.abs(), 0).amax(1)
+    top = x.new_zeros(n_blocks).scatter_reduce_(0, b, amax, "amax")
+    m, e = torch.frexp(top)
+    e = torch.where(top > 0, e - 9 + (m > 0.875).int() + 127, 1).clamp_(1, 253)
+    pb = b[first]
+    was = exps[pb].int()
+    now = torch.where(part, torch.maximum(was, e[pb]), e[pb])
+    e = e.scatter_(0, pb, now)
+    # what a part-filled block held before, at its new exponent
+    rows = torch.arange(codes.shape[2 if transposed else 1], device=x.device) < off[first][:, None]
+    rows = rows[:, None, :] if transposed else rows[:, :, None]
+    held = codes[pb].view(torch.float8_e4m3fn).float() * torch.exp2((was - now).float())[:, None, None]
+    codes[pb] = torch.where(rows & part[:, None, None], held.to(torch.float8_e4m3fn).view(torch.uint8), codes[pb])
+    exps[b] = e[b].to(torch.uint8)
+    y = (x * _two_to(e[b])[:, None]).to(torch.float8_e4m3fn).view(torch.uint8)
+    if transposed:
+        codes[b, :d, off] = y
+    else:
+        codes[b, off, :d] = y
+
+
+def _plain_store(s):
+    k, v, k_exp, v_exp = s["cache"]
+    b, off = s["slots"] // s["block"], s["slots"] % s["block"]
+    some = s["offsets"][1:] > s["offsets"][:-1]
+    first = torch.where(some, s["offsets"][:-1], 0)  # a cell without rows stands for the first cell that has some
+    part = off[first] > 0
+    _plain_store_rows(s["k"], k, k_exp, b, off, first, part, False)
+    _plain_store_rows(s["v"], v, v_exp, b, off, first, part, True)
+
+
+def _stored(cache):
+    k, v, k_exp, v_exp = cache
+    return dict(k=k.view(torch.float8_e4m3fn), v=v.view(torch.float8_e4m3fn), k_exp=k_exp, v_exp=v_exp)
+
+
+def _plain_decode(s):
+    c, q = s["case"], s["q"]
+    S, T, H, d = q.shape
+    Hkv, bs, lens = s["kv_heads"], c["block"], s["lens"].long()
+    kc, vc, k_exp, v_exp = s["cache"]
+    at = s["table"].clamp(min=0).long()
+    # [cells][keys][d]
+    two = lambda e: (e.to(torch.int32) << 23).view(torch.float32)  # noqa: E731
+    K = kc[at].view(torch.float8_e4m3fn).float()[..., :d] * two(k_exp[at])[:, :, None, None]
+    K = K.flatten(1, 2).transpose(1, 2).contiguous()
+    V = vc[at].view(torch.float8_e4m3fn).float()[:, :, :d] * two(v_exp[at])[:, :, None, None]
+    V = V.transpose(2, 3).flatten(1, 2).contiguous()
+    scale = s["scale"] if s["scale"] is not None else torch.full((Hkv,), 1.0 / math.sqrt(d), device=q.device)
+    Q = q.float().unflatten(2, (Hkv, -1)) * scale[:, None, None]
+    Q = Q.permute(0, 2, 1, 3, 4).reshape(S * Hkv, -1, d)  # rows: token, head of the group
+    z = torch.bmm(Q, K)
+    t = torch.arange(T, device=q.device).repeat_interleave(H // Hkv)
+    seen = lens[:, None] - (T - 1 - t)
+    z.masked_fill_(torch.arange(z.shape[2], device=q.device) >= seen[:, :, None], -math.inf)
+    o, lse = _softmax_v(z, V)
+    o = o.view(S, Hkv, T, -1, d).permute(0, 2, 1, 3, 4).flatten(2, 3)
+    lse = lse.view(S, Hkv, T, -1).permute(0, 2, 1, 3).flatten(2, 3)
+    return dict(o=o.to(q.dtype), lse=lse)
+
+
+# ---------------------------------------------------------------------------
+# one pass
+# ---------------------------------------------------------------------------
+def _own(s):
+    from paper_2608_25230_amd import fw
+    c, kind = s["case"], s["case"]["kind"]
+    if kind == "prompt":
+        r = fw.prompt_attention(s["q"], s["k"], s["v"], s["cu_q"], s["cu_k"], causal=c["causal"], scale=s["scale"])
+        return dict(o=r["o"], lse=r["lse"])
+    if kind == "tables":
+        a = (s["table"], s["free_list"], s["n_free"], c["block"])
+        up = fw.block_tables(s["old"], s["new"], *a, n_slots=s["n_slots"])
+        down = fw.block_tables(up["lens"], s["old"], *a, n_slots=0)
+        pick = ("slots", "offsets", "lens", "refused")
+        return dict(up={k: up[k] for k in pick}, down={k: down[k] for k in pick}, table=s["table"],
+                    free_list=s["free_list"], n_free=s["n_free"])
+    cache = fw.KvCache(*s["cache"], c["d"])
+    if kind == "store":
+        fw.cache_store(cache, s["k"], s["v"], s["offsets"], s["slots"])
+        return _stored(s["cache"])
+    r = fw.cache_attention(s["q"], cache, s["table"], s["lens"], scale=s["scale"])
+    return dict(o=r["o"], lse=r["lse"])
+
+
+def run(state):
+    if own:
+        return _own(state)
+    kind = state["case"]["kind"]
+    if kind == "store":
+        _plain_store(state)
+        return _stored(state["cache"])
+    return {"prompt": _plain_prompt, "tables": _plain_tables, "decode": _plain_decode}[kind](state)
+
+
+# ---------------------------------------------------------------------------
+# what a pass cannot do without
+# ---------------------------------------------------------------------------
+def work(case):
+    kind = case["kind"]
+    size = 2 if case.get("dtype") == BF16 else 4
+    if kind == "prompt":
+        lq, lk = _prompt_lengths(case)
+        H, Hkv, d = case["heads"], case["kv_heads"], case["d"]
+        pairs = sum(a * b - (a * (a - 1) // 2 if case["causal"] else 0) for a, b in zip(lq, lk))
+        return {"bytes": size * d * (2 * H * sum(lq) + 2 * Hkv * sum(lk)) + 4 * H * sum(lq),
+                "flops": 4.0 * d * H * pairs}
+    if kind == "tables":
+        lens, bs, add = _lengths(case, case["cells"]), case["block"], case["add"]
+        old = lens if add else [0] * len(lens)
+        new = [n + add for n in lens] if add else lens
+        took = sum(_blocks(b, bs) - _blocks(a, bs) for a, b in zip(old, new))
+        # growth: lengths read and written, offsets and slots written, a block read off the stack into the table;
+        # return: lengths again, a block from the table onto the stack
+        return {"bytes": len(lens) * (12 + 8 + 12) + 8 * (sum(new) - sum(old)) + 16 * took, "flops": 0.0}
+    if kind == "store":
+        lens = _lengths(case, case["cells"])
+        n = sum(lens) if not case["add"] else case["add"] * len(lens)
+        return {"bytes": n * (2 * size * case["d"] + 2 * case["d"] + 8), "flops": 0.0}
+    lens = _lengths(case, case["seqs"] * case["kv_heads"])
+    rows, d = case["tokens"] * case["group"], case["d"]
+    blocks = sum(_blocks(n, case["block"]) for n in lens)
+    return {"bytes": 2 * d * sum(lens) + 6 * blocks + len(lens) * (4 + rows * (2 * size * d + 4)),
+            "flops": 4.0 * d * rows * sum(lens)}
+
+
+# ---------------------------------------------------------------------------
+# the definitions in 64 bits
+# ---------------------------------------------------------------------------
+def _attend64(q, k, v, scale, seen):
+    """One head: rows q over keys k, of which row r sees the first seen[r]."""
+    z = (q * scale) @ k.T
+    z[torch.arange(k.shape[0], device=q.device)[None, :] >= seen[:, None]] = -math.inf
+    lse = torch.logsumexp(z, 1)
+    p = torch.where(lse[:, None] > -math.inf, torch.exp(z - lse[:, None]), 0.0)
+    return p @ v, lse
+
+
+def _exact_prompt(case, s):
+    H, Hkv, d = case["heads"], case["kv_heads"], case["d"]
+    lq, lk = _prompt_lengths(case)
+    o = torch.empty(sum(lq), H, d, dtype=torch.float64, device=_device())
+    lse = torch.empty(sum(lq), H, dtype=torch.float64, device=_device())
+    aq = ak = 0
+    for a, b in zip(lq, lk):
+        seen = torch.arange(a, device=_device()) + b - a + 1 if case["causal"] else torch.full((a,), b, device=_device())
+        for h in range(H):
+            g = h // (H // Hkv)
+            scale = 1.0 / math.sqrt(d) if s["scale"] is None else s["scale"][g].double()
+            o[aq:aq + a, h], lse[aq:aq + a, h] = _attend64(s["q"][aq:aq + a, h].double(), s["k"][ak:ak + b, g].double(),
+                                                           s["v"][ak:ak + b, g].double(), scale, seen)
+        aq, ak = aq + a, ak + b
+    return dict(o=o, lse=lse)
+
+
+_E4M3 = None
+
+
+def _e4m3_values():
+    """The value of each of the 256 codes: sign, 4 exponent bits (bias 7), 3 mantissa bits; 0x7f and 0xff are NaN."""
+    global _E4M3
+    if _E4M3 is None:
+        c = np.arange(128)
+        e, m = c >> 3, c & 7
+        x = np.where(e > 0, (8 + m) * 2.0 ** (e - 10), m * 2.0 ** -9)
+        x[127] = math.nan
+        _E4M3 = torch.tensor(np.concatenate([x, -x]), dtype=torch.float64)
+    return _E4M3.to(_device())
+
+
+def _e4m3_round(x):
+    """float64 values of magnitude at most 448 to the nearest e4m3 value, ties to even."""
+    step = torch.exp2((torch.floor(torch.log2(x.abs().clamp(min=2.0 ** -6))) - 3))
+    return torch.round(x / step) * step
+
+
+def _exact_store(case, s):
+    k, v, k_exp, v_exp = s["cache"]
+    offsets, slots, bs, d = s["offsets"].tolist(), s["slots"], case["block"], case["d"]
+    got = {}
+    value = _e4m3_values()
+    for name, codes, exps, x in (("k", k, k_exp, s["k"]), ("v", v.transpose(1, 2), v_exp, s["v"])):
+        vals = value[codes.long()]
+        b, off = slots // bs, slots % bs
+        x = x.double()
+        top = torch.zeros(exps.numel(), dtype=torch.float64, device=x.device).scatter_reduce_(0, b, x.abs().amax(1), "amax")
+        least = torch.ceil(torch.log2(top.clamp(min=2.0 ** -110) / E4M3_MAX))
+        e = exps.double() - 127
+        first = torch.tensor([a for a, z in zip(offsets, offsets[1:]) if z > a], device=x.device)
+        part = off[first] > 0
+        before = e[b[first]]
+        e[b] = least[b]
+        e[b[first]] = torch.where(part, torch.maximum(before, least[b[first]]), least[b[first]])
+        held = torch.arange(bs, device=x.device) < off[first][:, None]
+        moved = _e4m3_round(vals[b[first]] * torch.exp2(before - e[b[first]])[:, None, None])
+        vals[b[first]] = torch.where(held[:, :, None], moved, vals[b[first]])
+        vals[b, off, :d] = _e4m3_round(x * torch.exp2(-e[b])[:, None])
+        got[name] = vals if name == "k" else vals.transpose(1, 2).contiguous()
+    return dict(got, k_exp=None, v_exp=None)
+
+
+def _exact_decode(case, s):
+    q, lens, bs, d = s["q"], s["lens"].tolist(), case["block"], case["d"]
+    S, T, H, _ = q.shape
+    Hkv, G = case["kv_heads"], case["group"]
+    k, v, k_exp, v_exp = s["cache"]
+    value = _e4m3_values()
+    o = torch.empty(S, T, H, d, dtype=torch.float64, device=_device())
+    lse = torch.empty(S, T, H, dtype=torch.float64, device=_device())
+    t = torch.arange(T, device=_device()).repeat_interleave(G)
+    for c, n in enumerate(lens):
+        at = s["table"][c, :_blocks(n, bs)].long()
+        K = (value[k[at].long()] * torch.exp2(k_exp[at].double() - 127)[:, None, None]).flatten(0, 1)[:n, :d]
+        V = (value[v[at].long()] * torch.exp2(v_exp[at].double() - 127)[:, None, None]).transpose(1, 2).flatten(0, 1)[:n, :d]
+        b, h = divmod(c, Hkv)
+        rows = q[b, :, h * G:(h + 1) * G].double().reshape(T * G, d)
+        scale = 1.0 / math.sqrt(d) if s["scale"] is None else s["scale"][h].double()
+        x, y = _attend64(rows, K, V, scale, n - (T - 1 - t))
+        o[b, :, h * G:(h + 1) * G], lse[b, :, h * G:(h + 1) * G] = x.view(T, G, d), y.view(T, G)
+    return dict(o=o, lse=lse)
+
+
+def exact(case, seed):
+    if case["kind"] == "tables":
+        return None
+    s = prepare(case, seed)
+    return {"prompt": _exact_prompt, "store": _exact_store, "decode": _exact_decode}[case["kind"]](case, s)
