@@ -439,7 +439,7 @@ def _own(s):
                     free_list=s["free_list"], n_free=s["n_free"])
     cache = fw.KvCache(*s["cache"], c["d"])
     if kind == "store":
-        fw.cache_store(cache, s["k"], s["v"], s["offsets"], s["slots"])
+        fw.cache_store(cache, s["k"], s["v"], s["slots"])
         return _stored(s["cache"])
     r = fw.cache_attention(s["q"], cache, s["table"], s["lens"], scale=s["scale"])
     return dict(o=r["o"], lse=r["lse"])
