@@ -335,6 +335,157 @@ fw_status fw_ragged_compact(int32_t dtype, const void *k, const void *v, int64_t
 fw_status fw_maxpool_scores(const float *scores, int64_t H, int64_t n, int32_t kernel, float *out,
                             fw_stream stream);
 
+/* ---------------------------------------------------------------------------
+ * Serving a cache that eviction has thinned out: the prompt's attention, the
+ * blocks that hold what is kept, the store that rounds it to 8 bits, and the
+ * attention that reads it for every token after the prompt.
+ *
+ * A cell is one sequence's key/value head; cell c = sequence * Hkv + head.
+ * ContourKV keeps a different number of entries in every cell (Section 4), so
+ * lengths, block tables and slots are per cell.
+ * ------------------------------------------------------------------------- */
+
+/* Packed sequences: the rows of B sequences one after the other.
+ *   q      [Tq][Hq][d]  queries, strides q_row (between positions) and q_head
+ *                       (between heads) in elements, columns contiguous
+ *   k, v   [Tk][Hkv][d] keys and values, strides k_row, k_head, v_row, v_head
+ *   cu_q   [B+1] int64 device: sequence b's queries are rows
+ *          cu_q[b] .. cu_q[b+1] - 1 (ascending)
+ *   cu_k   [B+1] int64 device: likewise for keys and values
+ *   scale  [Hkv] float32 logit scale per key/value head, or NULL for 1/sqrt(d)
+ *   causal non-zero: query i of Lq sees keys 0 .. i + Lk - Lq (the last query
+ *          sees every key); zero: every key of its sequence
+ * Limits: B, Hkv, d >= 1, Tq, Tk >= 0; Hkv divides Hq; d <= 256;
+ * Tq*Hq < 2^31; Tk < 2^31; strides >= 0 and below 2^31. */
+typedef struct fw_packed {
+    int32_t dtype;
+    const void *q, *k, *v;
+    int64_t Tq, Tk, B, Hq, Hkv, d;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+    const int64_t *cu_q, *cu_k;
+    const float *scale;
+    int32_t causal;
+} fw_packed;
+
+/* ---------------------------------------------------------------------------
+ * fw_prompt_attention -- softmax attention of packed sequences with grouped
+ * heads (Definition 2.1's dense output mu for every row of a prompt): query
+ * head i uses key/value head i / (Hq / Hkv).
+ *   o    [Tq][Hq][d] contiguous, of the rows' type (required)
+ *   lse  [Tq][Hq] float32 natural logarithm of the row's sum of exponentials,
+ *        or NULL
+ * A row that sees no key gives o = 0 and lse = -inf.  Keys and values that a
+ * row does not see do not touch it, whatever they hold.  Rows of o and lse
+ * outside [cu_q[0], cu_q[B]) are left as they were.  Offsets that lead outside
+ * the arrays are clamped to them.  float32 rows are computed in float32; bf16
+ * rows round the softmax weights to bf16 for the product with the values.
+ * Errors: FW_E_NULL (packed, q, k, v, cu_q, cu_k or o NULL; q, k, v and o may
+ * be NULL where they have no rows), FW_E_SHAPE, FW_E_DTYPE, FW_E_WORKSPACE,
+ * FW_E_HIP.
+ * ------------------------------------------------------------------------- */
+size_t fw_prompt_attention_workspace_size(const fw_packed *packed);
+fw_status fw_prompt_attention(const fw_packed *packed, void *o, float *lse, void *ws, size_t ws_bytes,
+                              fw_stream stream);
+
+/* ---------------------------------------------------------------------------
+ * fw_block_tables -- gives every cell the blocks that its new length needs,
+ * takes back those it no longer needs, and lists the slot of every token that
+ * comes, all on the device.  A block holds block_size consecutive tokens of
+ * one cell; nb(L) = ceil(L / block_size).
+ *   old_len, new_len [C] int32 tokens of each cell before and after (negative
+ *             counts as 0)
+ *   block_size a power of two, 16 .. 256
+ *   table     [C][max_blocks] int32: block j of cell c (in and out; entries at
+ *             nb(new_len) and past it that held blocks become -1)
+ *   n_blocks  blocks of the cache
+ *   free_list [n_blocks] int32 stack of free blocks, n_free[0] int32 of them
+ *             (both in and out).  Growing cells, in order, take from the top;
+ *             shrinking cells give back so that the same growth would get the
+ *             same blocks again.
+ *   slots     [n_slots] int64: for each token that comes (cells in order,
+ *             positions ascending) block * block_size + position % block_size,
+ *             or -1 for a refused cell; entries past the last such token stay
+ *             as they were; tokens past n_slots are not listed.  NULL if
+ *             n_slots is 0.
+ *   offsets   [C+1] int64 exclusive prefix of the tokens that come, refused
+ *             ones included (required)
+ *   lens      [C] int32 lengths after the call; may be old_len (required)
+ *   refused   [1] int32 cells that were refused (required).  A cell is refused
+ *             as a whole, and keeps its length and blocks, if new_len exceeds
+ *             max_blocks * block_size, or if its need and that of the cells
+ *             before it exceed the free blocks.
+ * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_WORKSPACE, FW_E_HIP.
+ * ------------------------------------------------------------------------- */
+size_t fw_block_tables_workspace_size(int64_t C);
+fw_status fw_block_tables(int64_t C, const int32_t *old_len, const int32_t *new_len, int32_t block_size,
+                          int64_t max_blocks, int32_t *table, int64_t n_blocks, int32_t *free_list,
+                          int32_t *n_free, int64_t n_slots, int64_t *slots, int64_t *offsets, int32_t *lens,
+                          int32_t *refused, void *ws, size_t ws_bytes, fw_stream stream);
+
+/* The 8-bit cache: e4m3 codes (4 exponent bits, 3 mantissa bits, largest value
+ * 448) with one power-of-two scale per block for keys and one for values;
+ * code x exponent byte e stands for value(x) * 2^(e - 127).
+ *   k      [n_blocks][block_size][dp] keys, columns past d zero
+ *   v      [n_blocks][dp][block_size] values, tokens innermost
+ *   k_exp, v_exp [n_blocks] exponent bytes
+ * dp = fw_cache_row(d): the least of 32, 64, 96, 128, 192, 256 that holds d (0
+ * for d out of range).  k and v are 16-byte aligned.  A new cache is zeroed. */
+typedef struct fw_cache {
+    uint8_t *k, *v, *k_exp, *v_exp;
+    int64_t n_blocks, d;
+    int32_t block_size;
+} fw_cache;
+int32_t fw_cache_row(int64_t d);
+
+/* ---------------------------------------------------------------------------
+ * fw_cache_store -- rounds rows of keys and values to the cache's blocks
+ * (fw_ragged_compact's k_out and v_out, or one decoding step's rows).
+ *   dtype, k, v  [N][d] rows, strides k_row and v_row in elements
+ *   slots        [N] int64, of fw_block_tables; rows whose slot is not in
+ *                [0, n_blocks * block_size) are skipped
+ * The rows that go to one block are consecutive rows with consecutive slots.
+ * The block's exponent is the least with amax <= 448 * 2^(e - 127) over the
+ * finite values of these rows (1 <= e <= 253), and not below the present one
+ * if tokens lie before the first of them; those are then rounded again at the
+ * new exponent.  Values that are not finite are stored as NaN.  Two runs of
+ * rows for the same block in one call leave that block undefined.
+ * No workspace is used: the query returns 0 and ws may be NULL.
+ * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_DTYPE, FW_E_HIP.
+ * ------------------------------------------------------------------------- */
+size_t fw_cache_store_workspace_size(const fw_cache *cache, int64_t N);
+fw_status fw_cache_store(const fw_cache *cache, int32_t dtype, const void *k, int64_t k_row, const void *v,
+                         int64_t v_row, int64_t N, const int64_t *slots, void *ws, size_t ws_bytes,
+                         fw_stream stream);
+
+/* ---------------------------------------------------------------------------
+ * fw_cache_attention -- attention of T new positions of S sequences over the
+ * cached tokens of each cell, their own among them: position t sees all but
+ * the cell's last T - 1 - t tokens.
+ *   dtype, q     [S][T][Hq][d], strides q_seq, q_tok, q_head in elements
+ *   table        [S*Hkv][max_blocks] int32 blocks of each cell; tokens in a
+ *                block outside [0, n_blocks) are not seen
+ *   lens         [S*Hkv] int32 tokens of each cell, the new ones included
+ *                (clamped to [0, max_blocks * block_size])
+ *   scale        [Hkv] float32 logit scale per key/value head, or NULL for
+ *                1/sqrt(d)
+ *   o            [S][T][Hq][d] contiguous, of the queries' type (required)
+ *   lse          [S][T][Hq] float32, or NULL
+ * A row that sees no token gives o = 0 and lse = -inf; what lies in a block
+ * behind the cell's last token is not seen, whatever it holds.  float32
+ * queries are computed in float32; bf16 queries round the softmax weights to
+ * bf16 for the product with the values.
+ * Limits: S, T, Hkv, max_blocks >= 1; Hkv divides Hq; T*Hq/Hkv <= 4096;
+ * S*Hkv < 2^24; S*Hkv*T*Hq < 2^31 rows; max_blocks * block_size < 2^31;
+ * S*Hkv * max_blocks * block_size < 2^37.
+ * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_DTYPE, FW_E_WORKSPACE, FW_E_HIP.
+ * ------------------------------------------------------------------------- */
+size_t fw_cache_attention_workspace_size(const fw_cache *cache, int64_t S, int64_t T, int64_t Hq, int64_t Hkv,
+                                         int64_t max_blocks);
+fw_status fw_cache_attention(const fw_cache *cache, int32_t dtype, const void *q, int64_t S, int64_t T,
+                             int64_t Hq, int64_t Hkv, int64_t q_seq, int64_t q_tok, int64_t q_head,
+                             const int32_t *table, int64_t max_blocks, const int32_t *lens, const float *scale,
+                             void *o, float *lse, void *ws, size_t ws_bytes, fw_stream stream);
+
 /* Thread-local description of the calling thread's last error ("" if none). */
 const char *fw_last_error(void);
 /* Library version string. */

@@ -446,3 +446,181 @@ fw_status fw_group_vote(const fw_rows *rows, int32_t s, int32_t group_size, int3
 
 }  // extern "C"
 
+
+// ---------------------------------------------------------------------------
+// serving: prompt attention, block tables, the 8-bit cache
+// ---------------------------------------------------------------------------
+namespace {
+
+fw_status check_packed(const fw_packed *p) {
+    if (!p) return fail(FW_E_NULL, "packed is NULL");
+    if (p->dtype != FW_F32 && p->dtype != FW_BF16) return fail(FW_E_DTYPE, "unknown dtype %d", (int)p->dtype);
+    if (p->B < 1 || p->Hkv < 1 || p->Hq < 1 || p->Tq < 0 || p->Tk < 0)
+        return fail(FW_E_SHAPE, "need B, Hq, Hkv >= 1 and Tq, Tk >= 0 (B=%lld Hq=%lld Hkv=%lld Tq=%lld Tk=%lld)",
+                    (long long)p->B, (long long)p->Hq, (long long)p->Hkv, (long long)p->Tq, (long long)p->Tk);
+    if (p->Hq % p->Hkv != 0)
+        return fail(FW_E_SHAPE, "Hkv must divide Hq (Hq=%lld Hkv=%lld)", (long long)p->Hq, (long long)p->Hkv);
+    if (p->d < 1 || p->d > 256) return fail(FW_E_SHAPE, "d must be in [1, 256], got %lld", (long long)p->d);
+    constexpr int64_t most = (int64_t)1 << 31;
+    if (p->Hq >= most || p->Tq >= most || p->Tk >= most || p->B >= most || p->Tq * p->Hq >= most)
+        return fail(FW_E_SHAPE, "Tq*Hq, Tk and B must be < 2^31");
+    // one workgroup per row tile and key/value head, 64 rows or more to a tile
+    if ((p->Tq * (p->Hq / p->Hkv) / 64 + 1 + p->B) >= most / p->Hkv)
+        return fail(FW_E_SHAPE, "too many sequences and heads for one call");
+    const int64_t strides[] = {p->q_row, p->q_head, p->k_row, p->k_head, p->v_row, p->v_head};
+    for (int64_t s : strides)
+        if (s < 0 || s >= most) return fail(FW_E_SHAPE, "strides must be in [0, 2^31)");
+    if (!p->cu_q || !p->cu_k) return fail(FW_E_NULL, "cu_q and cu_k are required");
+    if (p->Tq > 0 && !p->q) return fail(FW_E_NULL, "q is NULL");
+    if (p->Tk > 0 && (!p->k || !p->v)) return fail(FW_E_NULL, "k or v is NULL");
+    return FW_OK;
+}
+
+struct PromptWs {
+    int splits;
+    float *part_o, *part_lse;
+    size_t bytes;
+};
+PromptWs prompt_layout(const fw_packed &p, void *ws) {
+    PromptWs w{};
+    w.splits = fw::prompt_splits(p);
+    if (w.splits > 1) {
+        Carve c(ws);
+        const size_t rows = (size_t)w.splits * p.Tq * p.Hq;
+        w.part_o = c.take<float>(rows * p.d);
+        w.part_lse = c.take<float>(rows);
+        w.bytes = c.size();
+    }
+    return w;
+}
+
+fw_status check_block(int32_t block_size) {
+    if (block_size < 16 || block_size > 256 || (block_size & (block_size - 1)))
+        return fail(FW_E_SHAPE, "block_size must be a power of two in [16, 256], got %d", (int)block_size);
+    return FW_OK;
+}
+
+fw_status check_cache(const fw_cache *c) {
+    if (!c) return fail(FW_E_NULL, "cache is NULL");
+    if (!c->k || !c->v || !c->k_exp || !c->v_exp) return fail(FW_E_NULL, "cache->k, v, k_exp and v_exp are required");
+    if ((uintptr_t)c->k % 16 || (uintptr_t)c->v % 16) return fail(FW_E_SHAPE, "cache->k and v must be 16-byte aligned");
+    if (c->d < 1 || c->d > 256) return fail(FW_E_SHAPE, "d must be in [1, 256], got %lld", (long long)c->d);
+    if (c->n_blocks < 1 || c->n_blocks >= ((int64_t)1 << 31)) return fail(FW_E_SHAPE, "n_blocks must be in [1, 2^31)");
+    return check_block(c->block_size);
+}
+
+fw_status check_decode(int32_t block_size, int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t max_blocks) {
+    if (S < 1 || T < 1 || Hq < 1 || Hkv < 1 || max_blocks < 1)
+        return fail(FW_E_SHAPE, "S, T, Hq, Hkv and max_blocks must be >= 1");
+    constexpr int64_t m31 = (int64_t)1 << 31, m24 = (int64_t)1 << 24;
+    if (S >= m24 || Hkv >= m24 || S * Hkv >= m24) return fail(FW_E_SHAPE, "S*Hkv must be < 2^24");
+    if (Hq % Hkv != 0) return fail(FW_E_SHAPE, "Hkv must divide Hq (Hq=%lld Hkv=%lld)", (long long)Hq, (long long)Hkv);
+    if (T > 4096 || Hq / Hkv > 4096 || T * (Hq / Hkv) > 4096) return fail(FW_E_SHAPE, "T*Hq/Hkv must be <= 4096");
+    if (S * Hkv * (T * (Hq / Hkv)) >= m31) return fail(FW_E_SHAPE, "S*T*Hq must be < 2^31");
+    if (max_blocks >= m31 / block_size) return fail(FW_E_SHAPE, "max_blocks * block_size must be < 2^31");
+    if ((double)(S * Hkv) * (double)(max_blocks * block_size) >= 137438953472.0)
+        return fail(FW_E_SHAPE, "S*Hkv * max_blocks * block_size must be < 2^37");
+    return FW_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fw_prompt_attention_workspace_size(const fw_packed *packed) {
+    if (check_packed(packed) != FW_OK) return 0;
+    return prompt_layout(*packed, nullptr).bytes;
+}
+
+fw_status fw_prompt_attention(const fw_packed *packed, void *o, float *lse, void *ws, size_t ws_bytes,
+                              fw_stream stream) {
+    fw_status s = check_packed(packed);
+    if (s != FW_OK) return s;
+    if (packed->Tq == 0) return FW_OK;
+    if (!o) return fail(FW_E_NULL, "o is required");
+    const PromptWs w = prompt_layout(*packed, ws);
+    if ((s = check_ws(ws, ws_bytes, w.bytes)) != FW_OK) return s;
+    return hip_status(fw::launch_prompt(*packed, o, lse, w.splits, w.part_o, w.part_lse, (hipStream_t)stream),
+                      "fw_prompt_attention");
+}
+
+// ---------------------------------------------------------------------------
+size_t fw_block_tables_workspace_size(int64_t C) {
+    if (C < 1 || C >= ((int64_t)1 << 24)) return 0;
+    return fw::tables_ws_bytes(C);
+}
+
+fw_status fw_block_tables(int64_t C, const int32_t *old_len, const int32_t *new_len, int32_t block_size,
+                          int64_t max_blocks, int32_t *table, int64_t n_blocks, int32_t *free_list, int32_t *n_free,
+                          int64_t n_slots, int64_t *slots, int64_t *offsets, int32_t *lens, int32_t *refused, void *ws,
+                          size_t ws_bytes, fw_stream stream) {
+    constexpr int64_t m31 = (int64_t)1 << 31;
+    if (C < 1 || C >= ((int64_t)1 << 24)) return fail(FW_E_SHAPE, "C must be in [1, 2^24), got %lld", (long long)C);
+    fw_status s = check_block(block_size);
+    if (s != FW_OK) return s;
+    if (max_blocks < 1 || max_blocks >= m31 / block_size)
+        return fail(FW_E_SHAPE, "need max_blocks >= 1 and max_blocks * block_size < 2^31");
+    if (n_blocks < 1 || n_blocks >= m31) return fail(FW_E_SHAPE, "n_blocks must be in [1, 2^31)");
+    if (n_slots < 0 || n_slots >= ((int64_t)1 << 40)) return fail(FW_E_SHAPE, "n_slots must be in [0, 2^40)");
+    if (!old_len || !new_len || !table || !free_list || !n_free || !offsets || !lens || !refused)
+        return fail(FW_E_NULL, "old_len, new_len, table, free_list, n_free, offsets, lens and refused are required");
+    if (n_slots > 0 && !slots) return fail(FW_E_NULL, "slots is NULL");
+    if ((s = check_ws(ws, ws_bytes, fw::tables_ws_bytes(C))) != FW_OK) return s;
+    return hip_status(fw::launch_tables(C, old_len, new_len, block_size, max_blocks, table, n_blocks, free_list, n_free,
+                                        n_slots, slots, offsets, lens, refused, ws, (hipStream_t)stream),
+                      "fw_block_tables");
+}
+
+// ---------------------------------------------------------------------------
+int32_t fw_cache_row(int64_t d) { return fw::cache_row(d); }
+
+size_t fw_cache_store_workspace_size(const fw_cache *cache, int64_t N) {
+    (void)cache;
+    (void)N;
+    return 0;
+}
+
+fw_status fw_cache_store(const fw_cache *cache, int32_t dtype, const void *k, int64_t k_row, const void *v,
+                         int64_t v_row, int64_t N, const int64_t *slots, void *ws, size_t ws_bytes, fw_stream stream) {
+    (void)ws;
+    (void)ws_bytes;
+    fw_status s = check_cache(cache);
+    if (s != FW_OK) return s;
+    if (dtype != FW_F32 && dtype != FW_BF16) return fail(FW_E_DTYPE, "unknown dtype %d", (int)dtype);
+    if (N < 0 || N >= ((int64_t)1 << 31)) return fail(FW_E_SHAPE, "N must be in [0, 2^31)");
+    if (k_row < 0 || v_row < 0 || k_row >= ((int64_t)1 << 31) || v_row >= ((int64_t)1 << 31))
+        return fail(FW_E_SHAPE, "strides must be in [0, 2^31)");
+    if (N == 0) return FW_OK;
+    if (!k || !v || !slots) return fail(FW_E_NULL, "k, v and slots are required");
+    return hip_status(fw::launch_store(*cache, dtype, k, k_row, v, v_row, N, slots, (hipStream_t)stream),
+                      "fw_cache_store");
+}
+
+// ---------------------------------------------------------------------------
+size_t fw_cache_attention_workspace_size(const fw_cache *cache, int64_t S, int64_t T, int64_t Hq, int64_t Hkv,
+                                         int64_t max_blocks) {
+    if (check_cache(cache) != FW_OK || check_decode(cache->block_size, S, T, Hq, Hkv, max_blocks) != FW_OK) return 0;
+    return fw::decode_ws_bytes(S * Hkv, T * (Hq / Hkv), cache->d, max_blocks, cache->block_size);
+}
+
+fw_status fw_cache_attention(const fw_cache *cache, int32_t dtype, const void *q, int64_t S, int64_t T, int64_t Hq,
+                             int64_t Hkv, int64_t q_seq, int64_t q_tok, int64_t q_head, const int32_t *table,
+                             int64_t max_blocks, const int32_t *lens, const float *scale, void *o, float *lse, void *ws,
+                             size_t ws_bytes, fw_stream stream) {
+    fw_status s = check_cache(cache);
+    if (s != FW_OK) return s;
+    if (dtype != FW_F32 && dtype != FW_BF16) return fail(FW_E_DTYPE, "unknown dtype %d", (int)dtype);
+    if ((s = check_decode(cache->block_size, S, T, Hq, Hkv, max_blocks)) != FW_OK) return s;
+    constexpr int64_t m31 = (int64_t)1 << 31;
+    if (q_seq < 0 || q_tok < 0 || q_head < 0 || q_seq >= m31 || q_tok >= m31 || q_head >= m31)
+        return fail(FW_E_SHAPE, "strides must be in [0, 2^31)");
+    if (!q || !table || !lens || !o) return fail(FW_E_NULL, "q, table, lens and o are required");
+    if ((s = check_ws(ws, ws_bytes,
+                      fw::decode_ws_bytes(S * Hkv, T * (Hq / Hkv), cache->d, max_blocks, cache->block_size))) != FW_OK)
+        return s;
+    return hip_status(fw::launch_decode(*cache, dtype, q, S, T, Hq, Hkv, q_seq, q_tok, q_head, table, max_blocks, lens,
+                                        scale, o, lse, ws, (hipStream_t)stream),
+                      "fw_cache_attention");
+}
+
+}  // extern "C"

@@ -84,4 +84,34 @@ hipError_t launch_compact(int dtype, const void *k, const void *v, int64_t H, in
                           hipStream_t st);
 hipError_t launch_maxpool(const float *scores, int64_t H, int64_t n, int kernel, float *out, hipStream_t st);
 
+
+// k_prompt.hip -- attention of packed prompts; with more than one split it
+// takes part_o [splits][Tq][Hq][d] and part_lse [splits][Tq][Hq]
+int prompt_splits(const fw_packed &p);
+hipError_t launch_prompt(const fw_packed &p, void *o, float *lse, int splits, float *part_o, float *part_lse,
+                         hipStream_t st);
+
+// bytes of a cached key's row (fw_cache_row)
+inline int cache_row(int64_t d) {
+    constexpr int rows[] = {32, 64, 96, 128, 192, 256};
+    if (d < 1) return 0;
+    for (int r : rows)
+        if (d <= r) return r;
+    return 0;
+}
+
+// k_cache.hip -- block tables and the 8-bit cache's store
+size_t tables_ws_bytes(int64_t C);
+hipError_t launch_tables(int64_t C, const int32_t *old_len, const int32_t *new_len, int block_size, int64_t W,
+                         int32_t *table, int64_t n_blocks, int32_t *free_list, int32_t *n_free, int64_t n_slots,
+                         int64_t *slots, int64_t *offsets, int32_t *lens, int32_t *refused, void *ws, hipStream_t st);
+hipError_t launch_store(const fw_cache &cache, int dtype, const void *k, int64_t k_row, const void *v, int64_t v_row,
+                        int64_t N, const int64_t *slots, hipStream_t st);
+
+// k_decode.hip -- attention over the 8-bit cache
+size_t decode_ws_bytes(int64_t C, int64_t R, int64_t d, int64_t W, int block_size);
+hipError_t launch_decode(const fw_cache &cache, int dtype, const void *q, int64_t S, int64_t T, int64_t Hq, int64_t Hkv,
+                         int64_t q_seq, int64_t q_tok, int64_t q_head, const int32_t *table, int64_t W,
+                         const int32_t *lens, const float *scale, void *o, float *lse, void *ws, hipStream_t st);
+
 }  // namespace fw

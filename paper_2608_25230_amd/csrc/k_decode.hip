@@ -1,0 +1,521 @@
+// Attention over the 8-bit cache (fw_cache_attention): the rows of a cell
+// (T new positions x the G query heads of its key/value head) over the cell's
+// cached tokens,
+//
+//   z_rj = scale_h 2^ek(j) <q_r, code_k(j)>,   o_r = sum_j p_rj 2^ev(j) code_v(j),
+//
+// p the softmax of z over the tokens that row r sees, ek and ev the exponents
+// of token j's block.  Every code is read once for all rows of the cell and
+// is exact in bf16, so the products run on the bf16 MFMA with the codes as
+// they are: the block's key scale multiplies the logits, its value scale (a
+// power of two) the rounded weights.  Float32 queries and weights are taken
+// apart into three bf16 parts, which hold all 24 bits, one product for each.
+//
+// A wave takes 64 tokens at a time.  S^T = K Q^T on 16x16x32 MFMA: row
+// m = 4 g + i of key tile t is token 16 g + 4 t + i, so after four tiles lane
+// group g = l / 16 holds the weights of tokens 16 g .. 16 g + 15 of query row
+// l % 16, which is the order of a 16-byte piece of a value column [d][token]:
+// O^T += V^T P^T takes weights and codes as they lie.  A block of 16 or more
+// tokens holds a lane group's tokens whole, so scales and page numbers are one
+// per lane.
+//
+// Cells differ in length by far, so the work is cut by length, on the device:
+// parts of `chunk` tiles, chunk = ceil(all tiles / target) at least kMinChunk;
+// every workgroup finds its cell and part from the lengths.  A cell of several
+// parts leaves partial results in the workspace, joined by decode_join.
+#include <algorithm>
+
+#include "fw_internal.hpp"
+
+namespace fw {
+
+namespace {
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int DW = 4;               // waves per workgroup
+constexpr int DTH = 64 * DW;
+constexpr int DT = 64;              // tokens per wave and step
+constexpr int kTarget = 1024;       // parts that the whole work is cut into
+constexpr int kMinChunk = 8;        // tiles of a part at least
+constexpr float DLOG2E = 1.4426950408889634f;
+constexpr float DLN2 = 0.6931471805599453f;
+constexpr float DMIN = -3.0e38f;
+constexpr float DRESCALE = 8.f;
+
+struct DecodeArgs {
+    const void *q;
+    int64_t q_seq, q_tok, q_head;
+    int64_t C, T, Hkv, G, W;        // cells, new positions, heads, group, blocks per table row
+    int R, d;                       // rows of a cell
+    const uint8_t *kc, *vc, *k_exp, *v_exp;
+    int64_t n_blocks;
+    int shift;
+    const int32_t *table, *lens;
+    const float *scale;
+    void *o;
+    float *lse;
+    int parts_max;                  // workgroups per row group; 1 part per cell without a workspace
+    int2 *cells;                    // [C] first part and parts of a cell
+    float *part_o, *part_lse;       // [parts][R][d], [parts][R] (base 2)
+};
+
+__device__ __forceinline__ int cell_len(const DecodeArgs &a, int64_t c) {
+    const int64_t most = a.W << a.shift;
+    const int n = a.lens[c];
+    return n < 0 ? 0 : n > most ? (int)most : n;
+}
+
+// exclusive sum of one int per thread over the workgroup
+__device__ __forceinline__ int sum_before(int v, int *red, int *total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int x = v;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(x, off);
+        if (lane >= off) x += y;
+    }
+    if (lane == 63) red[w] = x;
+    __syncthreads();
+    int before = 0, sum = 0;
+#pragma unroll
+    for (int i = 0; i < DW; ++i) {
+        if (i < w) before += red[i];
+        sum += red[i];
+    }
+    __syncthreads();
+    *total = sum;
+    return x - v + before;
+}
+
+// This workgroup's cell, its part of it and the part's tiles; false if there is no such part.
+struct Part {
+    int64_t cell;
+    int part, parts, t0, t1;
+};
+__device__ __forceinline__ bool find_part(const DecodeArgs &a, Part *p) {
+    __shared__ int red[DW], found[4];
+    const int64_t run = (a.C + DTH - 1) / DTH, c0 = threadIdx.x * run;
+    const int64_t c1 = c0 + run < a.C ? c0 + run : a.C;
+    int tiles = 0, all;
+    for (int64_t c = c0; c < c1; ++c) tiles += (cell_len(a, c) + DT - 1) / DT;
+    sum_before(tiles, red, &all);
+    int chunk = (all + kTarget - 1) / kTarget;
+    if (chunk < kMinChunk) chunk = kMinChunk;
+    int mine = 0, total;
+    for (int64_t c = c0; c < c1; ++c) {
+        const int n = ((cell_len(a, c) + DT - 1) / DT + chunk - 1) / chunk;
+        mine += n ? n : 1;
+    }
+    int first = sum_before(mine, red, &total);
+    const int x = blockIdx.x;
+    if (x >= total) return false;
+    if (x >= first && x < first + mine) {
+        for (int64_t c = c0; c < c1; ++c) {
+            const int nt = (cell_len(a, c) + DT - 1) / DT, n = nt ? (nt + chunk - 1) / chunk : 1;
+            if (x < first + n) {
+                found[0] = (int)c, found[1] = x - first, found[2] = n, found[3] = nt;
+                if (x == first && blockIdx.y == 0) a.cells[c] = make_int2(first, n);
+                break;
+            }
+            first += n;
+        }
+    }
+    __syncthreads();
+    p->cell = found[0], p->part = found[1], p->parts = found[2];
+    p->t0 = p->part * chunk;
+    p->t1 = p->t0 + chunk < found[3] ? p->t0 + chunk : found[3];
+    return true;
+}
+
+__device__ __forceinline__ float pow2_byte(int b) { return __uint_as_float((uint32_t)(b < 1 ? 1 : b) << 23); }
+
+// eight codes to bf16, exactly
+__device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
+    const bf16x2 e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+    return (bf16x8){a[0], a[1], b[0], b[1], c[0], c[1], e[0], e[1]};
+}
+
+// x as the sum of NP bf16 values (1: rounded; 3: all bits)
+template <int NP>
+__device__ __forceinline__ void take_apart(float x, __bf16 (&y)[NP]) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        y[i] = (__bf16)x;
+        x -= (float)y[i];
+    }
+}
+
+template <typename T> __device__ __forceinline__ T dnarrow(float x);
+template <> __device__ __forceinline__ float dnarrow<float>(float x) { return x; }
+template <> __device__ __forceinline__ uint16_t dnarrow<uint16_t>(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// keeps the first n of a 16-byte piece's bytes
+__device__ __forceinline__ uint4 first_bytes(uint4 x, int n) {
+    const auto keep = [&](int at) -> uint32_t {
+        const int k = n - at;
+        return k >= 4 ? ~0u : k <= 0 ? 0u : (1u << (8 * k)) - 1u;
+    };
+    x.x &= keep(0), x.y &= keep(4), x.z &= keep(8), x.w &= keep(12);
+    return x;
+}
+// bytes that hold a NaN code (0x7f or 0xff) as 0xff, the others as 0
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t x) {
+    const uint32_t t = ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+    return (t >> 7) * 0xFFu;
+}
+
+template <typename T, int DP, int RT>
+__global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_part(DecodeArgs a) {
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1;
+    constexpr int KS = DP / 32, DB = DP / 16, KB = DP / 4;  // key steps, value tiles, key bytes of a lane
+    constexpr int KW = KB / 4;                               // the same in words
+    __shared__ float mrg[DW / 2][16 * RT * (DP + 2)];
+    Part p;
+    if (a.parts_max > 0) {
+        if (!find_part(a, &p)) return;
+    } else {
+        p.cell = blockIdx.x, p.part = 0, p.parts = 1, p.t0 = 0;
+        p.t1 = (cell_len(a, p.cell) + DT - 1) / DT;
+    }
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rl = lane & 15, g = lane >> 4;
+    const int64_t c = p.cell, seq = c / a.Hkv, h = c % a.Hkv;
+    const int len = cell_len(a, c);
+    const int r0 = blockIdx.y * 16 * RT;
+    const int32_t *row = a.table + c * a.W;
+    const float sl2 = (a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d))) * DLOG2E;
+
+    bf16x8 qf[RT][KS][NP];
+    int seen[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = r0 + 16 * rt + rl;
+        const int rc = r < a.R ? r : a.R - 1, tok = rc / (int)a.G;
+        seen[rt] = len - (int)(a.T - 1 - tok);
+        const T *qp = (const T *)a.q + seq * a.q_seq + tok * a.q_tok + (h * a.G + rc % (int)a.G) * a.q_head;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int col = KB * g + 8 * s + j;
+                __bf16 y[NP];
+                take_apart<NP>(col < a.d ? Elem<T>::load(qp, col) : 0.f, y);
+#pragma unroll
+                for (int n = 0; n < NP; ++n) qf[rt][s][n][j] = y[n];
+            }
+    }
+    const int fewest = len - (int)(a.T - 1);   // tokens that every row sees
+    const int bmask = (1 << a.shift) - 1;
+
+    f32x4 acc[RT][DB];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = DMIN, l[rt] = 0.f;
+#pragma unroll
+        for (int n = 0; n < DB; ++n) acc[rt][n] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    // pages of this lane's key rows (group rl / 4) and of its weights and values (group g)
+    const auto page = [&](int tok) -> int {
+        const int b = tok < len ? row[tok >> a.shift] : -1;
+        return b >= 0 && b < a.n_blocks ? b : -1;
+    };
+    for (int t = p.t0 + w; t < p.t1; t += DW) {
+        const int base = t * DT;
+        const int ktok = base + 16 * (rl / 4), vtok = base + 16 * g;
+        const int kp = page(ktok), vp = page(vtok);
+        const int kb = kp < 0 ? 0 : kp, vb = vp < 0 ? 0 : vp;
+        // keys: tile x of 16 rows, row rl = token 16 (rl / 4) + 4 x + rl % 4
+        __align__(16) uint32_t kr[4][KW];
+        const uint8_t *kp_ = a.kc + (((int64_t)kb << a.shift) + (ktok & bmask) + (rl & 3)) * DP + KB * g;
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int y = 0; y < KW; y += (KW % 4 == 0 ? 4 : 2)) {
+                if constexpr (KW % 4 == 0) *(uint4 *)&kr[x][y] = *(const uint4 *)(kp_ + 4 * x * DP + 4 * y);
+                else *(uint2 *)&kr[x][y] = *(const uint2 *)(kp_ + 4 * x * DP + 4 * y);
+            }
+        uint4 vr[DB];
+        const uint8_t *vp_ = a.vc + (((int64_t)vb * DP + rl) << a.shift) + (vtok & bmask);
+#pragma unroll
+        for (int n = 0; n < DB; ++n) vr[n] = *(const uint4 *)(vp_ + ((int64_t)(16 * n) << a.shift));
+        const float kf = sl2 * pow2_byte(a.k_exp[vb]), vf = pow2_byte(a.v_exp[vb]);
+
+        f32x4 s[RT][4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) s[rt][x] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int y = 0; y < KS; ++y) {
+                const bf16x8 kk = widen8(kr[x][2 * y], kr[x][2 * y + 1]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int n = NP - 1; n >= 0; --n)
+                        s[rt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qf[rt][y][n], s[rt][x], 0, 0, 0);
+            }
+        }
+        const bool masked = base + DT > fewest || __any(vp < 0);
+        if (masked) {
+            const int valid = vp < 0 ? 0 : len - vtok;
+#pragma unroll
+            for (int n = 0; n < DB; ++n) vr[n] = first_bytes(vr[n], valid);
+        }
+        bf16x8 pf[RT][2][NP];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int lim = vp < 0 ? 0 : seen[rt] - vtok;
+            float mt = DMIN;
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[rt][x][i] *= kf;
+                    if (masked && 4 * x + i >= lim) s[rt][x][i] = -INFINITY;
+                    mt = fmaxf(mt, s[rt][x][i]);
+                }
+            mt = fmaxf(mt, __shfl_xor(mt, 16));
+            mt = fmaxf(mt, __shfl_xor(mt, 32));
+            if (__any(mt > m[rt] + DRESCALE)) {
+                const float mn = fmaxf(m[rt], mt), al = __builtin_amdgcn_exp2f(m[rt] - mn);
+                m[rt] = mn;
+                l[rt] *= al;
+#pragma unroll
+                for (int n = 0; n < DB; ++n) acc[rt][n] *= al;
+            }
+            float sum = 0.f;
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(s[rt][x][i] - m[rt]);
+                    sum += e;
+                    __bf16 y[NP];
+                    take_apart<NP>(e * vf, y);
+#pragma unroll
+                    for (int n = 0; n < NP; ++n) pf[rt][x / 2][n][4 * (x % 2) + i] = y[n];
+                }
+            l[rt] += sum;
+        }
+        // A row's hidden tokens have weight 0, but 0 times a NaN code is a NaN: where new positions see
+        // different tokens, NaN codes go through marks of what each row sees instead.
+        bool bad = false;
+        if (masked && a.T > 1) {
+            uint32_t e = 0;
+#pragma unroll
+            for (int n = 0; n < DB; ++n) e |= nan_bytes(vr[n].x) | nan_bytes(vr[n].y) | nan_bytes(vr[n].z) | nan_bytes(vr[n].w);
+            bad = __any(e != 0);
+        }
+        if (bad) {
+#pragma unroll
+            for (int n = 0; n < DB; ++n) {
+                const uint4 z = {nan_bytes(vr[n].x), nan_bytes(vr[n].y), nan_bytes(vr[n].z), nan_bytes(vr[n].w)};
+                vr[n] = (uint4){vr[n].x & ~z.x, vr[n].y & ~z.y, vr[n].z & ~z.z, vr[n].w & ~z.w};
+                const bf16x8 z0 = widen8(z.x & 0x38383838u, z.y & 0x38383838u), z1 = widen8(z.z & 0x38383838u, z.w & 0x38383838u);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const int lim = vp < 0 ? 0 : seen[rt] - vtok;
+                    bf16x8 y0, y1;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        y0[i] = (__bf16)(i < lim ? 1.f : 0.f);
+                        y1[i] = (__bf16)(8 + i < lim ? 1.f : 0.f);
+                    }
+                    f32x4 u = {0.f, 0.f, 0.f, 0.f};
+                    u = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z0, y0, u, 0, 0, 0);
+                    u = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z1, y1, u, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (u[i] > 0.f) acc[rt][n][i] = __uint_as_float(0x7FC00000u);
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < DB; ++n) {
+            const bf16x8 v0 = widen8(vr[n].x, vr[n].y), v1 = widen8(vr[n].z, vr[n].w);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int x = NP - 1; x >= 0; --x) {
+                    acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[rt][0][x], acc[rt][n], 0, 0, 0);
+                    acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[rt][1][x], acc[rt][n], 0, 0, 0);
+                }
+        }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] += __shfl_xor(l[rt], 16);
+        l[rt] += __shfl_xor(l[rt], 32);
+    }
+    // join the waves, in a fixed order: the upper half writes, the lower half takes
+#pragma unroll
+    for (int half = DW / 2; half >= 1; half /= 2) {
+        if (w >= half && w < 2 * half) {
+            float *z = mrg[w - half];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+                for (int n = 0; n < DB; ++n)
+                    *(f32x4 *)(z + ((rt * DB + n) * 64 + lane) * 4) = acc[rt][n];
+                z[16 * RT * DP + 16 * rt + rl] = m[rt];
+                z[16 * RT * (DP + 1) + 16 * rt + rl] = l[rt];
+            }
+        }
+        __syncthreads();
+        if (w < half) {
+            const float *z = mrg[w];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float m2 = z[16 * RT * DP + 16 * rt + rl], l2 = z[16 * RT * (DP + 1) + 16 * rt + rl];
+                const float M = fmaxf(m[rt], m2);
+                const float f1 = __builtin_amdgcn_exp2f(m[rt] - M), f2 = __builtin_amdgcn_exp2f(m2 - M);
+                m[rt] = M;
+                l[rt] = l[rt] * f1 + l2 * f2;
+#pragma unroll
+                for (int n = 0; n < DB; ++n) {
+                    const f32x4 y = *(const f32x4 *)(z + ((rt * DB + n) * 64 + lane) * 4);
+                    acc[rt][n] = acc[rt][n] * f1 + y * f2;
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (w != 0) return;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = r0 + 16 * rt + rl;
+        if (r >= a.R) continue;
+        const float il = l[rt] > 0.f || l[rt] != l[rt] ? 1.f / l[rt] : 0.f;
+        const float lse2 = l[rt] == 0.f ? -INFINITY : m[rt] + __builtin_amdgcn_logf(l[rt]);
+        if (p.parts > 1) {
+            const int64_t at = (int64_t)blockIdx.x * a.R + r;
+#pragma unroll
+            for (int n = 0; n < DB; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (16 * n + 4 * g + i < a.d) a.part_o[at * a.d + 16 * n + 4 * g + i] = acc[rt][n][i] * il;
+            if (g == 0) a.part_lse[at] = lse2;
+        } else {
+            const int64_t at = ((seq * a.T + r / (int)a.G) * a.Hkv + h) * a.G + r % (int)a.G;
+#pragma unroll
+            for (int n = 0; n < DB; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (16 * n + 4 * g + i < a.d)
+                        ((T *)a.o)[at * a.d + 16 * n + 4 * g + i] = dnarrow<T>(acc[rt][n][i] * il);
+            if (g == 0 && a.lse) a.lse[at] = lse2 * DLN2;
+        }
+    }
+}
+
+// Joins the parts of every row whose cell has several; one wave per row.
+template <typename T>
+__global__ void __launch_bounds__(256) decode_join(DecodeArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (x >= a.C * a.R) return;
+    const int64_t c = x / a.R;
+    const int r = (int)(x % a.R);
+    const int2 ci = a.cells[c];
+    if (ci.y <= 1) return;
+    const float *pl = a.part_lse + (int64_t)ci.x * a.R + r;
+    float M = -INFINITY;
+    for (int s = 0; s < ci.y; ++s) M = fmaxf(M, pl[(int64_t)s * a.R]);
+    const float base = M == -INFINITY ? 0.f : M;
+    float sum = 0.f;
+    for (int s = 0; s < ci.y; ++s) sum += __builtin_amdgcn_exp2f(pl[(int64_t)s * a.R] - base);
+    const float is = sum == 0.f ? 0.f : 1.f / sum;
+    const int64_t seq = c / a.Hkv, h = c % a.Hkv, at = ((seq * a.T + r / (int)a.G) * a.Hkv + h) * a.G + r % (int)a.G;
+    for (int col = lane; col < a.d; col += 64) {
+        float y = 0.f;
+        for (int s = 0; s < ci.y; ++s) {
+            const float e = pl[(int64_t)s * a.R];
+            if (e != -INFINITY)
+                y = fmaf(__builtin_amdgcn_exp2f(e - base) * is, a.part_o[(((int64_t)ci.x + s) * a.R + r) * a.d + col], y);
+        }
+        ((T *)a.o)[at * a.d + col] = dnarrow<T>(y);
+    }
+    if (lane == 0 && a.lse) a.lse[at] = (M + (sum == 0.f ? 0.f : __builtin_amdgcn_logf(sum))) * DLN2;
+}
+
+template <typename T, int DP, int RT>
+void launch_part(const DecodeArgs &a, unsigned parts, hipStream_t st) {
+    const dim3 grid(parts, (unsigned)((a.R + 16 * RT - 1) / (16 * RT)));
+    hipLaunchKernelGGL((decode_part<T, DP, RT>), grid, dim3(DTH), 0, st, a);
+}
+
+template <typename T, int DP>
+void launch_rows(const DecodeArgs &a, unsigned parts, hipStream_t st) {
+    if constexpr (sizeof(T) == 4) {
+        launch_part<T, DP, 1>(a, parts, st);
+    } else {
+        if (a.R <= 16) launch_part<T, DP, 1>(a, parts, st);
+        else if (a.R <= 32 || DP > 128) launch_part<T, DP, 2>(a, parts, st);
+        else launch_part<T, DP, DP <= 128 ? 4 : 2>(a, parts, st);
+    }
+}
+
+template <typename T>
+void launch_width(const DecodeArgs &a, int dp, unsigned parts, hipStream_t st) {
+    switch (dp) {
+        case 32: launch_rows<T, 32>(a, parts, st); break;
+        case 64: launch_rows<T, 64>(a, parts, st); break;
+        case 96: launch_rows<T, 96>(a, parts, st); break;
+        case 128: launch_rows<T, 128>(a, parts, st); break;
+        case 192: launch_rows<T, 192>(a, parts, st); break;
+        default: launch_rows<T, 256>(a, parts, st); break;
+    }
+}
+
+// An upper bound of the parts: the lengths are on the device.  0 when no cell can have a second part.
+int64_t most_parts(int64_t C, int64_t W, int block_size) {
+    const int64_t tiles = (W * block_size + DT - 1) / DT, per_cell = (tiles + kMinChunk - 1) / kMinChunk;
+    if (per_cell <= 1) return 0;
+    return std::min(C + kTarget, C * per_cell);
+}
+}  // namespace
+
+size_t decode_ws_bytes(int64_t C, int64_t R, int64_t d, int64_t W, int block_size) {
+    const int64_t parts = most_parts(C, W, block_size);
+    return parts ? align_up(C * sizeof(int2), 256) + align_up(parts * R * d * 4, 256) + align_up(parts * R * 4, 256) : 0;
+}
+
+hipError_t launch_decode(const fw_cache &cache, int dtype, const void *q, int64_t S, int64_t T, int64_t Hq, int64_t Hkv,
+                         int64_t q_seq, int64_t q_tok, int64_t q_head, const int32_t *table, int64_t W,
+                         const int32_t *lens, const float *scale, void *o, float *lse, void *ws, hipStream_t st) {
+    DecodeArgs a{};
+    a.q = q, a.q_seq = q_seq, a.q_tok = q_tok, a.q_head = q_head;
+    a.C = S * Hkv, a.T = T, a.Hkv = Hkv, a.G = Hq / Hkv, a.W = W;
+    a.R = (int)(T * a.G), a.d = (int)cache.d;
+    a.kc = cache.k, a.vc = cache.v, a.k_exp = cache.k_exp, a.v_exp = cache.v_exp;
+    a.n_blocks = cache.n_blocks, a.shift = __builtin_ctz(cache.block_size);
+    a.table = table, a.lens = lens, a.scale = scale, a.o = o, a.lse = lse;
+    const int64_t parts = most_parts(a.C, W, cache.block_size);
+    a.parts_max = (int)parts;
+    if (parts) {
+        char *p = (char *)ws;
+        a.cells = (int2 *)p;
+        p += align_up(a.C * sizeof(int2), 256);
+        a.part_o = (float *)p;
+        p += align_up(parts * a.R * a.d * 4, 256);
+        a.part_lse = (float *)p;
+    }
+    const int dp = cache_row(cache.d);
+    const unsigned grid = (unsigned)(parts ? parts : a.C);
+    if (dtype == FW_F32) launch_width<float>(a, dp, grid, st);
+    else launch_width<uint16_t>(a, dp, grid, st);
+    if (parts) {
+        const dim3 jg((unsigned)((a.C * a.R + 3) / 4));
+        if (dtype == FW_F32) hipLaunchKernelGGL(decode_join<float>, jg, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL(decode_join<uint16_t>, jg, dim3(256), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace fw

@@ -1,0 +1,684 @@
+// Attention of packed prompts (fw_prompt_attention): for every query row i of
+// a sequence, over the keys j of the same sequence that it sees,
+//
+//   z_ij = scale_h <q_i, k_j>,  m_i = max_j z_ij,  l_i = sum_j exp(z_ij - m_i),
+//   o_i = sum_j exp(z_ij - m_i) v_j / l_i,   lse_i = m_i + log l_i
+//
+// in one pass over the keys with the running maximum and sum of the softmax
+// (all exponentials base 2 on log2e-scaled logits).  A row that sees no key
+// gives o = 0 and lse = -inf.
+//
+// The G query heads of a key/value head share its tiles: rows of a workgroup
+// are (position, head of the group) pairs, position-major, so short sequences
+// fill a tile G times better and a key tile is read once for all of them.
+//
+// Two kernels share this file: `prompt_mfma` (bf16 rows of 16-byte aligned
+// strides) and `prompt_general` (any type, width and stride; float32 MFMA).
+#include "fw_internal.hpp"
+
+namespace fw {
+
+namespace {
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float PLOG2E = 1.4426950408889634f;
+constexpr float PLN2 = 0.6931471805599453f;
+constexpr float PMIN = -3.0e38f;  // running maximum before any key (finite: differences stay defined)
+
+struct PromptArgs {
+    const void *q, *k, *v;
+    int64_t Tq, Tk, B, Hq, Hkv;
+    int d, G;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+    const int64_t *cu_q, *cu_k;
+    const float *scale;
+    int causal, splits;
+    void *o;          // [Tq][Hq][d] of the rows' type
+    float *lse;       // [Tq][Hq] or NULL
+    float *part_o;    // [splits][Tq][Hq][d] when splits > 1
+    float *part_lse;  // [splits][Tq][Hq] base-2
+};
+
+// The sequence of row tile x and the tile's place in it: tiles of `rows` rows,
+// the last tile of a sequence (the one that sees most keys) first.  Every wave
+// takes the tiles' prefix sum over 64 sequences at a time.  Lengths come from
+// the offsets clamped to the arrays, so no offset leads outside them.
+struct Tile {
+    int64_t q0, Lq, k0, Lk;  // first query row, query rows, first key, keys of the sequence
+    int64_t r0;              // first (position, head) row of the tile
+};
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t hi) { return x < 0 ? 0 : (x > hi ? hi : x); }
+
+__device__ __forceinline__ bool find_tile(const PromptArgs &a, int64_t x, int rows, Tile *t) {
+    const int lane = threadIdx.x & 63;
+    int64_t before = 0;
+    for (int64_t b0 = 0; b0 < a.B; b0 += 64) {
+        const int64_t b = b0 + lane;
+        int64_t q0 = 0, n = 0, tiles = 0;
+        if (b < a.B) {
+            q0 = clamp64(a.cu_q[b], a.Tq);
+            n = clamp64(a.cu_q[b + 1], a.Tq) - q0;
+            if (n < 0) n = 0;
+            tiles = (n * a.G + rows - 1) / rows;
+        }
+        int64_t upto = tiles;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int64_t y = __shfl_up(upto, off);
+            if (lane >= off) upto += y;
+        }
+        upto += before;
+        const unsigned long long hit = __ballot(x < upto);
+        if (hit) {
+            const int s = __ffsll(hit) - 1;
+            const int64_t bs = b0 + s;
+            t->q0 = __shfl(q0, s);
+            t->Lq = __shfl(n, s);
+            t->r0 = (__shfl(upto, s) - 1 - x) * rows;
+            t->k0 = clamp64(a.cu_k[bs], a.Tk);
+            const int64_t e = clamp64(a.cu_k[bs + 1], a.Tk);
+            t->Lk = e > t->k0 ? e - t->k0 : 0;
+            return true;
+        }
+        before = __shfl(upto, 63);
+    }
+    return false;
+}
+
+__device__ __forceinline__ float head_scale(const PromptArgs &a, int64_t h) {
+    return a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d));
+}
+
+template <typename T> __device__ __forceinline__ T narrow(float x);
+template <> __device__ __forceinline__ float narrow<float>(float x) { return x; }
+template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float x) {
+    return __builtin_bit_cast(uint16_t, (__bf16)x);  // to nearest, ties to even
+}
+
+// ---------------------------------------------------------------------------
+// General kernel: any strides, widths and both types, float32 throughout.
+// Four waves of 16 rows; key tiles of 32 in LDS as float32, rows and columns
+// past the sequence's end and past d as zeros.
+//   S^T = K Q^T on v_mfma_f32_16x16x4_f32: lane l holds row l % 16, keys
+//   4 (l / 16) + i of each 16-key half.  Since the order of a contraction is
+//   free, lane group l / 16 takes columns 16 j + 4 (l / 16) + s at step (j, s),
+//   so one 16-byte LDS read feeds four steps.
+//   O^T += V^T P^T: step i takes keys 4 (l / 16) + i, which is where the
+//   weights already are: they never leave their lane.
+// ---------------------------------------------------------------------------
+constexpr int GK = 32;    // keys per tile
+constexpr int GR = 64;    // rows per workgroup
+constexpr int GTH = 256;
+
+// Returns whether this thread saw an infinity or a NaN.
+template <typename T>
+__device__ __forceinline__ bool load_tile(float *dst, int ld, int dp, const T *src, int64_t row, int64_t left, int d,
+                                          bool vec) {
+    // `left` valid rows from src on
+    bool bad = false;
+    if (vec) {
+        const int ch = dp / 4;
+        for (int x = threadIdx.x; x < GK * ch; x += GTH) {
+            const int r = x / ch, c = 4 * (x % ch);
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+            if (r < left && c < d) {
+                const T *p = src + r * row + c;
+                if constexpr (sizeof(T) == 4) {
+                    y = *(const f32x4 *)p;
+                } else {
+                    const uint2 w = *(const uint2 *)p;
+                    y = (f32x4){__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u),
+                                __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u)};
+                }
+            }
+            *(f32x4 *)(dst + r * ld + c) = y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bad |= !(fabsf(y[i]) < INFINITY);
+        }
+    } else {
+        for (int x = threadIdx.x; x < GK * dp; x += GTH) {
+            const int r = x / dp, c = x % dp;
+            const float y = (r < left && c < d) ? Elem<T>::load(src, (size_t)(r * row + c)) : 0.f;
+            dst[r * ld + c] = y;
+            bad |= !(fabsf(y) < INFINITY);
+        }
+    }
+    return bad;
+}
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(GTH) prompt_general(PromptArgs a, int vec) {
+    constexpr int DP = 16 * NT, LD = DP + 4;
+    __shared__ __align__(16) float ks[GK * LD];
+    __shared__ __align__(16) float vs[GK * LD];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, rl = lane & 15, g = lane >> 4;
+    const int64_t h = blockIdx.x % a.Hkv;
+    const int split = blockIdx.y;
+    Tile t;
+    if (!find_tile(a, blockIdx.x / a.Hkv, GR, &t)) return;
+    const int64_t rows = t.Lq * a.G;
+    const int64_t r = t.r0 + 16 * w + rl;
+    const bool live = r < rows;
+    const int64_t rc = live ? r : rows - 1;
+    const int64_t pos = rc / a.G, head = h * a.G + rc % a.G;
+    const int64_t qrow = t.q0 + pos;
+    const T *qp = (const T *)a.q + qrow * a.q_row + head * a.q_head;
+    const T *kp = (const T *)a.k + t.k0 * a.k_row + h * a.k_head;
+    const T *vp = (const T *)a.v + t.k0 * a.v_row + h * a.v_head;
+    const float sl2 = head_scale(a, h) * PLOG2E;
+    float qf[4 * NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int c = 16 * j + 4 * g + s;
+            qf[4 * j + s] = c < a.d ? Elem<T>::load(qp, c) * sl2 : 0.f;
+        }
+    const int64_t seen = a.causal ? clamp64(pos + 1 + t.Lk - t.Lq, t.Lk) : t.Lk;
+    // keys that the last and the first row of the workgroup and of the wave see
+    const int64_t last = t.r0 + GR - 1 < rows ? t.r0 + GR - 1 : rows - 1;
+    const int64_t most = a.causal ? clamp64(last / a.G + 1 + t.Lk - t.Lq, t.Lk) : t.Lk;
+    const int64_t nt = (most + GK - 1) / GK;
+    const int64_t j0 = nt * split / a.splits, j1 = nt * (split + 1) / a.splits;
+    const int64_t wfirst = t.r0 + 16 * w < rows ? t.r0 + 16 * w : rows - 1;
+    const int64_t fewest = a.causal ? clamp64(wfirst / a.G + 1 + t.Lk - t.Lq, t.Lk) : t.Lk;
+
+    f32x4 acc[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    float m = PMIN, l = 0.f;
+    for (int64_t j = j0; j < j1; ++j) {
+        const int64_t key0 = j * GK;
+        __syncthreads();
+        load_tile<T>(ks, LD, DP, kp + key0 * a.k_row, a.k_row, t.Lk - key0, a.d, vec);
+        const bool bad = __syncthreads_or(load_tile<T>(vs, LD, DP, vp + key0 * a.v_row, a.v_row, t.Lk - key0, a.d, vec));
+        f32x4 s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            s[b] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const f32x4 kk = *(const f32x4 *)(ks + (16 * b + rl) * LD + 16 * n + 4 * g);
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[x], qf[4 * n + x], s[b], 0, 0, 0);
+            }
+        }
+        const bool masked = key0 + GK > fewest;
+        if (masked) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (key0 + 16 * b + 4 * g + i >= seen) s[b][i] = -INFINITY;
+        }
+        float mt = PMIN;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mt = fmaxf(mt, s[b][i]);
+        mt = fmaxf(mt, __shfl_xor(mt, 16));
+        mt = fmaxf(mt, __shfl_xor(mt, 32));
+        const float mn = fmaxf(m, mt), al = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        float sum = 0.f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[b][i] = __builtin_amdgcn_exp2f(s[b][i] - mn);
+                sum += s[b][i];
+            }
+        l = fmaf(l, al, sum);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[n] *= al;
+        if (!(bad && masked)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(vs[(16 * b + 4 * g + i) * LD + 16 * n + rl], s[b][i],
+                                                                      acc[n], 0, 0, 0);
+        } else {
+            // A hidden key's weight is 0, but 0 times an infinity or a NaN is a NaN.  The finite values go
+            // through the product, and whether a row sees an infinity of either sign (or a NaN, taken as
+            // both) in a column comes from products of 0 / 1 marks.
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f32x4 up = {0.f, 0.f, 0.f, 0.f}, dn = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float y = vs[(16 * b + 4 * g + i) * LD + 16 * n + rl];
+                        const float sees = key0 + 16 * b + 4 * g + i < seen ? 1.f : 0.f;
+                        const bool fin = fabsf(y) < INFINITY;
+                        acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(fin ? y : 0.f, s[b][i], acc[n], 0, 0, 0);
+                        up = __builtin_amdgcn_mfma_f32_16x16x4f32(!fin && !(y < 0.f) ? 1.f : 0.f, sees, up, 0, 0, 0);
+                        dn = __builtin_amdgcn_mfma_f32_16x16x4f32(!fin && !(y > 0.f) ? 1.f : 0.f, sees, dn, 0, 0, 0);
+                    }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    acc[n][i] += up[i] > 0.f ? INFINITY : 0.f;
+                    acc[n][i] -= dn[i] > 0.f ? INFINITY : 0.f;
+                }
+            }
+        }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (!live) return;
+    const float il = l > 0.f || l != l ? 1.f / l : 0.f;
+    const float lse2 = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
+    const int64_t orow = qrow * a.Hq + head;
+    if (a.splits > 1) {
+        const int64_t prow = (int64_t)split * a.Tq * a.Hq + orow;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = 16 * n + 4 * g + i;
+                if (c < a.d) a.part_o[prow * a.d + c] = acc[n][i] * il;
+            }
+        if (g == 0) a.part_lse[prow] = lse2;
+    } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = 16 * n + 4 * g + i;
+                if (c < a.d) ((T *)a.o)[orow * a.d + c] = narrow<T>(acc[n][i] * il);
+            }
+        if (g == 0 && a.lse) a.lse[orow] = lse2 * PLN2;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// bf16 kernel on the bf16 MFMA (d a multiple of 8 up to D, 16-byte aligned
+// rows).  Four waves of 32 rows; key and value tiles of 64 rows in a ring of
+// two LDS slots, filled by direct-to-LDS loads one tile ahead.
+//   S^T = K Q^T on v_mfma_f32_32x32x16_bf16: lane l holds row l % 32 and, of
+//   each 32-key half, keys 8 (i / 4) + 4 (l / 32) + i % 4, i < 16, so a row's
+//   maximum is taken in the lane and with one exchange of the wave's halves.
+//   O^T += V^T P^T: since the order of a contraction is free, step kb takes
+//   keys 16 kb + 4 (l / 32) + {0..3, 8..11}: the eight weights that the lane
+//   already holds, rounded to bf16 in place.  V is read transposed
+//   (ds_read_b64_tr_b16), four keys of one column per lane.
+// The weights are rounded to bf16 for the product (relative error up to
+// 2^-8 each, averaged over the row); their sum is taken in float32 before
+// the rounding.  The maximum that the exponentials are taken from may lag
+// the true one by up to 2^8 (RESCALE): the accumulators are rescaled only
+// when some row's maximum grew by more, and the weights keep bf16's relative
+// precision at any scale.
+// 16-byte chunk c of row r lies at chunk c ^ (r & 7) of its LDS row (keys) or
+// c ^ 2 (r & 7) (values, whose transposed reads take pairs of chunks), so the
+// eight or four rows that a read touches at once lie in different banks.
+// ---------------------------------------------------------------------------
+constexpr int PW = 4;            // waves per workgroup
+constexpr int PTH = 64 * PW;
+constexpr int PR = 32 * PW;      // rows per workgroup
+constexpr int PK = 64;           // keys per tile
+constexpr float RESCALE = 8.f;
+
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+#define P_LDS(p) ((__attribute__((address_space(3))) void *)(p))
+
+// Rows [0, left) of a head from base on; reads past them return zeros.
+__device__ __forceinline__ rsrc_t rows_rsrc(const char *base, int64_t left, uint32_t row_bytes, int d) {
+    int64_t n = left > 0 ? (left - 1) * row_bytes + 2 * d : 0;
+    if (n > 0x7FFFFFFF) n = 0x7FFFFFFF;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), (short)0, (int)n, 0x00020000);
+}
+
+__device__ __forceinline__ float half_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int D>
+__device__ __forceinline__ int v_swizzle(int r) {
+    return D == 64 ? 2 * ((r >> 1) & 3) : 2 * (r & 7);
+}
+
+template <int D>
+__global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs a) {
+    constexpr int RB = 2 * D;               // bytes of an LDS row
+    constexpr int TB = PK * RB;             // bytes of a tile
+    constexpr int RPI = 1024 / RB;          // rows of one 64-lane load
+    constexpr int NI = PK / RPI / PW;       // loads per wave and tile
+    constexpr int KS = D / 16, DB = D / 32;
+    extern __shared__ __align__(16) unsigned char psm[];
+    __shared__ int bad_tile[2];             // 1 + the last tile of each slot that holds a non-finite value
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rl = lane & 31, hh = lane >> 5;
+    const int64_t h = blockIdx.x % a.Hkv;
+    const int split = blockIdx.y;
+    Tile t;
+    if (!find_tile(a, blockIdx.x / a.Hkv, PR, &t)) return;
+    if (threadIdx.x < 2) bad_tile[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t rows = t.Lq * a.G;
+    const int64_t r = t.r0 + 32 * w + rl;
+    const bool live = r < rows;
+    const int64_t rc = live ? r : rows - 1;
+    const int64_t pos = rc / a.G, head = h * a.G + rc % a.G;
+    const int64_t qrow = t.q0 + pos;
+    float sl2 = head_scale(a, h) * PLOG2E;
+
+    // the lane's query row; a negative scale moves into its sign, a zero one into its values
+    bf16x8 qf[KS];
+    {
+        const uint16_t *qp = (const uint16_t *)a.q + qrow * a.q_row + head * a.q_head;
+        const uint32_t flip = sl2 < 0.f ? 0x80008000u : 0u, keep = sl2 == 0.f ? 0u : ~0u;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int c = 16 * s + 8 * hh;
+            uint4 x = {0u, 0u, 0u, 0u};
+            if (c < a.d) x = *(const uint4 *)(qp + c);
+            x.x = (x.x ^ flip) & keep, x.y = (x.y ^ flip) & keep, x.z = (x.z ^ flip) & keep, x.w = (x.w ^ flip) & keep;
+            qf[s] = __builtin_bit_cast(bf16x8, x);
+        }
+        sl2 = sl2 == 0.f ? 1.f : fabsf(sl2);
+    }
+    const auto sees = [&](int64_t row) -> int64_t {
+        return a.causal ? clamp64(row / a.G + 1 + t.Lk - t.Lq, t.Lk) : t.Lk;
+    };
+    const int64_t seen = sees(rc);
+    const int64_t end = t.r0 + PR < rows ? t.r0 + PR : rows;
+    const int64_t nt = (sees(end - 1) + PK - 1) / PK;
+    const int64_t j0 = nt * split / a.splits, j1 = nt * (split + 1) / a.splits;
+    const int64_t gfew = sees(t.r0);                       // keys that every row of the workgroup sees
+    const int64_t w0 = t.r0 + 32 * w;
+    const bool wlive = w0 < rows;
+    const int64_t wfew = wlive ? sees(w0) : 0;             // keys that every row of the wave sees
+    const int64_t wmost = wlive ? sees(w0 + 31 < rows ? w0 + 31 : rows - 1) : 0;
+
+    // direct-to-LDS loads: load i of a tile fills rows RPI i .. of the slot in lane order
+    const uint32_t krb = (uint32_t)(a.k_row * 2), vrb = (uint32_t)(a.v_row * 2);
+    const char *kb_ = (const char *)a.k + (t.k0 * a.k_row + h * a.k_head) * 2;
+    const char *vb_ = (const char *)a.v + (t.k0 * a.v_row + h * a.v_head) * 2;
+    uint32_t kvo, vvo;
+    {
+        const int lr = RPI * w + lane / (D / 8), p = lane % (D / 8);
+        const int kc = p ^ (lr & 7), vc = p ^ v_swizzle<D>(lr);
+        kvo = 8 * kc < a.d ? (uint32_t)lr * krb + 16 * kc : 0x80000000u;   // columns past d: out of range, zeros
+        vvo = 8 * vc < a.d ? (uint32_t)lr * vrb + 16 * vc : 0x80000000u;
+    }
+    const auto issue = [&](int64_t j) {
+        const int64_t key0 = j * PK;
+        unsigned char *slot = psm + (j & 1) * 2 * TB + w * 1024;
+        const rsrc_t kr = rows_rsrc(kb_ + key0 * krb, t.Lk - key0, krb, a.d);
+        const rsrc_t vr = rows_rsrc(vb_ + key0 * vrb, t.Lk - key0, vrb, a.d);
+#pragma unroll
+        for (int x = 0; x < NI; ++x)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, P_LDS(slot + x * PW * 1024), 16, kvo + x * (RPI * PW) * krb, 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < NI; ++x)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, P_LDS(slot + TB + x * PW * 1024), 16, vvo + x * (RPI * PW) * vrb, 0,
+                                                     0, 0);
+    };
+    // LDS reads: keys rl of a half, chunk 2 s + hh; values key 4 hh + (lane % 16) / 4, columns 16 ((lane / 16) % 2) + 4 (lane % 4)
+    const uint32_t kro = (uint32_t)(rl * RB + ((hh ^ (rl & 7)) * 16));
+    uint32_t vro;
+    {
+        const int key = 4 * hh + (lane & 15) / 4, c = 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
+        vro = (uint32_t)(TB + key * RB + ((c ^ v_swizzle<D>(key)) * 16) + 8 * (lane & 1));
+    }
+
+    f32x16 acc[DB];
+#pragma unroll
+    for (int n = 0; n < DB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
+    float m = PMIN, l = 0.f;
+    if (j0 < j1) issue(j0);
+    for (int64_t j = j0; j < j1; ++j) {
+        const int64_t key0 = j * PK;
+        unsigned char *slot = psm + (j & 1) * 2 * TB;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (key0 + PK > gfew) {
+            // some row does not see the whole tile: look for non-finite values in what this wave loaded
+            uint32_t e = 0;
+#pragma unroll
+            for (int x = 0; x < NI; ++x) {
+                const uint4 y = *(const uint4 *)(slot + TB + (x * PW + w) * 1024 + lane * 16);
+                e |= ((y.x & 0x7F807F80u) + 0x00800080u) | ((y.y & 0x7F807F80u) + 0x00800080u) |
+                     ((y.z & 0x7F807F80u) + 0x00800080u) | ((y.w & 0x7F807F80u) + 0x00800080u);
+            }
+            if (e & 0x80008000u) bad_tile[j & 1] = (int)(j + 1);
+        }
+        // every wave's loads of this tile have landed, and every wave is done with the other slot
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (j + 1 < j1) issue(j + 1);
+        if (key0 >= wmost) continue;
+        f32x16 s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < KS; ++c)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const bf16x8 kf = *(const bf16x8 *)(slot + b * 32 * RB + (kro ^ (c * 32)));
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], s[b], 0, 0, 0);
+            }
+        const bool masked = key0 + PK > wfew;
+        const int lim = (int)(seen - key0 < PK ? seen - key0 : PK) - 4 * hh;
+        if (masked) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (32 * b + 8 * (i / 4) + i % 4 >= lim) s[b][i] = -INFINITY;
+        }
+        float mt = s[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[b][i]);
+        mt = half_max(mt) * sl2;
+        if (__any(mt > m + RESCALE)) {
+            const float mn = fmaxf(m, mt), al = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= al;
+#pragma unroll
+            for (int n = 0; n < DB; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[n][i] *= al;
+        }
+        bf16x8 pf[4];
+        float sum = 0.f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[b][i], sl2, -m));
+                sum += p;
+                pf[2 * b + i / 8][i % 8] = (__bf16)p;
+            }
+        l += sum;
+        const auto value = [&](int kb, int n) -> bf16x8 {
+            const uint32_t at = (vro ^ (n * 64)) + kb * 16 * RB;
+            typedef __attribute__((address_space(3))) bf16x4 lds4;
+            const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)P_LDS(slot + at));
+            const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)P_LDS(slot + at + 8 * RB));
+            return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        if (!(masked && bad_tile[j & 1] == (int)(j + 1))) {
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int n = 0; n < DB; ++n)
+                    acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(kb, n), pf[kb], acc[n], 0, 0, 0);
+        } else {
+            // A hidden key's weight is 0, but 0 times an infinity or a NaN is a NaN.  The finite values go
+            // through the product, and whether a row sees an infinity of either sign (or a NaN, taken as
+            // both) in a column comes from products of 0 / 1 marks.
+#pragma unroll 1
+            for (int kb = 0; kb < 4; ++kb) {
+                bf16x8 sees_;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    sees_[i] = (__bf16)(32 * (kb / 2) + 8 * (2 * (kb % 2) + i / 4) + i % 4 < lim ? 1.f : 0.f);
+                const bf16x8 pk = kb == 0 ? pf[0] : kb == 1 ? pf[1] : kb == 2 ? pf[2] : pf[3];
+#pragma unroll
+                for (int n = 0; n < DB; ++n) {
+                    bf16x8 x = value(kb, n), up, dn;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float y = (float)x[i];
+                        const bool fin = fabsf(y) < INFINITY;
+                        up[i] = (__bf16)(!fin && !(y < 0.f) ? 1.f : 0.f);
+                        dn[i] = (__bf16)(!fin && !(y > 0.f) ? 1.f : 0.f);
+                        x[i] = fin ? x[i] : (__bf16)0.f;
+                    }
+                    acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pk, acc[n], 0, 0, 0);
+                    f32x16 z;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+                    const f32x16 u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up, sees_, z, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[n][i] += u[i] > 0.f ? INFINITY : 0.f;
+                    const f32x16 e = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dn, sees_, z, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[n][i] -= e[i] > 0.f ? INFINITY : 0.f;
+                }
+            }
+        }
+    }
+    {
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    }
+    if (!live) return;
+    const float il = l > 0.f || l != l ? 1.f / l : 0.f;
+    const float lse2 = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
+    const int64_t orow = qrow * a.Hq + head, prow = (int64_t)split * a.Tq * a.Hq + orow;
+#pragma unroll
+    for (int n = 0; n < DB; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = 32 * n + 8 * i + 4 * hh;
+            if (c >= a.d) continue;
+            f32x4 y;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[x] = acc[n][4 * i + x] * il;
+            if (a.splits > 1) {
+                *(f32x4 *)(a.part_o + prow * a.d + c) = y;
+            } else {
+                bf16x4 z;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) z[x] = (__bf16)y[x];
+                *(bf16x4 *)((uint16_t *)a.o + orow * a.d + c) = z;
+            }
+        }
+    if (hh == 0) {
+        if (a.splits > 1) a.part_lse[prow] = lse2;
+        else if (a.lse) a.lse[orow] = lse2 * PLN2;
+    }
+}
+
+// Joins the splits of every row: o = sum_s 2^(e_s - M) o_s / sum_s 2^(e_s - M).
+// One wave per (position, head); rows outside the sequences stay as they are.
+template <typename T>
+__global__ void __launch_bounds__(256) prompt_join(PromptArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), n = a.Tq * a.Hq;
+    if (row >= n) return;
+    const int64_t pos = row / a.Hq;
+    if (pos < a.cu_q[0] || pos >= a.cu_q[a.B]) return;
+    float M = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) M = fmaxf(M, a.part_lse[s * n + row]);
+    const float base = M == -INFINITY ? 0.f : M;
+    float sum = 0.f;
+    for (int s = 0; s < a.splits; ++s) sum += __builtin_amdgcn_exp2f(a.part_lse[s * n + row] - base);
+    const float is = sum == 0.f ? 0.f : 1.f / sum;
+    for (int c = lane; c < a.d; c += 64) {
+        float y = 0.f;
+        for (int s = 0; s < a.splits; ++s) {
+            const float e = a.part_lse[s * n + row];
+            if (e != -INFINITY) y = fmaf(__builtin_amdgcn_exp2f(e - base) * is, a.part_o[(s * n + row) * a.d + c], y);
+        }
+        ((T *)a.o)[row * a.d + c] = narrow<T>(y);
+    }
+    if (lane == 0 && a.lse) a.lse[row] = (M + (sum == 0.f ? 0.f : __builtin_amdgcn_logf(sum))) * PLN2;
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+bool prompt_fast(const fw_packed &p) {
+    const auto ok = [](const void *x, int64_t row, int64_t head, int64_t d) {
+        return (uintptr_t)x % 16 == 0 && row % 8 == 0 && head % 8 == 0 && row >= d && row < ((int64_t)1 << 23);
+    };
+    return p.dtype == FW_BF16 && p.d % 8 == 0 && ok(p.q, p.q_row, p.q_head, 0) && ok(p.k, p.k_row, p.k_head, p.d) &&
+           ok(p.v, p.v_row, p.v_head, p.d);
+}
+
+int64_t row_tiles(const fw_packed &p, int rows) {  // an upper bound: the lengths are on the device
+    return (p.Tq * (p.Hq / p.Hkv) + rows - 1) / rows + p.B;
+}
+
+template <typename T>
+void launch_general(const PromptArgs &a, int vec, dim3 grid, hipStream_t st) {
+    const int nt = (a.d + 15) / 16;
+#define FW_G(n) hipLaunchKernelGGL((prompt_general<T, n>), grid, dim3(GTH), 0, st, a, vec)
+    if (nt <= 2) FW_G(2);
+    else if (nt <= 4) FW_G(4);
+    else if (nt <= 5) FW_G(5);
+    else if (nt <= 8) FW_G(8);
+    else FW_G(16);
+#undef FW_G
+}
+}  // namespace
+
+// Ranges that a row's keys are split into: one when the row tiles fill the
+// card twice over (two workgroups to a compute unit), otherwise as many as
+// fill it, with at least 256 keys of an average sequence to each.
+int prompt_splits(const fw_packed &p) {
+    const int64_t tiles = row_tiles(p, prompt_fast(p) ? PR : GR) * p.Hkv;
+    const int64_t fill = 512 / (tiles > 0 ? tiles : 1), keys = p.Tk / (p.B > 0 ? p.B : 1) / 256;
+    int64_t s = fill < keys ? fill : keys;
+    return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
+}
+
+hipError_t launch_prompt(const fw_packed &p, void *o, float *lse, int splits, float *part_o, float *part_lse,
+                         hipStream_t st) {
+    PromptArgs a{};
+    a.q = p.q, a.k = p.k, a.v = p.v;
+    a.Tq = p.Tq, a.Tk = p.Tk, a.B = p.B, a.Hq = p.Hq, a.Hkv = p.Hkv;
+    a.d = (int)p.d, a.G = (int)(p.Hq / p.Hkv);
+    a.q_row = p.q_row, a.q_head = p.q_head, a.k_row = p.k_row, a.k_head = p.k_head, a.v_row = p.v_row, a.v_head = p.v_head;
+    a.cu_q = p.cu_q, a.cu_k = p.cu_k, a.scale = p.scale;
+    a.causal = p.causal, a.splits = splits;
+    a.o = o, a.lse = lse, a.part_o = part_o, a.part_lse = part_lse;
+    if (prompt_fast(p)) {
+        const dim3 grid((unsigned)(row_tiles(p, PR) * p.Hkv), (unsigned)splits);
+        const int D = a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256;
+        const size_t lds = (size_t)2 * 2 * PK * 2 * D;
+        if (D == 64) hipLaunchKernelGGL((prompt_mfma<64>), grid, dim3(PTH), lds, st, a);
+        else if (D == 128) hipLaunchKernelGGL((prompt_mfma<128>), grid, dim3(PTH), lds, st, a);
+        else hipLaunchKernelGGL((prompt_mfma<256>), grid, dim3(PTH), lds, st, a);
+    } else {
+        const dim3 grid((unsigned)(row_tiles(p, GR) * p.Hkv), (unsigned)splits);
+        const int size = p.dtype == FW_F32 ? 4 : 2, q = 4;
+        const int vec = p.d % q == 0 && p.k_row % q == 0 && p.k_head % q == 0 && p.v_row % q == 0 && p.v_head % q == 0 &&
+                        (uintptr_t)p.k % (4 * size) == 0 && (uintptr_t)p.v % (4 * size) == 0;
+        if (p.dtype == FW_F32) launch_general<float>(a, vec, grid, st);
+        else launch_general<uint16_t>(a, vec, grid, st);
+    }
+    if (splits > 1) {
+        const dim3 grid((unsigned)((p.Tq * p.Hq + 3) / 4));
+        if (p.dtype == FW_F32) hipLaunchKernelGGL(prompt_join<float>, grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL(prompt_join<uint16_t>, grid, dim3(256), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace fw

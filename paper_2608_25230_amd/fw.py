@@ -7,7 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Dict, Optional, Sequence
+from typing import Any, Dict, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -18,7 +18,8 @@ FW_F32, FW_BF16 = 0, 1
 STATUS = {0: "FW_OK", 1: "FW_E_NULL", 2: "FW_E_SHAPE", 3: "FW_E_DTYPE", 4: "FW_E_UNSUPPORTED",
           5: "FW_E_WORKSPACE", 6: "FW_E_HIP"}
 ENTRY_POINTS = ("fw_dense_topk", "fw_best_subset", "fw_swap", "fw_dropped_mass_curve",
-                "fw_ragged_compact", "fw_pool_subset", "fw_group_vote", "fw_maxpool_scores")
+                "fw_ragged_compact", "fw_pool_subset", "fw_group_vote", "fw_maxpool_scores",
+                "fw_prompt_attention", "fw_block_tables", "fw_cache_store", "fw_cache_attention")
 # entry points that take no workspace: their scratch is a static device array
 NOALLOC_ENTRY_POINTS = ("fw_dense_topk_noalloc",)
 # columns of fw_pool_subset's stats (FW_POOL_* in include/fw.h)
@@ -39,10 +40,26 @@ class Rows(ctypes.Structure):
                 ("bias", ctypes.c_void_p)]
 
 
+class Packed(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("Tq", ctypes.c_int64), ("Tk", ctypes.c_int64), ("B", ctypes.c_int64), ("Hq", ctypes.c_int64),
+                ("Hkv", ctypes.c_int64), ("d", ctypes.c_int64), ("q_row", ctypes.c_int64), ("q_head", ctypes.c_int64),
+                ("k_row", ctypes.c_int64), ("k_head", ctypes.c_int64), ("v_row", ctypes.c_int64),
+                ("v_head", ctypes.c_int64), ("cu_q", ctypes.c_void_p), ("cu_k", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p), ("causal", ctypes.c_int32)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("n_blocks", ctypes.c_int64), ("d", ctypes.c_int64), ("block_size", ctypes.c_int32)]
+
+
 _lib = None
 P = ctypes.c_void_p
 I32, I64, SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 RP = ctypes.POINTER(Rows)
+PP = ctypes.POINTER(Packed)
+CP = ctypes.POINTER(Cache)
 
 _SIGS = {
     "fw_dense_topk_workspace_size": (SZ, [RP, P, I32]),
@@ -62,6 +79,15 @@ _SIGS = {
     "fw_pool_subset": (I32, [RP, I32, P, P, I32, I32, P, P, P, P, P, P, ctypes.c_float, P, P, P, SZ, P]),
     "fw_group_vote_workspace_size": (SZ, [RP, I32, I32]),
     "fw_group_vote": (I32, [RP, I32, I32, P, P, P, P, P, SZ, P]),
+    "fw_prompt_attention_workspace_size": (SZ, [PP]),
+    "fw_prompt_attention": (I32, [PP, P, P, P, SZ, P]),
+    "fw_block_tables_workspace_size": (SZ, [I64]),
+    "fw_block_tables": (I32, [I64, P, P, I32, I64, P, I64, P, P, I64, P, P, P, P, P, SZ, P]),
+    "fw_cache_row": (I32, [I64]),
+    "fw_cache_store_workspace_size": (SZ, [CP, I64]),
+    "fw_cache_store": (I32, [CP, I32, P, I64, P, I64, I64, P, P, SZ, P]),
+    "fw_cache_attention_workspace_size": (SZ, [CP, I64, I64, I64, I64, I64]),
+    "fw_cache_attention": (I32, [CP, I32, P, I64, I64, I64, I64, I64, I64, I64, P, I64, P, P, P, P, P, SZ, P]),
     "fw_last_error": (ctypes.c_char_p, []),
     "fw_version": (ctypes.c_char_p, []),
 }
@@ -339,6 +365,225 @@ def ragged_compact(k, v, importance, budget: int, floor: int, heads_per_layer: i
                                out["v_out"].data_ptr(), out["tau"].data_ptr(),
                                out["dropped"].data_ptr(), out["bytes_held"].data_ptr(),
                                ws.data_ptr(), ws.numel(), _stream()))
+    out["_ws"] = ws
+    return out
+
+
+# ---------------------------------------------------------------------------
+# serving: prompt attention, block tables, the 8-bit cache
+#
+# These calls run on the current stream of their tensors' device, whichever
+# device is current, and refuse tensors of different devices.
+# ---------------------------------------------------------------------------
+
+class KvCache(NamedTuple):
+    """Buffers of an 8-bit cache (fw_cache in include/fw.h): k [n_blocks][block_size][dp] and v
+    [n_blocks][dp][block_size] e4m3 codes, k_exp and v_exp [n_blocks] exponent bytes, all torch.uint8, and the width
+    d of its rows.  ``kv_cache`` makes an empty one."""
+    k: Any
+    v: Any
+    k_exp: Any
+    v_exp: Any
+    d: int
+
+    @property
+    def block_size(self) -> int:
+        return self.k.shape[1]
+
+
+def cache_row(d: int) -> int:
+    """Bytes of a cached key's row: d rounded up to 32, 64, 96, 128, 192 or 256."""
+    return lib().fw_cache_row(d)
+
+
+def kv_cache(n_blocks: int, block_size: int, d: int, device="cuda") -> KvCache:
+    torch = _torch()
+    dp = cache_row(d)
+    if dp == 0:
+        raise FwError(2, f"d must be in [1, 256], got {d}")
+    z = lambda *s: torch.zeros(*s, dtype=torch.uint8, device=device)
+    return KvCache(z(n_blocks, block_size, dp), z(n_blocks, dp, block_size), z(n_blocks), z(n_blocks), d)
+
+
+class _on:
+    """The device of the tensors made current, if it is not; its current stream."""
+
+    def __init__(self, t):
+        cuda = _torch().cuda
+        self.device = t.device
+        self.guard = None if cuda.current_device() == t.device.index else cuda.device(t.device)
+        self.stream = cuda.current_stream(t.device).cuda_stream
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.stream
+
+    def __exit__(self, *e):
+        if self.guard is not None:
+            self.guard.__exit__(*e)
+
+
+def _want(name: str, t, dtype, dim: int, device) -> None:
+    """A contiguous tensor of this type, dimensions and device."""
+    if t.dtype is not dtype or t.dim() != dim or t.device != device or not t.is_contiguous():
+        raise FwError(2, f"{name} must be a contiguous {dim}-dimensional {dtype} tensor on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _rows_of(name: str, t, dtype, dim: int, device) -> None:
+    """Rows with contiguous columns; the other dimensions may be strided."""
+    if t.dtype is not dtype or t.dim() != dim or t.device != device or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise FwError(2, f"{name} must be a {dim}-dimensional {dtype} tensor on {device} with contiguous columns, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _gpu(name: str, t) -> None:
+    if not t.is_cuda:
+        raise FwError(2, f"{name} must be a device tensor")
+
+
+def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=None, want_lse=True,
+                     ws=None) -> Dict[str, object]:
+    """Attention of packed sequences: q [Tq][Hq][d], k and v [Tk][Hkv][d] (strided views of a fused projection are
+    fine), cu_q and cu_k [B+1] int64 offsets (cu_k defaults to cu_q).  Returns o [Tq][Hq][d] of q's type and lse
+    [Tq][Hq] float32.  Rows outside the sequences are left unwritten."""
+    torch = _torch()
+    _gpu("q", q)
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(q)
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        _rows_of(name, t, dt, 3, dev)
+    if cu_k is None:
+        cu_k = cu_q
+    _want("cu_q", cu_q, torch.int64, 1, dev)
+    _want("cu_k", cu_k, torch.int64, 1, dev)
+    Tq, Hq, d = q.shape
+    Tk, Hkv, _ = k.shape
+    if k.shape != v.shape or k.shape[2] != d or cu_q.shape != cu_k.shape:
+        raise FwError(2, f"k and v must be [Tk][Hkv][{d}] alike and cu_q, cu_k [B+1] alike, got {tuple(k.shape)}, "
+                         f"{tuple(v.shape)}, {tuple(cu_q.shape)}, {tuple(cu_k.shape)}")
+    if scale is not None:
+        _want("scale", scale, torch.float32, 1, dev)
+        if scale.shape[0] != Hkv:
+            raise FwError(2, f"scale must be [{Hkv}]")
+    q_row, q_head, _ = q.stride()
+    k_row, k_head, _ = k.stride()
+    v_row, v_head, _ = v.stride()
+    p = Packed(code, q.data_ptr(), k.data_ptr(), v.data_ptr(), Tq, Tk, cu_q.shape[0] - 1, Hq, Hkv, d, q_row, q_head,
+               k_row, k_head, v_row, v_head, cu_q.data_ptr(), cu_k.data_ptr(), _ptr(scale), 1 if causal else 0)
+    L, ref = lib(), ctypes.byref(p)
+    with _on(q) as stream:
+        out = {"o": torch.empty((Tq, Hq, d), dtype=dt, device=dev),
+               "lse": torch.empty((Tq, Hq), dtype=torch.float32, device=dev) if want_lse else None}
+        need = L.fw_prompt_attention_workspace_size(ref)
+        if need and (ws is None or ws.numel() < need):
+            ws = _workspace(need, dev)
+        _check(L.fw_prompt_attention(ref, out["o"].data_ptr(), _ptr(out["lse"]), _ptr(ws),
+                                     0 if ws is None else ws.numel(), stream))
+    out["_ws"] = ws
+    return out
+
+
+def block_tables(old_len, new_len, table, free_list, n_free, block_size: int, *, n_slots: int, lens=None,
+                 ws=None) -> Dict[str, object]:
+    """Takes every cell from old_len to new_len tokens (int32 [C]): table [C][max_blocks], free_list [n_blocks] and
+    n_free [1] (int32) change in place.  n_slots: tokens that come, of refused cells too.  Returns slots [n_slots]
+    int64, offsets [C+1] int64, lens [C] int32 (in `lens`, which may be old_len, if given) and refused [1] int32."""
+    torch = _torch()
+    _gpu("table", table)
+    dev = table.device
+    i32 = torch.int32
+    _want("table", table, i32, 2, dev)
+    for name, t in (("old_len", old_len), ("new_len", new_len), ("free_list", free_list), ("n_free", n_free)):
+        _want(name, t, i32, 1, dev)
+    C, W = table.shape
+    if lens is not None:
+        _want("lens", lens, i32, 1, dev)
+    if old_len.shape[0] != C or new_len.shape[0] != C or n_free.shape[0] != 1 or (lens is not None and lens.shape[0] != C):
+        raise FwError(2, f"old_len, new_len and lens must be [{C}] and n_free [1]")
+    L = lib()
+    with _on(table) as stream:
+        out = {"slots": torch.empty(max(n_slots, 0), dtype=torch.int64, device=dev),
+               "offsets": torch.empty(C + 1, dtype=torch.int64, device=dev),
+               "lens": torch.empty(C, dtype=i32, device=dev) if lens is None else lens,
+               "refused": torch.empty(1, dtype=i32, device=dev)}
+        need = L.fw_block_tables_workspace_size(C)
+        if ws is None or ws.numel() < need:
+            ws = _workspace(need, dev)
+        _check(L.fw_block_tables(C, old_len.data_ptr(), new_len.data_ptr(), block_size, W, table.data_ptr(),
+                                 free_list.shape[0], free_list.data_ptr(), n_free.data_ptr(), n_slots,
+                                 out["slots"].data_ptr(), out["offsets"].data_ptr(), out["lens"].data_ptr(),
+                                 out["refused"].data_ptr(), ws.data_ptr(), ws.numel(), stream))
+    out["_ws"] = ws
+    return out
+
+
+def _cache(c: KvCache, device) -> Cache:
+    u8 = _torch().uint8
+    _want("cache.k", c.k, u8, 3, device)
+    _want("cache.v", c.v, u8, 3, device)
+    _want("cache.k_exp", c.k_exp, u8, 1, device)
+    _want("cache.v_exp", c.v_exp, u8, 1, device)
+    n, bs, dp = c.k.shape
+    if dp != cache_row(c.d) or c.v.shape != (n, dp, bs) or c.k_exp.shape[0] != n or c.v_exp.shape[0] != n:
+        raise FwError(2, f"the cache's buffers do not fit together: k {tuple(c.k.shape)}, v {tuple(c.v.shape)}, "
+                         f"k_exp {tuple(c.k_exp.shape)}, v_exp {tuple(c.v_exp.shape)}, d {c.d}")
+    return Cache(c.k.data_ptr(), c.v.data_ptr(), c.k_exp.data_ptr(), c.v_exp.data_ptr(), n, c.d, bs)
+
+
+def cache_store(cache: KvCache, k, v, slots) -> None:
+    """Rounds rows k and v [N][d] to the cache's blocks at slots [N] int64 (``block_tables``; rows with a slot out of
+    range are skipped).  The rows of one block are consecutive, with consecutive slots."""
+    torch = _torch()
+    _gpu("k", k)
+    dev, dt = k.device, k.dtype
+    code = _dtype_code(k)
+    _rows_of("k", k, dt, 2, dev)
+    _rows_of("v", v, dt, 2, dev)
+    _want("slots", slots, torch.int64, 1, dev)
+    if k.shape != v.shape or k.shape[0] != slots.shape[0] or k.shape[1] != cache.d:
+        raise FwError(2, f"k and v must be [N][{cache.d}] and slots [N], got {tuple(k.shape)}, {tuple(v.shape)}, "
+                         f"{tuple(slots.shape)}")
+    c = _cache(cache, dev)
+    with _on(k) as stream:
+        _check(lib().fw_cache_store(ctypes.byref(c), code, k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
+                                    k.shape[0], slots.data_ptr(), None, 0, stream))
+
+
+def cache_attention(q, cache: KvCache, table, lens, *, scale=None, want_lse=True, ws=None) -> Dict[str, object]:
+    """Attention of T new positions over each cell's cached tokens, their own included: q [S][T][Hq][d] (strided
+    views are fine), table [S*Hkv][max_blocks] and lens [S*Hkv] int32.  Returns o [S][T][Hq][d] of q's type and lse
+    [S][T][Hq] float32."""
+    torch = _torch()
+    _gpu("q", q)
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(q)
+    _rows_of("q", q, dt, 4, dev)
+    _want("table", table, torch.int32, 2, dev)
+    _want("lens", lens, torch.int32, 1, dev)
+    S, T, Hq, d = q.shape
+    C, W = table.shape
+    if S < 1 or C % S or lens.shape[0] != C or d != cache.d:
+        raise FwError(2, f"table must be [S*Hkv][max_blocks], lens [S*Hkv] and q [S][T][Hq][{cache.d}], got "
+                         f"{tuple(table.shape)}, {tuple(lens.shape)}, {tuple(q.shape)}")
+    Hkv = C // S
+    if scale is not None:
+        _want("scale", scale, torch.float32, 1, dev)
+        if scale.shape[0] != Hkv:
+            raise FwError(2, f"scale must be [{Hkv}]")
+    c = _cache(cache, dev)
+    L, ref = lib(), ctypes.byref(c)
+    q_seq, q_tok, q_head, _ = q.stride()
+    with _on(q) as stream:
+        out = {"o": torch.empty((S, T, Hq, d), dtype=dt, device=dev),
+               "lse": torch.empty((S, T, Hq), dtype=torch.float32, device=dev) if want_lse else None}
+        need = L.fw_cache_attention_workspace_size(ref, S, T, Hq, Hkv, W)
+        if need and (ws is None or ws.numel() < need):
+            ws = _workspace(need, dev)
+        _check(L.fw_cache_attention(ref, code, q.data_ptr(), S, T, Hq, Hkv, q_seq, q_tok, q_head, table.data_ptr(), W,
+                                    lens.data_ptr(), _ptr(scale), out["o"].data_ptr(), _ptr(out["lse"]), _ptr(ws),
+                                    0 if ws is None else ws.numel(), stream))
     out["_ws"] = ws
     return out
 
