@@ -356,7 +356,7 @@ fw_status fw_maxpool_scores(const float *scores, int64_t H, int64_t n, int32_t k
  *   causal non-zero: query i of Lq sees keys 0 .. i + Lk - Lq (the last query
  *          sees every key); zero: every key of its sequence
  * Limits: B, Hkv, d >= 1, Tq, Tk >= 0; Hkv divides Hq; d <= 256;
- * Tq*Hq < 2^31; Tk < 2^31; strides >= 0 and below 2^31. */
+ * Tq*Hq < 2^31; Tk <= 2^30; strides >= 0 and below 2^31. */
 typedef struct fw_packed {
     int32_t dtype;
     const void *q, *k, *v;

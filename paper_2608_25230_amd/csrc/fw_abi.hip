@@ -462,8 +462,8 @@ fw_status check_packed(const fw_packed *p) {
         return fail(FW_E_SHAPE, "Hkv must divide Hq (Hq=%lld Hkv=%lld)", (long long)p->Hq, (long long)p->Hkv);
     if (p->d < 1 || p->d > 256) return fail(FW_E_SHAPE, "d must be in [1, 256], got %lld", (long long)p->d);
     constexpr int64_t most = (int64_t)1 << 31;
-    if (p->Hq >= most || p->Tq >= most || p->Tk >= most || p->B >= most || p->Tq * p->Hq >= most)
-        return fail(FW_E_SHAPE, "Tq*Hq, Tk and B must be < 2^31");
+    if (p->Hq >= most || p->Tq >= most || p->Tk > (1ll << 30) || p->B >= most || p->Tq * p->Hq >= most)
+        return fail(FW_E_SHAPE, "need Tq*Hq < 2^31, Tk <= 2^30 and B < 2^31");
     // one workgroup per row tile and key/value head, 64 rows or more to a tile
     if ((p->Tq * (p->Hq / p->Hkv) / 64 + 1 + p->B) >= most / p->Hkv)
         return fail(FW_E_SHAPE, "too many sequences and heads for one call");

@@ -14,6 +14,8 @@
 //
 // Two kernels share this file: `prompt_mfma` (bf16 rows of 16-byte aligned
 // strides) and `prompt_general` (any type, width and stride; float32 MFMA).
+#include <type_traits>
+
 #include "fw_internal.hpp"
 
 namespace fw {
@@ -30,8 +32,8 @@ constexpr float PMIN = -3.0e38f;  // running maximum before any key (finite: dif
 
 struct PromptArgs {
     const void *q, *k, *v;
-    int64_t Tq, Tk, B, Hq, Hkv;
-    int d, G;
+    int64_t Tq, Tk, B;
+    int Hq, Hkv, d, G;
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;
     const int64_t *cu_q, *cu_k;
     const float *scale;
@@ -44,46 +46,47 @@ struct PromptArgs {
 
 // The sequence of row tile x and the tile's place in it: tiles of `rows` rows,
 // the last tile of a sequence (the one that sees most keys) first.  Every wave
-// takes the tiles' prefix sum over 64 sequences at a time.  Lengths come from
-// the offsets clamped to the arrays, so no offset leads outside them.
+// takes the tiles' prefix sum over 64 sequences at a time; the result is
+// wave-uniform and read into scalars.  Lengths come from the offsets clamped
+// to the arrays, so no offset leads outside them.
 struct Tile {
-    int64_t q0, Lq, k0, Lk;  // first query row, query rows, first key, keys of the sequence
-    int64_t r0;              // first (position, head) row of the tile
+    int q0, Lq, k0, Lk;  // first query position, queries, first key, keys of the sequence
+    int r0;              // first (position, head) row of the tile
 };
-__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t hi) { return x < 0 ? 0 : (x > hi ? hi : x); }
+__device__ __forceinline__ int clamp_off(int64_t x, int64_t hi) { return (int)(x < 0 ? 0 : (x > hi ? hi : x)); }
+__device__ __forceinline__ int clampi(int x, int hi) { return x < 0 ? 0 : (x > hi ? hi : x); }
 
-__device__ __forceinline__ bool find_tile(const PromptArgs &a, int64_t x, int rows, Tile *t) {
+__device__ __forceinline__ bool find_tile(const PromptArgs &a, int x, int rows, Tile *t) {
     const int lane = threadIdx.x & 63;
-    int64_t before = 0;
+    int before = 0;
     for (int64_t b0 = 0; b0 < a.B; b0 += 64) {
         const int64_t b = b0 + lane;
-        int64_t q0 = 0, n = 0, tiles = 0;
+        int q0 = 0, n = 0, tiles = 0;
         if (b < a.B) {
-            q0 = clamp64(a.cu_q[b], a.Tq);
-            n = clamp64(a.cu_q[b + 1], a.Tq) - q0;
+            q0 = clamp_off(a.cu_q[b], a.Tq);
+            n = clamp_off(a.cu_q[b + 1], a.Tq) - q0;
             if (n < 0) n = 0;
-            tiles = (n * a.G + rows - 1) / rows;
+            tiles = (int)(((uint32_t)(n * a.G) + rows - 1) / rows);
         }
-        int64_t upto = tiles;
+        int upto = tiles;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
-            const int64_t y = __shfl_up(upto, off);
+            const int y = __shfl_up(upto, off);
             if (lane >= off) upto += y;
         }
         upto += before;
         const unsigned long long hit = __ballot(x < upto);
         if (hit) {
             const int s = __ffsll(hit) - 1;
-            const int64_t bs = b0 + s;
-            t->q0 = __shfl(q0, s);
-            t->Lq = __shfl(n, s);
-            t->r0 = (__shfl(upto, s) - 1 - x) * rows;
-            t->k0 = clamp64(a.cu_k[bs], a.Tk);
-            const int64_t e = clamp64(a.cu_k[bs + 1], a.Tk);
+            t->q0 = __builtin_amdgcn_readlane(q0, s);
+            t->Lq = __builtin_amdgcn_readlane(n, s);
+            t->r0 = (__builtin_amdgcn_readlane(upto, s) - 1 - x) * rows;
+            t->k0 = clamp_off(a.cu_k[b0 + s], a.Tk);
+            const int e = clamp_off(a.cu_k[b0 + s + 1], a.Tk);
             t->Lk = e > t->k0 ? e - t->k0 : 0;
             return true;
         }
-        before = __shfl(upto, 63);
+        before = __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
 }
@@ -155,15 +158,15 @@ __global__ void __launch_bounds__(GTH) prompt_general(PromptArgs a, int vec) {
     __shared__ __align__(16) float ks[GK * LD];
     __shared__ __align__(16) float vs[GK * LD];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, rl = lane & 15, g = lane >> 4;
-    const int64_t h = blockIdx.x % a.Hkv;
+    const int h = blockIdx.x % a.Hkv;
     const int split = blockIdx.y;
     Tile t;
     if (!find_tile(a, blockIdx.x / a.Hkv, GR, &t)) return;
-    const int64_t rows = t.Lq * a.G;
-    const int64_t r = t.r0 + 16 * w + rl;
+    const int rows = t.Lq * a.G;
+    const int r = t.r0 + 16 * w + rl;
     const bool live = r < rows;
-    const int64_t rc = live ? r : rows - 1;
-    const int64_t pos = rc / a.G, head = h * a.G + rc % a.G;
+    const int rc = live ? r : rows - 1;
+    const int pos = rc / a.G, head = h * a.G + rc % a.G;
     const int64_t qrow = t.q0 + pos;
     const T *qp = (const T *)a.q + qrow * a.q_row + head * a.q_head;
     const T *kp = (const T *)a.k + t.k0 * a.k_row + h * a.k_head;
@@ -177,21 +180,21 @@ __global__ void __launch_bounds__(GTH) prompt_general(PromptArgs a, int vec) {
             const int c = 16 * j + 4 * g + s;
             qf[4 * j + s] = c < a.d ? Elem<T>::load(qp, c) * sl2 : 0.f;
         }
-    const int64_t seen = a.causal ? clamp64(pos + 1 + t.Lk - t.Lq, t.Lk) : t.Lk;
-    // keys that the last and the first row of the workgroup and of the wave see
-    const int64_t last = t.r0 + GR - 1 < rows ? t.r0 + GR - 1 : rows - 1;
-    const int64_t most = a.causal ? clamp64(last / a.G + 1 + t.Lk - t.Lq, t.Lk) : t.Lk;
-    const int64_t nt = (most + GK - 1) / GK;
-    const int64_t j0 = nt * split / a.splits, j1 = nt * (split + 1) / a.splits;
-    const int64_t wfirst = t.r0 + 16 * w < rows ? t.r0 + 16 * w : rows - 1;
-    const int64_t fewest = a.causal ? clamp64(wfirst / a.G + 1 + t.Lk - t.Lq, t.Lk) : t.Lk;
+    const auto sees = [&](int row) -> int {  // keys that a row sees
+        return a.causal ? clampi(row / a.G + 1 - t.Lq + t.Lk, t.Lk) : t.Lk;
+    };
+    const int seen = sees(rc);
+    const int last = t.r0 + GR < rows ? t.r0 + GR : rows;
+    const int nt = (sees(last - 1) + GK - 1) / GK;
+    const int j0 = (int)((int64_t)nt * split / a.splits), j1 = (int)((int64_t)nt * (split + 1) / a.splits);
+    const int fewest = sees(t.r0 + 16 * w < rows ? t.r0 + 16 * w : rows - 1);  // keys that every row of the wave sees
 
     f32x4 acc[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m = PMIN, l = 0.f;
-    for (int64_t j = j0; j < j1; ++j) {
-        const int64_t key0 = j * GK;
+    for (int j = j0; j < j1; ++j) {
+        const int64_t key0 = (int64_t)j * GK;
         __syncthreads();
         load_tile<T>(ks, LD, DP, kp + key0 * a.k_row, a.k_row, t.Lk - key0, a.d, vec);
         const bool bad = __syncthreads_or(load_tile<T>(vs, LD, DP, vp + key0 * a.v_row, a.v_row, t.Lk - key0, a.d, vec));
@@ -356,17 +359,17 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
     __shared__ int bad_tile[2];             // 1 + the last tile of each slot that holds a non-finite value
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rl = lane & 31, hh = lane >> 5;
-    const int64_t h = blockIdx.x % a.Hkv;
+    const int h = blockIdx.x % a.Hkv;
     const int split = blockIdx.y;
     Tile t;
     if (!find_tile(a, blockIdx.x / a.Hkv, PR, &t)) return;
     if (threadIdx.x < 2) bad_tile[threadIdx.x] = 0;
     __syncthreads();
-    const int64_t rows = t.Lq * a.G;
-    const int64_t r = t.r0 + 32 * w + rl;
+    const int rows = t.Lq * a.G;
+    const int r = t.r0 + 32 * w + rl;
     const bool live = r < rows;
-    const int64_t rc = live ? r : rows - 1;
-    const int64_t pos = rc / a.G, head = h * a.G + rc % a.G;
+    const int rc = live ? r : rows - 1;
+    const int pos = rc / a.G, head = h * a.G + rc % a.G;
     const int64_t qrow = t.q0 + pos;
     float sl2 = head_scale(a, h) * PLOG2E;
 
@@ -385,18 +388,18 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
         }
         sl2 = sl2 == 0.f ? 1.f : fabsf(sl2);
     }
-    const auto sees = [&](int64_t row) -> int64_t {
-        return a.causal ? clamp64(row / a.G + 1 + t.Lk - t.Lq, t.Lk) : t.Lk;
+    const auto sees = [&](int row) -> int {  // keys that a row sees
+        return a.causal ? clampi(row / a.G + 1 - t.Lq + t.Lk, t.Lk) : t.Lk;
     };
-    const int64_t seen = sees(rc);
-    const int64_t end = t.r0 + PR < rows ? t.r0 + PR : rows;
-    const int64_t nt = (sees(end - 1) + PK - 1) / PK;
-    const int64_t j0 = nt * split / a.splits, j1 = nt * (split + 1) / a.splits;
-    const int64_t gfew = sees(t.r0);                       // keys that every row of the workgroup sees
-    const int64_t w0 = t.r0 + 32 * w;
+    const int seen = sees(rc);
+    const int end = t.r0 + PR < rows ? t.r0 + PR : rows;
+    const int nt = (sees(end - 1) + PK - 1) / PK;
+    const int j0 = (int)((int64_t)nt * split / a.splits), j1 = (int)((int64_t)nt * (split + 1) / a.splits);
+    const int gfew = sees(t.r0);                           // keys that every row of the workgroup sees
+    const int w0 = t.r0 + 32 * w;
     const bool wlive = w0 < rows;
-    const int64_t wfew = wlive ? sees(w0) : 0;             // keys that every row of the wave sees
-    const int64_t wmost = wlive ? sees(w0 + 31 < rows ? w0 + 31 : rows - 1) : 0;
+    const int wfew = wlive ? sees(w0) : 0;                 // keys that every row of the wave sees
+    const int wmost = wlive ? sees(w0 + 31 < rows ? w0 + 31 : rows - 1) : 0;
 
     // direct-to-LDS loads: load i of a tile fills rows RPI i .. of the slot in lane order
     const uint32_t krb = (uint32_t)(a.k_row * 2), vrb = (uint32_t)(a.v_row * 2);
@@ -409,8 +412,8 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
         kvo = 8 * kc < a.d ? (uint32_t)lr * krb + 16 * kc : 0x80000000u;   // columns past d: out of range, zeros
         vvo = 8 * vc < a.d ? (uint32_t)lr * vrb + 16 * vc : 0x80000000u;
     }
-    const auto issue = [&](int64_t j) {
-        const int64_t key0 = j * PK;
+    const auto issue = [&](int j) {
+        const int64_t key0 = (int64_t)j * PK;
         unsigned char *slot = psm + (j & 1) * 2 * TB + w * 1024;
         const rsrc_t kr = rows_rsrc(kb_ + key0 * krb, t.Lk - key0, krb, a.d);
         const rsrc_t vr = rows_rsrc(vb_ + key0 * vrb, t.Lk - key0, vrb, a.d);
@@ -436,26 +439,16 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
     float m = PMIN, l = 0.f;
-    if (j0 < j1) issue(j0);
-    for (int64_t j = j0; j < j1; ++j) {
-        const int64_t key0 = j * PK;
-        unsigned char *slot = psm + (j & 1) * 2 * TB;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (key0 + PK > gfew) {
-            // some row does not see the whole tile: look for non-finite values in what this wave loaded
-            uint32_t e = 0;
-#pragma unroll
-            for (int x = 0; x < NI; ++x) {
-                const uint4 y = *(const uint4 *)(slot + TB + (x * PW + w) * 1024 + lane * 16);
-                e |= ((y.x & 0x7F807F80u) + 0x00800080u) | ((y.y & 0x7F807F80u) + 0x00800080u) |
-                     ((y.z & 0x7F807F80u) + 0x00800080u) | ((y.w & 0x7F807F80u) + 0x00800080u);
-            }
-            if (e & 0x80008000u) bad_tile[j & 1] = (int)(j + 1);
-        }
-        // every wave's loads of this tile have landed, and every wave is done with the other slot
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (j + 1 < j1) issue(j + 1);
-        if (key0 >= wmost) continue;
+    const auto value = [&](const unsigned char *slot, int kb, int n) -> bf16x8 {
+        const uint32_t at = (vro ^ (n * 64)) + kb * 16 * RB;
+        typedef __attribute__((address_space(3))) bf16x4 lds4;
+        const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)P_LDS(slot + at));
+        const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)P_LDS(slot + at + 8 * RB));
+        return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // one tile of keys; MASKED: some row of the wave does not see all of it
+    const auto step = [&](unsigned char *slot, int key0, auto masked) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked)::value;
         f32x16 s[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -468,9 +461,8 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
                 const bf16x8 kf = *(const bf16x8 *)(slot + b * 32 * RB + (kro ^ (c * 32)));
                 s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], s[b], 0, 0, 0);
             }
-        const bool masked = key0 + PK > wfew;
-        const int lim = (int)(seen - key0 < PK ? seen - key0 : PK) - 4 * hh;
-        if (masked) {
+        if (MASKED) {
+            const int lim = seen - key0 - 4 * hh;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -503,51 +495,84 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
                 pf[2 * b + i / 8][i % 8] = (__bf16)p;
             }
         l += sum;
-        const auto value = [&](int kb, int n) -> bf16x8 {
-            const uint32_t at = (vro ^ (n * 64)) + kb * 16 * RB;
-            typedef __attribute__((address_space(3))) bf16x4 lds4;
-            const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)P_LDS(slot + at));
-            const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)P_LDS(slot + at + 8 * RB));
-            return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-        };
-        if (!(masked && bad_tile[j & 1] == (int)(j + 1))) {
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
+        for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-                for (int n = 0; n < DB; ++n)
-                    acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(kb, n), pf[kb], acc[n], 0, 0, 0);
-        } else {
-            // A hidden key's weight is 0, but 0 times an infinity or a NaN is a NaN.  The finite values go
-            // through the product, and whether a row sees an infinity of either sign (or a NaN, taken as
-            // both) in a column comes from products of 0 / 1 marks.
+            for (int n = 0; n < DB; ++n)
+                acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(slot, kb, n), pf[kb], acc[n], 0, 0, 0);
+    };
+    // A hidden key's weight is 0, but 0 times an infinity or a NaN is a NaN.  In a tile that holds such a
+    // value and is hidden from some row, the value is taken out before `step`; whether a row sees an
+    // infinity of either sign (or a NaN, taken as both) in a column comes from products of 0 / 1 marks, and
+    // is added after it.
+    uint16_t *marks = (uint16_t *)(psm + 4 * TB) + threadIdx.x;
+    const auto take_out = [&](unsigned char *slot, int key0) __attribute__((always_inline)) {
+        const int lim = seen - key0 - 4 * hh;
 #pragma unroll 1
-            for (int kb = 0; kb < 4; ++kb) {
-                bf16x8 sees_;
+        for (int n = 0; n < DB; ++n) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    sees_[i] = (__bf16)(32 * (kb / 2) + 8 * (2 * (kb % 2) + i / 4) + i % 4 < lim ? 1.f : 0.f);
-                const bf16x8 pk = kb == 0 ? pf[0] : kb == 1 ? pf[1] : kb == 2 ? pf[2] : pf[3];
+            for (int sign = 0; sign < 2; ++sign) {
+                f32x16 u;
 #pragma unroll
-                for (int n = 0; n < DB; ++n) {
-                    bf16x8 x = value(kb, n), up, dn;
+                for (int i = 0; i < 16; ++i) u[i] = 0.f;
+                for (int kb = 0; kb < 4; ++kb) {
+                    const bf16x8 x = value(slot, kb, n);
+                    bf16x8 mark, sees_;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float y = (float)x[i];
-                        const bool fin = fabsf(y) < INFINITY;
-                        up[i] = (__bf16)(!fin && !(y < 0.f) ? 1.f : 0.f);
-                        dn[i] = (__bf16)(!fin && !(y > 0.f) ? 1.f : 0.f);
-                        x[i] = fin ? x[i] : (__bf16)0.f;
+                        const float y = sign ? -(float)x[i] : (float)x[i];
+                        mark[i] = (__bf16)(!(fabsf(y) < INFINITY) && !(y < 0.f) ? 1.f : 0.f);
+                        sees_[i] = (__bf16)(16 * kb + 8 * (i / 4) + i % 4 < lim ? 1.f : 0.f);
                     }
-                    acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pk, acc[n], 0, 0, 0);
-                    f32x16 z;
+                    u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(mark, sees_, u, 0, 0, 0);
+                }
+                uint32_t bits = 0;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] = 0.f;
-                    const f32x16 u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up, sees_, z, 0, 0, 0);
+                for (int i = 0; i < 16; ++i) bits |= u[i] > 0.f ? 1u << i : 0u;
+                marks[(2 * n + sign) * PTH] = (uint16_t)bits;
+            }
+        }
+        __syncthreads();
+        for (int x = threadIdx.x; x < TB / 4; x += PTH) {
+            uint32_t y = ((uint32_t *)(slot + TB))[x];
+            if ((y & 0x7F80u) == 0x7F80u) y &= 0xFFFF0000u;
+            if ((y & 0x7F800000u) == 0x7F800000u) y &= 0xFFFFu;
+            ((uint32_t *)(slot + TB))[x] = y;
+        }
+        __syncthreads();
+    };
+    if (j0 < j1) issue(j0);
+    for (int j = j0; j < j1; ++j) {
+        const int key0 = j * PK;
+        unsigned char *slot = psm + (j & 1) * 2 * TB;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const bool hidden = key0 + PK > gfew;  // from some row of the workgroup
+        if (hidden) {
+            // look for non-finite values in what this wave loaded
+            uint32_t e = 0;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[n][i] += u[i] > 0.f ? INFINITY : 0.f;
-                    const f32x16 e = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dn, sees_, z, 0, 0, 0);
+            for (int x = 0; x < NI; ++x) {
+                const uint4 y = *(const uint4 *)(slot + TB + (x * PW + w) * 1024 + lane * 16);
+                e |= ((y.x & 0x7F807F80u) + 0x00800080u) | ((y.y & 0x7F807F80u) + 0x00800080u) |
+                     ((y.z & 0x7F807F80u) + 0x00800080u) | ((y.w & 0x7F807F80u) + 0x00800080u);
+            }
+            if (e & 0x80008000u) bad_tile[j & 1] = j + 1;
+        }
+        // every wave's loads of this tile have landed, and every wave is done with the other slot
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (j + 1 < j1) issue(j + 1);
+        const bool bad = hidden && __builtin_amdgcn_readfirstlane(bad_tile[j & 1]) == j + 1;
+        if (bad) take_out(slot, key0);
+        if (key0 + PK <= wfew) step(slot, key0, std::false_type());
+        else if (key0 < wmost) step(slot, key0, std::true_type());
+        if (bad) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[n][i] -= e[i] > 0.f ? INFINITY : 0.f;
+            for (int n = 0; n < DB; ++n) {
+                const uint32_t up = marks[2 * n * PTH], dn = marks[(2 * n + 1) * PTH];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if (up >> i & 1) acc[n][i] += INFINITY;
+                    if (dn >> i & 1) acc[n][i] -= INFINITY;
                 }
             }
         }
@@ -652,7 +677,7 @@ hipError_t launch_prompt(const fw_packed &p, void *o, float *lse, int splits, fl
                          hipStream_t st) {
     PromptArgs a{};
     a.q = p.q, a.k = p.k, a.v = p.v;
-    a.Tq = p.Tq, a.Tk = p.Tk, a.B = p.B, a.Hq = p.Hq, a.Hkv = p.Hkv;
+    a.Tq = p.Tq, a.Tk = p.Tk, a.B = p.B, a.Hq = (int)p.Hq, a.Hkv = (int)p.Hkv;
     a.d = (int)p.d, a.G = (int)(p.Hq / p.Hkv);
     a.q_row = p.q_row, a.q_head = p.q_head, a.k_row = p.k_row, a.k_head = p.k_head, a.v_row = p.v_row, a.v_head = p.v_head;
     a.cu_q = p.cu_q, a.cu_k = p.cu_k, a.scale = p.scale;
@@ -661,7 +686,7 @@ hipError_t launch_prompt(const fw_packed &p, void *o, float *lse, int splits, fl
     if (prompt_fast(p)) {
         const dim3 grid((unsigned)(row_tiles(p, PR) * p.Hkv), (unsigned)splits);
         const int D = a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256;
-        const size_t lds = (size_t)2 * 2 * PK * 2 * D;
+        const size_t lds = (size_t)2 * 2 * PK * 2 * D + (size_t)D / 32 * 2 * 2 * PTH;  // two slots, marks
         if (D == 64) hipLaunchKernelGGL((prompt_mfma<64>), grid, dim3(PTH), lds, st, a);
         else if (D == 128) hipLaunchKernelGGL((prompt_mfma<128>), grid, dim3(PTH), lds, st, a);
         else hipLaunchKernelGGL((prompt_mfma<256>), grid, dim3(PTH), lds, st, a);
