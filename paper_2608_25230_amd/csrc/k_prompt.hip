@@ -318,9 +318,9 @@ __global__ void __launch_bounds__(GTH) prompt_general(PromptArgs a, int vec) {
 // the true one by up to 2^8 (RESCALE): the accumulators are rescaled only
 // when some row's maximum grew by more, and the weights keep bf16's relative
 // precision at any scale.
-// 16-byte chunk c of row r lies at chunk c ^ (r & 7) of its LDS row (keys) or
-// c ^ 2 (r & 7) (values, whose transposed reads take pairs of chunks), so the
-// eight or four rows that a read touches at once lie in different banks.
+// 16-byte chunk c of row r lies at chunk c ^ k_swizzle(r) or c ^ v_swizzle(r)
+// of its LDS row, so that the 16 rows of one chunk that half a wave reads of the keys,
+// and the 4 rows of 4 chunks that it reads of the values, fill all 64 banks once.
 // ---------------------------------------------------------------------------
 constexpr int PW = 4;            // waves per workgroup
 constexpr int PTH = 64 * PW;
@@ -344,8 +344,12 @@ __device__ __forceinline__ float half_max(float x) {
 }
 
 template <int D>
+__device__ __forceinline__ int k_swizzle(int r) {
+    return D == 64 ? (r >> 1) & 7 : r & 15;
+}
+template <int D>
 __device__ __forceinline__ int v_swizzle(int r) {
-    return D == 64 ? 2 * ((r >> 1) & 3) : 2 * (r & 7);
+    return D == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3);
 }
 
 template <int D>
@@ -397,19 +401,19 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
     const int j0 = (int)((int64_t)nt * split / a.splits), j1 = (int)((int64_t)nt * (split + 1) / a.splits);
     const int gfew = sees(t.r0);                           // keys that every row of the workgroup sees
     const int w0 = t.r0 + 32 * w;
-    const bool wlive = w0 < rows;
-    const int wfew = wlive ? sees(w0) : 0;                 // keys that every row of the wave sees
-    const int wmost = wlive ? sees(w0 + 31 < rows ? w0 + 31 : rows - 1) : 0;
+    const int wmost = w0 < rows ? sees(w0 + 31 < rows ? w0 + 31 : rows - 1) : 0;  // keys that some row of the wave sees
 
     // direct-to-LDS loads: load i of a tile fills rows RPI i .. of the slot in lane order
     const uint32_t krb = (uint32_t)(a.k_row * 2), vrb = (uint32_t)(a.v_row * 2);
     const char *kb_ = (const char *)a.k + (t.k0 * a.k_row + h * a.k_head) * 2;
     const char *vb_ = (const char *)a.v + (t.k0 * a.v_row + h * a.v_head) * 2;
-    uint32_t kvo, vvo;
+    uint32_t kvo, kvo1, vvo;
     {
+        // columns past d: out of range, zeros
         const int lr = RPI * w + lane / (D / 8), p = lane % (D / 8);
-        const int kc = p ^ (lr & 7), vc = p ^ v_swizzle<D>(lr);
-        kvo = 8 * kc < a.d ? (uint32_t)lr * krb + 16 * kc : 0x80000000u;   // columns past d: out of range, zeros
+        const int kc = p ^ k_swizzle<D>(lr), kc1 = p ^ k_swizzle<D>(lr + RPI * PW), vc = p ^ v_swizzle<D>(lr);
+        kvo = 8 * kc < a.d ? (uint32_t)lr * krb + 16 * kc : 0x80000000u;
+        kvo1 = 8 * kc1 < a.d ? (uint32_t)lr * krb + 16 * kc1 : 0x80000000u;  // every other load; the same for D < 256
         vvo = 8 * vc < a.d ? (uint32_t)lr * vrb + 16 * vc : 0x80000000u;
     }
     const auto issue = [&](int j) {
@@ -419,14 +423,14 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
         const rsrc_t vr = rows_rsrc(vb_ + key0 * vrb, t.Lk - key0, vrb, a.d);
 #pragma unroll
         for (int x = 0; x < NI; ++x)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, P_LDS(slot + x * PW * 1024), 16, kvo + x * (RPI * PW) * krb, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, P_LDS(slot + x * PW * 1024), 16, (D == 256 && x % 2 ? kvo1 : kvo) + x * (RPI * PW) * krb, 0, 0, 0);
 #pragma unroll
         for (int x = 0; x < NI; ++x)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, P_LDS(slot + TB + x * PW * 1024), 16, vvo + x * (RPI * PW) * vrb, 0,
                                                      0, 0);
     };
     // LDS reads: keys rl of a half, chunk 2 s + hh; values key 4 hh + (lane % 16) / 4, columns 16 ((lane / 16) % 2) + 4 (lane % 4)
-    const uint32_t kro = (uint32_t)(rl * RB + ((hh ^ (rl & 7)) * 16));
+    const uint32_t kro = (uint32_t)(rl * RB + ((hh ^ k_swizzle<D>(rl)) * 16));
     uint32_t vro;
     {
         const int key = 4 * hh + (lane & 15) / 4, c = 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
@@ -542,12 +546,22 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
         __syncthreads();
     };
     if (j0 < j1) issue(j0);
-    for (int j = j0; j < j1; ++j) {
+    int j = j0;
+    // tiles that every row of the workgroup sees whole
+    const int full = gfew / PK < j1 ? gfew / PK : j1;
+    for (; j < full; ++j) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        // every wave's loads of this tile have landed, and every wave is done with the other slot
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (j + 1 < j1) issue(j + 1);
+        step(psm + (j & 1) * 2 * TB, j * PK, std::false_type());
+    }
+    // tiles hidden from some row
+    for (; j < j1; ++j) {
         const int key0 = j * PK;
         unsigned char *slot = psm + (j & 1) * 2 * TB;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        const bool hidden = key0 + PK > gfew;  // from some row of the workgroup
-        if (hidden) {
+        {
             // look for non-finite values in what this wave loaded
             uint32_t e = 0;
 #pragma unroll
@@ -558,13 +572,11 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
             }
             if (e & 0x80008000u) bad_tile[j & 1] = j + 1;
         }
-        // every wave's loads of this tile have landed, and every wave is done with the other slot
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (j + 1 < j1) issue(j + 1);
-        const bool bad = hidden && __builtin_amdgcn_readfirstlane(bad_tile[j & 1]) == j + 1;
+        const bool bad = __builtin_amdgcn_readfirstlane(bad_tile[j & 1]) == j + 1;
         if (bad) take_out(slot, key0);
-        if (key0 + PK <= wfew) step(slot, key0, std::false_type());
-        else if (key0 < wmost) step(slot, key0, std::true_type());
+        if (key0 < wmost) step(slot, key0, std::true_type());
         if (bad) {
 #pragma unroll
             for (int n = 0; n < DB; ++n) {
