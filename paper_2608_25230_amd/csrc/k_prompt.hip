@@ -25,6 +25,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float PLOG2E = 1.4426950408889634f;
 constexpr float PLN2 = 0.6931471805599453f;
@@ -400,8 +401,6 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
     const int nt = (sees(end - 1) + PK - 1) / PK;
     const int j0 = (int)((int64_t)nt * split / a.splits), j1 = (int)((int64_t)nt * (split + 1) / a.splits);
     const int gfew = sees(t.r0);                           // keys that every row of the workgroup sees
-    const int w0 = t.r0 + 32 * w;
-    const int wmost = w0 < rows ? sees(w0 + 31 < rows ? w0 + 31 : rows - 1) : 0;  // keys that some row of the wave sees
 
     // direct-to-LDS loads: load i of a tile fills rows RPI i .. of the slot in lane order
     const uint32_t krb = (uint32_t)(a.k_row * 2), vrb = (uint32_t)(a.v_row * 2);
@@ -416,25 +415,30 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
         kvo1 = 8 * kc1 < a.d ? (uint32_t)lr * krb + 16 * kc1 : 0x80000000u;  // every other load; the same for D < 256
         vvo = 8 * vc < a.d ? (uint32_t)lr * vrb + 16 * vc : 0x80000000u;
     }
-    const auto issue = [&](int j) {
+    // slots: keys of tile j at (j & 1) TB, values at (2 + (j & 1)) TB
+    const auto issue_k = [&](int j) {
         const int64_t key0 = (int64_t)j * PK;
-        unsigned char *slot = psm + (j & 1) * 2 * TB + w * 1024;
+        unsigned char *slot = psm + (j & 1) * TB + w * 1024;
         const rsrc_t kr = rows_rsrc(kb_ + key0 * krb, t.Lk - key0, krb, a.d);
+#pragma unroll
+        for (int x = 0; x < NI; ++x)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, P_LDS(slot + x * PW * 1024), 16,
+                                                     (D == 256 && x % 2 ? kvo1 : kvo) + x * (RPI * PW) * krb, 0, 0, 0);
+    };
+    const auto issue_v = [&](int j) {
+        const int64_t key0 = (int64_t)j * PK;
+        unsigned char *slot = psm + (2 + (j & 1)) * TB + w * 1024;
         const rsrc_t vr = rows_rsrc(vb_ + key0 * vrb, t.Lk - key0, vrb, a.d);
 #pragma unroll
         for (int x = 0; x < NI; ++x)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, P_LDS(slot + x * PW * 1024), 16, (D == 256 && x % 2 ? kvo1 : kvo) + x * (RPI * PW) * krb, 0, 0, 0);
-#pragma unroll
-        for (int x = 0; x < NI; ++x)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, P_LDS(slot + TB + x * PW * 1024), 16, vvo + x * (RPI * PW) * vrb, 0,
-                                                     0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, P_LDS(slot + x * PW * 1024), 16, vvo + x * (RPI * PW) * vrb, 0, 0, 0);
     };
     // LDS reads: keys rl of a half, chunk 2 s + hh; values key 4 hh + (lane % 16) / 4, columns 16 ((lane / 16) % 2) + 4 (lane % 4)
     const uint32_t kro = (uint32_t)(rl * RB + ((hh ^ k_swizzle<D>(rl)) * 16));
     uint32_t vro;
     {
         const int key = 4 * hh + (lane & 15) / 4, c = 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
-        vro = (uint32_t)(TB + key * RB + ((c ^ v_swizzle<D>(key)) * 16) + 8 * (lane & 1));
+        vro = (uint32_t)(key * RB + ((c ^ v_swizzle<D>(key)) * 16) + 8 * (lane & 1));
     }
 
     f32x16 acc[DB];
@@ -443,73 +447,72 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
     float m = PMIN, l = 0.f;
-    const auto value = [&](const unsigned char *slot, int kb, int n) -> bf16x8 {
+    typedef __attribute__((address_space(3))) bf16x4 lds4;
+    const auto value = [&](const unsigned char *slot, int kb, int n) -> bf16x8 {  // keys of step kb, columns 32 n ..
         const uint32_t at = (vro ^ (n * 64)) + kb * 16 * RB;
-        typedef __attribute__((address_space(3))) bf16x4 lds4;
         const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)P_LDS(slot + at));
         const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)P_LDS(slot + at + 8 * RB));
         return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    // one tile of keys; MASKED: some row of the wave does not see all of it
-    const auto step = [&](unsigned char *slot, int key0, auto masked) __attribute__((always_inline)) {
-        constexpr bool MASKED = decltype(masked)::value;
-        f32x16 s[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-#pragma unroll
-        for (int c = 0; c < KS; ++c)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const bf16x8 kf = *(const bf16x8 *)(slot + b * 32 * RB + (kro ^ (c * 32)));
-                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], s[b], 0, 0, 0);
-            }
-        if (MASKED) {
+    const auto score = [&](const unsigned char *slot, int half, int c, f32x16 &s) __attribute__((always_inline)) {
+        const bf16x8 kf = *(const bf16x8 *)(slot + half * 32 * RB + (kro ^ (c * 32)));
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], s, 0, 0, 0);
+    };
+    const auto add_value = [&](const unsigned char *slot, int half, int x, const bf16x8 (&p)[2]) __attribute__((always_inline)) {
+        const int kb = x / DB, n = x % DB;
+        acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(slot, 2 * half + kb, n), p[kb], acc[n], 0, 0, 0);
+    };
+    // One pipeline step: the weights of unit u (32 keys) from its scores s, beside the scores of unit u + 1
+    // (half kh of the key tile kt) and the values of unit u - 1 (half vh of vt, weights pv): the products
+    // need no result of the exponentials and fill the time that they take.  The maximum m is a whole
+    // number, so a rescaling is by a power of two and exact, of the weights that wait in pv too.
+    const auto unit = [&](f32x16 &s, bf16x8 (&p)[2], const unsigned char *kt, int kh, f32x16 &sn, const unsigned char *vt,
+                          int vh, bf16x8 (&pv)[2], int key0, auto masked) __attribute__((always_inline)) {
+        if (decltype(masked)::value) {
             const int lim = seen - key0 - 4 * hh;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (32 * b + 8 * (i / 4) + i % 4 >= lim) s[b][i] = -INFINITY;
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i / 4) + i % 4 >= lim) s[i] = -INFINITY;
         }
-        float mt = s[0][0];
+        float mt = s[0];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[b][i]);
+        for (int i = 1; i < 16; ++i) mt = fmaxf(mt, s[i]);
         mt = half_max(mt) * sl2;
         if (__any(mt > m + RESCALE)) {
-            const float mn = fmaxf(m, mt), al = __builtin_amdgcn_exp2f(m - mn);
+            const float mn = fmaxf(m, ceilf(mt)), al = __builtin_amdgcn_exp2f(m - mn);
             m = mn;
             l *= al;
 #pragma unroll
             for (int n = 0; n < DB; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[n][i] *= al;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) pv[i / 8][i % 8] = (__bf16)((float)pv[i / 8][i % 8] * al);
         }
-        bf16x8 pf[4];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sn[i] = 0.f;
+#pragma unroll
+        for (int x = 0; x < KS || x < 2 * DB; ++x) {
+            if (x < KS) score(kt, kh, x, sn);
+            if (x < 2 * DB) add_value(vt, vh, x, pv);
+        }
         float sum = 0.f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[b][i], sl2, -m));
-                sum += p;
-                pf[2 * b + i / 8][i % 8] = (__bf16)p;
-            }
+        for (int i = 0; i < 16; ++i) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -m));
+            sum += e;
+            p[i / 8][i % 8] = (__bf16)e;
+        }
         l += sum;
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int n = 0; n < DB; ++n)
-                acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(slot, kb, n), pf[kb], acc[n], 0, 0, 0);
+        // here, beside the products, and not where they are used
+        asm volatile("" : "+v"(*(u32x4 *)&p[0]), "+v"(*(u32x4 *)&p[1]), "+v"(l));
     };
     // A hidden key's weight is 0, but 0 times an infinity or a NaN is a NaN.  In a tile that holds such a
-    // value and is hidden from some row, the value is taken out before `step`; whether a row sees an
+    // value and is hidden from some row, the value is taken out before its product; whether a row sees an
     // infinity of either sign (or a NaN, taken as both) in a column comes from products of 0 / 1 marks, and
-    // is added after it.
+    // is added at the very end.
     uint16_t *marks = (uint16_t *)(psm + 4 * TB) + threadIdx.x;
+    bool marked = false;
     const auto take_out = [&](unsigned char *slot, int key0) __attribute__((always_inline)) {
         const int lim = seen - key0 - 4 * hh;
 #pragma unroll 1
@@ -533,51 +536,70 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
                 uint32_t bits = 0;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) bits |= u[i] > 0.f ? 1u << i : 0u;
+                if (marked) bits |= marks[(2 * n + sign) * PTH];
                 marks[(2 * n + sign) * PTH] = (uint16_t)bits;
             }
         }
         __syncthreads();
         for (int x = threadIdx.x; x < TB / 4; x += PTH) {
-            uint32_t y = ((uint32_t *)(slot + TB))[x];
+            uint32_t y = ((uint32_t *)slot)[x];
             if ((y & 0x7F80u) == 0x7F80u) y &= 0xFFFF0000u;
             if ((y & 0x7F800000u) == 0x7F800000u) y &= 0xFFFFu;
-            ((uint32_t *)(slot + TB))[x] = y;
+            ((uint32_t *)slot)[x] = y;
         }
         __syncthreads();
+        marked = true;
     };
-    if (j0 < j1) issue(j0);
-    int j = j0;
-    // tiles that every row of the workgroup sees whole
-    const int full = gfew / PK < j1 ? gfew / PK : j1;
-    for (; j < full; ++j) {
+    f32x16 sa, sb;
+    bf16x8 pa[2], pb[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pb[kb][i] = (__bf16)0.f;
+    // tile j: unit 2 j, then 2 j + 1.  At its start the scores of unit 2 j are in sa, the weights of unit
+    // 2 j - 1 in pb, keys j and values j - 1 in their slots, keys j + 1 and values j on their way.
+    const auto tile = [&](int j, auto masked) __attribute__((always_inline)) {
+        unsigned char *k0s = psm + (j & 1) * TB, *k1s = psm + (~j & 1) * TB;
+        unsigned char *v0s = psm + (2 + (j & 1)) * TB, *v1s = psm + (2 + (~j & 1)) * TB;
+        unit(sa, pa, k0s, 1, sb, v1s, 1, pb, j * PK, masked);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        // every wave's loads of this tile have landed, and every wave is done with the other slot
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (j + 1 < j1) issue(j + 1);
-        step(psm + (j & 1) * 2 * TB, j * PK, std::false_type());
-    }
-    // tiles hidden from some row
-    for (; j < j1; ++j) {
-        const int key0 = j * PK;
-        unsigned char *slot = psm + (j & 1) * 2 * TB;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        {
+        if (decltype(masked)::value) {
             // look for non-finite values in what this wave loaded
             uint32_t e = 0;
 #pragma unroll
             for (int x = 0; x < NI; ++x) {
-                const uint4 y = *(const uint4 *)(slot + TB + (x * PW + w) * 1024 + lane * 16);
+                const uint4 y = *(const uint4 *)(v0s + (x * PW + w) * 1024 + lane * 16);
                 e |= ((y.x & 0x7F807F80u) + 0x00800080u) | ((y.y & 0x7F807F80u) + 0x00800080u) |
                      ((y.z & 0x7F807F80u) + 0x00800080u) | ((y.w & 0x7F807F80u) + 0x00800080u);
             }
             if (e & 0x80008000u) bad_tile[j & 1] = j + 1;
         }
+        // every wave's loads have landed, and every wave is done with keys j and values j - 1
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (j + 1 < j1) issue(j + 1);
-        const bool bad = __builtin_amdgcn_readfirstlane(bad_tile[j & 1]) == j + 1;
-        if (bad) take_out(slot, key0);
-        if (key0 < wmost) step(slot, key0, std::true_type());
-        if (bad) {
+        if (j + 2 < j1) issue_k(j + 2);
+        if (j + 1 < j1) issue_v(j + 1);
+        if (decltype(masked)::value && __builtin_amdgcn_readfirstlane(bad_tile[j & 1]) == j + 1) take_out(v0s, j * PK);
+        unit(sb, pb, k1s, 0, sa, v0s, 0, pa, j * PK + 32, masked);
+    };
+    if (j0 < j1) {
+        issue_k(j0);
+        if (j0 + 1 < j1) issue_k(j0 + 1);
+        issue_v(j0);
+        // the values before the first tile: zeros, as their weights are
+        for (int x = threadIdx.x; x < TB / 16; x += PTH) ((uint4 *)(psm + (2 + (~j0 & 1)) * TB))[x] = make_uint4(0, 0, 0, 0);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"i"(NI) : "memory");  // keys j0 (and j0 + 1): values j0 are not awaited
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sa[i] = 0.f;
+#pragma unroll
+        for (int x = 0; x < KS; ++x) score(psm + (j0 & 1) * TB, 0, x, sa);
+        int j = j0;
+        // tiles that every row of the workgroup sees whole, then those hidden from some row
+        for (const int full = gfew / PK < j1 ? gfew / PK : j1; j < full; ++j) tile(j, std::false_type());
+        for (; j < j1; ++j) tile(j, std::true_type());
+#pragma unroll
+        for (int x = 0; x < 2 * DB; ++x) add_value(psm + (2 + (~j1 & 1)) * TB, 1, x, pb);
+        if (marked) {
 #pragma unroll
             for (int n = 0; n < DB; ++n) {
                 const uint32_t up = marks[2 * n * PTH], dn = marks[(2 * n + 1) * PTH];
