@@ -25,7 +25,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float PLOG2E = 1.4426950408889634f;
 constexpr float PLN2 = 0.6931471805599453f;
@@ -326,8 +325,8 @@ __global__ void __launch_bounds__(GTH) prompt_general(PromptArgs a, int vec) {
 constexpr int PW = 4;            // waves per workgroup
 constexpr int PTH = 64 * PW;
 constexpr int PR = 32 * PW;      // rows per workgroup
-constexpr int PK = 64;           // keys per tile
-constexpr float RESCALE = 8.f;
+constexpr int PK = 32;           // keys per tile
+constexpr float GROWN = 1024.f;  // a row's sum over a tile that calls for a new maximum
 
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
 #define P_LDS(p) ((__attribute__((address_space(3))) void *)(p))
@@ -354,14 +353,14 @@ __device__ __forceinline__ int v_swizzle(int r) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs a) {
+__global__ void __launch_bounds__(PTH, D == 256 ? 1 : 3) prompt_mfma(PromptArgs a) {
     constexpr int RB = 2 * D;               // bytes of an LDS row
     constexpr int TB = PK * RB;             // bytes of a tile
     constexpr int RPI = 1024 / RB;          // rows of one 64-lane load
     constexpr int NI = PK / RPI / PW;       // loads per wave and tile
     constexpr int KS = D / 16, DB = D / 32;
-    extern __shared__ __align__(16) unsigned char psm[];
-    __shared__ int bad_tile[2];             // 1 + the last tile of each slot that holds a non-finite value
+    extern __shared__ __align__(1024) unsigned char psm[];
+    int *bad_tile = (int *)(psm + 4 * TB);  // 1 + the last tile of each slot that holds a non-finite value
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rl = lane & 31, hh = lane >> 5;
     const int h = blockIdx.x % a.Hkv;
@@ -371,17 +370,23 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
     if (threadIdx.x < 2) bad_tile[threadIdx.x] = 0;
     __syncthreads();
     const int rows = t.Lq * a.G;
-    const int r = t.r0 + 32 * w + rl;
-    const bool live = r < rows;
-    const int rc = live ? r : rows - 1;
-    const int pos = rc / a.G, head = h * a.G + rc % a.G;
-    const int64_t qrow = t.q0 + pos;
+    const auto sees = [&](int row) -> int {  // keys that a row sees
+        return a.causal ? clampi(row / a.G + 1 - t.Lq + t.Lk, t.Lk) : t.Lk;
+    };
+    // the lane's row (a row past the end computes the last one's and stores nothing); the copy of the lane
+    // number keeps what only the masked tiles and the end need from living in registers through the loop
+    const auto my_row = [&]() -> int {
+        int x = threadIdx.x;
+        asm volatile("" : "+v"(x));
+        return t.r0 + 32 * w + (x & 31);
+    };
     float sl2 = head_scale(a, h) * PLOG2E;
 
-    // the lane's query row; a negative scale moves into its sign, a zero one into its values
+    // the query row; a negative scale moves into its sign, a zero one into its values
     bf16x8 qf[KS];
     {
-        const uint16_t *qp = (const uint16_t *)a.q + qrow * a.q_row + head * a.q_head;
+        const int r = my_row(), rc = r < rows ? r : rows - 1;
+        const uint16_t *qp = (const uint16_t *)a.q + (int64_t)(t.q0 + rc / a.G) * a.q_row + (h * a.G + rc % a.G) * a.q_head;
         const uint32_t flip = sl2 < 0.f ? 0x80008000u : 0u, keep = sl2 == 0.f ? 0u : ~0u;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -393,14 +398,12 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
         }
         sl2 = sl2 == 0.f ? 1.f : fabsf(sl2);
     }
-    const auto sees = [&](int row) -> int {  // keys that a row sees
-        return a.causal ? clampi(row / a.G + 1 - t.Lq + t.Lk, t.Lk) : t.Lk;
-    };
-    const int seen = sees(rc);
     const int end = t.r0 + PR < rows ? t.r0 + PR : rows;
     const int nt = (sees(end - 1) + PK - 1) / PK;
     const int j0 = (int)((int64_t)nt * split / a.splits), j1 = (int)((int64_t)nt * (split + 1) / a.splits);
-    const int gfew = sees(t.r0);                           // keys that every row of the workgroup sees
+    const int gfew = sees(t.r0);            // keys that every row of the workgroup sees
+    const int w0 = t.r0 + 32 * w;
+    const int wmost = w0 < rows ? sees(w0 + 31 < rows ? w0 + 31 : rows - 1) : 0;  // keys that some row of the wave sees
 
     // direct-to-LDS loads: load i of a tile fills rows RPI i .. of the slot in lane order
     const uint32_t krb = (uint32_t)(a.k_row * 2), vrb = (uint32_t)(a.v_row * 2);
@@ -410,35 +413,31 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
     {
         // columns past d: out of range, zeros
         const int lr = RPI * w + lane / (D / 8), p = lane % (D / 8);
-        const int kc = p ^ k_swizzle<D>(lr), kc1 = p ^ k_swizzle<D>(lr + RPI * PW), vc = p ^ v_swizzle<D>(lr);
+        const int kc = p ^ k_swizzle<D>(lr), kc1 = D == 256 ? p ^ k_swizzle<D>(lr + RPI * PW) : kc, vc = p ^ v_swizzle<D>(lr);
         kvo = 8 * kc < a.d ? (uint32_t)lr * krb + 16 * kc : 0x80000000u;
         kvo1 = 8 * kc1 < a.d ? (uint32_t)lr * krb + 16 * kc1 : 0x80000000u;  // every other load; the same for D < 256
         vvo = 8 * vc < a.d ? (uint32_t)lr * vrb + 16 * vc : 0x80000000u;
     }
-    // slots: keys of tile j at (j & 1) TB, values at (2 + (j & 1)) TB
-    const auto issue_k = [&](int j) {
+    const auto issue = [&](int j) {
         const int64_t key0 = (int64_t)j * PK;
-        unsigned char *slot = psm + (j & 1) * TB + w * 1024;
+        unsigned char *slot = psm + ((j - j0) & 1) * 2 * TB + w * 1024;
         const rsrc_t kr = rows_rsrc(kb_ + key0 * krb, t.Lk - key0, krb, a.d);
-#pragma unroll
-        for (int x = 0; x < NI; ++x)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, P_LDS(slot + x * PW * 1024), 16,
-                                                     (D == 256 && x % 2 ? kvo1 : kvo) + x * (RPI * PW) * krb, 0, 0, 0);
-    };
-    const auto issue_v = [&](int j) {
-        const int64_t key0 = (int64_t)j * PK;
-        unsigned char *slot = psm + (2 + (j & 1)) * TB + w * 1024;
         const rsrc_t vr = rows_rsrc(vb_ + key0 * vrb, t.Lk - key0, vrb, a.d);
 #pragma unroll
         for (int x = 0; x < NI; ++x)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, P_LDS(slot + x * PW * 1024), 16, vvo + x * (RPI * PW) * vrb, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, P_LDS(slot + x * PW * 1024), 16, (D == 256 && x % 2 ? kvo1 : kvo) + x * (RPI * PW) * krb, 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < NI; ++x)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, P_LDS(slot + TB + x * PW * 1024), 16, vvo + x * (RPI * PW) * vrb, 0,
+                                                     0, 0);
     };
-    // LDS reads: keys rl of a half, chunk 2 s + hh; values key 4 hh + (lane % 16) / 4, columns 16 ((lane / 16) % 2) + 4 (lane % 4)
-    const uint32_t kro = (uint32_t)(rl * RB + ((hh ^ k_swizzle<D>(rl)) * 16));
+    // LDS reads: key rl, chunk 2 s + hh; value key 4 hh + (lane % 16) / 4, columns 16 ((lane / 16) % 2) + 4 (lane % 4)
+    const uint32_t base = (uint32_t)(uintptr_t)P_LDS(psm);
+    const uint32_t kro = base + rl * RB + ((hh ^ k_swizzle<D>(rl)) * 16);
     uint32_t vro;
     {
         const int key = 4 * hh + (lane & 15) / 4, c = 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
-        vro = (uint32_t)(key * RB + ((c ^ v_swizzle<D>(key)) * 16) + 8 * (lane & 1));
+        vro = base + TB + key * RB + ((c ^ v_swizzle<D>(key)) * 16) + 8 * (lane & 1);
     }
 
     f32x16 acc[DB];
@@ -448,158 +447,140 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
         for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
     float m = PMIN, l = 0.f;
     typedef __attribute__((address_space(3))) bf16x4 lds4;
-    const auto value = [&](const unsigned char *slot, int kb, int n) -> bf16x8 {  // keys of step kb, columns 32 n ..
-        const uint32_t at = (vro ^ (n * 64)) + kb * 16 * RB;
-        const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)P_LDS(slot + at));
-        const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)P_LDS(slot + at + 8 * RB));
+    typedef __attribute__((address_space(3))) bf16x8 lds8;
+    // 16 keys' values at an LDS address
+    const auto value = [&](uint32_t at) __attribute__((always_inline)) -> bf16x8 {
+        const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)at);
+        const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(at + 8 * RB));
         return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    const auto score = [&](const unsigned char *slot, int half, int c, f32x16 &s) __attribute__((always_inline)) {
-        const bf16x8 kf = *(const bf16x8 *)(slot + half * 32 * RB + (kro ^ (c * 32)));
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], s, 0, 0, 0);
-    };
-    const auto add_value = [&](const unsigned char *slot, int half, int x, const bf16x8 (&p)[2]) __attribute__((always_inline)) {
-        const int kb = x / DB, n = x % DB;
-        acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(slot, 2 * half + kb, n), p[kb], acc[n], 0, 0, 0);
-    };
-    // One pipeline step: the weights of unit u (32 keys) from its scores s, beside the scores of unit u + 1
-    // (half kh of the key tile kt) and the values of unit u - 1 (half vh of vt, weights pv): the products
-    // need no result of the exponentials and fill the time that they take.  The maximum m is a whole
-    // number, so a rescaling is by a power of two and exact, of the weights that wait in pv too.
-    const auto unit = [&](f32x16 &s, bf16x8 (&p)[2], const unsigned char *kt, int kh, f32x16 &sn, const unsigned char *vt,
-                          int vh, bf16x8 (&pv)[2], int key0, auto masked) __attribute__((always_inline)) {
+    // one tile of keys in the slot at `at`; masked: some row of the wave does not see all of it, the lane's
+    // row sees its keys up to lim (counted from the lane's first)
+    const auto step = [&](uint32_t at, int lim, auto masked) __attribute__((always_inline)) {
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < KS; ++c)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds8 *)(uintptr_t)((kro ^ (c * 32)) + at), qf[c], s, 0, 0, 0);
         if (decltype(masked)::value) {
-            const int lim = seen - key0 - 4 * hh;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (8 * (i / 4) + i % 4 >= lim) s[i] = -INFINITY;
         }
-        float mt = s[0];
+        bf16x8 pf[2];
+        float sum;
+        const auto weights = [&]() __attribute__((always_inline)) {
+            sum = 0.f;
 #pragma unroll
-        for (int i = 1; i < 16; ++i) mt = fmaxf(mt, s[i]);
-        mt = half_max(mt) * sl2;
-        if (__any(mt > m + RESCALE)) {
-            const float mn = fmaxf(m, ceilf(mt)), al = __builtin_amdgcn_exp2f(m - mn);
+            for (int i = 0; i < 16; ++i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -m));
+                sum += p;
+                pf[i / 8][i % 8] = (__bf16)p;
+            }
+        };
+        weights();
+        if (__any(!(sum <= GROWN))) {
+            // only the rows that ask for it take a new maximum: a row's bits do not depend on its neighbours
+            float mt = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mt = fmaxf(mt, s[i]);
+            const bool ask = half_max(sum <= GROWN ? 0.f : 1.f) > 0.f;
+            const float mn = ask ? fmaxf(m, half_max(mt) * sl2) : m, al = __builtin_amdgcn_exp2f(m - mn);
             m = mn;
             l *= al;
 #pragma unroll
             for (int n = 0; n < DB; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[n][i] *= al;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) pv[i / 8][i % 8] = (__bf16)((float)pv[i / 8][i % 8] * al);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sn[i] = 0.f;
-#pragma unroll
-        for (int x = 0; x < KS || x < 2 * DB; ++x) {
-            if (x < KS) score(kt, kh, x, sn);
-            if (x < 2 * DB) add_value(vt, vh, x, pv);
-        }
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -m));
-            sum += e;
-            p[i / 8][i % 8] = (__bf16)e;
+            weights();
         }
         l += sum;
-        // here, beside the products, and not where they are used
-        asm volatile("" : "+v"(*(u32x4 *)&p[0]), "+v"(*(u32x4 *)&p[1]), "+v"(l));
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int n = 0; n < DB; ++n)
+                acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value((vro ^ (n * 64)) + at + kb * 16 * RB), pf[kb], acc[n], 0, 0, 0);
     };
     // A hidden key's weight is 0, but 0 times an infinity or a NaN is a NaN.  In a tile that holds such a
-    // value and is hidden from some row, the value is taken out before its product; whether a row sees an
+    // value and is hidden from some row, the value is taken out before `step`; whether a row sees an
     // infinity of either sign (or a NaN, taken as both) in a column comes from products of 0 / 1 marks, and
-    // is added at the very end.
-    uint16_t *marks = (uint16_t *)(psm + 4 * TB) + threadIdx.x;
-    bool marked = false;
-    const auto take_out = [&](unsigned char *slot, int key0) __attribute__((always_inline)) {
-        const int lim = seen - key0 - 4 * hh;
+    // is added after it.
+    uint16_t *marks = (uint16_t *)(psm + 4 * TB + 16) + threadIdx.x;
+    const auto take_out = [&](uint32_t at, int lim) __attribute__((always_inline)) {
 #pragma unroll 1
-        for (int n = 0; n < DB; ++n) {
+        for (int it = 0; it < 2 * DB; ++it) {  // column block it / 2, infinities of either sign
+            const float sign = it & 1 ? -1.f : 1.f;
+            f32x16 u;
 #pragma unroll
-            for (int sign = 0; sign < 2; ++sign) {
-                f32x16 u;
+            for (int i = 0; i < 16; ++i) u[i] = 0.f;
+#pragma unroll 1
+            for (int kb = 0; kb < 2; ++kb) {
+                const bf16x8 x = value((vro ^ (it / 2 * 64)) + at + kb * 16 * RB);
+                bf16x8 mark, sees_;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) u[i] = 0.f;
-                for (int kb = 0; kb < 4; ++kb) {
-                    const bf16x8 x = value(slot, kb, n);
-                    bf16x8 mark, sees_;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float y = sign ? -(float)x[i] : (float)x[i];
-                        mark[i] = (__bf16)(!(fabsf(y) < INFINITY) && !(y < 0.f) ? 1.f : 0.f);
-                        sees_[i] = (__bf16)(16 * kb + 8 * (i / 4) + i % 4 < lim ? 1.f : 0.f);
-                    }
-                    u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(mark, sees_, u, 0, 0, 0);
+                for (int i = 0; i < 8; ++i) {
+                    const float y = sign * (float)x[i];
+                    mark[i] = (__bf16)(!(fabsf(y) < INFINITY) && !(y < 0.f) ? 1.f : 0.f);
+                    sees_[i] = (__bf16)(16 * kb + 8 * (i / 4) + i % 4 < lim ? 1.f : 0.f);
                 }
-                uint32_t bits = 0;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) bits |= u[i] > 0.f ? 1u << i : 0u;
-                if (marked) bits |= marks[(2 * n + sign) * PTH];
-                marks[(2 * n + sign) * PTH] = (uint16_t)bits;
+                u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(mark, sees_, u, 0, 0, 0);
             }
+            uint32_t bits = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) bits |= u[i] > 0.f ? 1u << i : 0u;
+            marks[it * PTH] = (uint16_t)bits;
         }
         __syncthreads();
         for (int x = threadIdx.x; x < TB / 4; x += PTH) {
-            uint32_t y = ((uint32_t *)slot)[x];
+            uint32_t y = ((uint32_t *)(psm + at + TB))[x];
             if ((y & 0x7F80u) == 0x7F80u) y &= 0xFFFF0000u;
             if ((y & 0x7F800000u) == 0x7F800000u) y &= 0xFFFFu;
-            ((uint32_t *)slot)[x] = y;
+            ((uint32_t *)(psm + at + TB))[x] = y;
         }
         __syncthreads();
-        marked = true;
     };
-    f32x16 sa, sb;
-    bf16x8 pa[2], pb[2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pb[kb][i] = (__bf16)0.f;
-    // tile j: unit 2 j, then 2 j + 1.  At its start the scores of unit 2 j are in sa, the weights of unit
-    // 2 j - 1 in pb, keys j and values j - 1 in their slots, keys j + 1 and values j on their way.
-    const auto tile = [&](int j, auto masked) __attribute__((always_inline)) {
-        unsigned char *k0s = psm + (j & 1) * TB, *k1s = psm + (~j & 1) * TB;
-        unsigned char *v0s = psm + (2 + (j & 1)) * TB, *v1s = psm + (2 + (~j & 1)) * TB;
-        unit(sa, pa, k0s, 1, sb, v1s, 1, pb, j * PK, masked);
+    if (j0 < j1) issue(j0);
+    int j = j0;
+    // tiles that every row of the workgroup sees whole; two by two, so that the slots are constants
+    const auto arrive = [&]() __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (decltype(masked)::value) {
+        // every wave's loads of this tile have landed, and every wave is done with the other slot
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (j + 1 < j1) issue(j + 1);
+    };
+    for (const int full = gfew / PK < j1 ? gfew / PK : j1; j < full;) {
+        arrive();
+        step(0, 0, std::false_type());
+        if (++j >= full) break;
+        arrive();
+        step(2 * TB, 0, std::false_type());
+        ++j;
+    }
+    // tiles hidden from some row
+    const int mine = my_row(), seen = sees(mine < rows ? mine : rows - 1);
+    for (; j < j1; ++j) {
+        const int key0 = j * PK;
+        const uint32_t at = ((j - j0) & 1) * 2 * TB;
+        const int lim = seen - key0 - 4 * hh;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        {
             // look for non-finite values in what this wave loaded
             uint32_t e = 0;
 #pragma unroll
             for (int x = 0; x < NI; ++x) {
-                const uint4 y = *(const uint4 *)(v0s + (x * PW + w) * 1024 + lane * 16);
+                const uint4 y = *(const uint4 *)(psm + at + TB + (x * PW + w) * 1024 + lane * 16);
                 e |= ((y.x & 0x7F807F80u) + 0x00800080u) | ((y.y & 0x7F807F80u) + 0x00800080u) |
                      ((y.z & 0x7F807F80u) + 0x00800080u) | ((y.w & 0x7F807F80u) + 0x00800080u);
             }
             if (e & 0x80008000u) bad_tile[j & 1] = j + 1;
         }
-        // every wave's loads have landed, and every wave is done with keys j and values j - 1
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (j + 2 < j1) issue_k(j + 2);
-        if (j + 1 < j1) issue_v(j + 1);
-        if (decltype(masked)::value && __builtin_amdgcn_readfirstlane(bad_tile[j & 1]) == j + 1) take_out(v0s, j * PK);
-        unit(sb, pb, k1s, 0, sa, v0s, 0, pa, j * PK + 32, masked);
-    };
-    if (j0 < j1) {
-        issue_k(j0);
-        if (j0 + 1 < j1) issue_k(j0 + 1);
-        issue_v(j0);
-        // the values before the first tile: zeros, as their weights are
-        for (int x = threadIdx.x; x < TB / 16; x += PTH) ((uint4 *)(psm + (2 + (~j0 & 1)) * TB))[x] = make_uint4(0, 0, 0, 0);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"i"(NI) : "memory");  // keys j0 (and j0 + 1): values j0 are not awaited
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sa[i] = 0.f;
-#pragma unroll
-        for (int x = 0; x < KS; ++x) score(psm + (j0 & 1) * TB, 0, x, sa);
-        int j = j0;
-        // tiles that every row of the workgroup sees whole, then those hidden from some row
-        for (const int full = gfew / PK < j1 ? gfew / PK : j1; j < full; ++j) tile(j, std::false_type());
-        for (; j < j1; ++j) tile(j, std::true_type());
-#pragma unroll
-        for (int x = 0; x < 2 * DB; ++x) add_value(psm + (2 + (~j1 & 1)) * TB, 1, x, pb);
-        if (marked) {
+        if (j + 1 < j1) issue(j + 1);
+        const bool bad = __builtin_amdgcn_readfirstlane(bad_tile[j & 1]) == j + 1;
+        if (bad) take_out(at, lim);
+        if (key0 < wmost) step(at, lim, std::true_type());
+        if (bad) {
 #pragma unroll
             for (int n = 0; n < DB; ++n) {
                 const uint32_t up = marks[2 * n * PTH], dn = marks[(2 * n + 1) * PTH];
@@ -615,10 +596,11 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 2) prompt_mfma(PromptArgs 
         const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
         l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
     }
-    if (!live) return;
+    const int r = my_row();
+    if (r >= rows) return;
     const float il = l > 0.f || l != l ? 1.f / l : 0.f;
     const float lse2 = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
-    const int64_t orow = qrow * a.Hq + head, prow = (int64_t)split * a.Tq * a.Hq + orow;
+    const int64_t orow = (int64_t)(t.q0 + r / a.G) * a.Hq + h * a.G + r % a.G, prow = (int64_t)split * a.Tq * a.Hq + orow;
 #pragma unroll
     for (int n = 0; n < DB; ++n)
 #pragma unroll
@@ -720,7 +702,7 @@ hipError_t launch_prompt(const fw_packed &p, void *o, float *lse, int splits, fl
     if (prompt_fast(p)) {
         const dim3 grid((unsigned)(row_tiles(p, PR) * p.Hkv), (unsigned)splits);
         const int D = a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256;
-        const size_t lds = (size_t)2 * 2 * PK * 2 * D + (size_t)D / 32 * 2 * 2 * PTH;  // two slots, marks
+        const size_t lds = (size_t)2 * 2 * PK * 2 * D + 16 + (size_t)D / 32 * 2 * 2 * PTH;  // two slots, flags, marks
         if (D == 64) hipLaunchKernelGGL((prompt_mfma<64>), grid, dim3(PTH), lds, st, a);
         else if (D == 128) hipLaunchKernelGGL((prompt_mfma<128>), grid, dim3(PTH), lds, st, a);
         else hipLaunchKernelGGL((prompt_mfma<256>), grid, dim3(PTH), lds, st, a);
