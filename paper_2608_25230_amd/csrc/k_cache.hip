@@ -235,6 +235,7 @@ struct StoreArgs {
     uint8_t *kc, *vc, *k_exp, *v_exp;
     int64_t n_blocks;
     int shift, bs, d, dp, chunk;
+    bool k_wide, v_wide;  // 16-byte pieces of keys, pairs of values are aligned
 };
 
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }  // -126 <= e <= 127
@@ -253,11 +254,12 @@ __device__ __forceinline__ float finite_abs(float x) {
     return x < INFINITY ? x : 0.f;
 }
 
-// two values at a power-of-two scale to two codes in the low half
-__device__ __forceinline__ uint32_t codes2(float x, float y, float s) {
+// two values at a power-of-two scale to two codes in the low half (or, with `hi`, the high half of `to`)
+template <bool HI = false>
+__device__ __forceinline__ uint32_t codes2(float x, float y, float s, uint32_t to = 0) {
     const float nan = __uint_as_float(0x7FC00000u);
     const float a = fabsf(x) < INFINITY ? x * s : nan, b = fabsf(y) < INFINITY ? y * s : nan;
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xFFFFu;
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)to, HI);
 }
 __device__ __forceinline__ uint32_t shift_codes(uint32_t c, float s) {  // four codes to a larger exponent
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
@@ -265,74 +267,214 @@ __device__ __forceinline__ uint32_t shift_codes(uint32_t c, float s) {  // four 
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b[0] * s, b[1] * s, r, true);
 }
 
+// Eight elements of a row from column c on, as they are; columns past d are zero.
+template <typename T> struct Raw8;
+template <> struct Raw8<uint16_t> {
+    uint4 x;
+    __device__ __forceinline__ void get(float (&y)[8]) const {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[2 * i] = __uint_as_float(w[i] << 16), y[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+    __device__ __forceinline__ void load(const uint16_t *p, int c, int d, bool wide) {
+        if (wide && c < d) {
+            x = *(const uint4 *)(p + c);
+            return;
+        }
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = (c + 2 * i < d ? p[c + 2 * i] : 0u) | (c + 2 * i + 1 < d ? (uint32_t)p[c + 2 * i + 1] << 16 : 0u);
+        x = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <> struct Raw8<float> {
+    float4 x, z;
+    __device__ __forceinline__ void get(float (&y)[8]) const {
+        y[0] = x.x, y[1] = x.y, y[2] = x.z, y[3] = x.w, y[4] = z.x, y[5] = z.y, y[6] = z.z, y[7] = z.w;
+    }
+    __device__ __forceinline__ void load(const float *p, int c, int d, bool wide) {
+        if (wide && c < d) {
+            x = *(const float4 *)(p + c), z = *(const float4 *)(p + c + 4);
+            return;
+        }
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = c + i < d ? p[c + i] : 0.f;
+        x = make_float4(w[0], w[1], w[2], w[3]), z = make_float4(w[4], w[5], w[6], w[7]);
+    }
+};
+// Two elements, likewise.
+template <typename T> struct Raw2;
+template <> struct Raw2<uint16_t> {
+    uint32_t x;
+    __device__ __forceinline__ void load(const uint16_t *p, int c, int d, bool wide) {
+        if (wide) x = *(const uint32_t *)(p + c);
+        else x = p[c] | (c + 1 < d ? (uint32_t)p[c + 1] << 16 : 0u);
+    }
+    __device__ __forceinline__ float lo() const { return __uint_as_float(x << 16); }
+    __device__ __forceinline__ float hi() const { return __uint_as_float(x & 0xFFFF0000u); }
+};
+template <> struct Raw2<float> {
+    float2 x;
+    __device__ __forceinline__ void load(const float *p, int c, int d, bool wide) {
+        if (wide) x = *(const float2 *)(p + c);
+        else x = make_float2(p[c], c + 1 < d ? p[c + 1] : 0.f);
+    }
+    __device__ __forceinline__ float lo() const { return x.x; }
+    __device__ __forceinline__ float hi() const { return x.y; }
+};
+
+// A thread holds KREG pieces of eight keys' columns, and of the values two
+// columns of 16 tokens, in registers between the maximum and the rounding: all
+// of a 64-token block of 128-wide rows.  What a larger run has beyond that is
+// read twice.
 template <typename T>
 __global__ void __launch_bounds__(ST) cache_store(StoreArgs a) {
+    constexpr int KREG = 4;
     __shared__ int starts[SMAX], n_starts, fail;
-    __shared__ float red[ST / 64];
+    __shared__ float red[2][ST / 64];
+    const int tid = threadIdx.x;
     const int64_t x0 = (int64_t)blockIdx.x * a.chunk;
     const int64_t limit = a.n_blocks << a.shift;
     const T *k = (const T *)a.k, *v = (const T *)a.v;
     // the tokens of this workgroup's chunk that open a run
-    if (threadIdx.x == 0) n_starts = 0;
+    if (tid == 0) n_starts = 0;
     __syncthreads();
     {
-        const int64_t x = x0 + threadIdx.x;
+        const int64_t x = x0 + tid;
         bool first = false;
-        if ((int)threadIdx.x < a.chunk && x < a.N) {
+        if (tid < a.chunk && x < a.N) {
             const int64_t s = a.slots[x], p = x > 0 ? a.slots[x - 1] : -1;
             first = s >= 0 && s < limit && (x == 0 || s != p + 1 || (s & (a.bs - 1)) == 0);
         }
-        if (first) starts[atomicAdd(&n_starts, 1)] = threadIdx.x;  // any order: runs do not meet
+        if (first) starts[atomicAdd(&n_starts, 1)] = tid;  // any order: runs do not meet
     }
     __syncthreads();
     const int runs = n_starts;
+    const int kch = a.dp / 8, kdiv = (65536 + kch - 1) / kch;  // i / kch = i kdiv >> 16 for i < 8192
+    const int vch = a.dp / 2, vdiv = (65536 + vch - 1) / vch;
     for (int y = 0; y < runs; ++y) {
         const int64_t x = x0 + starts[y], s = a.slots[x], b = s >> a.shift;
         const int off = (int)(s & (a.bs - 1));
         // its length: as long as the slots follow each other inside the block
-        if (threadIdx.x == 0) fail = a.bs - off;
+        if (tid == 0) fail = a.bs - off;
         __syncthreads();
-        if ((int)threadIdx.x < a.bs - off && (x + threadIdx.x >= a.N || a.slots[x + threadIdx.x] != s + threadIdx.x))
-            atomicMin(&fail, (int)threadIdx.x);
+        if (tid < a.bs - off && (x + tid >= a.N || a.slots[x + tid] != s + tid)) atomicMin(&fail, tid);
         __syncthreads();
         const int n = fail;
+        const int kn = n * kch, g0 = off >> 4, vn = (((off + n - 1) >> 4) - g0 + 1) * vch;
+        const T *kx = k + x * a.k_row, *vx = v + x * a.v_row;
+        const auto load_k = [&](int i, Raw8<T> &w) {  // piece i: row i / kch
+            const int r = (i * kdiv) >> 16;
+            w.load(kx + (int64_t)r * a.k_row, 8 * (i - r * kch), a.d, a.k_wide);
+        };
+        const auto load_v = [&](int i, Raw2<T> (&w)[16]) {  // piece i: tokens 16 (g0 + i / vch) .., columns 2 (i % vch) ..
+            const int g = (i * vdiv) >> 16, c = 2 * (i - g * vch), r0 = 16 * (g0 + g) - off;
+#pragma unroll
+            for (int t = 0; t < 16; ++t) {
+                w[t].x = decltype(w[t].x){};
+                if (c < a.d && r0 + t >= 0 && r0 + t < n) w[t].load(vx + (int64_t)(r0 + t) * a.v_row, c, a.d, a.v_wide);
+            }
+        };
+        Raw8<T> kr[KREG];
+        Raw2<T> vr[16];
+#pragma unroll
+        for (int u = 0; u < KREG; ++u)
+            if (tid + u * ST < kn) load_k(tid + u * ST, kr[u]);
+        if (tid < vn) load_v(tid, vr);
         float ak = 0.f, av = 0.f;
-        for (int i = threadIdx.x; i < n * a.d; i += ST) {
-            const int r = i / a.d, c = i % a.d;
-            ak = fmaxf(ak, finite_abs(Elem<T>::load(k, (size_t)((x + r) * a.k_row + c))));
-            av = fmaxf(av, finite_abs(Elem<T>::load(v, (size_t)((x + r) * a.v_row + c))));
+        const auto max_k = [&](const Raw8<T> &w) {
+            float z[8];
+            w.get(z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ak = fmaxf(ak, finite_abs(z[i]));
+        };
+        const auto max_v = [&](const Raw2<T> (&w)[16]) {
+#pragma unroll
+            for (int t = 0; t < 16; ++t) av = fmaxf(av, fmaxf(finite_abs(w[t].lo()), finite_abs(w[t].hi())));
+        };
+#pragma unroll
+        for (int u = 0; u < KREG; ++u)
+            if (tid + u * ST < kn) max_k(kr[u]);
+        for (int i = tid + KREG * ST; i < kn; i += ST) {
+            Raw8<T> w;
+            load_k(i, w);
+            max_k(w);
         }
-        ak = block_reduce(ak, red, OpMax());
-        av = block_reduce(av, red, OpMax());
+        if (tid < vn) max_v(vr);
+        for (int i = tid + ST; i < vn; i += ST) {
+            Raw2<T> w[16];
+            load_v(i, w);
+            max_v(w);
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) ak = fmaxf(ak, __shfl_xor(ak, o)), av = fmaxf(av, __shfl_xor(av, o));
+        if ((tid & 63) == 0) red[0][tid >> 6] = ak, red[1][tid >> 6] = av;
         const int wk = off ? min((int)a.k_exp[b], 253) : 0, wv = off ? min((int)a.v_exp[b], 253) : 0;
+        __syncthreads();  // also: everyone has read the old exponents
+#pragma unroll
+        for (int i = 0; i < ST / 64; ++i) ak = fmaxf(ak, red[0][i]), av = fmaxf(av, red[1][i]);
         const int ek = max(scale_byte(ak), wk), ev = max(scale_byte(av), wv);
         uint8_t *kb = a.kc + b * a.bs * a.dp, *vb = a.vc + b * a.bs * a.dp;
         if (off && ek > wk) {
             const float f = ek - wk > 126 ? 0.f : pow2(wk - ek);
-            for (int i = threadIdx.x; i < off * a.dp / 4; i += ST) ((uint32_t *)kb)[i] = shift_codes(((uint32_t *)kb)[i], f);
+            for (int i = tid; i < off * a.dp / 4; i += ST) ((uint32_t *)kb)[i] = shift_codes(((uint32_t *)kb)[i], f);
         }
         if (off && ev > wv) {
             const float f = ev - wv > 126 ? 0.f : pow2(wv - ev);
-            for (int i = threadIdx.x; i < a.dp * off; i += ST) {
+            for (int i = tid; i < a.dp * off; i += ST) {
                 uint8_t *p = vb + (i / off) * a.bs + i % off;
                 *p = (uint8_t)shift_codes(*p, f);
             }
         }
-        __syncthreads();  // everyone has read the old exponents
-        if (threadIdx.x == 0) {
+        if (tid == 0) {
             a.k_exp[b] = (uint8_t)ek;
             a.v_exp[b] = (uint8_t)ev;
         }
         const float fk = pow2(127 - ek), fv = pow2(127 - ev);
-        for (int i = threadIdx.x; i < n * a.dp / 2; i += ST) {
-            const int r = i / (a.dp / 2), c = 2 * (i % (a.dp / 2));
-            const float p = c < a.d ? Elem<T>::load(k, (size_t)((x + r) * a.k_row + c)) : 0.f;
-            const float q = c + 1 < a.d ? Elem<T>::load(k, (size_t)((x + r) * a.k_row + c + 1)) : 0.f;
-            *(uint16_t *)(kb + (off + r) * a.dp + c) = (uint16_t)codes2(p, q, fk);
+        const auto put_k = [&](int i, const Raw8<T> &w) {  // pieces lie in the block in their order
+            float z[8];
+            w.get(z);
+            const uint32_t lo = codes2<true>(z[2], z[3], fk, codes2(z[0], z[1], fk));
+            const uint32_t hi = codes2<true>(z[6], z[7], fk, codes2(z[4], z[5], fk));
+            *(uint2 *)(kb + (int64_t)off * a.dp + 8 * i) = make_uint2(lo, hi);
+        };
+        const auto put_v = [&](int i, const Raw2<T> (&w)[16]) {
+            const int g = (i * vdiv) >> 16, c = 2 * (i - g * vch), t0 = 16 * (g0 + g), r0 = t0 - off;
+            if (c >= a.d) return;
+            uint32_t lo[4], hi[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                lo[q] = codes2<true>(w[4 * q + 2].lo(), w[4 * q + 3].lo(), fv, codes2(w[4 * q].lo(), w[4 * q + 1].lo(), fv));
+                hi[q] = codes2<true>(w[4 * q + 2].hi(), w[4 * q + 3].hi(), fv, codes2(w[4 * q].hi(), w[4 * q + 1].hi(), fv));
+            }
+            uint8_t *p = vb + c * a.bs + t0;
+            if (r0 >= 0 && r0 + 16 <= n) {
+                *(uint4 *)p = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                if (c + 1 < a.d) *(uint4 *)(p + a.bs) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 16; ++t)
+                    if (r0 + t >= 0 && r0 + t < n) {
+                        p[t] = (uint8_t)(lo[t / 4] >> 8 * (t % 4));
+                        if (c + 1 < a.d) p[a.bs + t] = (uint8_t)(hi[t / 4] >> 8 * (t % 4));
+                    }
+            }
+        };
+#pragma unroll
+        for (int u = 0; u < KREG; ++u)
+            if (tid + u * ST < kn) put_k(tid + u * ST, kr[u]);
+        for (int i = tid + KREG * ST; i < kn; i += ST) {
+            Raw8<T> w;
+            load_k(i, w);
+            put_k(i, w);
         }
-        for (int i = threadIdx.x; i < n * a.d; i += ST) {
-            const int r = i / a.d, c = i % a.d;
-            vb[c * a.bs + off + r] = (uint8_t)codes2(Elem<T>::load(v, (size_t)((x + r) * a.v_row + c)), 0.f, fv);
+        if (tid < vn) put_v(tid, vr);
+        for (int i = tid + ST; i < vn; i += ST) {
+            Raw2<T> w[16];
+            load_v(i, w);
+            put_v(i, w);
         }
         __syncthreads();
     }
@@ -379,6 +521,9 @@ hipError_t launch_store(const fw_cache &cache, int dtype, const void *k, int64_t
     a.kc = cache.k, a.vc = cache.v, a.k_exp = cache.k_exp, a.v_exp = cache.v_exp;
     a.n_blocks = cache.n_blocks, a.bs = cache.block_size, a.shift = __builtin_ctz(cache.block_size);
     a.d = (int)cache.d, a.dp = cache_row(cache.d);
+    const int size = dtype == FW_F32 ? 4 : 2;
+    a.k_wide = a.d % 8 == 0 && k_row * size % 16 == 0 && (uintptr_t)k % 16 == 0;
+    a.v_wide = a.d % 2 == 0 && v_row % 2 == 0 && (uintptr_t)v % (2 * size) == 0;
     a.chunk = 1;
     while (a.chunk < a.bs && N / (2 * a.chunk) >= 2048) a.chunk *= 2;
     const dim3 grid((unsigned)((N + a.chunk - 1) / a.chunk));
