@@ -235,7 +235,6 @@ struct StoreArgs {
     uint8_t *kc, *vc, *k_exp, *v_exp;
     int64_t n_blocks;
     int shift, bs, d, dp, chunk;
-    bool k_wide, v_wide;  // 16-byte pieces of keys, pairs of values are aligned
 };
 
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }  // -126 <= e <= 127
@@ -247,11 +246,6 @@ __device__ __forceinline__ int scale_byte(float amax) {
     const float m = frexpf(amax, &x);  // amax = m 2^x, m in [1/2, 1); 448 = 7/8 2^9
     const int b = x - 9 + (m > 0.875f) + 127;
     return b < 1 ? 1 : b > 253 ? 253 : b;
-}
-
-__device__ __forceinline__ float finite_abs(float x) {
-    x = fabsf(x);
-    return x < INFINITY ? x : 0.f;
 }
 
 // two values at a power-of-two scale to two codes in the low half (or, with `hi`, the high half of `to`)
@@ -267,69 +261,83 @@ __device__ __forceinline__ uint32_t shift_codes(uint32_t c, float s) {  // four 
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b[0] * s, b[1] * s, r, true);
 }
 
-// Eight elements of a row from column c on, as they are; columns past d are zero.
-template <typename T> struct Raw8;
-template <> struct Raw8<uint16_t> {
-    uint4 x;
-    __device__ __forceinline__ void get(float (&y)[8]) const {
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[2 * i] = __uint_as_float(w[i] << 16), y[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+// Rows [0, n) of a run.  WIDE: 16-byte aligned rows of a multiple of 8
+// columns, through a buffer descriptor that ends with the run: a row before
+// or past it, or a column past d, reads zeros, with no branch and 32-bit
+// offsets.  Otherwise element by element.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T, bool WIDE>
+struct RunRows {
+    const T *base;
+    int64_t row;   // elements
+    uint32_t bytes;
+    int n, d;
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ __forceinline__ RunRows(const T *p, int64_t row_, int n_, int d_) : base(p), row(row_), n(n_), d(d_) {
+        bytes = (uint32_t)(row_ * sizeof(T));
+        if constexpr (WIDE)
+            rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(p), (short)0, (int)((n - 1) * bytes + d * sizeof(T)),
+                                                     0x00020000);
     }
-    __device__ __forceinline__ void load(const uint16_t *p, int c, int d, bool wide) {
-        if (wide && c < d) {
-            x = *(const uint4 *)(p + c);
-            return;
+    // columns c .. c + 8 of row r
+    __device__ __forceinline__ void load8(int r, int c, float (&y)[8]) const {
+        if constexpr (WIDE) {
+            const uint32_t at = c < d ? r * bytes + c * (uint32_t)sizeof(T) : 0x80000000u;
+            if constexpr (sizeof(T) == 2) {
+                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[2 * i] = __uint_as_float(x[i] << 16), y[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+            } else {
+                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0);
+                const u32x4 z = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + 16, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = __uint_as_float(x[i]), y[4 + i] = __uint_as_float(z[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = r < n && c + i < d ? Elem<T>::load(base, (size_t)(r * row + c + i)) : 0.f;
         }
-        uint32_t w[4];
+    }
+    // columns c, c + 1 of rows r0 .. r0 + 15, those outside the run as zeros
+    __device__ __forceinline__ void load2(int r0, int c, float (&lo)[16], float (&hi)[16]) const {
+        if constexpr (WIDE) {
+            const uint32_t at = c < d ? r0 * bytes + c * (uint32_t)sizeof(T) : 0x80000000u;
+            const uint32_t step = c < d ? bytes : 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w[i] = (c + 2 * i < d ? p[c + 2 * i] : 0u) | (c + 2 * i + 1 < d ? (uint32_t)p[c + 2 * i + 1] << 16 : 0u);
-        x = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-};
-template <> struct Raw8<float> {
-    float4 x, z;
-    __device__ __forceinline__ void get(float (&y)[8]) const {
-        y[0] = x.x, y[1] = x.y, y[2] = x.z, y[3] = x.w, y[4] = z.x, y[5] = z.y, y[6] = z.z, y[7] = z.w;
-    }
-    __device__ __forceinline__ void load(const float *p, int c, int d, bool wide) {
-        if (wide && c < d) {
-            x = *(const float4 *)(p + c), z = *(const float4 *)(p + c + 4);
-            return;
+            for (int t = 0; t < 16; ++t) {
+                if constexpr (sizeof(T) == 2) {
+                    const uint32_t x = __builtin_amdgcn_raw_buffer_load_b32(rsrc, at + t * step, 0, 0);
+                    lo[t] = __uint_as_float(x << 16), hi[t] = __uint_as_float(x & 0xFFFF0000u);
+                } else {
+                    const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(rsrc, at + t * step, 0, 0);
+                    lo[t] = __uint_as_float(x[0]), hi[t] = __uint_as_float(x[1]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 16; ++t) {
+                const int r = r0 + t;
+                const bool in = r >= 0 && r < n;
+                lo[t] = in && c < d ? Elem<T>::load(base, (size_t)(r * row + c)) : 0.f;
+                hi[t] = in && c + 1 < d ? Elem<T>::load(base, (size_t)(r * row + c + 1)) : 0.f;
+            }
         }
-        float w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = c + i < d ? p[c + i] : 0.f;
-        x = make_float4(w[0], w[1], w[2], w[3]), z = make_float4(w[4], w[5], w[6], w[7]);
     }
-};
-// Two elements, likewise.
-template <typename T> struct Raw2;
-template <> struct Raw2<uint16_t> {
-    uint32_t x;
-    __device__ __forceinline__ void load(const uint16_t *p, int c, int d, bool wide) {
-        if (wide) x = *(const uint32_t *)(p + c);
-        else x = p[c] | (c + 1 < d ? (uint32_t)p[c + 1] << 16 : 0u);
-    }
-    __device__ __forceinline__ float lo() const { return __uint_as_float(x << 16); }
-    __device__ __forceinline__ float hi() const { return __uint_as_float(x & 0xFFFF0000u); }
-};
-template <> struct Raw2<float> {
-    float2 x;
-    __device__ __forceinline__ void load(const float *p, int c, int d, bool wide) {
-        if (wide) x = *(const float2 *)(p + c);
-        else x = make_float2(p[c], c + 1 < d ? p[c + 1] : 0.f);
-    }
-    __device__ __forceinline__ float lo() const { return x.x; }
-    __device__ __forceinline__ float hi() const { return x.y; }
 };
 
-// A thread holds KREG pieces of eight keys' columns, and of the values two
-// columns of 16 tokens, in registers between the maximum and the rounding: all
+// The largest finite magnitude: the largest of the bits that is a number.
+__device__ __forceinline__ float larger(float top, float x) {
+    const float y = fabsf(x);
+    return y < INFINITY ? fmaxf(top, y) : top;
+}
+
+// Between the maximum and the rounding a thread holds KREG pieces of eight
+// keys' columns and two columns of 16 tokens of the values in registers: all
 // of a 64-token block of 128-wide rows.  What a larger run has beyond that is
 // read twice.
-template <typename T>
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(ST) cache_store(StoreArgs a) {
     constexpr int KREG = 4;
     __shared__ int starts[SMAX], n_starts, fail;
@@ -337,7 +345,6 @@ __global__ void __launch_bounds__(ST) cache_store(StoreArgs a) {
     const int tid = threadIdx.x;
     const int64_t x0 = (int64_t)blockIdx.x * a.chunk;
     const int64_t limit = a.n_blocks << a.shift;
-    const T *k = (const T *)a.k, *v = (const T *)a.v;
     // the tokens of this workgroup's chunk that open a run
     if (tid == 0) n_starts = 0;
     __syncthreads();
@@ -355,58 +362,48 @@ __global__ void __launch_bounds__(ST) cache_store(StoreArgs a) {
     const int kch = a.dp / 8, kdiv = (65536 + kch - 1) / kch;  // i / kch = i kdiv >> 16 for i < 8192
     const int vch = a.dp / 2, vdiv = (65536 + vch - 1) / vch;
     for (int y = 0; y < runs; ++y) {
-        const int64_t x = x0 + starts[y], s = a.slots[x], b = s >> a.shift;
+        const int64_t x = x0 + __builtin_amdgcn_readfirstlane(starts[y]), s = a.slots[x], b = s >> a.shift;
         const int off = (int)(s & (a.bs - 1));
         // its length: as long as the slots follow each other inside the block
         if (tid == 0) fail = a.bs - off;
         __syncthreads();
         if (tid < a.bs - off && (x + tid >= a.N || a.slots[x + tid] != s + tid)) atomicMin(&fail, tid);
         __syncthreads();
-        const int n = fail;
+        const int n = __builtin_amdgcn_readfirstlane(fail);
+        const RunRows<T, WIDE> kx((const T *)a.k + x * a.k_row, a.k_row, n, a.d), vx((const T *)a.v + x * a.v_row, a.v_row, n, a.d);
         const int kn = n * kch, g0 = off >> 4, vn = (((off + n - 1) >> 4) - g0 + 1) * vch;
-        const T *kx = k + x * a.k_row, *vx = v + x * a.v_row;
-        const auto load_k = [&](int i, Raw8<T> &w) {  // piece i: row i / kch
+        const auto load_k = [&](int i, float (&w)[8]) {  // piece i: row i / kch
             const int r = (i * kdiv) >> 16;
-            w.load(kx + (int64_t)r * a.k_row, 8 * (i - r * kch), a.d, a.k_wide);
+            kx.load8(r, 8 * (i - r * kch), w);
         };
-        const auto load_v = [&](int i, Raw2<T> (&w)[16]) {  // piece i: tokens 16 (g0 + i / vch) .., columns 2 (i % vch) ..
-            const int g = (i * vdiv) >> 16, c = 2 * (i - g * vch), r0 = 16 * (g0 + g) - off;
-#pragma unroll
-            for (int t = 0; t < 16; ++t) {
-                w[t].x = decltype(w[t].x){};
-                if (c < a.d && r0 + t >= 0 && r0 + t < n) w[t].load(vx + (int64_t)(r0 + t) * a.v_row, c, a.d, a.v_wide);
-            }
+        const auto load_v = [&](int i, float (&lo)[16], float (&hi)[16]) {  // piece i: tokens 16 (g0 + i / vch) .., columns 2 (i % vch) ..
+            const int g = (i * vdiv) >> 16;
+            vx.load2(16 * (g0 + g) - off, 2 * (i - g * vch), lo, hi);
         };
-        Raw8<T> kr[KREG];
-        Raw2<T> vr[16];
+        float ak = 0.f, av = 0.f, kr[KREG][8], vlo[16], vhi[16];
 #pragma unroll
-        for (int u = 0; u < KREG; ++u)
-            if (tid + u * ST < kn) load_k(tid + u * ST, kr[u]);
-        if (tid < vn) load_v(tid, vr);
-        float ak = 0.f, av = 0.f;
-        const auto max_k = [&](const Raw8<T> &w) {
-            float z[8];
-            w.get(z);
+        for (int u = 0; u < KREG; ++u) load_k(tid + u * ST, kr[u]);  // rows past the run: zeros
+        load_v(tid, vlo, vhi);
+        const auto max_k = [&](const float (&w)[8]) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ak = fmaxf(ak, finite_abs(z[i]));
+            for (int i = 0; i < 8; ++i) ak = larger(ak, w[i]);
         };
-        const auto max_v = [&](const Raw2<T> (&w)[16]) {
+        const auto max_v = [&](const float (&lo)[16], const float (&hi)[16]) {
 #pragma unroll
-            for (int t = 0; t < 16; ++t) av = fmaxf(av, fmaxf(finite_abs(w[t].lo()), finite_abs(w[t].hi())));
+            for (int t = 0; t < 16; ++t) av = larger(larger(av, lo[t]), hi[t]);
         };
 #pragma unroll
-        for (int u = 0; u < KREG; ++u)
-            if (tid + u * ST < kn) max_k(kr[u]);
+        for (int u = 0; u < KREG; ++u) max_k(kr[u]);
+        max_v(vlo, vhi);
         for (int i = tid + KREG * ST; i < kn; i += ST) {
-            Raw8<T> w;
+            float w[8];
             load_k(i, w);
             max_k(w);
         }
-        if (tid < vn) max_v(vr);
         for (int i = tid + ST; i < vn; i += ST) {
-            Raw2<T> w[16];
-            load_v(i, w);
-            max_v(w);
+            float lo[16], hi[16];
+            load_v(i, lo, hi);
+            max_v(lo, hi);
         }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) ak = fmaxf(ak, __shfl_xor(ak, o)), av = fmaxf(av, __shfl_xor(av, o));
@@ -433,21 +430,19 @@ __global__ void __launch_bounds__(ST) cache_store(StoreArgs a) {
             a.v_exp[b] = (uint8_t)ev;
         }
         const float fk = pow2(127 - ek), fv = pow2(127 - ev);
-        const auto put_k = [&](int i, const Raw8<T> &w) {  // pieces lie in the block in their order
-            float z[8];
-            w.get(z);
+        const auto put_k = [&](int i, const float (&z)[8]) {  // pieces lie in the block in their order
             const uint32_t lo = codes2<true>(z[2], z[3], fk, codes2(z[0], z[1], fk));
             const uint32_t hi = codes2<true>(z[6], z[7], fk, codes2(z[4], z[5], fk));
-            *(uint2 *)(kb + (int64_t)off * a.dp + 8 * i) = make_uint2(lo, hi);
+            *(uint2 *)(kb + off * a.dp + 8 * i) = make_uint2(lo, hi);
         };
-        const auto put_v = [&](int i, const Raw2<T> (&w)[16]) {
+        const auto put_v = [&](int i, const float (&wl)[16], const float (&wh)[16]) {
             const int g = (i * vdiv) >> 16, c = 2 * (i - g * vch), t0 = 16 * (g0 + g), r0 = t0 - off;
             if (c >= a.d) return;
             uint32_t lo[4], hi[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                lo[q] = codes2<true>(w[4 * q + 2].lo(), w[4 * q + 3].lo(), fv, codes2(w[4 * q].lo(), w[4 * q + 1].lo(), fv));
-                hi[q] = codes2<true>(w[4 * q + 2].hi(), w[4 * q + 3].hi(), fv, codes2(w[4 * q].hi(), w[4 * q + 1].hi(), fv));
+                lo[q] = codes2<true>(wl[4 * q + 2], wl[4 * q + 3], fv, codes2(wl[4 * q], wl[4 * q + 1], fv));
+                hi[q] = codes2<true>(wh[4 * q + 2], wh[4 * q + 3], fv, codes2(wh[4 * q], wh[4 * q + 1], fv));
             }
             uint8_t *p = vb + c * a.bs + t0;
             if (r0 >= 0 && r0 + 16 <= n) {
@@ -466,15 +461,15 @@ __global__ void __launch_bounds__(ST) cache_store(StoreArgs a) {
         for (int u = 0; u < KREG; ++u)
             if (tid + u * ST < kn) put_k(tid + u * ST, kr[u]);
         for (int i = tid + KREG * ST; i < kn; i += ST) {
-            Raw8<T> w;
+            float w[8];
             load_k(i, w);
             put_k(i, w);
         }
-        if (tid < vn) put_v(tid, vr);
+        if (tid < vn) put_v(tid, vlo, vhi);
         for (int i = tid + ST; i < vn; i += ST) {
-            Raw2<T> w[16];
-            load_v(i, w);
-            put_v(i, w);
+            float lo[16], hi[16];
+            load_v(i, lo, hi);
+            put_v(i, lo, hi);
         }
         __syncthreads();
     }
@@ -522,13 +517,20 @@ hipError_t launch_store(const fw_cache &cache, int dtype, const void *k, int64_t
     a.n_blocks = cache.n_blocks, a.bs = cache.block_size, a.shift = __builtin_ctz(cache.block_size);
     a.d = (int)cache.d, a.dp = cache_row(cache.d);
     const int size = dtype == FW_F32 ? 4 : 2;
-    a.k_wide = a.d % 8 == 0 && k_row * size % 16 == 0 && (uintptr_t)k % 16 == 0;
-    a.v_wide = a.d % 2 == 0 && v_row % 2 == 0 && (uintptr_t)v % (2 * size) == 0;
+    const auto ok = [&](const void *p, int64_t row) {  // a run's offsets stay below 2^31
+        return (uintptr_t)p % 16 == 0 && row * size % 16 == 0 && row >= a.d && row * size < (1 << 22);
+    };
+    const bool wide = a.d % 8 == 0 && ok(k, k_row) && ok(v, v_row);
     a.chunk = 1;
     while (a.chunk < a.bs && N / (2 * a.chunk) >= 2048) a.chunk *= 2;
     const dim3 grid((unsigned)((N + a.chunk - 1) / a.chunk));
-    if (dtype == FW_F32) hipLaunchKernelGGL(cache_store<float>, grid, dim3(ST), 0, st, a);
-    else hipLaunchKernelGGL(cache_store<uint16_t>, grid, dim3(ST), 0, st, a);
+    if (dtype == FW_F32) {
+        if (wide) hipLaunchKernelGGL((cache_store<float, true>), grid, dim3(ST), 0, st, a);
+        else hipLaunchKernelGGL((cache_store<float, false>), grid, dim3(ST), 0, st, a);
+    } else {
+        if (wide) hipLaunchKernelGGL((cache_store<uint16_t, true>), grid, dim3(ST), 0, st, a);
+        else hipLaunchKernelGGL((cache_store<uint16_t, false>), grid, dim3(ST), 0, st, a);
+    }
     return hipGetLastError();
 }
 
