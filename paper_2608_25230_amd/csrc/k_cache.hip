@@ -25,9 +25,12 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // is served if its running sum of needs stays within top.
 //
 // tables_scan, one workgroup, takes the sums (each thread a run of cells) and
-// writes lengths, offsets and the sums; tables_back and tables_grow, over the
-// whole card, move the blocks and write the slots.  Small calls run all three
-// in the one workgroup: a launch costs more than their work.
+// writes lengths, offsets and sums; tables_move, over the whole card, moves
+// the blocks and writes the slots.  Blocks that come back may be taken in the
+// same call, so where cells shrink and grow in one call the scan moves the
+// returned blocks itself.  Small calls run in the one workgroup alone, a
+// cell's few blocks and slots by the thread that has its sums: a launch costs
+// more than their work.
 // ---------------------------------------------------------------------------
 constexpr int TT = 1024;  // threads of the scan
 
@@ -70,24 +73,34 @@ __device__ __forceinline__ CellPlan plan_cell(const TableArgs &a, int64_t c) {
     return p;
 }
 
-// inclusive sums of one value per thread over the workgroup; `red` holds TT / 64 values
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *red, int64_t *total) {
+// Exclusive sums of NV values per thread over the workgroup, and their totals.
+template <int NV>
+__device__ __forceinline__ void block_sums(const int64_t (&v)[NV], int64_t (&before)[NV], int64_t (&total)[NV],
+                                           int64_t (*red)[TT / 64]) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int64_t y = __shfl_up(v, off);
-        if (lane >= off) v += y;
+    for (int i = 0; i < NV; ++i) {
+        int64_t x = v[i];
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int64_t y = __shfl_up(x, off);
+            if (lane >= off) x += y;
+        }
+        if (lane == 63) red[i][w] = x;
+        before[i] = x - v[i];
     }
-    if (lane == 63) red[w] = v;
     __syncthreads();
-    int64_t before = 0, sum = 0;
-    for (int i = 0; i < TT / 64; ++i) {
-        if (i < w) before += red[i];
-        sum += red[i];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        total[i] = 0;
+#pragma unroll
+        for (int j = 0; j < TT / 64; ++j) {
+            const int64_t y = red[i][j];
+            if (j < w) before[i] += y;
+            total[i] += y;
+        }
     }
     __syncthreads();
-    *total = sum;
-    return v + before;
 }
 
 // the last c of [0, n) with off[c] <= x (off ascending, off[0] <= x)
@@ -118,96 +131,136 @@ __device__ __forceinline__ void take_blocks(const TableArgs &a, const TableHead 
     }
 }
 
-// slots of tokens i .. i + 3; new blocks straight off the stack (take_blocks writes the same into the table)
-__device__ __forceinline__ void write_slots(const TableArgs &a, const TableHead &hd, int64_t n, int64_t first, int64_t step) {
-    const int64_t mask = ((int64_t)1 << a.shift) - 1;
+// The slot of a cell's token at `pos`; a new block straight off the stack, where take_blocks finds the same.
+__device__ __forceinline__ int64_t slot_of(const TableArgs &a, const TableHead &hd, int64_t c, const TableCell &t, int64_t need_off,
+                                           int64_t pos) {
+    if (!t.served) return -1;
+    const int64_t b = pos >> a.shift;
+    const int32_t e = b < t.had ? a.table[c * a.W + b] : a.free_list[hd.top - 1 - (need_off + b - t.had)];
+    return e < 0 ? -1 : ((int64_t)e << a.shift) + (pos & (((int64_t)1 << a.shift) - 1));
+}
+
+// four tokens' slots at a time; `offsets` may be a copy in LDS
+__device__ __forceinline__ void write_slots(const TableArgs &a, const TableHead &hd, const int64_t *offsets, int64_t first,
+                                            int64_t step) {
+    const int64_t total = offsets[a.C], n = a.slots ? (total < a.n_slots ? total : a.n_slots) : 0;
     for (int64_t i0 = 4 * first; i0 < n; i0 += 4 * step) {
-        int64_t c = find_cell(a.offsets, a.C, i0);
+        int64_t c = find_cell(offsets, a.C, i0);
         for (int64_t i = i0; i < i0 + 4 && i < n; ++i) {
-            while (i >= a.offsets[c + 1]) ++c;
+            while (i >= offsets[c + 1]) ++c;
             const TableCell t = a.cells[c];
-            const int64_t pos = t.old_len + (i - a.offsets[c]), b = pos >> a.shift;
-            int64_t s = -1;
-            if (t.served) {
-                const int32_t e = b < t.had ? a.table[c * a.W + b] : a.free_list[hd.top - 1 - (a.need_off[c] + b - t.had)];
-                if (e >= 0) s = ((int64_t)e << a.shift) + (pos & mask);
-            }
-            a.slots[i] = s;
+            a.slots[i] = slot_of(a, hd, c, t, a.need_off[c], t.old_len + (i - offsets[c]));
         }
     }
 }
 
-__device__ __forceinline__ int64_t slot_count(const TableArgs &a) {
-    const int64_t n = a.offsets[a.C];
-    return a.slots ? (n < a.n_slots ? n : a.n_slots) : 0;
-}
+constexpr int kFew = 8;            // blocks or tokens of a cell that its own thread moves
+constexpr int64_t kInline = 4096;  // returned blocks that the one workgroup moves in a call of several launches
 
 template <bool ALL>
 __global__ void __launch_bounds__(TT) tables_scan(TableArgs a) {
-    __shared__ int64_t red[TT / 64];
+    __shared__ int64_t red[3][TT / 64];
     const int64_t run = (a.C + TT - 1) / TT, c0 = threadIdx.x * run;
     const int64_t c1 = c0 + run < a.C ? c0 + run : a.C;
-    int64_t back = 0, need = 0, add = 0;
+    int64_t sum[3] = {0, 0, 0}, at[3], total[3];  // blocks back, blocks needed, tokens added
+    bool few = true;
     for (int64_t c = c0; c < c1; ++c) {
         const CellPlan p = plan_cell(a, c);
-        back += p.back, need += p.need, add += p.add;
+        sum[0] += p.back, sum[1] += p.need, sum[2] += p.add;
+        few = few && p.back <= kFew && p.need <= kFew && p.add <= kFew;
     }
     int64_t n_free = a.n_free[0];
     n_free = n_free < 0 ? 0 : n_free > a.n_blocks ? a.n_blocks : n_free;
+    const bool direct = ALL && !__syncthreads_or(!few);
+    block_sums<3>(sum, at, total, red);
     TableHead hd;
-    int64_t total;
-    int64_t ob = block_scan(back, red, &hd.back) - back;
-    int64_t on = block_scan(need, red, &total) - need;
-    if (threadIdx.x == TT - 1) a.need_off[a.C] = total;
-    int64_t oa = block_scan(add, red, &total) - add;
-    if (threadIdx.x == TT - 1) a.offsets[a.C] = total, a.back_off[a.C] = hd.back;
-    hd.n_free = n_free;
+    hd.back = total[0], hd.n_free = n_free;
     hd.top = n_free + hd.back < a.n_blocks ? n_free + hd.back : a.n_blocks;
+    if (threadIdx.x == 0) a.offsets[a.C] = total[2];
     int64_t take = 0, refused = 0;
+    if (direct) {
+        if (hd.back > 0) {
+            int64_t r = at[0];
+            for (int64_t c = c0; c < c1; ++c) {
+                const CellPlan p = plan_cell(a, c);
+                for (int64_t i = 0; i < p.back; ++i, ++r) {
+                    int32_t *e = a.table + c * a.W + p.want + i;
+                    if (n_free + hd.back - 1 - r < a.n_blocks) a.free_list[n_free + hd.back - 1 - r] = *e;
+                    *e = -1;
+                }
+            }
+            __syncthreads();  // blocks that came back may be taken
+        }
+    } else if (threadIdx.x == 0) {
+        a.need_off[a.C] = total[1], a.back_off[a.C] = hd.back;
+    }
     for (int64_t c = c0; c < c1; ++c) {
         const CellPlan p = plan_cell(a, c);
-        const bool served = p.fits && on + p.need <= hd.top;
-        a.cells[c] = TableCell{p.o, (int32_t)p.had, (int32_t)p.want, served};
-        a.back_off[c] = ob, a.need_off[c] = on, a.offsets[c] = oa;
-        if (served) take = on + p.need;
+        const bool served = p.fits && at[1] + p.need <= hd.top;
+        const TableCell t = {p.o, (int32_t)p.had, (int32_t)p.want, served};
+        a.offsets[c] = at[2];
+        a.lens[c] = served ? p.n : p.o;  // may be old_len: this thread alone reads and writes the cell
+        if (direct) {
+            if (served)
+                for (int64_t i = 0; i < p.need; ++i) a.table[c * a.W + p.had + i] = a.free_list[hd.top - 1 - (at[1] + i)];
+            for (int64_t i = 0; i < p.add && at[2] + i < a.n_slots; ++i) a.slots[at[2] + i] = slot_of(a, hd, c, t, at[1], p.o + i);
+        } else {
+            a.cells[c] = t, a.back_off[c] = at[0], a.need_off[c] = at[1];
+        }
+        if (served) take = at[1] + p.need;
         refused += !served;
-        a.lens[c] = served ? p.n : p.o;   // may be old_len: this thread alone reads and writes the cell
-        ob += p.back, on += p.need, oa += p.add;
+        at[0] += p.back, at[1] += p.need, at[2] += p.add;
     }
     // running sums only grow, so what is taken is the largest served one
-    block_scan(refused, red, &total);
-    if (threadIdx.x == 0) a.refused[0] = (int32_t)total;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
         const int64_t y = __shfl_xor(take, off);
         take = y > take ? y : take;
+        refused += __shfl_xor(refused, off);
     }
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = take;
-    __syncthreads();
-    for (int i = 0; i < TT / 64; ++i) take = red[i] > take ? red[i] : take;
+    if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = take, red[1][threadIdx.x >> 6] = refused;
+    __syncthreads();  // also: the cells' records are read by every thread from here on
+    refused = 0;
+#pragma unroll
+    for (int i = 0; i < TT / 64; ++i) {
+        take = red[0][i] > take ? red[0][i] : take;
+        refused += red[1][i];
+    }
     hd.take = take;
     if (threadIdx.x == 0) {
-        a.head[0] = hd;
         a.n_free[0] = (int32_t)(hd.top - hd.take);
+        a.refused[0] = (int32_t)refused;
+    }
+    if (direct) return;
+    const bool mine = ALL || hd.back <= kInline || hd.take > 0;
+    if (mine && hd.back > 0) {
+        move_back(a, hd, threadIdx.x, TT);
+        __syncthreads();  // blocks that came back may be taken
     }
     if (ALL) {
-        __syncthreads();  // the cells' records are read by every thread from here on
-        move_back(a, hd, threadIdx.x, TT);
-        __syncthreads();  // blocks that just came back may be taken
         take_blocks(a, hd, threadIdx.x, TT);
-        write_slots(a, hd, slot_count(a), threadIdx.x, TT);
+        write_slots(a, hd, a.offsets, threadIdx.x, TT);
+    } else if (threadIdx.x == 0) {
+        if (mine) hd.back = 0;
+        a.head[0] = hd;
     }
 }
 
-__global__ void __launch_bounds__(256) tables_back(TableArgs a) {
-    move_back(a, a.head[0], (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
-}
-
-__global__ void __launch_bounds__(256) tables_grow(TableArgs a) {
+// What the scan left: returned blocks (then none is taken), or blocks taken and slots.
+constexpr int kStage = 2048;  // cells whose offsets are staged in LDS
+__global__ void __launch_bounds__(256) tables_move(TableArgs a) {
+    __shared__ int64_t staged[kStage + 1];
     const TableHead hd = a.head[0];
     const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+    move_back(a, hd, first, step);
     take_blocks(a, hd, first, step);
-    write_slots(a, hd, slot_count(a), first, step);
+    if (a.C <= kStage) {
+        for (int64_t c = threadIdx.x; c <= a.C; c += 256) staged[c] = a.offsets[c];
+        __syncthreads();
+        write_slots(a, hd, staged, first, step);
+    } else {
+        write_slots(a, hd, a.offsets, first, step);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -502,9 +555,8 @@ hipError_t launch_tables(int64_t C, const int32_t *old_len, const int32_t *new_l
         return hipGetLastError();
     }
     hipLaunchKernelGGL(tables_scan<false>, dim3(1), dim3(TT), 0, st, a);
-    const auto blocks = [](int64_t items) { return (unsigned)std::min<int64_t>(std::max<int64_t>((items + 255) / 256, 1), 2048); };
-    hipLaunchKernelGGL(tables_back, dim3(blocks(C * W / 8)), dim3(256), 0, st, a);
-    hipLaunchKernelGGL(tables_grow, dim3(blocks(std::max(n_slots / 4, C * W / 8))), dim3(256), 0, st, a);
+    const int64_t items = std::max(n_slots / 4, C * W / 8);
+    hipLaunchKernelGGL(tables_move, dim3((unsigned)std::min<int64_t>((items + 255) / 256 + 1, 2048)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

@@ -405,23 +405,17 @@ def kv_cache(n_blocks: int, block_size: int, d: int, device="cuda") -> KvCache:
     return KvCache(z(n_blocks, block_size, dp), z(n_blocks, dp, block_size), z(n_blocks), z(n_blocks), d)
 
 
-class _on:
-    """The device of the tensors made current, if it is not; its current stream."""
+_raw_stream = None
 
-    def __init__(self, t):
-        cuda = _torch().cuda
-        self.device = t.device
-        self.guard = None if cuda.current_device() == t.device.index else cuda.device(t.device)
-        self.stream = cuda.current_stream(t.device).cuda_stream
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream
-
-    def __exit__(self, *e):
-        if self.guard is not None:
-            self.guard.__exit__(*e)
+def _stream_of(index: int) -> int:
+    """The handle of the device's current stream, without a stream object where torch offers that."""
+    global _raw_stream
+    if _raw_stream is None:
+        torch = _torch()
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                              lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _raw_stream(index)
 
 
 def _want(name: str, t, dtype, dim: int, device) -> None:
@@ -438,9 +432,12 @@ def _rows_of(name: str, t, dtype, dim: int, device) -> None:
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _gpu(name: str, t) -> None:
+def _elsewhere(name: str, t):
+    """None where the tensor's device is the current one, else a guard that makes it so."""
     if not t.is_cuda:
         raise FwError(2, f"{name} must be a device tensor")
+    cuda = _torch().cuda
+    return None if cuda.current_device() == t.get_device() else cuda.device(t.device)
 
 
 def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=None, want_lse=True,
@@ -449,11 +446,15 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=Non
     fine), cu_q and cu_k [B+1] int64 offsets (cu_k defaults to cu_q).  Returns o [Tq][Hq][d] of q's type and lse
     [Tq][Hq] float32.  Rows outside the sequences are left unwritten."""
     torch = _torch()
-    _gpu("q", q)
+    guard = _elsewhere("q", q)
+    if guard is not None:
+        with guard:
+            return prompt_attention(q, k, v, cu_q, cu_k, causal=causal, scale=scale, want_lse=want_lse, ws=ws)
     dev, dt = q.device, q.dtype
     code = _dtype_code(q)
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        _rows_of(name, t, dt, 3, dev)
+    _rows_of("q", q, dt, 3, dev)
+    _rows_of("k", k, dt, 3, dev)
+    _rows_of("v", v, dt, 3, dev)
     if cu_k is None:
         cu_k = cu_q
     _want("cu_q", cu_q, torch.int64, 1, dev)
@@ -473,16 +474,14 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=Non
     p = Packed(code, q.data_ptr(), k.data_ptr(), v.data_ptr(), Tq, Tk, cu_q.shape[0] - 1, Hq, Hkv, d, q_row, q_head,
                k_row, k_head, v_row, v_head, cu_q.data_ptr(), cu_k.data_ptr(), _ptr(scale), 1 if causal else 0)
     L, ref = lib(), ctypes.byref(p)
-    with _on(q) as stream:
-        out = {"o": torch.empty((Tq, Hq, d), dtype=dt, device=dev),
-               "lse": torch.empty((Tq, Hq), dtype=torch.float32, device=dev) if want_lse else None}
-        need = L.fw_prompt_attention_workspace_size(ref)
-        if need and (ws is None or ws.numel() < need):
-            ws = _workspace(need, dev)
-        _check(L.fw_prompt_attention(ref, out["o"].data_ptr(), _ptr(out["lse"]), _ptr(ws),
-                                     0 if ws is None else ws.numel(), stream))
-    out["_ws"] = ws
-    return out
+    o = q.new_empty((Tq, Hq, d))
+    lse = q.new_empty((Tq, Hq), dtype=torch.float32) if want_lse else None
+    need = L.fw_prompt_attention_workspace_size(ref)
+    if need and (ws is None or ws.numel() < need):
+        ws = _workspace(need, dev)
+    _check(L.fw_prompt_attention(ref, o.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(),
+                                 _stream_of(q.get_device())))
+    return {"o": o, "lse": lse, "_ws": ws}
 
 
 def block_tables(old_len, new_len, table, free_list, n_free, block_size: int, *, n_slots: int, lens=None,
@@ -491,52 +490,62 @@ def block_tables(old_len, new_len, table, free_list, n_free, block_size: int, *,
     n_free [1] (int32) change in place.  n_slots: tokens that come, of refused cells too.  Returns slots [n_slots]
     int64, offsets [C+1] int64, lens [C] int32 (in `lens`, which may be old_len, if given) and refused [1] int32."""
     torch = _torch()
-    _gpu("table", table)
+    guard = _elsewhere("table", table)
+    if guard is not None:
+        with guard:
+            return block_tables(old_len, new_len, table, free_list, n_free, block_size, n_slots=n_slots, lens=lens, ws=ws)
     dev = table.device
     i32 = torch.int32
     _want("table", table, i32, 2, dev)
-    for name, t in (("old_len", old_len), ("new_len", new_len), ("free_list", free_list), ("n_free", n_free)):
-        _want(name, t, i32, 1, dev)
+    _want("old_len", old_len, i32, 1, dev)
+    _want("new_len", new_len, i32, 1, dev)
+    _want("free_list", free_list, i32, 1, dev)
+    _want("n_free", n_free, i32, 1, dev)
     C, W = table.shape
     if lens is not None:
         _want("lens", lens, i32, 1, dev)
     if old_len.shape[0] != C or new_len.shape[0] != C or n_free.shape[0] != 1 or (lens is not None and lens.shape[0] != C):
         raise FwError(2, f"old_len, new_len and lens must be [{C}] and n_free [1]")
+    if n_slots < 0:
+        raise FwError(2, "n_slots must be >= 0")
     L = lib()
-    with _on(table) as stream:
-        out = {"slots": torch.empty(max(n_slots, 0), dtype=torch.int64, device=dev),
-               "offsets": torch.empty(C + 1, dtype=torch.int64, device=dev),
-               "lens": torch.empty(C, dtype=i32, device=dev) if lens is None else lens,
-               "refused": torch.empty(1, dtype=i32, device=dev)}
-        need = L.fw_block_tables_workspace_size(C)
-        if ws is None or ws.numel() < need:
-            ws = _workspace(need, dev)
-        _check(L.fw_block_tables(C, old_len.data_ptr(), new_len.data_ptr(), block_size, W, table.data_ptr(),
-                                 free_list.shape[0], free_list.data_ptr(), n_free.data_ptr(), n_slots,
-                                 out["slots"].data_ptr(), out["offsets"].data_ptr(), out["lens"].data_ptr(),
-                                 out["refused"].data_ptr(), ws.data_ptr(), ws.numel(), stream))
-    out["_ws"] = ws
-    return out
+    slots = table.new_empty(n_slots, dtype=torch.int64)
+    offsets = table.new_empty(C + 1, dtype=torch.int64)
+    if lens is None:
+        lens = table.new_empty(C)
+    refused = table.new_empty(1)
+    need = L.fw_block_tables_workspace_size(C)
+    if ws is None or ws.numel() < need:
+        ws = _workspace(need, dev)
+    _check(L.fw_block_tables(C, old_len.data_ptr(), new_len.data_ptr(), block_size, W, table.data_ptr(),
+                             free_list.shape[0], free_list.data_ptr(), n_free.data_ptr(), n_slots, slots.data_ptr(),
+                             offsets.data_ptr(), lens.data_ptr(), refused.data_ptr(), ws.data_ptr(), ws.numel(),
+                             _stream_of(table.get_device())))
+    return {"slots": slots, "offsets": offsets, "lens": lens, "refused": refused, "_ws": ws}
 
 
 def _cache(c: KvCache, device) -> Cache:
+    k, v, k_exp, v_exp, d = c
     u8 = _torch().uint8
-    _want("cache.k", c.k, u8, 3, device)
-    _want("cache.v", c.v, u8, 3, device)
-    _want("cache.k_exp", c.k_exp, u8, 1, device)
-    _want("cache.v_exp", c.v_exp, u8, 1, device)
-    n, bs, dp = c.k.shape
-    if dp != cache_row(c.d) or c.v.shape != (n, dp, bs) or c.k_exp.shape[0] != n or c.v_exp.shape[0] != n:
-        raise FwError(2, f"the cache's buffers do not fit together: k {tuple(c.k.shape)}, v {tuple(c.v.shape)}, "
-                         f"k_exp {tuple(c.k_exp.shape)}, v_exp {tuple(c.v_exp.shape)}, d {c.d}")
-    return Cache(c.k.data_ptr(), c.v.data_ptr(), c.k_exp.data_ptr(), c.v_exp.data_ptr(), n, c.d, bs)
+    _want("cache.k", k, u8, 3, device)
+    _want("cache.v", v, u8, 3, device)
+    _want("cache.k_exp", k_exp, u8, 1, device)
+    _want("cache.v_exp", v_exp, u8, 1, device)
+    n, bs, dp = k.shape
+    if dp != cache_row(d) or v.shape != (n, dp, bs) or k_exp.shape[0] != n or v_exp.shape[0] != n:
+        raise FwError(2, f"the cache's buffers do not fit together: k {tuple(k.shape)}, v {tuple(v.shape)}, "
+                         f"k_exp {tuple(k_exp.shape)}, v_exp {tuple(v_exp.shape)}, d {d}")
+    return Cache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), n, d, bs)
 
 
 def cache_store(cache: KvCache, k, v, slots) -> None:
     """Rounds rows k and v [N][d] to the cache's blocks at slots [N] int64 (``block_tables``; rows with a slot out of
     range are skipped).  The rows of one block are consecutive, with consecutive slots."""
     torch = _torch()
-    _gpu("k", k)
+    guard = _elsewhere("k", k)
+    if guard is not None:
+        with guard:
+            return cache_store(cache, k, v, slots)
     dev, dt = k.device, k.dtype
     code = _dtype_code(k)
     _rows_of("k", k, dt, 2, dev)
@@ -546,9 +555,8 @@ def cache_store(cache: KvCache, k, v, slots) -> None:
         raise FwError(2, f"k and v must be [N][{cache.d}] and slots [N], got {tuple(k.shape)}, {tuple(v.shape)}, "
                          f"{tuple(slots.shape)}")
     c = _cache(cache, dev)
-    with _on(k) as stream:
-        _check(lib().fw_cache_store(ctypes.byref(c), code, k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
-                                    k.shape[0], slots.data_ptr(), None, 0, stream))
+    _check(lib().fw_cache_store(ctypes.byref(c), code, k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
+                                k.shape[0], slots.data_ptr(), None, 0, _stream_of(k.get_device())))
 
 
 def cache_attention(q, cache: KvCache, table, lens, *, scale=None, want_lse=True, ws=None) -> Dict[str, object]:
@@ -556,7 +564,10 @@ def cache_attention(q, cache: KvCache, table, lens, *, scale=None, want_lse=True
     views are fine), table [S*Hkv][max_blocks] and lens [S*Hkv] int32.  Returns o [S][T][Hq][d] of q's type and lse
     [S][T][Hq] float32."""
     torch = _torch()
-    _gpu("q", q)
+    guard = _elsewhere("q", q)
+    if guard is not None:
+        with guard:
+            return cache_attention(q, cache, table, lens, scale=scale, want_lse=want_lse, ws=ws)
     dev, dt = q.device, q.dtype
     code = _dtype_code(q)
     _rows_of("q", q, dt, 4, dev)
@@ -575,17 +586,15 @@ def cache_attention(q, cache: KvCache, table, lens, *, scale=None, want_lse=True
     c = _cache(cache, dev)
     L, ref = lib(), ctypes.byref(c)
     q_seq, q_tok, q_head, _ = q.stride()
-    with _on(q) as stream:
-        out = {"o": torch.empty((S, T, Hq, d), dtype=dt, device=dev),
-               "lse": torch.empty((S, T, Hq), dtype=torch.float32, device=dev) if want_lse else None}
-        need = L.fw_cache_attention_workspace_size(ref, S, T, Hq, Hkv, W)
-        if need and (ws is None or ws.numel() < need):
-            ws = _workspace(need, dev)
-        _check(L.fw_cache_attention(ref, code, q.data_ptr(), S, T, Hq, Hkv, q_seq, q_tok, q_head, table.data_ptr(), W,
-                                    lens.data_ptr(), _ptr(scale), out["o"].data_ptr(), _ptr(out["lse"]), _ptr(ws),
-                                    0 if ws is None else ws.numel(), stream))
-    out["_ws"] = ws
-    return out
+    o = q.new_empty((S, T, Hq, d))
+    lse = q.new_empty((S, T, Hq), dtype=torch.float32) if want_lse else None
+    need = L.fw_cache_attention_workspace_size(ref, S, T, Hq, Hkv, W)
+    if need and (ws is None or ws.numel() < need):
+        ws = _workspace(need, dev)
+    _check(L.fw_cache_attention(ref, code, q.data_ptr(), S, T, Hq, Hkv, q_seq, q_tok, q_head, table.data_ptr(), W,
+                                lens.data_ptr(), _ptr(scale), o.data_ptr(), _ptr(lse), _ptr(ws),
+                                0 if ws is None else ws.numel(), _stream_of(q.get_device())))
+    return {"o": o, "lse": lse, "_ws": ws}
 
 
 # ---------------------------------------------------------------------------
