@@ -34,11 +34,11 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int DW = 4;               // waves per workgroup
-constexpr int DTH = 64 * DW;
+constexpr int DW = 4;               // waves per workgroup; 8 where one takes a whole cell (kWhole)
 constexpr int DT = 64;              // tokens per wave and step
 constexpr int kTarget = 1024;       // parts that the whole work is cut into
 constexpr int kMinChunk = 8;        // tiles of a part at least
+constexpr int kWhole = 32;          // tiles of a table row up to which a cell is one part
 constexpr float DLOG2E = 1.4426950408889634f;
 constexpr float DLN2 = 0.6931471805599453f;
 constexpr float DMIN = -3.0e38f;
@@ -47,8 +47,8 @@ constexpr float DRESCALE = 8.f;
 struct DecodeArgs {
     const void *q;
     int64_t q_seq, q_tok, q_head;
-    int64_t C, T, Hkv, G, W;        // cells, new positions, heads, group, blocks per table row
-    int R, d;                       // rows of a cell
+    int C, T, Hkv, G, W;            // cells, new positions, heads, group, blocks per table row
+    int R, d;                       // rows of a cell, their width
     const uint8_t *kc, *vc, *k_exp, *v_exp;
     int64_t n_blocks;
     int shift;
@@ -61,10 +61,9 @@ struct DecodeArgs {
     float *part_o, *part_lse;       // [parts][R][d], [parts][R] (base 2)
 };
 
-__device__ __forceinline__ int cell_len(const DecodeArgs &a, int64_t c) {
-    const int64_t most = a.W << a.shift;
-    const int n = a.lens[c];
-    return n < 0 ? 0 : n > most ? (int)most : n;
+__device__ __forceinline__ int cell_len(const DecodeArgs &a, int c) {
+    const int most = a.W << a.shift, n = a.lens[c];
+    return n < 0 ? 0 : n > most ? most : n;
 }
 
 // exclusive sum of one int per thread over the workgroup
@@ -91,20 +90,19 @@ __device__ __forceinline__ int sum_before(int v, int *red, int *total) {
 
 // This workgroup's cell, its part of it and the part's tiles; false if there is no such part.
 struct Part {
-    int64_t cell;
-    int part, parts, t0, t1;
+    int cell, part, parts, t0, t1;
 };
 __device__ __forceinline__ bool find_part(const DecodeArgs &a, Part *p) {
     __shared__ int red[DW], found[4];
-    const int64_t run = (a.C + DTH - 1) / DTH, c0 = threadIdx.x * run;
-    const int64_t c1 = c0 + run < a.C ? c0 + run : a.C;
+    const int run = (a.C + 64 * DW - 1) / (64 * DW), c0 = threadIdx.x * run;
+    const int c1 = c0 + run < a.C ? c0 + run : a.C;
     int tiles = 0, all;
-    for (int64_t c = c0; c < c1; ++c) tiles += (cell_len(a, c) + DT - 1) / DT;
+    for (int c = c0; c < c1; ++c) tiles += (cell_len(a, c) + DT - 1) / DT;
     sum_before(tiles, red, &all);
     int chunk = (all + kTarget - 1) / kTarget;
     if (chunk < kMinChunk) chunk = kMinChunk;
     int mine = 0, total;
-    for (int64_t c = c0; c < c1; ++c) {
+    for (int c = c0; c < c1; ++c) {
         const int n = ((cell_len(a, c) + DT - 1) / DT + chunk - 1) / chunk;
         mine += n ? n : 1;
     }
@@ -112,10 +110,10 @@ __device__ __forceinline__ bool find_part(const DecodeArgs &a, Part *p) {
     const int x = blockIdx.x;
     if (x >= total) return false;
     if (x >= first && x < first + mine) {
-        for (int64_t c = c0; c < c1; ++c) {
+        for (int c = c0; c < c1; ++c) {
             const int nt = (cell_len(a, c) + DT - 1) / DT, n = nt ? (nt + chunk - 1) / chunk : 1;
             if (x < first + n) {
-                found[0] = (int)c, found[1] = x - first, found[2] = n, found[3] = nt;
+                found[0] = c, found[1] = x - first, found[2] = n, found[3] = nt;
                 if (x == first && blockIdx.y == 0) a.cells[c] = make_int2(first, n);
                 break;
             }
@@ -169,14 +167,14 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t x) {
     return (t >> 7) * 0xFFu;
 }
 
-template <typename T, int DP, int RT>
-__global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_part(DecodeArgs a) {
+template <typename T, int DP, int RT, int NW>
+__global__ void __launch_bounds__(64 * NW, (RT == 1 && DP <= 128) ? 2 : 1) decode_part(DecodeArgs a) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1;
     constexpr int KS = DP / 32, DB = DP / 16, KB = DP / 4;  // key steps, value tiles, key bytes of a lane
     constexpr int KW = KB / 4;                               // the same in words
-    __shared__ float mrg[DW / 2][16 * RT * (DP + 2)];
+    __shared__ float mrg[NW / 2][16 * RT * (DP + 2)];
     Part p;
-    if (a.parts_max > 0) {
+    if (NW == DW && a.parts_max > 0) {
         if (!find_part(a, &p)) return;
     } else {
         p.cell = blockIdx.x, p.part = 0, p.parts = 1, p.t0 = 0;
@@ -184,10 +182,10 @@ __global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_pa
     }
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rl = lane & 15, g = lane >> 4;
-    const int64_t c = p.cell, seq = c / a.Hkv, h = c % a.Hkv;
+    const int c = p.cell, seq = c / a.Hkv, h = c % a.Hkv;
     const int len = cell_len(a, c);
     const int r0 = blockIdx.y * 16 * RT;
-    const int32_t *row = a.table + c * a.W;
+    const int32_t *row = a.table + (int64_t)c * a.W;
     const float sl2 = (a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d))) * DLOG2E;
 
     bf16x8 qf[RT][KS][NP];
@@ -195,9 +193,9 @@ __global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_pa
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int r = r0 + 16 * rt + rl;
-        const int rc = r < a.R ? r : a.R - 1, tok = rc / (int)a.G;
-        seen[rt] = len - (int)(a.T - 1 - tok);
-        const T *qp = (const T *)a.q + seq * a.q_seq + tok * a.q_tok + (h * a.G + rc % (int)a.G) * a.q_head;
+        const int rc = r < a.R ? r : a.R - 1, tok = rc / a.G;
+        seen[rt] = len - (a.T - 1 - tok);
+        const T *qp = (const T *)a.q + seq * a.q_seq + tok * a.q_tok + (h * a.G + rc % a.G) * a.q_head;
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
@@ -209,7 +207,7 @@ __global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_pa
                 for (int n = 0; n < NP; ++n) qf[rt][s][n][j] = y[n];
             }
     }
-    const int fewest = len - (int)(a.T - 1);   // tokens that every row sees
+    const int fewest = len - (a.T - 1);   // tokens that every row sees
     const int bmask = (1 << a.shift) - 1;
 
     f32x4 acc[RT][DB];
@@ -225,13 +223,14 @@ __global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_pa
         const int b = tok < len ? row[tok >> a.shift] : -1;
         return b >= 0 && b < a.n_blocks ? b : -1;
     };
-    for (int t = p.t0 + w; t < p.t1; t += DW) {
-        const int base = t * DT;
-        const int ktok = base + 16 * (rl / 4), vtok = base + 16 * g;
-        const int kp = page(ktok), vp = page(vtok);
-        const int kb = kp < 0 ? 0 : kp, vb = vp < 0 ? 0 : vp;
-        // keys: tile x of 16 rows, row rl = token 16 (rl / 4) + 4 x + rl % 4
-        __align__(16) uint32_t kr[4][KW];
+    // Loads run ahead: the next tile's keys are asked for when this tile's are used up, its values likewise,
+    // and page numbers a tile before that.  Tokens past the end and bad pages read block 0, and are masked.
+    __align__(16) uint32_t kr[4][KW];
+    uint4 vr[DB];
+    int ke, ve;  // exponent bytes of the lane's weights' block
+    const auto load_keys = [&](int base, int kp, int vp) {
+        // tile x of 16 rows: row rl = token 16 (rl / 4) + 4 x + rl % 4
+        const int ktok = base + 16 * (rl / 4), kb = kp < 0 ? 0 : kp, vb = vp < 0 ? 0 : vp;
         const uint8_t *kp_ = a.kc + (((int64_t)kb << a.shift) + (ktok & bmask) + (rl & 3)) * DP + KB * g;
 #pragma unroll
         for (int x = 0; x < 4; ++x)
@@ -240,11 +239,25 @@ __global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_pa
                 if constexpr (KW % 4 == 0) *(uint4 *)&kr[x][y] = *(const uint4 *)(kp_ + 4 * x * DP + 4 * y);
                 else *(uint2 *)&kr[x][y] = *(const uint2 *)(kp_ + 4 * x * DP + 4 * y);
             }
-        uint4 vr[DB];
+        ke = a.k_exp[vb], ve = a.v_exp[vb];
+    };
+    const auto load_values = [&](int base, int vp) {
+        const int vtok = base + 16 * g, vb = vp < 0 ? 0 : vp;
         const uint8_t *vp_ = a.vc + (((int64_t)vb * DP + rl) << a.shift) + (vtok & bmask);
 #pragma unroll
         for (int n = 0; n < DB; ++n) vr[n] = *(const uint4 *)(vp_ + ((int64_t)(16 * n) << a.shift));
-        const float kf = sl2 * pow2_byte(a.k_exp[vb]), vf = pow2_byte(a.v_exp[vb]);
+    };
+    const int t0 = p.t0 + w;
+    int kp = -1, vp = -1, kpn = -1, vpn = -1;
+    if (t0 < p.t1) {
+        kp = page(t0 * DT + 16 * (rl / 4)), vp = page(t0 * DT + 16 * g);
+        load_keys(t0 * DT, kp, vp);
+        load_values(t0 * DT, vp);
+        if (t0 + NW < p.t1) kpn = page((t0 + NW) * DT + 16 * (rl / 4)), vpn = page((t0 + NW) * DT + 16 * g);
+    }
+    for (int t = t0; t < p.t1; t += NW) {
+        const int base = t * DT, vtok = base + 16 * g;
+        const float kf = sl2 * pow2_byte(ke), vf = pow2_byte(ve);
 
         f32x4 s[RT][4];
 #pragma unroll
@@ -261,6 +274,8 @@ __global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_pa
                         s[rt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qf[rt][y][n], s[rt][x], 0, 0, 0);
             }
         }
+        const bool more = t + NW < p.t1;
+        if (more) load_keys(base + NW * DT, kpn, vpn);
         const bool masked = base + DT > fewest || __any(vp < 0);
         if (masked) {
             const int valid = vp < 0 ? 0 : len - vtok;
@@ -347,6 +362,11 @@ __global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_pa
                     acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[rt][1][x], acc[rt][n], 0, 0, 0);
                 }
         }
+        if (more) load_values(base + NW * DT, vpn);
+        kp = kpn, vp = vpn;
+        const int ahead = base + 2 * NW * DT;
+        kpn = vpn = -1;
+        if (t + 2 * NW < p.t1) kpn = page(ahead + 16 * (rl / 4)), vpn = page(ahead + 16 * g);
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -355,7 +375,7 @@ __global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_pa
     }
     // join the waves, in a fixed order: the upper half writes, the lower half takes
 #pragma unroll
-    for (int half = DW / 2; half >= 1; half /= 2) {
+    for (int half = NW / 2; half >= 1; half /= 2) {
         if (w >= half && w < 2 * half) {
             float *z = mrg[w - half];
 #pragma unroll
@@ -402,7 +422,7 @@ __global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_pa
                     if (16 * n + 4 * g + i < a.d) a.part_o[at * a.d + 16 * n + 4 * g + i] = acc[rt][n][i] * il;
             if (g == 0) a.part_lse[at] = lse2;
         } else {
-            const int64_t at = ((seq * a.T + r / (int)a.G) * a.Hkv + h) * a.G + r % (int)a.G;
+            const int64_t at = (int64_t)((seq * a.T + r / a.G) * a.Hkv + h) * a.G + r % a.G;
 #pragma unroll
             for (int n = 0; n < DB; ++n)
 #pragma unroll
@@ -414,50 +434,72 @@ __global__ void __launch_bounds__(DTH, (RT == 1 && DP <= 128) ? 2 : 1) decode_pa
     }
 }
 
-// Joins the parts of every row whose cell has several; one wave per row.
-template <typename T>
-__global__ void __launch_bounds__(256) decode_join(DecodeArgs a) {
+// Joins the parts of every row whose cell has several; one wave per row: a
+// lane per part for the parts' weights, then a lane per column.
+template <typename T, int NC>
+__global__ void __launch_bounds__(256) decode_join(DecodeArgs a) {  // NC: columns of a lane, ceil(d / 64)
     const int lane = threadIdx.x & 63;
-    const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (x >= a.C * a.R) return;
-    const int64_t c = x / a.R;
-    const int r = (int)(x % a.R);
+    const int x = (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    if ((uint32_t)x >= (uint32_t)a.C * a.R) return;
+    const int c = (uint32_t)x / a.R, r = (uint32_t)x % a.R;
     const int2 ci = a.cells[c];
-    if (ci.y <= 1) return;
+    const int parts = __builtin_amdgcn_readfirstlane(ci.y);
+    if (parts <= 1) return;
     const float *pl = a.part_lse + (int64_t)ci.x * a.R + r;
+    const float *po = a.part_o + ((int64_t)ci.x * a.R + r) * a.d;
     float M = -INFINITY;
-    for (int s = 0; s < ci.y; ++s) M = fmaxf(M, pl[(int64_t)s * a.R]);
+    for (int s = lane; s < parts; s += 64) M = fmaxf(M, pl[(int64_t)s * a.R]);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
     const float base = M == -INFINITY ? 0.f : M;
-    float sum = 0.f;
-    for (int s = 0; s < ci.y; ++s) sum += __builtin_amdgcn_exp2f(pl[(int64_t)s * a.R] - base);
-    const float is = sum == 0.f ? 0.f : 1.f / sum;
-    const int64_t seq = c / a.Hkv, h = c % a.Hkv, at = ((seq * a.T + r / (int)a.G) * a.Hkv + h) * a.G + r % (int)a.G;
-    for (int col = lane; col < a.d; col += 64) {
-        float y = 0.f;
-        for (int s = 0; s < ci.y; ++s) {
-            const float e = pl[(int64_t)s * a.R];
-            if (e != -INFINITY)
-                y = fmaf(__builtin_amdgcn_exp2f(e - base) * is, a.part_o[(((int64_t)ci.x + s) * a.R + r) * a.d + col], y);
+    float sum = 0.f, y[NC];
+    int col[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) y[i] = 0.f, col[i] = lane + 64 * i < a.d ? lane + 64 * i : 0;
+    for (int s0 = 0; s0 < parts; s0 += 64) {
+        const float e = s0 + lane < parts ? pl[(int64_t)(s0 + lane) * a.R] : -INFINITY;
+        const float w = __builtin_amdgcn_exp2f(e - base);
+        sum += w;
+        const int n = parts - s0 < 64 ? parts - s0 : 64;
+#pragma unroll 8
+        for (int s = 0; s < n; ++s) {
+            const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
+            const float *row = po + (int64_t)(s0 + s) * a.R * a.d;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) y[i] = fmaf(ws, row[col[i]], y[i]);
         }
-        ((T *)a.o)[at * a.d + col] = dnarrow<T>(y);
     }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+    const float is = sum == 0.f ? 0.f : 1.f / sum;
+    const int seq = c / a.Hkv, h = c % a.Hkv;
+    const int64_t at = (int64_t)((seq * a.T + r / a.G) * a.Hkv + h) * a.G + r % a.G;
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+        if (lane + 64 * i < a.d) ((T *)a.o)[at * a.d + lane + 64 * i] = dnarrow<T>(y[i] * is);
     if (lane == 0 && a.lse) a.lse[at] = (M + (sum == 0.f ? 0.f : __builtin_amdgcn_logf(sum))) * DLN2;
 }
 
-template <typename T, int DP, int RT>
+template <typename T, int DP, int RT, int NW = DW>
 void launch_part(const DecodeArgs &a, unsigned parts, hipStream_t st) {
     const dim3 grid(parts, (unsigned)((a.R + 16 * RT - 1) / (16 * RT)));
-    hipLaunchKernelGGL((decode_part<T, DP, RT>), grid, dim3(DTH), 0, st, a);
+    hipLaunchKernelGGL((decode_part<T, DP, RT, NW>), grid, dim3(64 * NW), 0, st, a);
 }
 
+// Row tiles of 16 per wave, as many as its registers hold without spilling:
+// further rows of a cell go to workgroups of their own, which read it again.
 template <typename T, int DP>
 void launch_rows(const DecodeArgs &a, unsigned parts, hipStream_t st) {
-    if constexpr (sizeof(T) == 4) {
+    constexpr int most = sizeof(T) == 4 || DP > 192 ? 1 : DP > 96 ? 2 : 4;
+    if (a.R <= 16 || most == 1) {
+        if constexpr (DP <= 128) {
+            if (a.parts_max == 0) return launch_part<T, DP, 1, 2 * DW>(a, parts, st);
+        }
         launch_part<T, DP, 1>(a, parts, st);
+    } else if (a.R <= 32 || most == 2) {
+        launch_part<T, DP, most == 1 ? 1 : 2>(a, parts, st);
     } else {
-        if (a.R <= 16) launch_part<T, DP, 1>(a, parts, st);
-        else if (a.R <= 32 || DP > 128) launch_part<T, DP, 2>(a, parts, st);
-        else launch_part<T, DP, DP <= 128 ? 4 : 2>(a, parts, st);
+        launch_part<T, DP, most>(a, parts, st);
     }
 }
 
@@ -473,10 +515,20 @@ void launch_width(const DecodeArgs &a, int dp, unsigned parts, hipStream_t st) {
     }
 }
 
+template <typename T>
+void launch_join(const DecodeArgs &a, dim3 grid, hipStream_t st) {
+    switch ((a.d + 63) / 64) {
+        case 1: hipLaunchKernelGGL((decode_join<T, 1>), grid, dim3(256), 0, st, a); break;
+        case 2: hipLaunchKernelGGL((decode_join<T, 2>), grid, dim3(256), 0, st, a); break;
+        case 3: hipLaunchKernelGGL((decode_join<T, 3>), grid, dim3(256), 0, st, a); break;
+        default: hipLaunchKernelGGL((decode_join<T, 4>), grid, dim3(256), 0, st, a); break;
+    }
+}
+
 // An upper bound of the parts: the lengths are on the device.  0 when no cell can have a second part.
 int64_t most_parts(int64_t C, int64_t W, int block_size) {
     const int64_t tiles = (W * block_size + DT - 1) / DT, per_cell = (tiles + kMinChunk - 1) / kMinChunk;
-    if (per_cell <= 1) return 0;
+    if (tiles <= kWhole) return 0;
     return std::min(C + kTarget, C * per_cell);
 }
 }  // namespace
@@ -491,8 +543,8 @@ hipError_t launch_decode(const fw_cache &cache, int dtype, const void *q, int64_
                          const int32_t *lens, const float *scale, void *o, float *lse, void *ws, hipStream_t st) {
     DecodeArgs a{};
     a.q = q, a.q_seq = q_seq, a.q_tok = q_tok, a.q_head = q_head;
-    a.C = S * Hkv, a.T = T, a.Hkv = Hkv, a.G = Hq / Hkv, a.W = W;
-    a.R = (int)(T * a.G), a.d = (int)cache.d;
+    a.C = (int)(S * Hkv), a.T = (int)T, a.Hkv = (int)Hkv, a.G = (int)(Hq / Hkv), a.W = (int)W;
+    a.R = a.T * a.G, a.d = (int)cache.d;
     a.kc = cache.k, a.vc = cache.v, a.k_exp = cache.k_exp, a.v_exp = cache.v_exp;
     a.n_blocks = cache.n_blocks, a.shift = __builtin_ctz(cache.block_size);
     a.table = table, a.lens = lens, a.scale = scale, a.o = o, a.lse = lse;
@@ -501,7 +553,7 @@ hipError_t launch_decode(const fw_cache &cache, int dtype, const void *q, int64_
     if (parts) {
         char *p = (char *)ws;
         a.cells = (int2 *)p;
-        p += align_up(a.C * sizeof(int2), 256);
+        p += align_up((size_t)a.C * sizeof(int2), 256);
         a.part_o = (float *)p;
         p += align_up(parts * a.R * a.d * 4, 256);
         a.part_lse = (float *)p;
@@ -511,9 +563,9 @@ hipError_t launch_decode(const fw_cache &cache, int dtype, const void *q, int64_
     if (dtype == FW_F32) launch_width<float>(a, dp, grid, st);
     else launch_width<uint16_t>(a, dp, grid, st);
     if (parts) {
-        const dim3 jg((unsigned)((a.C * a.R + 3) / 4));
-        if (dtype == FW_F32) hipLaunchKernelGGL(decode_join<float>, jg, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL(decode_join<uint16_t>, jg, dim3(256), 0, st, a);
+        const dim3 jg((unsigned)(((int64_t)a.C * a.R + 3) / 4));
+        if (dtype == FW_F32) launch_join<float>(a, jg, st);
+        else launch_join<uint16_t>(a, jg, st);
     }
     return hipGetLastError();
 }
