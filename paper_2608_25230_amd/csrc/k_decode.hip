@@ -20,9 +20,10 @@
 // per lane.
 //
 // Cells differ in length by far, so the work is cut by length, on the device:
-// parts of `chunk` tiles, chunk = ceil(all tiles / target) at least kMinChunk;
-// every workgroup finds its cell and part from the lengths.  A cell of several
-// parts leaves partial results in the workspace, joined by decode_join.
+// all cells' tiles in a row, and kCell more for what a cell costs besides
+// them, every workgroup takes the same number of them and finds from the
+// lengths where it begins.  A cell that one workgroup has whole is done with
+// it; the others' parts go to the workspace, joined by decode_join.
 #include <algorithm>
 
 #include "fw_internal.hpp"
@@ -32,13 +33,15 @@ namespace fw {
 namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int DW = 4;               // waves per workgroup; 8 where one takes a whole cell (kWhole)
 constexpr int DT = 64;              // tokens per wave and step
-constexpr int kTarget = 1024;       // parts that the whole work is cut into
-constexpr int kMinChunk = 8;        // tiles of a part at least
-constexpr int kWhole = 32;          // tiles of a table row up to which a cell is one part
+constexpr int kGroups = 512;        // workgroups that share the tiles: two to a compute unit
+constexpr int kMinTiles = 8;        // tiles of a workgroup at least
+constexpr int kCell = 4;            // what a cell costs besides its tiles, in tiles
+constexpr int kWhole = 32;          // tiles of a table row up to which a workgroup takes one cell whole
 constexpr float DLOG2E = 1.4426950408889634f;
 constexpr float DLN2 = 0.6931471805599453f;
 constexpr float DMIN = -3.0e38f;
@@ -56,7 +59,8 @@ struct DecodeArgs {
     const float *scale;
     void *o;
     float *lse;
-    int parts_max;                  // workgroups per row group; 1 part per cell without a workspace
+    int groups;                     // workgroups that share the tiles; 0: one for each cell
+    bool wide;                      // 16-byte aligned queries of a multiple of 8 columns
     int2 *cells;                    // [C] first part and parts of a cell
     float *part_o, *part_lse;       // [parts][R][d], [parts][R] (base 2)
 };
@@ -88,42 +92,38 @@ __device__ __forceinline__ int sum_before(int v, int *red, int *total) {
     return x - v + before;
 }
 
-// This workgroup's cell, its part of it and the part's tiles; false if there is no such part.
-struct Part {
-    int cell, part, parts, t0, t1;
+// Tiles of a cell; an empty one has a tile too, in which nothing is seen.
+__device__ __forceinline__ int tiles_of(int len) { return len > 0 ? (len + DT - 1) / DT : 1; }
+
+// This workgroup's share of the tiles [g0, g1), the cell that holds the first and that cell's first tile; false if
+// nothing is left for it.
+struct Share {
+    int g0, g1, cell, first, per;
 };
-__device__ __forceinline__ bool find_part(const DecodeArgs &a, Part *p) {
-    __shared__ int red[DW], found[4];
+__device__ __forceinline__ bool find_share(const DecodeArgs &a, Share *s) {
+    __shared__ int red[DW], found[2];
     const int run = (a.C + 64 * DW - 1) / (64 * DW), c0 = threadIdx.x * run;
     const int c1 = c0 + run < a.C ? c0 + run : a.C;
-    int tiles = 0, all;
-    for (int c = c0; c < c1; ++c) tiles += (cell_len(a, c) + DT - 1) / DT;
-    sum_before(tiles, red, &all);
-    int chunk = (all + kTarget - 1) / kTarget;
-    if (chunk < kMinChunk) chunk = kMinChunk;
-    int mine = 0, total;
-    for (int c = c0; c < c1; ++c) {
-        const int n = ((cell_len(a, c) + DT - 1) / DT + chunk - 1) / chunk;
-        mine += n ? n : 1;
-    }
-    int first = sum_before(mine, red, &total);
-    const int x = blockIdx.x;
-    if (x >= total) return false;
-    if (x >= first && x < first + mine) {
+    int mine = 0, all;
+    for (int c = c0; c < c1; ++c) mine += tiles_of(cell_len(a, c)) + kCell;
+    int first = sum_before(mine, red, &all);
+    s->per = (all + a.groups - 1) / a.groups;
+    if (s->per < kMinTiles) s->per = kMinTiles;
+    s->g0 = blockIdx.x * s->per;   // below 2^31: less than twice all tiles or kMinTiles each
+    if (s->g0 >= all) return false;
+    s->g1 = s->g0 + s->per < all ? s->g0 + s->per : all;
+    if (s->g0 >= first && s->g0 < first + mine) {
         for (int c = c0; c < c1; ++c) {
-            const int nt = (cell_len(a, c) + DT - 1) / DT, n = nt ? (nt + chunk - 1) / chunk : 1;
-            if (x < first + n) {
-                found[0] = c, found[1] = x - first, found[2] = n, found[3] = nt;
-                if (x == first && blockIdx.y == 0) a.cells[c] = make_int2(first, n);
+            const int n = tiles_of(cell_len(a, c)) + kCell;
+            if (s->g0 < first + n) {
+                found[0] = c, found[1] = first;
                 break;
             }
             first += n;
         }
     }
     __syncthreads();
-    p->cell = found[0], p->part = found[1], p->parts = found[2];
-    p->t0 = p->part * chunk;
-    p->t1 = p->t0 + chunk < found[3] ? p->t0 + chunk : found[3];
+    s->cell = __builtin_amdgcn_readfirstlane(found[0]), s->first = __builtin_amdgcn_readfirstlane(found[1]);
     return true;
 }
 
@@ -168,23 +168,33 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t x) {
 }
 
 template <typename T, int DP, int RT, int NW>
-__global__ void __launch_bounds__(64 * NW, (RT == 1 && DP <= 128) ? 2 : 1) decode_part(DecodeArgs a) {
+__global__ void __launch_bounds__(64 * NW, RT == 1 && DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1) decode_part(DecodeArgs a) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1;
     constexpr int KS = DP / 32, DB = DP / 16, KB = DP / 4;  // key steps, value tiles, key bytes of a lane
     constexpr int KW = KB / 4;                               // the same in words
+    constexpr bool AHEAD = NP == 1 || DP < 256;              // loads run a tile ahead, where registers hold them
     __shared__ float mrg[NW / 2][16 * RT * (DP + 2)];
-    Part p;
-    if (NW == DW && a.parts_max > 0) {
-        if (!find_part(a, &p)) return;
-    } else {
-        p.cell = blockIdx.x, p.part = 0, p.parts = 1, p.t0 = 0;
-        p.t1 = (cell_len(a, p.cell) + DT - 1) / DT;
-    }
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rl = lane & 15, g = lane >> 4;
-    const int c = p.cell, seq = c / a.Hkv, h = c % a.Hkv;
-    const int len = cell_len(a, c);
     const int r0 = blockIdx.y * 16 * RT;
+    Share sh;
+    int len;
+    if (NW == DW && a.groups > 0) {
+        if (!find_share(a, &sh)) return;
+        len = cell_len(a, sh.cell);
+    } else {
+        len = cell_len(a, blockIdx.x);
+        sh.cell = blockIdx.x, sh.first = sh.g0 = 0, sh.per = sh.g1 = tiles_of(len);
+    }
+    for (int c = sh.cell, first = sh.first;;) {
+    const int nt = tiles_of(len), t0 = sh.g0 > first ? sh.g0 - first : 0, t1 = sh.g1 - first < nt ? sh.g1 - first : nt;
+    const bool whole = t0 == 0 && t1 == nt;
+    const bool last = first + nt + kCell >= sh.g1 || c + 1 >= a.C;
+    const int next_len = last ? 0 : cell_len(a, c + 1);
+    if (t0 == 0 && a.groups > 0 && threadIdx.x == 0 && blockIdx.y == 0)   // parts are numbered by workgroup and cell together
+        a.cells[c] = make_int2(blockIdx.x + c, whole ? 1 : (first + nt - 1) / sh.per - (int)blockIdx.x + 1);
+    if (NW != DW || t0 < t1) {  // else the share begins behind the cell's tiles
+    const int seq = c / a.Hkv, h = c % a.Hkv;
     const int32_t *row = a.table + (int64_t)c * a.W;
     const float sl2 = (a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d))) * DLOG2E;
 
@@ -197,15 +207,34 @@ __global__ void __launch_bounds__(64 * NW, (RT == 1 && DP <= 128) ? 2 : 1) decod
         seen[rt] = len - (a.T - 1 - tok);
         const T *qp = (const T *)a.q + seq * a.q_seq + tok * a.q_tok + (h * a.G + rc % a.G) * a.q_head;
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+        for (int s = 0; s < KS; ++s) {
+            const int col = KB * g + 8 * s;
+            if (a.wide) {
+                if constexpr (NP == 1) {
+                    uint4 x = {0u, 0u, 0u, 0u};
+                    if (col < a.d) x = *(const uint4 *)(qp + col);
+                    qf[rt][s][0] = __builtin_bit_cast(bf16x8, x);
+                } else {
+                    f32x4 x = {0.f, 0.f, 0.f, 0.f}, z = x;
+                    if (col < a.d) x = *(const f32x4 *)(qp + col), z = *(const f32x4 *)(qp + col + 4);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int col = KB * g + 8 * s + j;
-                __bf16 y[NP];
-                take_apart<NP>(col < a.d ? Elem<T>::load(qp, col) : 0.f, y);
+                    for (int j = 0; j < 8; ++j) {
+                        __bf16 y[NP];
+                        take_apart<NP>(j < 4 ? x[j] : z[j - 4], y);
 #pragma unroll
-                for (int n = 0; n < NP; ++n) qf[rt][s][n][j] = y[n];
+                        for (int n = 0; n < NP; ++n) qf[rt][s][n][j] = y[n];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    __bf16 y[NP];
+                    take_apart<NP>(col + j < a.d ? Elem<T>::load(qp, col + j) : 0.f, y);
+#pragma unroll
+                    for (int n = 0; n < NP; ++n) qf[rt][s][n][j] = y[n];
+                }
             }
+        }
     }
     const int fewest = len - (a.T - 1);   // tokens that every row sees
     const int bmask = (1 << a.shift) - 1;
@@ -247,16 +276,21 @@ __global__ void __launch_bounds__(64 * NW, (RT == 1 && DP <= 128) ? 2 : 1) decod
 #pragma unroll
         for (int n = 0; n < DB; ++n) vr[n] = *(const uint4 *)(vp_ + ((int64_t)(16 * n) << a.shift));
     };
-    const int t0 = p.t0 + w;
+    const int ts = t0 + w;
     int kp = -1, vp = -1, kpn = -1, vpn = -1;
-    if (t0 < p.t1) {
-        kp = page(t0 * DT + 16 * (rl / 4)), vp = page(t0 * DT + 16 * g);
-        load_keys(t0 * DT, kp, vp);
-        load_values(t0 * DT, vp);
-        if (t0 + NW < p.t1) kpn = page((t0 + NW) * DT + 16 * (rl / 4)), vpn = page((t0 + NW) * DT + 16 * g);
+    if (AHEAD && ts < t1) {
+        kp = page(ts * DT + 16 * (rl / 4)), vp = page(ts * DT + 16 * g);
+        load_keys(ts * DT, kp, vp);
+        load_values(ts * DT, vp);
+        if (ts + NW < t1) kpn = page((ts + NW) * DT + 16 * (rl / 4)), vpn = page((ts + NW) * DT + 16 * g);
     }
-    for (int t = t0; t < p.t1; t += NW) {
+    for (int t = ts; t < t1; t += NW) {
         const int base = t * DT, vtok = base + 16 * g;
+        if (!AHEAD) {
+            kp = page(base + 16 * (rl / 4)), vp = page(vtok);
+            load_keys(base, kp, vp);
+            load_values(base, vp);
+        }
         const float kf = sl2 * pow2_byte(ke), vf = pow2_byte(ve);
 
         f32x4 s[RT][4];
@@ -274,7 +308,7 @@ __global__ void __launch_bounds__(64 * NW, (RT == 1 && DP <= 128) ? 2 : 1) decod
                         s[rt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qf[rt][y][n], s[rt][x], 0, 0, 0);
             }
         }
-        const bool more = t + NW < p.t1;
+        const bool more = AHEAD && t + NW < t1;
         if (more) load_keys(base + NW * DT, kpn, vpn);
         const bool masked = base + DT > fewest || __any(vp < 0);
         if (masked) {
@@ -366,7 +400,7 @@ __global__ void __launch_bounds__(64 * NW, (RT == 1 && DP <= 128) ? 2 : 1) decod
         kp = kpn, vp = vpn;
         const int ahead = base + 2 * NW * DT;
         kpn = vpn = -1;
-        if (t + 2 * NW < p.t1) kpn = page(ahead + 16 * (rl / 4)), vpn = page(ahead + 16 * g);
+        if (AHEAD && t + 2 * NW < t1) kpn = page(ahead + 16 * (rl / 4)), vpn = page(ahead + 16 * g);
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -406,31 +440,49 @@ __global__ void __launch_bounds__(64 * NW, (RT == 1 && DP <= 128) ? 2 : 1) decod
         }
         __syncthreads();
     }
-    if (w != 0) return;
+    if (w == 0) {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int r = r0 + 16 * rt + rl;
-        if (r >= a.R) continue;
-        const float il = l[rt] > 0.f || l[rt] != l[rt] ? 1.f / l[rt] : 0.f;
-        const float lse2 = l[rt] == 0.f ? -INFINITY : m[rt] + __builtin_amdgcn_logf(l[rt]);
-        if (p.parts > 1) {
-            const int64_t at = (int64_t)blockIdx.x * a.R + r;
-#pragma unroll
-            for (int n = 0; n < DB; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (16 * n + 4 * g + i < a.d) a.part_o[at * a.d + 16 * n + 4 * g + i] = acc[rt][n][i] * il;
-            if (g == 0) a.part_lse[at] = lse2;
-        } else {
+        for (int rt = 0; rt < RT; ++rt) {
+            const int r = r0 + 16 * rt + rl;
+            if (r >= a.R) continue;
+            const float il = l[rt] > 0.f || l[rt] != l[rt] ? 1.f / l[rt] : 0.f;
+            const float lse2 = l[rt] == 0.f ? -INFINITY : m[rt] + __builtin_amdgcn_logf(l[rt]);
+            const int64_t part = (int64_t)(blockIdx.x + c) * a.R + r;
             const int64_t at = (int64_t)((seq * a.T + r / a.G) * a.Hkv + h) * a.G + r % a.G;
+            int d = a.d;
+            asm volatile("" : "+s"(d));  // its comparisons are made here, not kept through the loop over cells
 #pragma unroll
-            for (int n = 0; n < DB; ++n)
+            for (int n = 0; n < DB; ++n) {
+                const int col = 16 * n + 4 * g;
+                if (col >= d) continue;
+                const f32x4 y = acc[rt][n] * il;
+                if (d % 4 == 0) {
+                    if (!whole) {
+                        *(f32x4 *)(a.part_o + part * a.d + col) = y;
+                    } else if constexpr (NP == 3) {
+                        *(f32x4 *)((T *)a.o + at * a.d + col) = y;
+                    } else {
+                        const bf16x4 z = {(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+                        *(bf16x4 *)((T *)a.o + at * a.d + col) = z;
+                    }
+                } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (16 * n + 4 * g + i < a.d)
-                        ((T *)a.o)[at * a.d + 16 * n + 4 * g + i] = dnarrow<T>(acc[rt][n][i] * il);
-            if (g == 0 && a.lse) a.lse[at] = lse2 * DLN2;
+                    for (int i = 0; i < 4; ++i) {
+                        if (col + i >= d) continue;
+                        if (whole) ((T *)a.o)[at * a.d + col + i] = dnarrow<T>(y[i]);
+                        else a.part_o[part * a.d + col + i] = y[i];
+                    }
+                }
+            }
+            if (g == 0) {
+                if (!whole) a.part_lse[part] = lse2;
+                else if (a.lse) a.lse[at] = lse2 * DLN2;
+            }
         }
+    }
+    }
+    if (NW != DW || last) return;
+    first += nt + kCell, len = next_len, ++c;
     }
 }
 
@@ -490,10 +542,10 @@ void launch_part(const DecodeArgs &a, unsigned parts, hipStream_t st) {
 // further rows of a cell go to workgroups of their own, which read it again.
 template <typename T, int DP>
 void launch_rows(const DecodeArgs &a, unsigned parts, hipStream_t st) {
-    constexpr int most = sizeof(T) == 4 || DP > 192 ? 1 : DP > 96 ? 2 : 4;
+    constexpr int most = sizeof(T) == 4 || DP > 128 ? 1 : DP > 64 ? 2 : 4;
     if (a.R <= 16 || most == 1) {
-        if constexpr (DP <= 128) {
-            if (a.parts_max == 0) return launch_part<T, DP, 1, 2 * DW>(a, parts, st);
+        if constexpr (DP <= (sizeof(T) == 4 ? 96 : 128)) {
+            if (a.groups == 0) return launch_part<T, DP, 1, 2 * DW>(a, parts, st);
         }
         launch_part<T, DP, 1>(a, parts, st);
     } else if (a.R <= 32 || most == 2) {
@@ -525,17 +577,17 @@ void launch_join(const DecodeArgs &a, dim3 grid, hipStream_t st) {
     }
 }
 
-// An upper bound of the parts: the lengths are on the device.  0 when no cell can have a second part.
-int64_t most_parts(int64_t C, int64_t W, int block_size) {
-    const int64_t tiles = (W * block_size + DT - 1) / DT, per_cell = (tiles + kMinChunk - 1) / kMinChunk;
-    if (tiles <= kWhole) return 0;
-    return std::min(C + kTarget, C * per_cell);
+// Workgroups that share the tiles, at most so many as all tables could hold work for (the lengths are on the
+// device); 0 where the tables are so short that each cell has a workgroup of its own.
+int64_t share_groups(int64_t C, int64_t W, int block_size) {
+    const int64_t tiles = (W * block_size + DT - 1) / DT;
+    return tiles <= kWhole ? 0 : std::min<int64_t>(kGroups, (C * (tiles + kCell) + kMinTiles - 1) / kMinTiles);
 }
 }  // namespace
 
 size_t decode_ws_bytes(int64_t C, int64_t R, int64_t d, int64_t W, int block_size) {
-    const int64_t parts = most_parts(C, W, block_size);
-    return parts ? align_up(C * sizeof(int2), 256) + align_up(parts * R * d * 4, 256) + align_up(parts * R * 4, 256) : 0;
+    const int64_t groups = share_groups(C, W, block_size), parts = groups + C;  // a part ends with its workgroup or its cell
+    return groups ? align_up(C * sizeof(int2), 256) + align_up(parts * R * d * 4, 256) + align_up(parts * R * 4, 256) : 0;
 }
 
 hipError_t launch_decode(const fw_cache &cache, int dtype, const void *q, int64_t S, int64_t T, int64_t Hq, int64_t Hkv,
@@ -548,9 +600,11 @@ hipError_t launch_decode(const fw_cache &cache, int dtype, const void *q, int64_
     a.kc = cache.k, a.vc = cache.v, a.k_exp = cache.k_exp, a.v_exp = cache.v_exp;
     a.n_blocks = cache.n_blocks, a.shift = __builtin_ctz(cache.block_size);
     a.table = table, a.lens = lens, a.scale = scale, a.o = o, a.lse = lse;
-    const int64_t parts = most_parts(a.C, W, cache.block_size);
-    a.parts_max = (int)parts;
-    if (parts) {
+    const int size = dtype == FW_F32 ? 4 : 2;
+    a.wide = a.d % 8 == 0 && (uintptr_t)q % 16 == 0 && q_seq * size % 16 == 0 && q_tok * size % 16 == 0 && q_head * size % 16 == 0;
+    a.groups = (int)share_groups(a.C, W, cache.block_size);
+    if (a.groups) {
+        const int64_t parts = (int64_t)a.groups + a.C;
         char *p = (char *)ws;
         a.cells = (int2 *)p;
         p += align_up((size_t)a.C * sizeof(int2), 256);
@@ -559,10 +613,10 @@ hipError_t launch_decode(const fw_cache &cache, int dtype, const void *q, int64_
         a.part_lse = (float *)p;
     }
     const int dp = cache_row(cache.d);
-    const unsigned grid = (unsigned)(parts ? parts : a.C);
+    const unsigned grid = (unsigned)(a.groups ? a.groups : a.C);
     if (dtype == FW_F32) launch_width<float>(a, dp, grid, st);
     else launch_width<uint16_t>(a, dp, grid, st);
-    if (parts) {
+    if (a.groups) {
         const dim3 jg((unsigned)(((int64_t)a.C * a.R + 3) / 4));
         if (dtype == FW_F32) launch_join<float>(a, jg, st);
         else launch_join<uint16_t>(a, jg, st);
