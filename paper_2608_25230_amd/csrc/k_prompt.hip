@@ -104,7 +104,8 @@ template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float x) {
 // ---------------------------------------------------------------------------
 // General kernel: any strides, widths and both types, float32 throughout.
 // Four waves of 16 rows; key tiles of 32 in LDS as float32, rows and columns
-// past the sequence's end and past d as zeros.
+// past the sequence's end and past d as zeros; the next tile's loads fly while
+// this one is computed.
 //   S^T = K Q^T on v_mfma_f32_16x16x4_f32: lane l holds row l % 16, keys
 //   4 (l / 16) + i of each 16-key half.  Since the order of a contraction is
 //   free, lane group l / 16 takes columns 16 j + 4 (l / 16) + s at step (j, s),
@@ -116,44 +117,25 @@ constexpr int GK = 32;    // keys per tile
 constexpr int GR = 64;    // rows per workgroup
 constexpr int GTH = 256;
 
-// Returns whether this thread saw an infinity or a NaN.
+// Columns c .. c + 4 of a row as float32, those past d as zeros.
 template <typename T>
-__device__ __forceinline__ bool load_tile(float *dst, int ld, int dp, const T *src, int64_t row, int64_t left, int d,
-                                          bool vec) {
-    // `left` valid rows from src on
-    bool bad = false;
+__device__ __forceinline__ f32x4 load4(const T *p, int c, int d, bool vec) {
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
     if (vec) {
-        const int ch = dp / 4;
-        for (int x = threadIdx.x; x < GK * ch; x += GTH) {
-            const int r = x / ch, c = 4 * (x % ch);
-            f32x4 y = {0.f, 0.f, 0.f, 0.f};
-            if (r < left && c < d) {
-                const T *p = src + r * row + c;
-                if constexpr (sizeof(T) == 4) {
-                    y = *(const f32x4 *)p;
-                } else {
-                    const uint2 w = *(const uint2 *)p;
-                    y = (f32x4){__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u),
-                                __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u)};
-                }
-            }
-            *(f32x4 *)(dst + r * ld + c) = y;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) bad |= !(fabsf(y[i]) < INFINITY);
-        }
-    } else {
-        for (int x = threadIdx.x; x < GK * dp; x += GTH) {
-            const int r = x / dp, c = x % dp;
-            const float y = (r < left && c < d) ? Elem<T>::load(src, (size_t)(r * row + c)) : 0.f;
-            dst[r * ld + c] = y;
-            bad |= !(fabsf(y) < INFINITY);
-        }
+        if (c >= d) return y;
+        if constexpr (sizeof(T) == 4) return *(const f32x4 *)(p + c);
+        const uint2 w = *(const uint2 *)(p + c);
+        return (f32x4){__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
+                       __uint_as_float(w.y & 0xFFFF0000u)};
     }
-    return bad;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (c + i < d) y[i] = Elem<T>::load(p, c + i);
+    return y;
 }
 
 template <typename T, int NT>
-__global__ void __launch_bounds__(GTH) prompt_general(PromptArgs a, int vec) {
+__global__ void __launch_bounds__(GTH, NT <= 5 ? 3 : 1) prompt_general(PromptArgs a, int vec) {
     constexpr int DP = 16 * NT, LD = DP + 4;
     __shared__ __align__(16) float ks[GK * LD];
     __shared__ __align__(16) float vs[GK * LD];
@@ -193,11 +175,35 @@ __global__ void __launch_bounds__(GTH) prompt_general(PromptArgs a, int vec) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m = PMIN, l = 0.f;
+    constexpr int CH = DP / 4, NV = (GK * CH + GTH - 1) / GTH;  // pieces of four columns, of a row and of a thread
+    f32x4 kn[NV], vn[NV];
+    const auto fetch = [&](int j) {
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            const int x = threadIdx.x + u * GTH, r = x / CH, c = 4 * (x % CH);
+            const int64_t key = (int64_t)j * GK + r;
+            kn[u] = vn[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if (r < GK && key < t.Lk) {
+                kn[u] = load4<T>(kp + key * a.k_row, c, a.d, vec);
+                vn[u] = load4<T>(vp + key * a.v_row, c, a.d, vec);
+            }
+        }
+    };
+    if (j0 < j1) fetch(j0);
     for (int j = j0; j < j1; ++j) {
-        const int64_t key0 = (int64_t)j * GK;
-        __syncthreads();
-        load_tile<T>(ks, LD, DP, kp + key0 * a.k_row, a.k_row, t.Lk - key0, a.d, vec);
-        const bool bad = __syncthreads_or(load_tile<T>(vs, LD, DP, vp + key0 * a.v_row, a.v_row, t.Lk - key0, a.d, vec));
+        const int key0 = j * GK;
+        bool bad = false;  // an infinity or a NaN among the values
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            const int x = threadIdx.x + u * GTH, at = x / CH * LD + 4 * (x % CH);
+            if (x >= GK * CH) break;
+            *(f32x4 *)(ks + at) = kn[u];
+            *(f32x4 *)(vs + at) = vn[u];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bad |= !(fabsf(vn[u][i]) < INFINITY);
+        }
+        bad = __syncthreads_or(bad);
+        if (j + 1 < j1) fetch(j + 1);
         f32x4 s[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -272,6 +278,7 @@ __global__ void __launch_bounds__(GTH) prompt_general(PromptArgs a, int vec) {
                 }
             }
         }
+        __syncthreads();  // every wave is done with the tile
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -680,12 +687,13 @@ void launch_general(const PromptArgs &a, int vec, dim3 grid, hipStream_t st) {
 }  // namespace
 
 // Ranges that a row's keys are split into: one when the row tiles fill the
-// card twice over (two workgroups to a compute unit), otherwise as many as
-// fill it, with at least 256 keys of an average sequence to each.
+// card (three workgroups to a compute unit), otherwise as many as fill it,
+// with at least 256 keys to each of a sequence halfway between the average
+// one and one that has all the keys (the lengths are on the device).
 int prompt_splits(const fw_packed &p) {
     const int64_t tiles = row_tiles(p, prompt_fast(p) ? PR : GR) * p.Hkv;
-    const int64_t fill = 512 / (tiles > 0 ? tiles : 1), keys = p.Tk / (p.B > 0 ? p.B : 1) / 256;
-    int64_t s = fill < keys ? fill : keys;
+    const int64_t fill = (768 + tiles / 2) / (tiles > 0 ? tiles : 1), keys = (p.Tk / (p.B > 0 ? p.B : 1) + p.Tk) / 512;
+    const int64_t s = fill < keys ? fill : keys;
     return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
 }
 
