@@ -632,30 +632,68 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 3) prompt_mfma(PromptArgs 
     }
 }
 
-// Joins the splits of every row: o = sum_s 2^(e_s - M) o_s / sum_s 2^(e_s - M).
-// One wave per (position, head); rows outside the sequences stay as they are.
-template <typename T>
+// Joins the splits of every row: o = sum_s 2^(e_s - M) o_s / sum_s 2^(e_s - M),
+// M the largest e.  A thread has V columns of a row and takes four splits at a
+// time, their loads in flight together, with a running maximum.  Rows outside
+// the sequences stay as they are.
+template <typename T, int V>
 __global__ void __launch_bounds__(256) prompt_join(PromptArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), n = a.Tq * a.Hq;
-    if (row >= n) return;
-    const int64_t pos = row / a.Hq;
+    const uint32_t per = (uint32_t)a.d / V, n = (uint32_t)(a.Tq * a.Hq);
+    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (x >= (int64_t)n * per) return;
+    const uint32_t row = (uint32_t)(x / per), c = (uint32_t)(x - (int64_t)row * per) * V;
+    const int64_t pos = row / (uint32_t)a.Hq;
     if (pos < a.cu_q[0] || pos >= a.cu_q[a.B]) return;
-    float M = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) M = fmaxf(M, a.part_lse[s * n + row]);
-    const float base = M == -INFINITY ? 0.f : M;
-    float sum = 0.f;
-    for (int s = 0; s < a.splits; ++s) sum += __builtin_amdgcn_exp2f(a.part_lse[s * n + row] - base);
-    const float is = sum == 0.f ? 0.f : 1.f / sum;
-    for (int c = lane; c < a.d; c += 64) {
-        float y = 0.f;
-        for (int s = 0; s < a.splits; ++s) {
-            const float e = a.part_lse[s * n + row];
-            if (e != -INFINITY) y = fmaf(__builtin_amdgcn_exp2f(e - base) * is, a.part_o[(s * n + row) * a.d + c], y);
+    float M = PMIN, sum = 0.f, y[V] = {};
+    for (int s0 = 0; s0 < a.splits; s0 += 4) {
+        float e[4], o[4][V];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int64_t at = (int64_t)(s0 + s < a.splits ? s0 + s : s0) * n + row;
+            e[s] = a.part_lse[at];
+            const float *p = a.part_o + at * a.d + c;
+            if constexpr (V == 4) {
+                const f32x4 w = *(const f32x4 *)p;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[s][i] = w[i];
+            } else {
+                o[s][0] = *p;
+            }
         }
-        ((T *)a.o)[row * a.d + c] = narrow<T>(y);
+        float top = M;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) top = fmaxf(top, e[s]);
+        const float al = __builtin_amdgcn_exp2f(M - top);
+        M = top, sum *= al;
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] *= al;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if (s0 + s >= a.splits) break;
+            const float w = __builtin_amdgcn_exp2f(e[s] - M);
+            sum += w;
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = fmaf(w, o[s][i], y[i]);
+        }
     }
-    if (lane == 0 && a.lse) a.lse[row] = (M + (sum == 0.f ? 0.f : __builtin_amdgcn_logf(sum))) * PLN2;
+    const float is = sum == 0.f ? 0.f : 1.f / sum;
+    T *out = (T *)a.o + (int64_t)row * a.d + c;
+    if constexpr (V == 4 && sizeof(T) == 4) {
+        *(f32x4 *)out = (f32x4){y[0] * is, y[1] * is, y[2] * is, y[3] * is};
+    } else if constexpr (V == 4) {
+        *(bf16x4 *)out = (bf16x4){(__bf16)(y[0] * is), (__bf16)(y[1] * is), (__bf16)(y[2] * is), (__bf16)(y[3] * is)};
+    } else {
+        *out = narrow<T>(y[0] * is);
+    }
+    if (c == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(sum)) * PLN2;
+}
+
+template <typename T>
+void launch_join(const PromptArgs &a, hipStream_t st) {
+    const int64_t items = a.Tq * a.Hq * (a.d % 4 == 0 ? a.d / 4 : a.d);
+    const dim3 grid((unsigned)((items + 255) / 256));
+    if (a.d % 4 == 0) hipLaunchKernelGGL((prompt_join<T, 4>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((prompt_join<T, 1>), grid, dim3(256), 0, st, a);
 }
 
 // ---------------------------------------------------------------------------
@@ -723,9 +761,8 @@ hipError_t launch_prompt(const fw_packed &p, void *o, float *lse, int splits, fl
         else launch_general<uint16_t>(a, vec, grid, st);
     }
     if (splits > 1) {
-        const dim3 grid((unsigned)((p.Tq * p.Hq + 3) / 4));
-        if (p.dtype == FW_F32) hipLaunchKernelGGL(prompt_join<float>, grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL(prompt_join<uint16_t>, grid, dim3(256), 0, st, a);
+        if (p.dtype == FW_F32) launch_join<float>(a, st);
+        else launch_join<uint16_t>(a, st);
     }
     return hipGetLastError();
 }
