@@ -476,7 +476,7 @@ fw_status fw_cache_store(const fw_cache *cache, int32_t dtype, const void *k, in
  * bf16 for the product with the values.
  * Limits: S, T, Hkv, max_blocks >= 1; Hkv divides Hq; T*Hq/Hkv <= 4096;
  * S*Hkv < 2^24; S*Hkv*T*Hq < 2^31 rows; max_blocks * block_size < 2^31;
- * S*Hkv * max_blocks * block_size < 2^37.
+ * S*Hkv * max_blocks * block_size < 2^36.
  * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_DTYPE, FW_E_WORKSPACE, FW_E_HIP.
  * ------------------------------------------------------------------------- */
 size_t fw_cache_attention_workspace_size(const fw_cache *cache, int64_t S, int64_t T, int64_t Hq, int64_t Hkv,

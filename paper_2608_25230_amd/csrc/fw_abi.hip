@@ -518,8 +518,8 @@ fw_status check_decode(int32_t block_size, int64_t S, int64_t T, int64_t Hq, int
     if (T > 4096 || Hq / Hkv > 4096 || T * (Hq / Hkv) > 4096) return fail(FW_E_SHAPE, "T*Hq/Hkv must be <= 4096");
     if (S * Hkv * (T * (Hq / Hkv)) >= m31) return fail(FW_E_SHAPE, "S*T*Hq must be < 2^31");
     if (max_blocks >= m31 / block_size) return fail(FW_E_SHAPE, "max_blocks * block_size must be < 2^31");
-    if ((double)(S * Hkv) * (double)(max_blocks * block_size) >= 137438953472.0)
-        return fail(FW_E_SHAPE, "S*Hkv * max_blocks * block_size must be < 2^37");
+    if ((double)(S * Hkv) * (double)(max_blocks * block_size) >= 68719476736.0)
+        return fail(FW_E_SHAPE, "S*Hkv * max_blocks * block_size must be < 2^36");
     return FW_OK;
 }
 

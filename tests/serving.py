@@ -14,14 +14,19 @@ def tolerances(ref, dtype, d, n):
     the exponential), with |z| <= the same sum.  Weights are then off by a
     factor of 1 +- dp, dp = 2 (dz + 4 2^-24 (1 + dots)); their sums and the
     sums over values add n + 16 float32 roundings (16: rescalings, joins of
-    parts).  bf16: each weight and the result are rounded once to bf16.  The
-    last terms are float32's and bf16's least subnormals, which a product of
-    small weights and values may lose.
+    parts).  bf16: each weight and the result are rounded once to bf16.
+
+    The last term is what underflow can lose.  A weight, relative to a maximum
+    that is at most the row's largest logit, so that the weights' sum is at
+    least 1, is flushed to zero below float32's and bf16's least normal value
+    2^-126; in the cache this goes for the weight times its block's value
+    scale.  What multiplies it is a value (below 2^9 in these tests) or a code
+    (at most 448 < 2^9), so each of n keys loses at most 2^-126 2^9.
     """
     u = 2.0 ** -24
     dp = 2 * ((d + 4) * u * ref["dots"] + 4 * u * (1 + ref["dots"]))
     rel = dp + (n + 16) * u + (HALF["bf16"] if dtype == "bf16" else 0.0)
-    tol_o = rel[..., None] * ref["abs_o"] * (1 + 2.0 ** -7) + HALF[dtype] * np.abs(ref["o"]) * (1 + 2.0 ** -7) + 2.0 ** -120
+    tol_o = rel[..., None] * ref["abs_o"] * (1 + 2.0 ** -7) + HALF[dtype] * np.abs(ref["o"]) * (1 + 2.0 ** -7) + n * 2.0 ** -117
     lse = np.where(np.isfinite(ref["lse"]), ref["lse"], 0)
     tol_lse = dp + (n + 16) * u + 4 * u * np.abs(lse)
     return tol_o, tol_lse

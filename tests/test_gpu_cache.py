@@ -388,6 +388,34 @@ def test_decode_scales(tf, scale, dtype):
     _attend(tf, cache, table, q, lens, dtype, scale=scale, what=f"scale {scale} {dtype}")
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f32", 32)])
+@pytest.mark.parametrize("case", ["one long", "equal", "short and long", "all empty"])
+def test_decode_shares_of_the_tiles(tf, dtype, d, case):
+    """Workgroups that begin and end inside cells, at their edges, behind their tiles; cells in one part and in many."""
+    rng = np.random.default_rng(7)
+    S, Hkv = 40, 2
+    lens = {"one long": [1] * 79 + [6000], "equal": [512] * 80, "short and long": [int(x) for x in rng.choice([0, 5, 64, 700, 2500], 80)],
+            "all empty": [0] * 80}[case]
+    print(f"shares {case} {dtype}", flush=True)
+    extra = max(0, 2100 // 16 - max(lens) // 16)       # the table's row is long even where no cell is
+    for T in (1, 3):
+        cache, table, q = _setup(tf, 30 + T, S, T, Hkv, 2, d, 16, lens, dtype, extra=extra)
+        out = _attend(tf, cache, table, q, lens, dtype, what=f"shares {case} {dtype} T={T}")
+        assert out["_ws"] is not None
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_rising_logits(tf, dtype):
+    """Scales at which the logits of later blocks exceed the first maximum by far."""
+    torch, fw = tf
+    lens = [700, 90]
+    cache, table, q = _setup(tf, 31, 1, 1, 2, 4, 64, 16, lens, dtype)
+    for c, n in enumerate(lens):
+        for j in range(-(-n // 16)):
+            cache.k_exp[int(table[c, j])] = 112 + min(j, 14)
+    _attend(tf, cache, table, q, lens, dtype, what=f"rising {dtype}")
+
+
 def test_decode_many_cells(tf):
     """More cells than threads of a workgroup."""
     rng = np.random.default_rng(0)

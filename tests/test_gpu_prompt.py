@@ -80,6 +80,58 @@ def test_lengths(tf, lq, lk, dtype, causal):
     _run(tf, 1, lq, lk, 4, 2, 128 if dtype == "bf16" else 64, dtype, causal)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f32", 32)])
+@pytest.mark.parametrize("B", [64, 65, 200])
+def test_many_sequences(tf, dtype, d, B):
+    """More sequences than a wave has lanes, empty ones among them, lengths of keys apart from those of queries."""
+    print(f"sequences {B} {dtype}", flush=True)
+    rng = np.random.default_rng(B)
+    lq = [int(x) for x in rng.integers(0, 6, B)]
+    lk = [int(x) for x in rng.integers(0, 9, B)]
+    lq[B - 1], lk[B - 1], lq[63], lk[63] = 40, 70, 33, 20
+    for causal in (True, False):
+        _run(tf, B, lq, lk, 4, 2, d, dtype, causal)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+def test_a_row_does_not_depend_on_its_neighbours(tf, dtype, d):
+    """The same bits for a sequence alone and beside others, whatever they hold."""
+    torch, fw = tf
+    dev, f64, cu, cun = _inputs(torch, 21, [90, 75, 60], [90, 75, 60], 4, 2, d, dtype)
+    a = fw.prompt_attention(*dev, *cu)
+    for x, lo, hi in ((dev[0], 0, 90), (dev[1], 165, 225), (dev[2], 0, 90), (dev[2], 165, 225)):
+        x[lo:hi] = float("nan")
+    b = fw.prompt_attention(*dev, *cu)
+    torch.cuda.synchronize()
+    assert torch.equal(a["o"][90:165], b["o"][90:165]) and torch.equal(a["lse"][90:165], b["lse"][90:165])
+    q = dev[0].clone()
+    q[100] *= 40.0          # one position's logits far above the others'
+    c = fw.prompt_attention(q, dev[1], dev[2], *cu)
+    torch.cuda.synchronize()
+    keep = [i for i in range(90, 165) if i != 100]
+    assert torch.equal(b["o"][keep], c["o"][keep]) and torch.equal(b["lse"][keep], c["lse"][keep])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("order", ["rising", "falling", "jump"])
+def test_logits_that_outgrow_the_first_maximum(tf, dtype, d, order):
+    """Keys whose logits rise along the row by far more than an exponential's range, fall, or jump once."""
+    torch, fw = tf
+    print(f"maximum {order} {dtype} {d}", flush=True)
+    n = 300
+    dev, f64, cu, cun = _inputs(torch, 22, [n], [n], 2, 1, d, dtype)
+    dt = dev[0].dtype
+    ramp = {"rising": np.linspace(-150, 150, n), "falling": np.linspace(150, -150, n),
+            "jump": np.where(np.arange(n) < 170, -40.0, 60.0)}[order]
+    q, k = torch.zeros_like(dev[0]), dev[1].clone() * 0.1
+    q[:, :, 0] = float(np.sqrt(d))
+    k[:, 0, 0] = torch.tensor(ramp).to(dt).cuda()
+    out = fw.prompt_attention(q, k, dev[2], *cu)
+    torch.cuda.synchronize()
+    ref = O.prompt_attention(q.double().cpu().numpy(), k.double().cpu().numpy(), f64[2], *cun, None, True)
+    check(out["o"].float().cpu().numpy(), out["lse"].cpu().numpy(), ref, dtype, d, n, order)
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 8), ("bf16", 16), ("bf16", 64), ("bf16", 72), ("bf16", 80), ("bf16", 96),
                                      ("bf16", 128), ("bf16", 136), ("bf16", 192), ("bf16", 256), ("bf16", 1), ("bf16", 33),
                                      ("bf16", 100), ("f32", 1), ("f32", 7), ("f32", 32), ("f32", 80), ("f32", 128),
