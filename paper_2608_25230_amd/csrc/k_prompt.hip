@@ -364,7 +364,8 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 3) prompt_mfma(PromptArgs 
     constexpr int RB = 2 * D;               // bytes of an LDS row
     constexpr int TB = PK * RB;             // bytes of a tile
     constexpr int RPI = 1024 / RB;          // rows of one 64-lane load
-    constexpr int NI = PK / RPI / PW;       // loads per wave and tile
+    constexpr int TL = PK / RPI;            // loads of a tile
+    constexpr int NI = (TL + PW - 1) / PW;  // of them per wave, at most
     constexpr int KS = D / 16, DB = D / 32;
     extern __shared__ __align__(1024) unsigned char psm[];
     int *bad_tile = (int *)(psm + 4 * TB);  // 1 + the last tile of each slot that holds a non-finite value
@@ -416,27 +417,24 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 3) prompt_mfma(PromptArgs 
     const uint32_t krb = (uint32_t)(a.k_row * 2), vrb = (uint32_t)(a.v_row * 2);
     const char *kb_ = (const char *)a.k + (t.k0 * a.k_row + h * a.k_head) * 2;
     const char *vb_ = (const char *)a.v + (t.k0 * a.v_row + h * a.v_head) * 2;
-    uint32_t kvo, kvo1, vvo;
-    {
-        // columns past d: out of range, zeros
-        const int lr = RPI * w + lane / (D / 8), p = lane % (D / 8);
-        const int kc = p ^ k_swizzle<D>(lr), kc1 = D == 256 ? p ^ k_swizzle<D>(lr + RPI * PW) : kc, vc = p ^ v_swizzle<D>(lr);
-        kvo = 8 * kc < a.d ? (uint32_t)lr * krb + 16 * kc : 0x80000000u;
-        kvo1 = 8 * kc1 < a.d ? (uint32_t)lr * krb + 16 * kc1 : 0x80000000u;  // every other load; the same for D < 256
-        vvo = 8 * vc < a.d ? (uint32_t)lr * vrb + 16 * vc : 0x80000000u;
-    }
+    // load i: rows RPI i ..; columns past d are out of range and read zeros
+    const auto offset = [&](int i, uint32_t rb, bool keys) -> uint32_t {
+        const int lr = RPI * i + lane / (D / 8), c = lane % (D / 8) ^ (keys ? k_swizzle<D>(lr) : v_swizzle<D>(lr));
+        return 8 * c < a.d ? (uint32_t)lr * rb + 16 * c : 0x80000000u;
+    };
     const auto issue = [&](int j) {
         const int64_t key0 = (int64_t)j * PK;
-        unsigned char *slot = psm + ((j - j0) & 1) * 2 * TB + w * 1024;
+        unsigned char *slot = psm + ((j - j0) & 1) * 2 * TB;
         const rsrc_t kr = rows_rsrc(kb_ + key0 * krb, t.Lk - key0, krb, a.d);
         const rsrc_t vr = rows_rsrc(vb_ + key0 * vrb, t.Lk - key0, vrb, a.d);
 #pragma unroll
-        for (int x = 0; x < NI; ++x)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, P_LDS(slot + x * PW * 1024), 16, (D == 256 && x % 2 ? kvo1 : kvo) + x * (RPI * PW) * krb, 0, 0, 0);
-#pragma unroll
-        for (int x = 0; x < NI; ++x)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, P_LDS(slot + TB + x * PW * 1024), 16, vvo + x * (RPI * PW) * vrb, 0,
-                                                     0, 0);
+        for (int x = 0; x < NI; ++x) {
+            const int i = w + x * PW;
+            if (TL % PW && i >= TL) break;
+            const uint32_t ko = offset(i, krb, true), vo = offset(i, vrb, false);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, P_LDS(slot + i * 1024), 16, ko, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, P_LDS(slot + TB + i * 1024), 16, vo, 0, 0, 0);
+        }
     };
     // LDS reads: key rl, chunk 2 s + hh; value key 4 hh + (lane % 16) / 4, columns 16 ((lane / 16) % 2) + 4 (lane % 4)
     const uint32_t base = (uint32_t)(uintptr_t)P_LDS(psm);
@@ -576,6 +574,7 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 3) prompt_mfma(PromptArgs 
             uint32_t e = 0;
 #pragma unroll
             for (int x = 0; x < NI; ++x) {
+                if (TL % PW && w + x * PW >= TL) break;
                 const uint4 y = *(const uint4 *)(psm + at + TB + (x * PW + w) * 1024 + lane * 16);
                 e |= ((y.x & 0x7F807F80u) + 0x00800080u) | ((y.y & 0x7F807F80u) + 0x00800080u) |
                      ((y.z & 0x7F807F80u) + 0x00800080u) | ((y.w & 0x7F807F80u) + 0x00800080u);
