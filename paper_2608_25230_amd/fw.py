@@ -474,11 +474,11 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=Non
     p = Packed(code, q.data_ptr(), k.data_ptr(), v.data_ptr(), Tq, Tk, cu_q.shape[0] - 1, Hq, Hkv, d, q_row, q_head,
                k_row, k_head, v_row, v_head, cu_q.data_ptr(), cu_k.data_ptr(), _ptr(scale), 1 if causal else 0)
     L, ref = lib(), ctypes.byref(p)
-    o = q.new_empty((Tq, Hq, d))
+    o = torch.empty_like(q) if q.is_contiguous() else q.new_empty((Tq, Hq, d))
     lse = q.new_empty((Tq, Hq), dtype=torch.float32) if want_lse else None
     need = L.fw_prompt_attention_workspace_size(ref)
     if need and (ws is None or ws.numel() < need):
-        ws = _workspace(need, dev)
+        ws = q.new_empty(need, dtype=torch.uint8)
     _check(L.fw_prompt_attention(ref, o.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(),
                                  _stream_of(q.get_device())))
     return {"o": o, "lse": lse, "_ws": ws}
@@ -512,11 +512,11 @@ def block_tables(old_len, new_len, table, free_list, n_free, block_size: int, *,
     slots = table.new_empty(n_slots, dtype=torch.int64)
     offsets = table.new_empty(C + 1, dtype=torch.int64)
     if lens is None:
-        lens = table.new_empty(C)
-    refused = table.new_empty(1)
+        lens = torch.empty_like(old_len)
+    refused = torch.empty_like(n_free)
     need = L.fw_block_tables_workspace_size(C)
     if ws is None or ws.numel() < need:
-        ws = _workspace(need, dev)
+        ws = table.new_empty(need, dtype=torch.uint8)
     _check(L.fw_block_tables(C, old_len.data_ptr(), new_len.data_ptr(), block_size, W, table.data_ptr(),
                              free_list.shape[0], free_list.data_ptr(), n_free.data_ptr(), n_slots, slots.data_ptr(),
                              offsets.data_ptr(), lens.data_ptr(), refused.data_ptr(), ws.data_ptr(), ws.numel(),
@@ -586,11 +586,11 @@ def cache_attention(q, cache: KvCache, table, lens, *, scale=None, want_lse=True
     c = _cache(cache, dev)
     L, ref = lib(), ctypes.byref(c)
     q_seq, q_tok, q_head, _ = q.stride()
-    o = q.new_empty((S, T, Hq, d))
+    o = torch.empty_like(q) if q.is_contiguous() else q.new_empty((S, T, Hq, d))
     lse = q.new_empty((S, T, Hq), dtype=torch.float32) if want_lse else None
     need = L.fw_cache_attention_workspace_size(ref, S, T, Hq, Hkv, W)
     if need and (ws is None or ws.numel() < need):
-        ws = _workspace(need, dev)
+        ws = q.new_empty(need, dtype=torch.uint8)
     _check(L.fw_cache_attention(ref, code, q.data_ptr(), S, T, Hq, Hkv, q_seq, q_tok, q_head, table.data_ptr(), W,
                                 lens.data_ptr(), _ptr(scale), o.data_ptr(), _ptr(lse), _ptr(ws),
                                 0 if ws is None else ws.numel(), _stream_of(q.get_device())))
