@@ -24,6 +24,17 @@
 // them, every workgroup takes the same number of them and finds from the
 // lengths where it begins.  A cell that one workgroup has whole is done with
 // it; the others' parts go to the workspace, joined by decode_join.
+//
+// Bound by HBM where there is much to read: 64 cells of 131,000 tokens, d =
+// 128 (2.15 GB) in 367 us with the join, 5.9 TB/s; 512 cells of 800 to 10,000
+// tokens (237 MB) 44 us and 5 for the join, 58 where the cache was not read
+// just before.  8 cells of 200 to 800 tokens: 10 us, the launch and a chain of
+// dependent loads (lengths, page numbers, codes).  60 cells of up to 6000
+// tokens, four float32 positions: 14 us and 5.5 for the join.
+// What the constants below measured, whole calls.  kWhole 8: the third case 18
+// us instead of 14; 128: the fourth 34 instead of 19.  kMinTiles 16: the
+// fourth 24 instead of 19; 4: the same.  kCell 0: the fourth 32 instead of 19,
+// the second 50.3 instead of 48.5; 8: the same.
 #include <algorithm>
 
 #include "fw_internal.hpp"
@@ -38,7 +49,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int DW = 4;               // waves per workgroup; 8 where one takes a whole cell (kWhole)
 constexpr int DT = 64;              // tokens per wave and step
-constexpr int kGroups = 512;        // workgroups that share the tiles: two to a compute unit
+constexpr int kGroups = 256;        // workgroups that share the tiles, one to a compute unit; twice that for many or narrow cells
+constexpr int kMany = 256;          // cells up to which one to a compute unit is right; kManyNarrow for narrow ones
+constexpr int kManyNarrow = 8;
 constexpr int kMinTiles = 8;        // tiles of a workgroup at least
 constexpr int kCell = 4;            // what a cell costs besides its tiles, in tiles
 constexpr int kWhole = 32;          // tiles of a table row up to which a workgroup takes one cell whole
@@ -579,14 +592,23 @@ void launch_join(const DecodeArgs &a, dim3 grid, hipStream_t st) {
 
 // Workgroups that share the tiles, at most so many as all tables could hold work for (the lengths are on the
 // device); 0 where the tables are so short that each cell has a workgroup of its own.
-int64_t share_groups(int64_t C, int64_t W, int block_size) {
+//
+// One to a compute unit (four waves, a tile ahead) reads as fast as two where a tile is 128 columns wide or more, or
+// meets more than 16 rows, and leaves half the parts to join; narrower tiles need two, except that with few cells the
+// join counts for more.  256 against 512 workgroups, in us; d = 128: 8 cells of 131,000 tokens 58 / 69, 64 of 131,000
+// 367 / 396, 256 of 800 to 10,000 33.3 / 33.0, 512 of those 51.3 / 48.5 (768 workgroups 56, 1536 57).  d = 64: 8 cells
+// of 65,000 31 / 35, 16 of 130,000 64 / 53, 64 of 32,000 63 / 48.
+int64_t share_groups(int64_t C, int64_t R, int64_t d, int64_t W, int block_size) {
     const int64_t tiles = (W * block_size + DT - 1) / DT;
-    return tiles <= kWhole ? 0 : std::min<int64_t>(kGroups, (C * (tiles + kCell) + kMinTiles - 1) / kMinTiles);
+    if (tiles <= kWhole) return 0;
+    const bool narrow = cache_row(d) < 128 && R <= 16;
+    const int64_t groups = C > (narrow ? kManyNarrow : kMany) ? 2 * kGroups : kGroups;
+    return std::min<int64_t>(groups, (C * (tiles + kCell) + kMinTiles - 1) / kMinTiles);
 }
 }  // namespace
 
 size_t decode_ws_bytes(int64_t C, int64_t R, int64_t d, int64_t W, int block_size) {
-    const int64_t groups = share_groups(C, W, block_size), parts = groups + C;  // a part ends with its workgroup or its cell
+    const int64_t groups = share_groups(C, R, d, W, block_size), parts = groups + C;  // a part ends with its workgroup or its cell
     return groups ? align_up(C * sizeof(int2), 256) + align_up(parts * R * d * 4, 256) + align_up(parts * R * 4, 256) : 0;
 }
 
@@ -602,7 +624,7 @@ hipError_t launch_decode(const fw_cache &cache, int dtype, const void *q, int64_
     a.table = table, a.lens = lens, a.scale = scale, a.o = o, a.lse = lse;
     const int size = dtype == FW_F32 ? 4 : 2;
     a.wide = a.d % 8 == 0 && (uintptr_t)q % 16 == 0 && q_seq * size % 16 == 0 && q_tok * size % 16 == 0 && q_head * size % 16 == 0;
-    a.groups = (int)share_groups(a.C, W, cache.block_size);
+    a.groups = (int)share_groups(a.C, a.R, a.d, W, cache.block_size);
     if (a.groups) {
         const int64_t parts = (int64_t)a.groups + a.C;
         char *p = (char *)ws;
