@@ -14,6 +14,11 @@
 //
 // Two kernels share this file: `prompt_mfma` (bf16 rows of 16-byte aligned
 // strides) and `prompt_general` (any type, width and stride; float32 MFMA).
+// Measured on one MI355X: 16,384 tokens, 32 query and 8 key/value heads, d =
+// 128: 1.88 to 2.0 ms, 1100 to 1170 TFLOP/s of the visible pairs; 16 packed
+// sequences of 66 to 4096 (some with 1777 earlier keys) 523 to 538 us, 980 to
+// 1000 TFLOP/s; five float32 sequences of up to 1999, d = 80: 104 us, 74
+// TFLOP/s.  A large library product reaches 1573 (bf16) and 153 (float32).
 #include <type_traits>
 
 #include "fw_internal.hpp"
@@ -112,6 +117,10 @@ template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float x) {
 //   so one 16-byte LDS read feeds four steps.
 //   O^T += V^T P^T: step i takes keys 4 (l / 16) + i, which is where the
 //   weights already are: they never leave their lane.
+// Bound by the float32 MFMA, at 57 % of its cycles while a compute unit has
+// work: chains of dependent products and LDS reads between them take the rest.
+// 104 us at this tile; 64-key tiles 105 without loads that run ahead and 135
+// with them (registers spill), 32-key tiles without them 109.
 // ---------------------------------------------------------------------------
 constexpr int GK = 32;    // keys per tile
 constexpr int GR = 64;    // rows per workgroup
@@ -310,24 +319,37 @@ __global__ void __launch_bounds__(GTH, NT <= 5 ? 3 : 1) prompt_general(PromptArg
 
 // ---------------------------------------------------------------------------
 // bf16 kernel on the bf16 MFMA (d a multiple of 8 up to D, 16-byte aligned
-// rows).  Four waves of 32 rows; key and value tiles of 64 rows in a ring of
+// rows).  Four waves of 32 rows; key and value tiles of 32 rows in a ring of
 // two LDS slots, filled by direct-to-LDS loads one tile ahead.
-//   S^T = K Q^T on v_mfma_f32_32x32x16_bf16: lane l holds row l % 32 and, of
-//   each 32-key half, keys 8 (i / 4) + 4 (l / 32) + i % 4, i < 16, so a row's
-//   maximum is taken in the lane and with one exchange of the wave's halves.
+//   S^T = K Q^T on v_mfma_f32_32x32x16_bf16: lane l holds row l % 32 and keys
+//   8 (i / 4) + 4 (l / 32) + i % 4, i < 16.
 //   O^T += V^T P^T: since the order of a contraction is free, step kb takes
 //   keys 16 kb + 4 (l / 32) + {0..3, 8..11}: the eight weights that the lane
 //   already holds, rounded to bf16 in place.  V is read transposed
 //   (ds_read_b64_tr_b16), four keys of one column per lane.
-// The weights are rounded to bf16 for the product (relative error up to
-// 2^-8 each, averaged over the row); their sum is taken in float32 before
-// the rounding.  The maximum that the exponentials are taken from may lag
-// the true one by up to 2^8 (RESCALE): the accumulators are rescaled only
-// when some row's maximum grew by more, and the weights keep bf16's relative
-// precision at any scale.
+// The weights are rounded to bf16 for the product (relative error up to 2^-8
+// each); their sum is taken in float32 before the rounding, so that lse keeps
+// float32's precision.
+// No maximum is taken of a tile.  The exponentials are taken from the maximum
+// m so far, and only a row whose weights over the tile sum to more than GROWN
+// (or to no number) takes a new one, rescales and computes the tile's weights
+// again: the first tile of every row, and few after it.  bf16 keeps its
+// relative precision at any such scale.
 // 16-byte chunk c of row r lies at chunk c ^ k_swizzle(r) or c ^ v_swizzle(r)
 // of its LDS row, so that the 16 rows of one chunk that half a wave reads of the keys,
-// and the 4 rows of 4 chunks that it reads of the values, fill all 64 banks once.
+// and the 4 rows of 4 chunks that it reads of the values, fill all 64 banks once
+// (no bank conflicts counted).
+//
+// What bounds it: power, as it seems.  The MFMA is busy 68 % of the cycles, and
+// the clock falls as that share rises (1.84 GHz at 54 %, 1.53 at 68 %, same
+// card), so what helped were fewer instructions per key: 32 rows a wave need 24 LDS
+// reads, 16 exponentials, 16 fused multiply-adds, 16 additions and 8
+// conversions for 16 products, with three workgroups of 168 registers to a
+// compute unit.  On 16,384 tokens: 64-key tiles at two workgroups 2.00 to 2.07
+// ms; scores, weights and values of three tiles interleaved in one wave 2.1;
+// 64 rows a wave 2.5; 8 or 12 waves a workgroup 2.0 and 1.9; this 1.88.  Tiles
+// in the order of their keys over all sequences were slower than sequence by
+// sequence (16 packed sequences: 555 against 536 us).
 // ---------------------------------------------------------------------------
 constexpr int PW = 4;            // waves per workgroup
 constexpr int PTH = 64 * PW;
@@ -723,15 +745,28 @@ void launch_general(const PromptArgs &a, int vec, dim3 grid, hipStream_t st) {
 }
 }  // namespace
 
-// Ranges that a row's keys are split into: one when the row tiles fill the
-// card (three workgroups to a compute unit), otherwise as many as fill it,
-// with at least 256 keys to each of a sequence halfway between the average
-// one and one that has all the keys (the lengths are on the device).
+// Ranges that a row's keys are split into: at most as many as fill the card
+// (three workgroups to a compute unit), and of those the cheapest by the time
+// of one range, and, if there is more than one, of writing and joining the
+// rows' parts.  In keys of a workgroup's time (0.0215 us in the bf16 kernel,
+// 0.08 in the other): a part 1 / 96 or 1 / 384, the join's launch 160 or 40.
+// Taken for a sequence halfway between the average one and one that has all
+// the keys, since the lengths are on the device.  One sequence, split so
+// against whole, in us: bf16, d = 128, 1000 tokens, 4 heads 18.6 / 27.4, 8
+// heads 21.2 / 27.6, 32 heads whole 29.4 (in two 38.1); 4096 tokens, 4 heads
+// 50 / 91, 8 heads 72 / 94; float32, d = 80, 6 heads, 500 tokens 24 / 45, 2000
+// 76 / 157; d = 128, 32 heads, 500 tokens 70 / 65, 1000 137 / 146.
 int prompt_splits(const fw_packed &p) {
-    const int64_t tiles = row_tiles(p, prompt_fast(p) ? PR : GR) * p.Hkv;
-    const int64_t fill = (768 + tiles / 2) / (tiles > 0 ? tiles : 1), keys = (p.Tk / (p.B > 0 ? p.B : 1) + p.Tk) / 512;
-    const int64_t s = fill < keys ? fill : keys;
-    return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
+    const bool fast = prompt_fast(p);
+    const int64_t tiles = row_tiles(p, fast ? PR : GR) * p.Hkv, rows = p.Tq * p.Hq;
+    const int64_t fill = std::min<int64_t>((768 + tiles / 2) / (tiles > 0 ? tiles : 1), 16);
+    const int64_t keys = (p.Tk / (p.B > 0 ? p.B : 1) + p.Tk) / 2;
+    int64_t best = 1, least = keys;
+    for (int64_t s = 2; s <= fill; ++s) {
+        const int64_t cost = keys / s + rows * s / (fast ? 96 : 384) + (fast ? 160 : 40);
+        if (cost < least) best = s, least = cost;
+    }
+    return (int)best;
 }
 
 hipError_t launch_prompt(const fw_packed &p, void *o, float *lse, int splits, float *part_o, float *part_lse,
