@@ -412,8 +412,8 @@ fw_status fw_prompt_attention(const fw_packed *packed, void *o, float *lse, void
  *   lens      [C] int32 lengths after the call; may be old_len (required)
  *   refused   [1] int32 cells that were refused (required).  A cell is refused
  *             as a whole, and keeps its length and blocks, if new_len exceeds
- *             max_blocks * block_size, or if its need and that of the cells
- *             before it exceed the free blocks.
+ *             max_blocks * block_size, or if it needs blocks and its need and
+ *             that of the cells before it exceed the free blocks.
  * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_WORKSPACE, FW_E_HIP.
  * ------------------------------------------------------------------------- */
 size_t fw_block_tables_workspace_size(int64_t C);

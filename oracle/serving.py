@@ -85,7 +85,7 @@ def block_tables(old, new, table, free_list, n_free: int, block_size: int, n_slo
         fits = nb(new[c]) <= W
         need = max(0, nb(new[c]) - nb(old[c])) if fits else 0
         asked += need
-        ok = fits and asked <= top
+        ok = fits and (need == 0 or asked <= top)
         if ok:
             for j in range(need):
                 table[c, nb(old[c]) + j] = stack[top - taken - 1]

@@ -22,7 +22,8 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // every place: the r-th block given back goes to stack position
 // n_free + R - 1 - r, the k-th block needed comes from top - 1 - k (top =
 // n_free + R), so a return right after a growth restores the stack.  A cell
-// is served if its running sum of needs stays within top.
+// that needs blocks is served if its running sum of needs stays within top,
+// one that needs none always.
 //
 // tables_scan, one workgroup, takes the sums (each thread a run of cells) and
 // writes lengths, offsets and sums; tables_move, over the whole card, moves
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(TT) tables_scan(TableArgs a) {
     }
     for (int64_t c = c0; c < c1; ++c) {
         const CellPlan p = plan_cell(a, c);
-        const bool served = p.fits && at[1] + p.need <= hd.top;
+        const bool served = p.fits && (p.need == 0 || at[1] + p.need <= hd.top);
         const TableCell t = {p.o, (int32_t)p.had, (int32_t)p.want, served};
         a.offsets[c] = at[2];
         a.lens[c] = served ? p.n : p.o;  // may be old_len: this thread alone reads and writes the cell
@@ -213,7 +214,7 @@ __global__ void __launch_bounds__(TT) tables_scan(TableArgs a) {
         } else {
             a.cells[c] = t, a.back_off[c] = at[0], a.need_off[c] = at[1];
         }
-        if (served) take = at[1] + p.need;
+        if (served && p.need > 0) take = at[1] + p.need;
         refused += !served;
         at[0] += p.back, at[1] += p.need, at[2] += p.add;
     }

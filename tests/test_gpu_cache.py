@@ -107,6 +107,25 @@ def test_tables_refuse_whole_cells(tf, C, spare):
     _check_tables(tf, old, new, table, free, n_free, bs, n)
 
 
+@pytest.mark.parametrize("C,W,few", [(6, 6, True), (1500, 6, True), (6, 40, False), (300, 40, False), (4000, 6, True),
+                                     (4000, 6, False), (2500, 30, False)])
+def test_tables_serve_cells_without_need_after_the_stack_ran_out(tf, C, W, few):
+    """Every third cell grows until there are no blocks; the others shrink or stay within their last block."""
+    rng = np.random.default_rng(C + W)
+    bs = 16
+    old = rng.integers(bs + 1, W * bs + 1, C)
+    most = 3 * bs if few else W * bs
+    new = np.where(np.arange(C) % 3 == 0, np.minimum(old + rng.integers(bs, most + 1, C), W * bs), old)
+    new = np.where(np.arange(C) % 3 == 1, np.maximum(old - rng.integers(0, 2 * bs, C), 0), new)
+    new = np.where(np.arange(C) % 3 == 2, -(-old // bs) * bs, new)
+    table, free, n_free = _tables(rng, old, W, bs, int(np.sum(-(-old // bs))))
+    n = int(np.maximum(new - old, 0).sum())
+    _, _, nf, out = _check_tables(tf, old, new, table, free, n_free, bs, n)
+    lens = out["lens"].cpu().numpy()
+    assert np.array_equal(lens[1::3], new[1::3]) and np.array_equal(lens[2::3], new[2::3]) and int(nf) >= 0
+    _check_tables(tf, old, new, table, free, n_free, bs, 0, alias=True)
+
+
 def test_tables_write_no_slot_past_the_last_token(tf):
     torch, fw = tf
     L = fw.lib()

@@ -73,6 +73,30 @@ def test_block_tables_by_hand():
     assert r["slots"][20:119] == [-1] * 99 and r["slots"][119:] == [None] * 81
 
 
+def test_block_tables_refuse_only_cells_that_need_blocks():
+    """After the stack has run out, a cell that shrinks, stays, or grows within its last block is served."""
+    t = np.full((5, 4), -1)
+    t[0, 0], t[1, :3], t[2, 0], t[3, :2], t[4, 0] = 0, [1, 2, 3], 4, [5, 6], 7
+    f = np.array([8, 9] + [-7] * 8)
+    # 2 free and 2 given back; cell 0 wants 3 more, cell 2 another 3 (refused), cell 4 the block that is left (refused)
+    r = O.block_tables([16, 40, 10, 20, 16], [64, 5, 64, 25, 17], t, f, 2, 16, 200)
+    assert r["lens"].tolist() == [64, 5, 10, 25, 16] and r["refused"] == 2
+    assert r["table"].tolist() == [[0, 2, 3, 9], [1, -1, -1, -1], [4, -1, -1, -1], [5, 6, -1, -1], [7, -1, -1, -1]]
+    assert r["n_free"] == 1 and r["free_list"][0] == 8
+    assert r["offsets"].tolist() == [0, 48, 48, 102, 107, 108]
+    assert r["slots"][48:102] == [-1] * 54 and r["slots"][102:107] == [6 * 16 + i for i in range(4, 9)]
+    assert r["slots"][107] == -1
+    # shrinking behind the refused cell: what it gives back leaves its table and its length together
+    t[3, 2:] = [10, 11]
+    r = O.block_tables([16, 5, 10, 60], [16, 5, 99, 20], t[:4], np.array([8] + [-7] * 11), 1, 16, 0)
+    assert r["refused"] == 1 and r["lens"].tolist() == [16, 5, 10, 20] and r["table"][3].tolist() == [5, 6, -1, -1]
+    assert r["n_free"] == 3 and r["free_list"][:3].tolist() == [8, 11, 10]
+    t[3, 2:] = [10, 11]
+    r = O.block_tables([16, 5, 10, 60], [64, 5, 64, 20], t[:4], np.array([8] + [-7] * 11), 1, 16, 0)
+    assert r["refused"] == 1 and r["lens"].tolist() == [64, 5, 10, 20] and r["n_free"] == 0
+    assert r["table"].tolist() == [[0, 10, 11, 8], [1, 2, 3, -1], [4, -1, -1, -1], [5, 6, -1, -1]]
+
+
 def test_block_tables_return_restores_the_stack():
     rng = np.random.default_rng(2)
     old, new = rng.integers(0, 50, 9), rng.integers(50, 150, 9)
