@@ -356,7 +356,8 @@ fw_status fw_maxpool_scores(const float *scores, int64_t H, int64_t n, int32_t k
  *   causal non-zero: query i of Lq sees keys 0 .. i + Lk - Lq (the last query
  *          sees every key); zero: every key of its sequence
  * Limits: B, Hkv, d >= 1, Tq, Tk >= 0; Hkv divides Hq; d <= 256;
- * Tq*Hq < 2^31; Tk <= 2^30; strides >= 0 and below 2^31. */
+ * Tq*Hq < 2^31; (Tq*Hq/Hkv/64 + 1 + B)*Hkv < 2^24; Tk <= 2^30; strides >= 0
+ * and below 2^31. */
 typedef struct fw_packed {
     int32_t dtype;
     const void *q, *k, *v;
@@ -440,7 +441,7 @@ int32_t fw_cache_row(int64_t d);
 /* ---------------------------------------------------------------------------
  * fw_cache_store -- rounds rows of keys and values to the cache's blocks
  * (fw_ragged_compact's k_out and v_out, or one decoding step's rows).
- *   dtype, k, v  [N][d] rows, strides k_row and v_row in elements
+ *   dtype, k, v  [N][d] rows, N < 2^28, strides k_row and v_row in elements
  *   slots        [N] int64, of fw_block_tables; rows whose slot is not in
  *                [0, n_blocks * block_size) are skipped
  * The rows that go to one block are consecutive rows with consecutive slots.
@@ -475,7 +476,7 @@ fw_status fw_cache_store(const fw_cache *cache, int32_t dtype, const void *k, in
  * queries are computed in float32; bf16 queries round the softmax weights to
  * bf16 for the product with the values.
  * Limits: S, T, Hkv, max_blocks >= 1; Hkv divides Hq; T*Hq/Hkv <= 4096;
- * S*Hkv < 2^24; S*Hkv*T*Hq < 2^31 rows; max_blocks * block_size < 2^31;
+ * S*Hkv < 2^22; S*T*Hq < 2^26; max_blocks * block_size < 2^31;
  * S*Hkv * max_blocks * block_size < 2^36.
  * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_DTYPE, FW_E_WORKSPACE, FW_E_HIP.
  * ------------------------------------------------------------------------- */

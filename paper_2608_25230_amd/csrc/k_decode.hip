@@ -122,7 +122,7 @@ __device__ __forceinline__ bool find_share(const DecodeArgs &a, Share *s) {
     int first = sum_before(mine, red, &all);
     s->per = (all + a.groups - 1) / a.groups;
     if (s->per < kMinTiles) s->per = kMinTiles;
-    s->g0 = blockIdx.x * s->per;   // below 2^31: under 2^30 tiles, kCell more for 2^24 cells at most
+    s->g0 = blockIdx.x * s->per;   // below 2^31: under 2^30 tiles, kCell more for 2^22 cells at most
     if (s->g0 >= all) return false;
     s->g1 = s->g0 + s->per < all ? s->g0 + s->per : all;
     if (s->g0 >= first && s->g0 < first + mine) {

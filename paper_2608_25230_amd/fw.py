@@ -477,6 +477,8 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=Non
     o = torch.empty_like(q) if q.is_contiguous() else q.new_empty((Tq, Hq, d))
     lse = q.new_empty((Tq, Hq), dtype=torch.float32) if want_lse else None
     need = L.fw_prompt_attention_workspace_size(ref)
+    if ws is not None:
+        _want("ws", ws, torch.uint8, 1, dev)
     if need and (ws is None or ws.numel() < need):
         ws = q.new_empty(need, dtype=torch.uint8)
     _check(L.fw_prompt_attention(ref, o.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(),
@@ -515,6 +517,8 @@ def block_tables(old_len, new_len, table, free_list, n_free, block_size: int, *,
         lens = torch.empty_like(old_len)
     refused = torch.empty_like(n_free)
     need = L.fw_block_tables_workspace_size(C)
+    if ws is not None:
+        _want("ws", ws, torch.uint8, 1, dev)
     if ws is None or ws.numel() < need:
         ws = table.new_empty(need, dtype=torch.uint8)
     _check(L.fw_block_tables(C, old_len.data_ptr(), new_len.data_ptr(), block_size, W, table.data_ptr(),
@@ -589,6 +593,8 @@ def cache_attention(q, cache: KvCache, table, lens, *, scale=None, want_lse=True
     o = torch.empty_like(q) if q.is_contiguous() else q.new_empty((S, T, Hq, d))
     lse = q.new_empty((S, T, Hq), dtype=torch.float32) if want_lse else None
     need = L.fw_cache_attention_workspace_size(ref, S, T, Hq, Hkv, W)
+    if ws is not None:
+        _want("ws", ws, torch.uint8, 1, dev)
     if need and (ws is None or ws.numel() < need):
         ws = q.new_empty(need, dtype=torch.uint8)
     _check(L.fw_cache_attention(ref, code, q.data_ptr(), S, T, Hq, Hkv, q_seq, q_tok, q_head, table.data_ptr(), W,

@@ -564,7 +564,9 @@ def test_cache_refusals(tf):
              lambda: fw.block_tables(n, n, t, n, n[:1], 48, n_slots=0),
              lambda: fw.block_tables(n, n, t, n, n, 32, n_slots=0),
              lambda: fw.block_tables(n, n.long(), t, n, n[:1], 32, n_slots=0),
-             lambda: fw.block_tables(n, n, t, n, n[:1], 32, n_slots=-1)]
+             lambda: fw.block_tables(n, n, t, n, n[:1], 32, n_slots=-1),
+             lambda: fw.block_tables(n, n, t, n, n[:1], 32, n_slots=0, ws=torch.empty(1 << 20, dtype=torch.uint8)),
+             lambda: fw.cache_attention(q, cache, t, n, ws=torch.empty(1 << 20, dtype=torch.uint8))]
     for i, f in enumerate(calls):
         with pytest.raises(fw.FwError):
             f()

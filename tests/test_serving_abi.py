@@ -111,6 +111,17 @@ def test_cache_attention_validation(L):
     assert L.fw_cache_attention_workspace_size(_cache(), 0, 1, 8, 2, 100) == 0
 
 
+def test_grids_beyond_the_card_are_refused(L):
+    """A grid holds 2^32 threads; sizes past that are refused before anything is launched."""
+    for bad in (dict(B=1 << 24), dict(B=1 << 23, Hkv=2, Hq=2), dict(Tq=1 << 30, Hq=1, Hkv=1)):
+        assert L.fw_prompt_attention(_packed(**bad), 16, None, 16, 1 << 40, None) == 2, bad
+    assert L.fw_cache_store(_cache(), 1, 16, 64, 16, 64, 1 << 28, 16, None, 0, None) == 2
+    for S, T, Hq, Hkv in ((1 << 22, 1, 1, 1), (1 << 20, 1, 4, 4), (1 << 20, 16, 4, 1), (1 << 14, 4096, 1, 1)):
+        assert L.fw_cache_attention(_cache(), 1, 16, S, T, Hq, Hkv, 512, 512, 64, 16, 100, 16, None, 16, None, 16,
+                                    1 << 60, None) == 2, (S, T, Hq, Hkv)
+        assert L.fw_cache_attention_workspace_size(_cache(), S, T, Hq, Hkv, 100) == 0
+
+
 def test_host_tensors_are_refused(L):
     torch = pytest.importorskip("torch")
     z = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
