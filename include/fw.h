@@ -406,8 +406,10 @@ fw_status fw_prompt_attention(const fw_packed *packed, void *o, float *lse, void
  *   slots     [n_slots] int64: for each token that comes (cells in order,
  *             positions ascending) block * block_size + position % block_size,
  *             or -1 for a refused cell; entries past the last such token stay
- *             as they were; tokens past n_slots are not listed.  NULL if
- *             n_slots is 0.
+ *             as they were (fill them with -1 before the call where n_slots is
+ *             an upper bound and the list goes to fw_cache_store: an old entry
+ *             may be a slot of another cell); tokens past n_slots are not
+ *             listed.  NULL if n_slots is 0.
  *   offsets   [C+1] int64 exclusive prefix of the tokens that come, refused
  *             ones included (required)
  *   lens      [C] int32 lengths after the call; may be old_len (required)

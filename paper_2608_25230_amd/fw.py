@@ -489,8 +489,9 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=Non
 def block_tables(old_len, new_len, table, free_list, n_free, block_size: int, *, n_slots: int, lens=None,
                  ws=None) -> Dict[str, object]:
     """Takes every cell from old_len to new_len tokens (int32 [C]): table [C][max_blocks], free_list [n_blocks] and
-    n_free [1] (int32) change in place.  n_slots: tokens that come, of refused cells too.  Returns slots [n_slots]
-    int64, offsets [C+1] int64, lens [C] int32 (in `lens`, which may be old_len, if given) and refused [1] int32."""
+    n_free [1] (int32) change in place.  n_slots: tokens that come, of refused cells too, or an upper bound.  Returns
+    slots [n_slots] int64 (-1 for refused cells' tokens and behind the last token), offsets [C+1] int64, lens [C] int32
+    (in `lens`, which may be old_len, if given) and refused [1] int32."""
     torch = _torch()
     guard = _elsewhere("table", table)
     if guard is not None:
@@ -511,7 +512,8 @@ def block_tables(old_len, new_len, table, free_list, n_free, block_size: int, *,
     if n_slots < 0:
         raise FwError(2, "n_slots must be >= 0")
     L = lib()
-    slots = table.new_empty(n_slots, dtype=torch.int64)
+    # the kernel writes the tokens' slots alone; what lies behind them in memory may be slots of other cells
+    slots = table.new_full((n_slots,), -1, dtype=torch.int64)
     offsets = table.new_empty(C + 1, dtype=torch.int64)
     if lens is None:
         lens = torch.empty_like(old_len)

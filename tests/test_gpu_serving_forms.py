@@ -1,0 +1,70 @@
+"""Serving calls in forms that a program meets beside the plain ones."""
+import numpy as np
+import pytest
+
+from oracle import serving as O
+from tests.test_gpu_cache import _empty, _host, _i32, _tables, tf  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------
+# block tables
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("C,bs,W,grow,n_slots", [(4, 16, 8, 3, 50), (4, 16, 8, 0, 5), (2048, 64, 65, 1, 4096),
+                                                 (256, 16, 120, 90, 40000), (3000, 16, 12, 5, 30000)])
+def test_no_slot_behind_the_last_token(tf, C, bs, W, grow, n_slots):
+    """n_slots is an upper bound: entries without a token are -1, whatever the memory held before."""
+    torch, fw = tf
+    print(f"slots C={C} grow={grow} n_slots={n_slots}", flush=True)
+    old = np.full(C, 7)
+    new = old + np.where(np.arange(C) % 3 == 0, grow, 0)
+    rng = np.random.default_rng(C)
+    table, free, n_free = _tables(rng, old, W, bs, int(np.sum(-(-new // bs))) + 2)
+    old_memory = torch.full((n_slots,), 3, dtype=torch.int64, device="cuda")     # a slot that exists
+    del old_memory
+    out = fw.block_tables(_i32(torch, old), _i32(torch, new), _i32(torch, table), _i32(torch, free), _i32(torch, [n_free]),
+                          bs, n_slots=n_slots)
+    torch.cuda.synchronize()
+    ref = O.block_tables(old, new, table, free, n_free, bs, n_slots)
+    got, n = out["slots"].cpu().numpy(), int((new - old).sum())
+    assert n < n_slots and got[:n].tolist() == ref["slots"][:n]
+    assert np.all(got[n:] == -1)
+
+
+def test_captured_steps_in_which_fewer_cells_grow(tf):
+    """One captured step, with n_slots for every cell, replayed while cells stop one after the other: a replay stores
+    the tokens that come and touches no others."""
+    torch, fw = tf
+    rng = np.random.default_rng(3)
+    C, bs, W, d = 6, 16, 4, 32
+    old = np.array([15, 3, 20, 31, 1, 40])
+    table, free, n_free = _tables(rng, old, W, bs, 30)
+    cache = _empty(fw, 30, bs, d, seed=1)
+    t, f, nf = _i32(torch, table), _i32(torch, free), _i32(torch, [n_free])
+    lens, grows = _i32(torch, old), _i32(torch, np.zeros(C, int))
+    k, v = (torch.zeros(C, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    fw.cache_store(cache, k, v, torch.full((C,), -1, dtype=torch.int64, device="cuda"))    # loads the kernels
+    fw.block_tables(lens, lens, t, f, nf, bs, n_slots=C)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = fw.block_tables(lens, lens + grows, t, f, nf, bs, n_slots=C, lens=lens)
+        fw.cache_store(cache, k, v, out["slots"])
+    ref, rt, rf, rn, rl = dict(_host(cache), d=d), table, free, n_free, old
+    for step, grow in enumerate(([1] * 6, [1, 0, 1, 0, 1, 1], [0, 0, 1, 0, 0, 1], [0] * 6, [0, 1, 0, 0, 0, 0])):
+        n = sum(grow)
+        x = torch.tensor(rng.standard_normal((2, C, d)).astype(np.float32)).bfloat16()
+        k.copy_(x[0])
+        v.copy_(x[1])
+        grows.copy_(_i32(torch, grow))
+        g.replay()
+        torch.cuda.synchronize()
+        r = O.block_tables(rl, rl + np.array(grow), rt, rf, rn, bs, C)
+        rt, rf, rn, rl = r["table"], r["free_list"], r["n_free"], r["lens"]
+        ref = dict(O.cache_store(ref, x[0, :n].double().numpy(), x[1, :n].double().numpy(), r["slots"][:n]), d=d)
+        got = _host(cache)
+        assert np.array_equal(lens.cpu().numpy(), rl) and np.array_equal(t.cpu().numpy(), rt), step
+        for name in ("k", "v", "k_exp", "v_exp"):
+            assert np.array_equal(got[name], ref[name]), (step, name)
