@@ -475,8 +475,8 @@ fw_status fw_cache_store(const fw_cache *cache, int32_t dtype, const void *k, in
  *   lse          [S][T][Hq] float32, or NULL
  * A row that sees no token gives o = 0 and lse = -inf; what lies in a block
  * behind the cell's last token is not seen, whatever it holds.  float32
- * queries are computed in float32; bf16 queries round the softmax weights to
- * bf16 for the product with the values.
+ * queries are computed in float32; with bf16 queries the softmax weights enter
+ * the product with the values to 2^-16 of each.
  * Limits: S, T, Hkv, max_blocks >= 1; Hkv divides Hq; T*Hq/Hkv <= 4096;
  * S*Hkv < 2^22; S*T*Hq < 2^26; max_blocks * block_size < 2^31;
  * S*Hkv * max_blocks * block_size < 2^36.

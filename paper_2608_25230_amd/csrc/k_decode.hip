@@ -8,8 +8,13 @@
 // of token j's block.  Every code is read once for all rows of the cell and
 // is exact in bf16, so the products run on the bf16 MFMA with the codes as
 // they are: the block's key scale multiplies the logits, its value scale (a
-// power of two) the rounded weights.  Float32 queries and weights are taken
-// apart into three bf16 parts, which hold all 24 bits, one product for each.
+// power of two) the weights.  Float32 queries and weights are taken apart into
+// three bf16 parts, which hold all 24 bits, one product for each.  The weights
+// of bf16 queries take two parts: one would leave an error of 2^-8 of each
+// weight, which adds a third to the output's own rounding, two leave 2^-16.
+// The second part's products cost 4 to 5 % where a cell has few rows (64 cells
+// of 131,000 tokens: 366 to 384 us; 512 of 800 to 10,000: 58.5 to 60) and 8 to
+// 13 % at 32 or 64 rows.
 //
 // A wave takes 64 tokens at a time.  S^T = K Q^T on 16x16x32 MFMA: row
 // m = 4 g + i of key tile t is token 16 g + 4 t + i, so after four tiles lane
@@ -151,7 +156,7 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
     return (bf16x8){a[0], a[1], b[0], b[1], c[0], c[1], e[0], e[1]};
 }
 
-// x as the sum of NP bf16 values (1: rounded; 3: all bits)
+// x as the sum of NP bf16 values (1: rounded; 2: to 2^-16; 3: all bits)
 template <int NP>
 __device__ __forceinline__ void take_apart(float x, __bf16 (&y)[NP]) {
 #pragma unroll
@@ -182,7 +187,7 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t x) {
 
 template <typename T, int DP, int RT, int NW>
 __global__ void __launch_bounds__(64 * NW, RT == 1 && DP <= (sizeof(T) == 4 ? 96 : 128) ? 2 : 1) decode_part(DecodeArgs a) {
-    constexpr int NP = sizeof(T) == 4 ? 3 : 1;
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1, NV = sizeof(T) == 4 ? 3 : 2;  // bf16 parts of queries, of weights
     constexpr int KS = DP / 32, DB = DP / 16, KB = DP / 4;  // key steps, value tiles, key bytes of a lane
     constexpr int KW = KB / 4;                               // the same in words
     constexpr bool AHEAD = NP == 1 || DP < 256;              // loads run a tile ahead, where registers hold them
@@ -329,7 +334,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 && DP <= (sizeof(T) == 4 ? 96
 #pragma unroll
             for (int n = 0; n < DB; ++n) vr[n] = first_bytes(vr[n], valid);
         }
-        bf16x8 pf[RT][2][NP];
+        bf16x8 pf[RT][2][NV];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const int lim = vp < 0 ? 0 : seen[rt] - vtok;
@@ -358,10 +363,10 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 && DP <= (sizeof(T) == 4 ? 96
                 for (int i = 0; i < 4; ++i) {
                     const float e = __builtin_amdgcn_exp2f(s[rt][x][i] - m[rt]);
                     sum += e;
-                    __bf16 y[NP];
-                    take_apart<NP>(e * vf, y);
+                    __bf16 y[NV];
+                    take_apart<NV>(e * vf, y);
 #pragma unroll
-                    for (int n = 0; n < NP; ++n) pf[rt][x / 2][n][4 * (x % 2) + i] = y[n];
+                    for (int n = 0; n < NV; ++n) pf[rt][x / 2][n][4 * (x % 2) + i] = y[n];
                 }
             l[rt] += sum;
         }
@@ -404,7 +409,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 && DP <= (sizeof(T) == 4 ? 96
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int x = NP - 1; x >= 0; --x) {
+                for (int x = NV - 1; x >= 0; --x) {
                     acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[rt][0][x], acc[rt][n], 0, 0, 0);
                     acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[rt][1][x], acc[rt][n], 0, 0, 0);
                 }

@@ -3,7 +3,8 @@ import numpy as np
 import pytest
 
 from oracle import serving as O
-from tests.test_gpu_cache import _empty, _host, _i32, _tables, tf  # noqa: F401
+from tests.serving import HALF, tolerances
+from tests.test_gpu_cache import _empty, _host, _i32, _setup, _tables, tf  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -68,3 +69,29 @@ def test_captured_steps_in_which_fewer_cells_grow(tf):
         assert np.array_equal(lens.cpu().numpy(), rl) and np.array_equal(t.cpu().numpy(), rt), step
         for name in ("k", "v", "k_exp", "v_exp"):
             assert np.array_equal(got[name], ref[name]), (step, name)
+
+
+# ---------------------------------------------------------------------------
+# attention over the cache
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d,T,G,lens", [(128, 1, 4, [700, 90]), (64, 1, 4, [64, 333]), (128, 4, 8, [300, 41]),
+                                        (64, 8, 8, [500, 100]), (256, 1, 2, [200, 65]), (128, 1, 4, [9000, 17]),
+                                        (64, 5, 4, [5000, 2500])])
+def test_decode_weights_keep_their_bits(tf, d, T, G, lens):
+    """bf16 queries: the product with the values takes the softmax weights to 2^-16 of each, so that an output is off
+    by its own rounding and what float32 loses, however much its terms cancel."""
+    torch, fw = tf
+    print(f"weights d={d} T={T} G={G} {lens}", flush=True)
+    cache, table, q = _setup(tf, 40 + d + T, 1, T, 2, G, d, 64, lens, "bf16", garbage=False)
+    out = fw.cache_attention(q.cuda(), cache, _i32(torch, table), _i32(torch, lens))
+    torch.cuda.synchronize()
+    ref = O.cache_attention(q.double().numpy(), _host(cache), table, lens, None)
+    n = max(lens)
+    # tolerances() of float32 rows, but for the output's rounding, which is bf16's; then each weight is the sum of
+    # two bf16 roundings (2^-8 of what the first leaves, which is 2^-8 of the weight), either of which may underflow
+    tol, _ = tolerances(ref, "f32", d, n)
+    tol += 2.0 ** -16 * ref["abs_o"] * (1 + 2.0 ** -7) + n * 2.0 ** -117
+    tol += HALF["bf16"] * (np.abs(ref["o"]) + tol)
+    worst = np.max(np.abs(out["o"].double().cpu().numpy() - ref["o"]) / tol)
+    assert worst <= 1, worst
