@@ -476,7 +476,9 @@ fw_status fw_cache_store(const fw_cache *cache, int32_t dtype, const void *k, in
  * A row that sees no token gives o = 0 and lse = -inf; what lies in a block
  * behind the cell's last token is not seen, whatever it holds.  float32
  * queries are computed in float32; with bf16 queries the softmax weights enter
- * the product with the values to 2^-16 of each.
+ * the product with the values to 2^-16 of each.  A row's bits come from its own
+ * query, what it sees and the call's sizes and lengths (which fix how cells are
+ * cut into parts), not from other rows' queries or other cells' tokens.
  * Limits: S, T, Hkv, max_blocks >= 1; Hkv divides Hq; T*Hq/Hkv <= 4096;
  * S*Hkv < 2^22; S*T*Hq < 2^26; max_blocks * block_size < 2^31;
  * S*Hkv * max_blocks * block_size < 2^36.

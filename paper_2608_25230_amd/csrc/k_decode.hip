@@ -349,8 +349,10 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 && DP <= (sizeof(T) == 4 ? 96
                 }
             mt = fmaxf(mt, __shfl_xor(mt, 16));
             mt = fmaxf(mt, __shfl_xor(mt, 32));
-            if (__any(mt > m[rt] + DRESCALE)) {
-                const float mn = fmaxf(m[rt], mt), al = __builtin_amdgcn_exp2f(m[rt] - mn);
+            const bool ask = mt > m[rt] + DRESCALE;
+            if (__any(ask)) {
+                // only the rows that ask for it take a new maximum: a row's bits do not depend on its neighbours
+                const float mn = ask ? mt : m[rt], al = __builtin_amdgcn_exp2f(m[rt] - mn);
                 m[rt] = mn;
                 l[rt] *= al;
 #pragma unroll

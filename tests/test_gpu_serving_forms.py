@@ -95,3 +95,34 @@ def test_decode_weights_keep_their_bits(tf, d, T, G, lens):
     tol += HALF["bf16"] * (np.abs(ref["o"]) + tol)
     worst = np.max(np.abs(out["o"].double().cpu().numpy() - ref["o"]) / tol)
     assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("dtype,d,T,G,lens", [("bf16", 64, 1, 8, [300, 200]), ("f32", 64, 1, 8, [300, 200]),
+                                              ("bf16", 128, 3, 4, [5000, 70]), ("f32", 96, 3, 4, [3000, 70]),
+                                              ("bf16", 64, 8, 8, [700, 90]), ("bf16", 256, 2, 4, [100, 2500])])
+def test_decode_rows_do_not_depend_on_their_neighbours(tf, dtype, d, T, G, lens):
+    """With the same lengths, a row's bits come from its query and what it sees: not from the other rows of its cell
+    or from other cells."""
+    torch, fw = tf
+    print(f"neighbours {dtype} d={d} T={T} G={G}", flush=True)
+    cache, table, q = _setup(tf, 50 + d, 1, T, 2, G, d, 16, lens, dtype)
+    # every row's maximum rises along its keys, and by more than its neighbours' or by less
+    for c, n in enumerate(lens):
+        for j in range(-(-n // 16)):
+            cache.k_exp[int(table[c, j])] = 112 + min(j, 10)
+    q, t, n = q.cuda(), _i32(torch, table), _i32(torch, lens)
+    a = fw.cache_attention(q, cache, t, n)
+    q2 = q.clone()
+    q2[:, 0, 1::2] *= 16.0
+    b = fw.cache_attention(q2, cache, t, n)
+    torch.cuda.synchronize()
+    keep = torch.ones(q.shape[:3], dtype=torch.bool)
+    keep[:, 0, 1::2] = False
+    assert torch.equal(a["o"].cpu()[keep], b["o"].cpu()[keep]) and torch.equal(a["lse"].cpu()[keep], b["lse"].cpu()[keep])
+    for blk in table[1]:
+        if blk >= 0:
+            cache.k_exp[int(blk)] += 3
+            cache.v[int(blk)] = 0x7F
+    c = fw.cache_attention(q, cache, t, n)
+    torch.cuda.synchronize()
+    assert torch.equal(a["o"][:, :, :G], c["o"][:, :, :G]) and torch.equal(a["lse"][:, :, :G], c["lse"][:, :, :G])
