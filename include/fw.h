@@ -355,6 +355,9 @@ fw_status fw_maxpool_scores(const float *scores, int64_t H, int64_t n, int32_t k
  *   scale  [Hkv] float32 logit scale per key/value head, or NULL for 1/sqrt(d)
  *   causal non-zero: query i of Lq sees keys 0 .. i + Lk - Lq (the last query
  *          sees every key); zero: every key of its sequence
+ *   fine_weights  bf16 rows: zero rounds each softmax weight to bf16 for the
+ *          product with the values, non-zero takes it to 2^-16 (slower by up
+ *          to a half); no effect on float32 rows
  * Limits: B, Hkv, d >= 1, Tq, Tk >= 0; Hkv divides Hq; d <= 256;
  * Tq*Hq < 2^31; (Tq*Hq/Hkv/64 + 1 + B)*Hkv < 2^24; Tk <= 2^30; strides >= 0
  * and below 2^31. */
@@ -366,6 +369,7 @@ typedef struct fw_packed {
     const int64_t *cu_q, *cu_k;
     const float *scale;
     int32_t causal;
+    int32_t fine_weights;
 } fw_packed;
 
 /* ---------------------------------------------------------------------------
@@ -378,8 +382,7 @@ typedef struct fw_packed {
  * A row that sees no key gives o = 0 and lse = -inf.  Keys and values that a
  * row does not see do not touch it, whatever they hold.  Rows of o and lse
  * outside [cu_q[0], cu_q[B]) are left as they were.  Offsets that lead outside
- * the arrays are clamped to them.  float32 rows are computed in float32; bf16
- * rows round the softmax weights to bf16 for the product with the values.
+ * the arrays are clamped to them.  float32 rows are computed in float32.
  * Errors: FW_E_NULL (packed, q, k, v, cu_q, cu_k or o NULL; q, k, v and o may
  * be NULL where they have no rows), FW_E_SHAPE, FW_E_DTYPE, FW_E_WORKSPACE,
  * FW_E_HIP.

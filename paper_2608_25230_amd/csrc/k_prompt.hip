@@ -327,9 +327,14 @@ __global__ void __launch_bounds__(GTH, NT <= 5 ? 3 : 1) prompt_general(PromptArg
 //   keys 16 kb + 4 (l / 32) + {0..3, 8..11}: the eight weights that the lane
 //   already holds, rounded to bf16 in place.  V is read transposed
 //   (ds_read_b64_tr_b16), four keys of one column per lane.
-// The weights are rounded to bf16 for the product (relative error up to 2^-8
-// each); their sum is taken in float32 before the rounding, so that lse keeps
-// float32's precision.
+// The weights enter the product in bf16.  By default each is rounded once
+// (relative error up to 2^-8), which puts the result about a third further from
+// the exact one than its own rounding to bf16 does, and buys a third of the
+// products: 16,384 tokens in 1.93 ms, 16 packed sequences 0.52.  A caller that
+// wants the weights' bits asks for two parts (fine_weights; 2^-16 left of each):
+// 2.85 and 0.75 ms at two workgroups a compute unit, 2.80 and 0.75 at three,
+// which spill.  Either way their sum is taken in float32 before the rounding,
+// so that lse keeps float32's precision.
 // No maximum is taken of a tile.  The exponentials are taken from the maximum
 // m so far, and only a row whose weights over the tile sum to more than GROWN
 // (or to no number) takes a new one, rescales and computes the tile's weights
@@ -381,8 +386,9 @@ __device__ __forceinline__ int v_swizzle(int r) {
     return D == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3);
 }
 
-template <int D>
-__global__ void __launch_bounds__(PTH, D == 256 ? 1 : 3) prompt_mfma(PromptArgs a) {
+// PARTS: bf16 parts of a weight
+template <int D, int PARTS>
+__global__ void __launch_bounds__(PTH, D == 256 ? 1 : D == 128 && PARTS == 2 ? 2 : 3) prompt_mfma(PromptArgs a) {
     constexpr int RB = 2 * D;               // bytes of an LDS row
     constexpr int TB = PK * RB;             // bytes of a tile
     constexpr int RPI = 1024 / RB;          // rows of one 64-lane load
@@ -495,7 +501,7 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 3) prompt_mfma(PromptArgs 
             for (int i = 0; i < 16; ++i)
                 if (8 * (i / 4) + i % 4 >= lim) s[i] = -INFINITY;
         }
-        bf16x8 pf[2];
+        bf16x8 pf[2][PARTS];
         float sum;
         const auto weights = [&]() __attribute__((always_inline)) {
             sum = 0.f;
@@ -503,7 +509,8 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 3) prompt_mfma(PromptArgs 
             for (int i = 0; i < 16; ++i) {
                 const float p = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -m));
                 sum += p;
-                pf[i / 8][i % 8] = (__bf16)p;
+                pf[i / 8][0][i % 8] = (__bf16)p;
+                if constexpr (PARTS == 2) pf[i / 8][1][i % 8] = (__bf16)(p - (float)pf[i / 8][0][i % 8]);
             }
         };
         weights();
@@ -526,8 +533,11 @@ __global__ void __launch_bounds__(PTH, D == 256 ? 1 : 3) prompt_mfma(PromptArgs 
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int n = 0; n < DB; ++n)
-                acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value((vro ^ (n * 64)) + at + kb * 16 * RB), pf[kb], acc[n], 0, 0, 0);
+            for (int n = 0; n < DB; ++n) {
+                const bf16x8 v = value((vro ^ (n * 64)) + at + kb * 16 * RB);
+#pragma unroll
+                for (int x = PARTS - 1; x >= 0; --x) acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[kb][x], acc[n], 0, 0, 0);
+            }
     };
     // A hidden key's weight is 0, but 0 times an infinity or a NaN is a NaN.  In a tile that holds such a
     // value and is hidden from some row, the value is taken out before `step`; whether a row sees an
@@ -732,6 +742,13 @@ int64_t row_tiles(const fw_packed &p, int rows) {  // an upper bound: the length
     return (p.Tq * (p.Hq / p.Hkv) + rows - 1) / rows + p.B;
 }
 
+template <int PARTS>
+void launch_mfma(const PromptArgs &a, int D, dim3 grid, size_t lds, hipStream_t st) {
+    if (D == 64) hipLaunchKernelGGL((prompt_mfma<64, PARTS>), grid, dim3(PTH), lds, st, a);
+    else if (D == 128) hipLaunchKernelGGL((prompt_mfma<128, PARTS>), grid, dim3(PTH), lds, st, a);
+    else hipLaunchKernelGGL((prompt_mfma<256, PARTS>), grid, dim3(PTH), lds, st, a);
+}
+
 template <typename T>
 void launch_general(const PromptArgs &a, int vec, dim3 grid, hipStream_t st) {
     const int nt = (a.d + 15) / 16;
@@ -783,9 +800,8 @@ hipError_t launch_prompt(const fw_packed &p, void *o, float *lse, int splits, fl
         const dim3 grid((unsigned)(row_tiles(p, PR) * p.Hkv), (unsigned)splits);
         const int D = a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256;
         const size_t lds = (size_t)2 * 2 * PK * 2 * D + 16 + (size_t)D / 32 * 2 * 2 * PTH;  // two slots, flags, marks
-        if (D == 64) hipLaunchKernelGGL((prompt_mfma<64>), grid, dim3(PTH), lds, st, a);
-        else if (D == 128) hipLaunchKernelGGL((prompt_mfma<128>), grid, dim3(PTH), lds, st, a);
-        else hipLaunchKernelGGL((prompt_mfma<256>), grid, dim3(PTH), lds, st, a);
+        if (p.fine_weights) launch_mfma<2>(a, D, grid, lds, st);
+        else launch_mfma<1>(a, D, grid, lds, st);
     } else {
         const dim3 grid((unsigned)(row_tiles(p, GR) * p.Hkv), (unsigned)splits);
         const int size = p.dtype == FW_F32 ? 4 : 2, q = 4;

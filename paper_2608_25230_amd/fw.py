@@ -46,7 +46,7 @@ class Packed(ctypes.Structure):
                 ("Hkv", ctypes.c_int64), ("d", ctypes.c_int64), ("q_row", ctypes.c_int64), ("q_head", ctypes.c_int64),
                 ("k_row", ctypes.c_int64), ("k_head", ctypes.c_int64), ("v_row", ctypes.c_int64),
                 ("v_head", ctypes.c_int64), ("cu_q", ctypes.c_void_p), ("cu_k", ctypes.c_void_p),
-                ("scale", ctypes.c_void_p), ("causal", ctypes.c_int32)]
+                ("scale", ctypes.c_void_p), ("causal", ctypes.c_int32), ("fine_weights", ctypes.c_int32)]
 
 
 class Cache(ctypes.Structure):
@@ -440,16 +440,18 @@ def _elsewhere(name: str, t):
     return None if cuda.current_device() == t.get_device() else cuda.device(t.device)
 
 
-def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=None, want_lse=True,
-                     ws=None) -> Dict[str, object]:
+def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=None, fine_weights: bool = False,
+                     want_lse=True, ws=None) -> Dict[str, object]:
     """Attention of packed sequences: q [Tq][Hq][d], k and v [Tk][Hkv][d] (strided views of a fused projection are
     fine), cu_q and cu_k [B+1] int64 offsets (cu_k defaults to cu_q).  Returns o [Tq][Hq][d] of q's type and lse
-    [Tq][Hq] float32.  Rows outside the sequences are left unwritten."""
+    [Tq][Hq] float32.  Rows outside the sequences are left unwritten.  bf16 rows round each softmax weight to bf16 for
+    the product with the values; fine_weights takes it to 2^-16, in up to half as much time again."""
     torch = _torch()
     guard = _elsewhere("q", q)
     if guard is not None:
         with guard:
-            return prompt_attention(q, k, v, cu_q, cu_k, causal=causal, scale=scale, want_lse=want_lse, ws=ws)
+            return prompt_attention(q, k, v, cu_q, cu_k, causal=causal, scale=scale, fine_weights=fine_weights,
+                                    want_lse=want_lse, ws=ws)
     dev, dt = q.device, q.dtype
     code = _dtype_code(q)
     _rows_of("q", q, dt, 3, dev)
@@ -472,7 +474,8 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=Non
     k_row, k_head, _ = k.stride()
     v_row, v_head, _ = v.stride()
     p = Packed(code, q.data_ptr(), k.data_ptr(), v.data_ptr(), Tq, Tk, cu_q.shape[0] - 1, Hq, Hkv, d, q_row, q_head,
-               k_row, k_head, v_row, v_head, cu_q.data_ptr(), cu_k.data_ptr(), _ptr(scale), 1 if causal else 0)
+               k_row, k_head, v_row, v_head, cu_q.data_ptr(), cu_k.data_ptr(), _ptr(scale), 1 if causal else 0,
+               1 if fine_weights else 0)
     L, ref = lib(), ctypes.byref(p)
     o = torch.empty_like(q) if q.is_contiguous() else q.new_empty((Tq, Hq, d))
     lse = q.new_empty((Tq, Hq), dtype=torch.float32) if want_lse else None

@@ -5,6 +5,7 @@ import pytest
 from oracle import serving as O
 from tests.serving import HALF, tolerances
 from tests.test_gpu_cache import _empty, _host, _i32, _setup, _tables, tf  # noqa: F401
+from tests.test_gpu_prompt import _inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -72,6 +73,67 @@ def test_captured_steps_in_which_fewer_cells_grow(tf):
 
 
 # ---------------------------------------------------------------------------
+# weights in two bf16 parts
+# ---------------------------------------------------------------------------
+
+def _two_parts(ref, d, n):
+    """tolerances() of float32 rows, but for the output's rounding, which is bf16's; and each weight is the sum of two
+    bf16 roundings (the second is off by 2^-8 of what the first leaves, which is 2^-8 of the weight), either of which
+    may underflow."""
+    tol, _ = tolerances(ref, "f32", d, n)
+    tol += 2.0 ** -16 * ref["abs_o"] * (1 + 2.0 ** -7) + n * 2.0 ** -117
+    return tol + HALF["bf16"] * (np.abs(ref["o"]) + tol)
+
+
+@pytest.mark.parametrize("d,lq,lk,causal", [(128, [300, 65], None, True), (64, [1, 129, 40], None, True),
+                                            (80, [200, 33], None, False), (256, [150], None, True),
+                                            (128, [3, 40], [4097, 2500], True), (64, [7], [3000], False),
+                                            (192, [70, 5, 3], [10, 0, 300], True)])
+def test_prompt_weights_keep_their_bits(tf, d, lq, lk, causal):
+    """fine_weights: an output is off by its own rounding and what float32 loses, however much its terms cancel."""
+    torch, fw = tf
+    print(f"fine weights d={d} {lq} {lk}", flush=True)
+    lk = lk or lq
+    dev, f64, cu, cun = _inputs(torch, 60 + d, lq, lk, 4, 2, d, "bf16")
+    out = fw.prompt_attention(*dev, *cu, causal=causal, fine_weights=True)
+    plain = fw.prompt_attention(*dev, *cu, causal=causal)
+    torch.cuda.synchronize()
+    assert torch.equal(out["lse"], plain["lse"])
+    ref = O.prompt_attention(*f64, *cun, None, causal)
+    worst = np.max(np.abs(out["o"].double().cpu().numpy() - ref["o"]) / _two_parts(ref, d, max(lk)))
+    assert worst <= 1, worst
+
+
+def test_prompt_fine_weights_of_hidden_values_and_scales(tf):
+    """Values that are not finite reach the rows that see them and no others; zero and negative scales."""
+    torch, fw = tf
+    for d in (64, 128, 256):
+        dev, f64, cu, cun = _inputs(torch, 70, [70, 100], [70, 100], 2, 1, d, "bf16")
+        clean = fw.prompt_attention(*dev, *cu, fine_weights=True)
+        v = dev[2].clone()
+        v[40, 0, 3], v[169, 0, 5] = float("inf"), float("nan")
+        got = fw.prompt_attention(dev[0], dev[1], v, *cu, fine_weights=True)
+        torch.cuda.synchronize()
+        hit = torch.zeros(got["o"].shape, dtype=torch.bool)
+        hit[40:70, :, 3] = True
+        hit[169, :, 5] = True
+        o, c = got["o"].float().cpu(), clean["o"].float().cpu()
+        assert torch.equal(~torch.isfinite(o), hit) and torch.equal(o[~hit], c[~hit])
+        for s in (0.0, -0.3):
+            out = fw.prompt_attention(*dev, *cu, scale=torch.tensor([s], device="cuda"), fine_weights=True)
+            ref = O.prompt_attention(*f64, *cun, np.float32([s]).astype(np.float64), True)
+            assert np.all(np.abs(out["o"].double().cpu().numpy() - ref["o"]) <= _two_parts(ref, d, 100))
+
+
+def test_fine_weights_leave_float32_rows_alone(tf):
+    torch, fw = tf
+    dev, f64, cu, cun = _inputs(torch, 71, [90], [90], 4, 2, 40, "f32")
+    a, b = (fw.prompt_attention(*dev, *cu, fine_weights=x) for x in (False, True))
+    torch.cuda.synchronize()
+    assert torch.equal(a["o"], b["o"]) and torch.equal(a["lse"], b["lse"])
+
+
+# ---------------------------------------------------------------------------
 # attention over the cache
 # ---------------------------------------------------------------------------
 
@@ -88,12 +150,7 @@ def test_decode_weights_keep_their_bits(tf, d, T, G, lens):
     torch.cuda.synchronize()
     ref = O.cache_attention(q.double().numpy(), _host(cache), table, lens, None)
     n = max(lens)
-    # tolerances() of float32 rows, but for the output's rounding, which is bf16's; then each weight is the sum of
-    # two bf16 roundings (2^-8 of what the first leaves, which is 2^-8 of the weight), either of which may underflow
-    tol, _ = tolerances(ref, "f32", d, n)
-    tol += 2.0 ** -16 * ref["abs_o"] * (1 + 2.0 ** -7) + n * 2.0 ** -117
-    tol += HALF["bf16"] * (np.abs(ref["o"]) + tol)
-    worst = np.max(np.abs(out["o"].double().cpu().numpy() - ref["o"]) / tol)
+    worst = np.max(np.abs(out["o"].double().cpu().numpy() - ref["o"]) / _two_parts(ref, d, n))
     assert worst <= 1, worst
 
 
