@@ -446,7 +446,7 @@ int32_t fw_cache_row(int64_t d);
 /* ---------------------------------------------------------------------------
  * fw_cache_store -- rounds rows of keys and values to the cache's blocks
  * (fw_ragged_compact's k_out and v_out, or one decoding step's rows).
- *   dtype, k, v  [N][d] rows, N < 2^28, strides k_row and v_row in elements
+ *   dtype, k, v  [N][d] rows, N <= 2^28 - 16, strides k_row and v_row in elements
  *   slots        [N] int64, of fw_block_tables; rows whose slot is not in
  *                [0, n_blocks * block_size) are skipped
  * The rows that go to one block are consecutive rows with consecutive slots.
@@ -483,7 +483,7 @@ fw_status fw_cache_store(const fw_cache *cache, int32_t dtype, const void *k, in
  * query, what it sees and the call's sizes and lengths (which fix how cells are
  * cut into parts), not from other rows' queries or other cells' tokens.
  * Limits: S, T, Hkv, max_blocks >= 1; Hkv divides Hq; T*Hq/Hkv <= 4096;
- * S*Hkv < 2^22; S*T*Hq < 2^26; max_blocks * block_size < 2^31;
+ * S*Hkv < 2^22; S*T*Hq <= 2^26 - 4; max_blocks * block_size < 2^31;
  * S*Hkv * max_blocks * block_size < 2^36.
  * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_DTYPE, FW_E_WORKSPACE, FW_E_HIP.
  * ------------------------------------------------------------------------- */

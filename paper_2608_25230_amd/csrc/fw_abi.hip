@@ -464,7 +464,7 @@ fw_status check_packed(const fw_packed *p) {
     constexpr int64_t most = (int64_t)1 << 31;
     if (p->Hq >= most || p->Tq >= most || p->Tk > (1ll << 30) || p->B >= most || p->Tq * p->Hq >= most)
         return fail(FW_E_SHAPE, "need Tq*Hq < 2^31, Tk <= 2^30 and B < 2^31");
-    // one workgroup of 256 threads per row tile and key/value head, 64 rows or more to a tile; a grid holds 2^32 threads
+    // one workgroup of 256 threads per row tile and key/value head, 64 rows or more to a tile; a grid holds fewer than 2^32 threads
     if ((p->Tq * (p->Hq / p->Hkv) / 64 + 1 + p->B) >= ((int64_t)1 << 24) / p->Hkv)
         return fail(FW_E_SHAPE, "too many sequences and heads for one call");
     const int64_t strides[] = {p->q_row, p->q_head, p->k_row, p->k_head, p->v_row, p->v_head};
@@ -512,12 +512,13 @@ fw_status check_cache(const fw_cache *c) {
 fw_status check_decode(int32_t block_size, int64_t S, int64_t T, int64_t Hq, int64_t Hkv, int64_t max_blocks) {
     if (S < 1 || T < 1 || Hq < 1 || Hkv < 1 || max_blocks < 1)
         return fail(FW_E_SHAPE, "S, T, Hq, Hkv and max_blocks must be >= 1");
-    // a grid holds 2^32 threads: up to 512 for a cell, 64 for a row
+    // a grid holds fewer than 2^32 threads: up to 512 for a cell, 64 for a row
     constexpr int64_t m31 = (int64_t)1 << 31, m26 = (int64_t)1 << 26, m22 = (int64_t)1 << 22;
     if (S >= m22 || Hkv >= m22 || S * Hkv >= m22) return fail(FW_E_SHAPE, "S*Hkv must be < 2^22");
     if (Hq % Hkv != 0) return fail(FW_E_SHAPE, "Hkv must divide Hq (Hq=%lld Hkv=%lld)", (long long)Hq, (long long)Hkv);
     if (T > 4096 || Hq / Hkv > 4096 || T * (Hq / Hkv) > 4096) return fail(FW_E_SHAPE, "T*Hq/Hkv must be <= 4096");
-    if (S * Hkv * (T * (Hq / Hkv)) >= m26) return fail(FW_E_SHAPE, "S*T*Hq must be < 2^26");
+    // decode_join: four rows to a workgroup of 256 threads
+    if (S * Hkv * (T * (Hq / Hkv)) > m26 - 4) return fail(FW_E_SHAPE, "S*T*Hq must be <= 2^26 - 4");
     if (max_blocks >= m31 / block_size) return fail(FW_E_SHAPE, "max_blocks * block_size must be < 2^31");
     if ((double)(S * Hkv) * (double)(max_blocks * block_size) >= 68719476736.0)
         return fail(FW_E_SHAPE, "S*Hkv * max_blocks * block_size must be < 2^36");
@@ -588,8 +589,8 @@ fw_status fw_cache_store(const fw_cache *cache, int32_t dtype, const void *k, in
     fw_status s = check_cache(cache);
     if (s != FW_OK) return s;
     if (dtype != FW_F32 && dtype != FW_BF16) return fail(FW_E_DTYPE, "unknown dtype %d", (int)dtype);
-    // a grid holds 2^32 threads: 256 for 16 rows or more
-    if (N < 0 || N >= ((int64_t)1 << 28)) return fail(FW_E_SHAPE, "N must be in [0, 2^28)");
+    // a grid holds fewer than 2^32 threads: 256 for 16 rows or more
+    if (N < 0 || N > ((int64_t)1 << 28) - 16) return fail(FW_E_SHAPE, "N must be in [0, 2^28 - 16]");
     if (k_row < 0 || v_row < 0 || k_row >= ((int64_t)1 << 31) || v_row >= ((int64_t)1 << 31))
         return fail(FW_E_SHAPE, "strides must be in [0, 2^31)");
     if (N == 0) return FW_OK;

@@ -122,6 +122,18 @@ def test_grids_beyond_the_card_are_refused(L):
         assert L.fw_cache_attention_workspace_size(_cache(), S, T, Hq, Hkv, 100) == 0
 
 
+def test_the_last_sizes_before_a_grid_is_full(L):
+    """A grid holds fewer than 2^32 threads, its workgroups rounded up: sixteen rows of the store, four of the join."""
+    for N in ((1 << 28) - 15, (1 << 28) - 1):
+        for bs in (16, 256):
+            assert L.fw_cache_store(_cache(block_size=bs), 1, 16, 64, 16, 64, N, 16, None, 0, None) == 2, N
+    for S, T, Hq, Hkv in ((24573, 2731, 1, 1), (24573, 1, 2731, 1)):
+        assert L.fw_cache_attention(_cache(), 1, 16, S, T, Hq, Hkv, 512, 512, 64, 16, 100, 16, None, 16, None, 16,
+                                    1 << 60, None) == 2, (S, T, Hq, Hkv)
+        assert L.fw_cache_attention_workspace_size(_cache(), S, T, Hq, Hkv, 100) == 0
+    assert L.fw_cache_attention_workspace_size(_cache(), 16383, 4096, 1, 1, 100) > 0       # 2^26 - 4096 rows
+
+
 def test_host_tensors_are_refused(L):
     torch = pytest.importorskip("torch")
     z = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
