@@ -359,7 +359,8 @@ fw_status fw_maxpool_scores(const float *scores, int64_t H, int64_t n, int32_t k
  *          product with the values, non-zero takes it to 2^-16 (slower by up
  *          to a half); no effect on float32 rows
  * Limits: B, Hkv, d >= 1, Tq, Tk >= 0; Hkv divides Hq; d <= 256;
- * Tq*Hq < 2^31; (Tq*Hq/Hkv/64 + 1 + B)*Hkv < 2^24; Tk <= 2^30; strides >= 0
+ * Tq*Hq < 2^31; (Tq*Hq/Hkv/64 + 1 + B)*Hkv < 2^24, and times B < 2^36 (every
+ * workgroup looks through the sequences for its own); Tk <= 2^30; strides >= 0
  * and below 2^31. */
 typedef struct fw_packed {
     int32_t dtype;

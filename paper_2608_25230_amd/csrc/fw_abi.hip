@@ -467,6 +467,10 @@ fw_status check_packed(const fw_packed *p) {
     // one workgroup of 256 threads per row tile and key/value head, 64 rows or more to a tile; a grid holds fewer than 2^32 threads
     if ((p->Tq * (p->Hq / p->Hkv) / 64 + 1 + p->B) >= ((int64_t)1 << 24) / p->Hkv)
         return fail(FW_E_SHAPE, "too many sequences and heads for one call");
+    // every workgroup looks through the sequences for its own: 65,536 sequences of one position and 8 heads take 157
+    // ms, a quarter of them 11, and 2^23 of one head would hold the GPU for minutes
+    if ((p->Tq * (p->Hq / p->Hkv) / 64 + 1 + p->B) * p->Hkv >= ((int64_t)1 << 36) / p->B)
+        return fail(FW_E_SHAPE, "(Tq*Hq/Hkv/64 + 1 + B)*Hkv * B must be < 2^36");
     const int64_t strides[] = {p->q_row, p->q_head, p->k_row, p->k_head, p->v_row, p->v_head};
     for (int64_t s : strides)
         if (s < 0 || s >= most) return fail(FW_E_SHAPE, "strides must be in [0, 2^31)");

@@ -134,6 +134,14 @@ def test_the_last_sizes_before_a_grid_is_full(L):
     assert L.fw_cache_attention_workspace_size(_cache(), 16383, 4096, 1, 1, 100) > 0       # 2^26 - 4096 rows
 
 
+def test_sequences_beyond_what_a_call_can_look_through_are_refused(L):
+    """Each workgroup looks through the sequences: millions of them would take minutes."""
+    for bad in (dict(B=1 << 23, Hkv=1, Hq=1), dict(B=1 << 17, Hkv=4, Hq=4), dict(B=1 << 18, Hkv=1, Hq=1),
+                dict(B=1 << 16, Hkv=16, Hq=16), dict(Tq=1 << 22, B=1 << 17, Hkv=1, Hq=8)):
+        assert L.fw_prompt_attention(_packed(**bad), 16, None, 16, 1 << 40, None) == 2, bad
+        assert L.fw_prompt_attention_workspace_size(_packed(**bad)) == 0
+
+
 def test_host_tensors_are_refused(L):
     torch = pytest.importorskip("torch")
     z = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
