@@ -34,10 +34,19 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // more than their work.
 //
 // Bound by chains of dependent loads and by launches.  2048 cells that grow by
-// a token: 10 us on the GPU in one launch, 9 + 7.5 in two.  256 cells, 1.5 M slots and 23 k blocks: 6.5 + 12 us
-// (12 MB, 2.4 us at copy rate); one workgroup alone would take 1.9 ms.  So one
-// launch is for at most 8192 slots or, where nothing is listed and any length
-// may go, tables of at most 16,384 blocks.
+// a token: 10 us on the GPU in one launch, 9 + 7.5 in two.  256 cells, 1.5 M
+// slots and 23 k blocks: 6.5 + 12 us (12 MB, 2.4 us at copy rate); one workgroup
+// alone would take 1.9 ms.  So one launch is for calls that list at most 8192
+// slots and, where they list none and any length may go, for tables of at most
+// 16,384 blocks.  A call between two events, in us: 4135 cells of 3 blocks, 748
+// k slots 34 (one launch 1250); 500 cells that grow by 17 each 19.6 (32).
+//
+// Where one call gives back and takes (or lists few slots), one workgroup moves
+// all that comes back: with 2048 cells, 8 that end and the others growing by a
+// token 27, 64 of 20,000 tokens ending 80, half of 20,000 tokens ending (281 k
+// blocks) 1000; 256 of 20,000 ending while 256 begin 257, where either alone
+// takes under 40.  A program that ends very many long cells at once gives them
+// back in a call of its own.
 // ---------------------------------------------------------------------------
 constexpr int TT = 1024;  // threads of the scan
 
@@ -287,8 +296,8 @@ __global__ void __launch_bounds__(256) tables_move(TableArgs a) {
 //
 // Bound by HBM: 1.49 M bf16 rows of 128 in 257 us, 4.64 TB/s of the bytes read
 // and written (a large copy: 4.96).  Loads with branches and 64-bit addresses
-// took 318 us, keys and values on workgroups of their own 480 (registers).  One
-// token for each of a step's cells: 9 us, launch and load latency.
+// took 318 us, keys and values on workgroups of their own 480 (registers).
+// One token for each of a step's cells: 9 us, launch and load latency.
 // ---------------------------------------------------------------------------
 constexpr int ST = 256;
 constexpr int SMAX = 256;  // largest block size
@@ -562,7 +571,7 @@ hipError_t launch_tables(int64_t C, const int32_t *old_len, const int32_t *new_l
     a.back_off = (int64_t *)p;
     p += align_up((C + 1) * sizeof(int64_t), 256);
     a.need_off = (int64_t *)p;
-    if ((n_slots > 0 && n_slots <= 8192) || C * W <= 16384) {
+    if (n_slots <= 8192 && (n_slots > 0 || C * W <= 16384)) {
         hipLaunchKernelGGL(tables_scan<true>, dim3(1), dim3(TT), 0, st, a);
         return hipGetLastError();
     }

@@ -4,7 +4,7 @@ import pytest
 
 from oracle import serving as O
 from tests.serving import HALF, tolerances
-from tests.test_gpu_cache import _empty, _host, _i32, _setup, _tables, tf  # noqa: F401
+from tests.test_gpu_cache import _check_tables, _empty, _host, _i32, _setup, _tables, tf  # noqa: F401
 from tests.test_gpu_prompt import _inputs
 
 pytestmark = pytest.mark.gpu
@@ -70,6 +70,45 @@ def test_captured_steps_in_which_fewer_cells_grow(tf):
         assert np.array_equal(lens.cpu().numpy(), rl) and np.array_equal(t.cpu().numpy(), rt), step
         for name in ("k", "v", "k_exp", "v_exp"):
             assert np.array_equal(got[name], ref[name]), (step, name)
+
+
+@pytest.mark.parametrize("C,W,bs", [(256, 120, 16), (2048, 9, 16), (2049, 10, 16), (40, 500, 32)])
+def test_tables_over_the_whole_card(tf, C, W, bs):
+    """Growth, release and exchange of so many blocks and slots that several launches do it, for at most 2048 cells
+    (whose offsets are staged) and more; a pure release of more blocks than the scan's workgroup moves itself."""
+    torch, fw = tf
+    print(f"whole card C={C} W={W}", flush=True)
+    rng = np.random.default_rng(C)
+    old, new = np.zeros(C, int), rng.integers(W * bs // 3, W * bs + 1, C)
+    blocks = int(np.sum(-(-new // bs)))
+    table, free, n_free = _tables(rng, old, W, bs, blocks + 5)
+    n = int(new.sum())
+    assert n > 8192 and C * W > 16384 and blocks > 4096
+    t, f, nf, out = _check_tables(tf, old, new, table, free, n_free, bs, n)
+    grown = (t.cpu().numpy(), f.cpu().numpy(), int(nf))
+    _check_tables(tf, new, old, *grown, bs, 0)                                   # everything comes back
+    some = np.where(np.arange(C) % 2 == 0, 0, new)
+    half = O.block_tables(new, some, *grown, bs, 0)
+    m = (half["table"], half["free_list"], half["n_free"])
+    swap = np.where(np.arange(C) % 2 == 0, new, 0)                               # one half ends, the other begins
+    k = int(np.maximum(swap - some, 0).sum())
+    assert k > 8192
+    _check_tables(tf, some, swap, *m, bs, k)
+    step = np.where(np.arange(C) % 2 == 0, np.minimum(1 + np.arange(C) % 3, W * bs), 0)   # few slots, many blocks back
+    _check_tables(tf, some, step, *m, bs, int(step.sum()))
+
+
+@pytest.mark.parametrize("C,W,bs,grow", [(3000, 3, 64, 100), (50, 20, 128, 1200), (16384, 1, 16, 9), (500, 30, 16, 17)])
+def test_short_tables_that_list_many_slots(tf, C, W, bs, grow):
+    torch, fw = tf
+    print(f"short tables C={C} grow={grow}", flush=True)
+    rng = np.random.default_rng(C)
+    old = rng.integers(0, W * bs - grow + 1, C)
+    new = old + grow
+    table, free, n_free = _tables(rng, old, W, bs, int(np.sum(-(-new // bs))) + 1)
+    assert C * grow > 8192 and C * W <= 16384
+    t, f, nf, out = _check_tables(tf, old, new, table, free, n_free, bs, C * grow)
+    _check_tables(tf, new, old, t.cpu().numpy(), f.cpu().numpy(), int(nf), bs, 0)
 
 
 # ---------------------------------------------------------------------------
