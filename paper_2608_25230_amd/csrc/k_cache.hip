@@ -39,7 +39,8 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // alone would take 1.9 ms.  So one launch is for calls that list at most 8192
 // slots and, where they list none and any length may go, for tables of at most
 // 16,384 blocks.  A call between two events, in us: 4135 cells of 3 blocks, 748
-// k slots 34 (one launch 1250); 500 cells that grow by 17 each 19.6 (32).
+// k slots 34 (one launch 1250); 500 cells that grow by 17 each 19.6 (32), by 15
+// in one launch 21 (cells' own threads; the workgroup together 29).
 //
 // Where one call gives back and takes (or lists few slots), one workgroup moves
 // all that comes back: with 2048 cells, 8 that end and the others growing by a
@@ -170,8 +171,9 @@ __device__ __forceinline__ void write_slots(const TableArgs &a, const TableHead 
     }
 }
 
-constexpr int kFew = 8;            // blocks or tokens of a cell that its own thread moves
-constexpr int64_t kInline = 4096;  // returned blocks that the one workgroup moves in a call of several launches
+// Blocks or tokens of a cell that its own thread moves, if no cell has more.  500 cells that grow by 15 tokens: 21 us
+// against 29 by the workgroup together (8 as the limit); by 8: 17 against 21 (1 as the limit).
+constexpr int kFew = 32;
 
 template <bool ALL>
 __global__ void __launch_bounds__(TT) tables_scan(TableArgs a) {
@@ -248,7 +250,7 @@ __global__ void __launch_bounds__(TT) tables_scan(TableArgs a) {
         a.refused[0] = (int32_t)refused;
     }
     if (direct) return;
-    const bool mine = ALL || hd.back <= kInline || hd.take > 0;
+    const bool mine = ALL || hd.take > 0;
     if (mine && hd.back > 0) {
         move_back(a, hd, threadIdx.x, TT);
         __syncthreads();  // blocks that came back may be taken
@@ -263,13 +265,16 @@ __global__ void __launch_bounds__(TT) tables_scan(TableArgs a) {
 }
 
 // What the scan left: returned blocks (then none is taken), or blocks taken and slots.
-constexpr int kStage = 2048;  // cells whose offsets are staged in LDS
+// Cells whose offsets are staged in LDS where slots are listed: 256 cells, 3.3 M slots 39.5 us against 45 without; 500
+// cells, 8500 slots 19.6 against 21.
+constexpr int kStage = 2048;
 __global__ void __launch_bounds__(256) tables_move(TableArgs a) {
     __shared__ int64_t staged[kStage + 1];
     const TableHead hd = a.head[0];
     const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
     move_back(a, hd, first, step);
     take_blocks(a, hd, first, step);
+    if (a.n_slots == 0) return;
     if (a.C <= kStage) {
         for (int64_t c = threadIdx.x; c <= a.C; c += 256) staged[c] = a.offsets[c];
         __syncthreads();
@@ -297,7 +302,14 @@ __global__ void __launch_bounds__(256) tables_move(TableArgs a) {
 // Bound by HBM: 1.49 M bf16 rows of 128 in 257 us, 4.64 TB/s of the bytes read
 // and written (a large copy: 4.96).  Loads with branches and 64-bit addresses
 // took 318 us, keys and values on workgroups of their own 480 (registers).
-// One token for each of a step's cells: 9 us, launch and load latency.
+// Float32 rows: 396 us at d = 128, 5.0 TB/s, 275 at d = 80, 4.5.  One token for
+// each of a step's cells: 9 us, launch and load latency.
+//
+// A workgroup looks at `chunk` rows for runs that begin there: as many as leave
+// 2048 workgroups, up to a block.  Calls in us against chunks that leave 512 and
+// 8192: 512 cells of 1 to 60 tokens 17 / 22.5 / 18, of 200 to 600 31 / 31 / 39,
+// 64 of 500 to 2000 15.7 / 14.4 / 27, 20 tokens each for 512 16 / 16 / 37.  One
+// row each: 2180 instead of 257 for the large call.
 // ---------------------------------------------------------------------------
 constexpr int ST = 256;
 constexpr int SMAX = 256;  // largest block size
