@@ -4,7 +4,7 @@ import pytest
 
 from oracle import serving as O
 from tests.serving import HALF, tolerances
-from tests.test_gpu_cache import _check_tables, _empty, _host, _i32, _setup, _tables, tf  # noqa: F401
+from tests.test_gpu_cache import _attend, _check_tables, _empty, _host, _i32, _setup, _tables, tf  # noqa: F401
 from tests.test_gpu_prompt import _inputs
 
 pytestmark = pytest.mark.gpu
@@ -222,3 +222,18 @@ def test_decode_rows_do_not_depend_on_their_neighbours(tf, dtype, d, T, G, lens)
     c = fw.cache_attention(q, cache, t, n)
     torch.cuda.synchronize()
     assert torch.equal(a["o"][:, :, :G], c["o"][:, :, :G]) and torch.equal(a["lse"][:, :, :G], c["lse"][:, :, :G])
+
+
+@pytest.mark.parametrize("dtype,d,T,G", [("bf16", 192, 1, 4), ("bf16", 256, 1, 2), ("bf16", 256, 4, 8), ("bf16", 96, 1, 3),
+                                         ("bf16", 32, 1, 1), ("bf16", 33, 2, 3), ("bf16", 128, 4, 8), ("bf16", 128, 8, 8),
+                                         ("f32", 80, 1, 3), ("f32", 80, 4, 3), ("f32", 128, 1, 2), ("f32", 192, 1, 2),
+                                         ("f32", 256, 1, 2), ("f32", 200, 3, 7), ("f32", 96, 5, 4), ("f32", 64, 8, 8)])
+def test_decode_widths_and_rows_over_shared_cells(tf, dtype, d, T, G):
+    """Every width and several row tiles where cells are cut over workgroups and joined; some hold no token, one, or
+    fewer than the new positions."""
+    lens = [2600, 3, 0, 700, 2049, 512, 1111, 1]
+    print(f"shared {dtype} d={d} T={T} G={G}", flush=True)
+    cache, table, q = _setup(tf, 80 + d + T, 2, T, 4, G, d, 64, lens, dtype, extra=1)
+    assert table.shape[1] > 32                # tiles of 64 tokens: more than one workgroup takes whole
+    out = _attend(tf, cache, table, q, lens, dtype, what=f"shared {dtype} d={d} T={T} G={G}")
+    assert out["_ws"] is not None
