@@ -751,12 +751,17 @@ void launch_mfma(const PromptArgs &a, int D, dim3 grid, size_t lds, hipStream_t 
 
 template <typename T>
 void launch_general(const PromptArgs &a, int vec, dim3 grid, hipStream_t st) {
+    // Widths in steps that each save a quarter or more of the next instance's products: two float32 sequences of 1500,
+    // 8 query and 2 key/value heads, in us: d = 32 68, 64 111, 80 138, 96 216 (266 in 128 columns), 128 272, 192 413 (531
+    // in 256), 256 542.
     const int nt = (a.d + 15) / 16;
 #define FW_G(n) hipLaunchKernelGGL((prompt_general<T, n>), grid, dim3(GTH), 0, st, a, vec)
     if (nt <= 2) FW_G(2);
     else if (nt <= 4) FW_G(4);
     else if (nt <= 5) FW_G(5);
+    else if (nt <= 6) FW_G(6);
     else if (nt <= 8) FW_G(8);
+    else if (nt <= 12) FW_G(12);
     else FW_G(16);
 #undef FW_G
 }

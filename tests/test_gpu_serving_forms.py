@@ -5,7 +5,7 @@ import pytest
 from oracle import serving as O
 from tests.serving import HALF, tolerances
 from tests.test_gpu_cache import _attend, _check_tables, _empty, _host, _i32, _setup, _tables, tf  # noqa: F401
-from tests.test_gpu_prompt import _inputs
+from tests.test_gpu_prompt import _inputs, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -109,6 +109,19 @@ def test_short_tables_that_list_many_slots(tf, C, W, bs, grow):
     assert C * grow > 8192 and C * W <= 16384
     t, f, nf, out = _check_tables(tf, old, new, table, free, n_free, bs, C * grow)
     _check_tables(tf, new, old, t.cpu().numpy(), f.cpu().numpy(), int(nf), bs, 0)
+
+
+# ---------------------------------------------------------------------------
+# prompt attention
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,d", [("f32", 81), ("f32", 96), ("f32", 97), ("f32", 129), ("f32", 161), ("f32", 192),
+                                     ("f32", 193), ("bf16", 91), ("bf16", 163), ("bf16", 190)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompt_widths_of_the_general_kernel(tf, dtype, d, causal):
+    print(f"general width {dtype} {d} causal={causal}", flush=True)
+    _run(tf, 90, [70, 1, 33], [70, 5, 20], 4, 2, d, dtype, causal)
+    _run(tf, 91, [3], [2500], 2, 1, d, dtype, causal)          # ranges of keys, joined
 
 
 # ---------------------------------------------------------------------------
