@@ -31,15 +31,17 @@
 // it; the others' parts go to the workspace, joined by decode_join.
 //
 // Bound by HBM where there is much to read: 64 cells of 131,000 tokens, d =
-// 128 (2.15 GB) in 367 us with the join, 5.9 TB/s; 512 cells of 800 to 10,000
-// tokens (237 MB) 44 us and 5 for the join, 58 where the cache was not read
-// just before.  8 cells of 200 to 800 tokens: 10 us, the launch and a chain of
+// 128 (2.15 GB) in 372 to 384 us with the join, 5.6 to 5.8 TB/s; 512 cells of
+// 800 to 10,000 tokens (237 MB) 60 us with the join (50 where the last-level
+// cache still holds them).  More than 16 rows of a cell read it again for every
+// 16, or 32 or 64 (launch_rows): 64 rows, d = 128, 64 cells of 20,000 to 33,000
+// tokens 188 us, where 4 rows take 80.  8 cells of 200 to 800 tokens: 10 us, the launch and a chain of
 // dependent loads (lengths, page numbers, codes).  60 cells of up to 6000
 // tokens, four float32 positions: 14 us and 5.5 for the join.
 // What the constants below measured, whole calls.  kWhole 8: the third case 18
 // us instead of 14; 128: the fourth 34 instead of 19.  kMinTiles 16: the
-// fourth 24 instead of 19; 4: the same.  kCell 0: the fourth 32 instead of 19,
-// the second 50.3 instead of 48.5; 8: the same.
+// fourth 24 instead of 19; 4: the same.  kCell 0: the fourth 33 instead of 19,
+// the second 63.4 instead of 60.5; 8: 20 and 61.6.
 #include <algorithm>
 
 #include "fw_internal.hpp"
@@ -558,18 +560,28 @@ void launch_part(const DecodeArgs &a, unsigned parts, hipStream_t st) {
     hipLaunchKernelGGL((decode_part<T, DP, RT, NW>), grid, dim3(64 * NW), 0, st, a);
 }
 
-// Row tiles of 16 per wave, as many as its registers hold without spilling:
-// further rows of a cell go to workgroups of their own, which read it again.
+// Row tiles of 16 per wave: further rows of a cell go to workgroups of their
+// own, which read it again.  One tile a wave leaves room for two workgroups a
+// compute unit, so it is taken while the second reading comes from the
+// last-level cache (256 MB), by what all tables could hold; beyond that as many
+// as a wave's registers hold.  bf16, one tile / several, in us: 64 rows, d =
+// 128, 8 cells of 300 to 900 tokens 15 / 22, 512 of up to 2000 (170 MB) 119 /
+// 122, 512 of up to 8000 (610 MB) 478 / 348; 32 rows, d = 128, 160 MB 68 / 72,
+// 600 MB 247 / 178; d = 96, 120 MB 51 / 62, 450 MB 188 / 159; d = 64, 80 MB 39 /
+// 51; 64 rows, d = 64, 85 MB 68 / 84, 550 MB 367 / 321; d = 32, two tiles, 280
+// MB 247 / 200 (four 273).  Two tiles at d = 64 gain nothing: 32 rows, 300 MB
+// 123 / 132, 550 MB 157 / 200, 1100 MB 403 / 393.
+constexpr int64_t kCached = (int64_t)256 << 20;
+
 template <typename T, int DP>
 void launch_rows(const DecodeArgs &a, unsigned parts, hipStream_t st) {
-    constexpr int most = sizeof(T) == 4 || DP > 128 ? 1 : DP > 64 ? 2 : 4;
-    if (a.R <= 16 || most == 1) {
+    constexpr int most = sizeof(T) == 4 || DP > 128 ? 1 : DP == 64 ? 4 : 2;
+    const bool cached = ((int64_t)a.C * a.W << a.shift) * 2 * DP <= kCached;
+    if (a.R <= (most == 4 ? 32 : 16) || most == 1 || cached) {
         if constexpr (DP <= (sizeof(T) == 4 ? 96 : 128)) {
             if (a.groups == 0) return launch_part<T, DP, 1, 2 * DW>(a, parts, st);
         }
         launch_part<T, DP, 1>(a, parts, st);
-    } else if (a.R <= 32 || most == 2) {
-        launch_part<T, DP, most == 1 ? 1 : 2>(a, parts, st);
     } else {
         launch_part<T, DP, most>(a, parts, st);
     }
@@ -602,9 +614,10 @@ void launch_join(const DecodeArgs &a, dim3 grid, hipStream_t st) {
 //
 // One to a compute unit (four waves, a tile ahead) reads as fast as two where a tile is 128 columns wide or more, or
 // meets more than 16 rows, and leaves half the parts to join; narrower tiles need two, except that with few cells the
-// join counts for more.  256 against 512 workgroups, in us; d = 128: 8 cells of 131,000 tokens 58 / 69, 64 of 131,000
-// 367 / 396, 256 of 800 to 10,000 33.3 / 33.0, 512 of those 51.3 / 48.5 (768 workgroups 56, 1536 57).  d = 64: 8 cells
-// of 65,000 31 / 35, 16 of 130,000 64 / 53, 64 of 32,000 63 / 48.
+// join counts for more.  256 against 512 workgroups, in us, tokens from HBM; d = 128: 8 cells of 131,000 tokens 58 / 69,
+// 64 of 131,000 385 / 400, 256 of 800 to 10,000 41.7 / 40.5, 384 of those 54.9 / 52.9, 512 of them 66 / 63 (768 workgroups
+// 56 and 1536 57 against 48.5 from the last-level cache).  d = 64: 8 cells of 65,000 31 / 35, 16 of 20,000 to 65,000 31 /
+// 38 but of 130,000 64 / 53, 64 of 20,000 to 65,000 67 / 55, 512 of 800 to 10,000 50 / 39.
 int64_t share_groups(int64_t C, int64_t R, int64_t d, int64_t W, int block_size) {
     const int64_t tiles = (W * block_size + DT - 1) / DT;
     if (tiles <= kWhole) return 0;

@@ -250,3 +250,53 @@ def test_decode_widths_and_rows_over_shared_cells(tf, dtype, d, T, G):
     assert table.shape[1] > 32                # tiles of 64 tokens: more than one workgroup takes whole
     out = _attend(tf, cache, table, q, lens, dtype, what=f"shared {dtype} d={d} T={T} G={G}")
     assert out["_ws"] is not None
+
+
+WIDE = [(128, 4, 8), (128, 8, 8), (128, 1, 17), (96, 5, 7), (64, 4, 8), (64, 8, 8), (64, 1, 33), (64, 20, 4), (32, 8, 8),
+        (32, 3, 9)]
+
+
+def _wide(table, d, bs):
+    """The table with columns of -1 up to what holds more than 256 MB of codes for its cells."""
+    dp = next(x for x in (32, 64, 96, 128) if x >= d)
+    W = (1 << 28) // (table.shape[0] * bs * 2 * dp) + 1
+    assert W > table.shape[1]
+    return np.concatenate([table, np.full((table.shape[0], W - table.shape[1]), -1)], 1)
+
+
+@pytest.mark.parametrize("d,T,G", WIDE)
+def test_decode_row_tiles_of_tables_past_the_last_level_cache(tf, d, T, G):
+    """bf16 queries of more than 16 rows a cell over tables that could hold more than 256 MB: several row tiles in a
+    wave; NaN codes that some rows see and others do not."""
+    torch, fw = tf
+    print(f"row tiles d={d} T={T} G={G}", flush=True)
+    lens = [2600, 3, 0, 700, 2049, 512, 1111, 70]
+    cache, table, q = _setup(tf, 95 + d + T, 2, T, 4, G, d, 256, lens, "bf16")
+    table = _wide(table, d, 256)
+    clean = _attend(tf, cache, table, q, lens, "bf16", what=f"row tiles d={d} T={T} G={G}")
+    if T > 1:
+        b, at = int(table[3, 699 // 256]), 699 % 256
+        cache.v[b, 5, at] = 0x7F            # the last token of cell 3, which its last position alone sees
+        got = fw.cache_attention(q.cuda(), cache, _i32(torch, table), _i32(torch, lens))
+        torch.cuda.synchronize()
+        hit = torch.zeros(got["o"].shape, dtype=torch.bool)
+        hit[0, T - 1, 3 * G:4 * G, 5] = True
+        o, c = got["o"].cpu(), clean["o"].cpu()
+        assert torch.equal(torch.isnan(o), hit) and torch.equal(o[~hit], c[~hit])
+        assert torch.equal(got["lse"], clean["lse"])
+
+
+@pytest.mark.parametrize("d,T,G", [(128, 4, 8), (96, 6, 8), (64, 8, 8), (64, 4, 5)])
+def test_decode_row_tiles_of_many_short_tables(tf, d, T, G):
+    """Tables that one workgroup takes whole, together past 256 MB."""
+    print(f"row tiles, short tables d={d} T={T} G={G}", flush=True)
+    rng = np.random.default_rng(d + T)
+    Hkv, bs = 2, 256
+    S = {64: 520, 96: 345, 128: 260}[d]
+    lens = rng.integers(0, 9, S * Hkv)
+    lens[5], lens[S] = 300, 100
+    cache, table, q = _setup(tf, 96 + d, S, T, Hkv, G, d, bs, lens, "bf16")
+    table = np.concatenate([table, np.full((S * Hkv, 8 - table.shape[1]), -1)], 1)       # 2048 tokens: 32 tiles
+    assert S * Hkv * 2048 * 2 * d > 1 << 28
+    out = _attend(tf, cache, table, q, lens, "bf16", what=f"many short tables d={d} T={T} G={G}")
+    assert out["_ws"] is None
