@@ -5,8 +5,8 @@
 //   z_rj = scale_h 2^ek(j) <q_r, code_k(j)>,   o_r = sum_j p_rj 2^ev(j) code_v(j),
 //
 // p the softmax of z over the tokens that row r sees, ek and ev the exponents
-// of token j's block.  Every code is read once for all rows of the cell and
-// is exact in bf16, so the products run on the bf16 MFMA with the codes as
+// of token j's block.  Every code is read once for 16 rows of the cell or more
+// (launch_rows) and is exact in bf16, so the products run on the bf16 MFMA with the codes as
 // they are: the block's key scale multiplies the logits, its value scale (a
 // power of two) the weights.  Float32 queries and weights are taken apart into
 // three bf16 parts, which hold all 24 bits, one product for each.  The weights
@@ -35,9 +35,9 @@
 // 800 to 10,000 tokens (237 MB) 60 us with the join (50 where the last-level
 // cache still holds them).  More than 16 rows of a cell read it again for every
 // 16, or 32 or 64 (launch_rows): 64 rows, d = 128, 64 cells of 20,000 to 33,000
-// tokens 188 us, where 4 rows take 80.  8 cells of 200 to 800 tokens: 10 us, the launch and a chain of
-// dependent loads (lengths, page numbers, codes).  60 cells of up to 6000
-// tokens, four float32 positions: 14 us and 5.5 for the join.
+// tokens 188 us, where 4 rows take 78.  8 cells of 200 to 800 tokens: 10 us,
+// the launch and a chain of dependent loads (lengths, page numbers, codes).  60
+// cells of up to 6000 tokens, four float32 positions: 14 us and 5.5 for the join.
 // What the constants below measured, whole calls.  kWhole 8: the third case 18
 // us instead of 14; 128: the fourth 34 instead of 19.  kMinTiles 16: the
 // fourth 24 instead of 19; 4: the same.  kCell 0: the fourth 33 instead of 19,

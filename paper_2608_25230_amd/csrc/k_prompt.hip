@@ -15,9 +15,9 @@
 // Two kernels share this file: `prompt_mfma` (bf16 rows of 16-byte aligned
 // strides) and `prompt_general` (any type, width and stride; float32 MFMA).
 // Measured on one MI355X: 16,384 tokens, 32 query and 8 key/value heads, d =
-// 128: 1.88 to 2.0 ms, 1100 to 1170 TFLOP/s of the visible pairs; 16 packed
-// sequences of 66 to 4096 (some with 1777 earlier keys) 523 to 538 us, 980 to
-// 1000 TFLOP/s; five float32 sequences of up to 1999, d = 80: 104 us, 74
+// 128: 1.93 to 1.99 ms, 1100 to 1140 TFLOP/s of the visible pairs; 16 packed
+// sequences of 66 to 4096 (some with 1777 earlier keys) 520 to 540 us, 980 to
+// 1010 TFLOP/s; five float32 sequences of up to 1999, d = 80: 104 us, 74
 // TFLOP/s.  A large library product reaches 1573 (bf16) and 153 (float32).
 #include <type_traits>
 
@@ -345,9 +345,10 @@ __global__ void __launch_bounds__(GTH, NT <= 5 ? 3 : 1) prompt_general(PromptArg
 // and the 4 rows of 4 chunks that it reads of the values, fill all 64 banks once
 // (no bank conflicts counted).
 //
-// What bounds it: power, as it seems.  The MFMA is busy 68 % of the cycles, and
-// the clock falls as that share rises (1.84 GHz at 54 %, 1.53 at 68 %, same
-// card), so what helped were fewer instructions per key: 32 rows a wave need 24 LDS
+// What bounds it: the softmax between the products.  The MFMA is busy 69 % of
+// the cycles at 1.62 GHz, that of a large library product 93 % at 1.69, with
+// 4.1 and 0.05 other vector instructions per MFMA one.  So what helped were fewer
+// instructions per key: 32 rows a wave need 24 LDS
 // reads, 16 exponentials, 16 fused multiply-adds, 16 additions and 8
 // conversions for 16 products, with three workgroups of 168 registers to a
 // compute unit.  On 16,384 tokens: 64-key tiles at two workgroups 2.00 to 2.07
