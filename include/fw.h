@@ -355,9 +355,9 @@ fw_status fw_maxpool_scores(const float *scores, int64_t H, int64_t n, int32_t k
  *   scale  [Hkv] float32 logit scale per key/value head, or NULL for 1/sqrt(d)
  *   causal non-zero: query i of Lq sees keys 0 .. i + Lk - Lq (the last query
  *          sees every key); zero: every key of its sequence
- *   fine_weights  bf16 rows: zero rounds each softmax weight to bf16 for the
- *          product with the values, non-zero takes it to 2^-16 (slower by up
- *          to a half); no effect on float32 rows
+ *   fine_weights  bf16 rows: zero lets each softmax weight be rounded to bf16
+ *          for the product with the values, non-zero keeps it to 2^-16 at
+ *          least (slower by up to a half); no effect on float32 rows
  * Limits: B, Hkv, d >= 1, Tq, Tk >= 0; Hkv divides Hq; d <= 256;
  * Tq*Hq < 2^31; (Tq*Hq/Hkv/64 + 1 + B)*Hkv < 2^24, and times B < 2^36 (every
  * workgroup looks through the sequences for its own); Tk <= 2^30; strides >= 0

@@ -444,8 +444,8 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal: bool = True, scale=Non
                      want_lse=True, ws=None) -> Dict[str, object]:
     """Attention of packed sequences: q [Tq][Hq][d], k and v [Tk][Hkv][d] (strided views of a fused projection are
     fine), cu_q and cu_k [B+1] int64 offsets (cu_k defaults to cu_q).  Returns o [Tq][Hq][d] of q's type and lse
-    [Tq][Hq] float32.  Rows outside the sequences are left unwritten.  bf16 rows round each softmax weight to bf16 for
-    the product with the values; fine_weights takes it to 2^-16, in up to half as much time again."""
+    [Tq][Hq] float32.  Rows outside the sequences are left unwritten.  The softmax weights of bf16 rows may be rounded
+    to bf16 for the product with the values; fine_weights keeps them to 2^-16, in up to half as much time again."""
     torch = _torch()
     guard = _elsewhere("q", q)
     if guard is not None:
