@@ -495,6 +495,177 @@ fw_status fw_cache_attention(const fw_cache *cache, int32_t dtype, const void *q
                              const int32_t *table, int64_t max_blocks, const int32_t *lens, const float *scale,
                              void *o, float *lse, void *ws, size_t ws_bytes, fw_stream stream);
 
+/* ---------------------------------------------------------------------------
+ * Around the cache while it serves: what turns queries and keys to their
+ * positions before they are attended or stored, and what lets cells shrink from
+ * the middle and share what they hold.
+ * ------------------------------------------------------------------------- */
+
+/* A projection's queries and keys, a head at a time.
+ *   q, k   [T][Hq][d], [T][Hkv][d] rows, strides q_row, q_head, k_row, k_head
+ *          in elements, columns contiguous; Hq or Hkv may be 0 (then q or k is
+ *          not read)
+ *   rot    even, 0 .. d: the first rot columns turn
+ *   pos    [T] int64 position of each token (may be negative); NULL if rot = 0
+ *   freq   [rot/2] float32 radians per position; NULL if rot = 0
+ *   interleaved  pair i is columns 2i, 2i + 1; zero: columns i, i + rot/2
+ *   norm   non-zero: each row is divided by sqrt(mean of its d squares + eps)
+ *          and multiplied by the weights before it turns
+ *   q_weight, k_weight [d] of type w_dtype, or NULL for ones
+ * Limits: T, Hq, Hkv >= 0; 1 <= d <= 256; T <= 2^25; T * (Hq + Hkv) < 2^30; strides >= 0
+ * and below 2^31; eps >= 0. */
+typedef struct fw_heads {
+    int32_t dtype;
+    const void *q, *k;
+    int64_t T, Hq, Hkv, d;
+    int64_t q_row, q_head, k_row, k_head;
+    int64_t rot;
+    const int64_t *pos;
+    const float *freq;
+    int32_t interleaved, norm;
+    float eps;
+    int32_t w_dtype;
+    const void *q_weight, *k_weight;
+} fw_heads;
+
+/* ---------------------------------------------------------------------------
+ * fw_rotate_heads -- norms and turns every head's row: pair (x, y) of angle
+ * a = pos * freq becomes (x cos a - y sin a, y cos a + x sin a).  Angles are
+ * reduced in float64 (less than 2^-50 of the angle is lost), rows computed in
+ * float32 (their squares too) and rounded once.
+ *   q_out, k_out  rows of the same type, strides qo_row .. ko_head; either may
+ *                 be its own input with its strides (in place).  Rows of an
+ *                 output must not meet each other.
+ * No workspace is used: the query returns 0 and ws may be NULL.
+ * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_DTYPE, FW_E_HIP.
+ * ------------------------------------------------------------------------- */
+size_t fw_rotate_heads_workspace_size(const fw_heads *heads);
+fw_status fw_rotate_heads(const fw_heads *heads, void *q_out, int64_t qo_row, int64_t qo_head, void *k_out,
+                          int64_t ko_row, int64_t ko_head, void *ws, size_t ws_bytes, fw_stream stream);
+
+/* ---------------------------------------------------------------------------
+ * fw_cache_scores -- the observation window's importance (Section 4) of every
+ * cached token: the mean over a cell's T * Hq/Hkv rows of the token's softmax
+ * weight exp(z - lse), 0 for rows that do not see it.  Arguments as in
+ * fw_cache_attention, of which lse is the output (keys alone are read here).
+ *   lse       [S][T][Hq] float32
+ *   earlier   [S*Hkv][n] float32 scores that are added, or NULL; may be scores
+ *   scores    [S*Hkv][n] float32 (required): token j of a cell in column j;
+ *             columns at its length and past it stay as they were, tokens past
+ *             n are not scored
+ * Tokens in a block outside [0, n_blocks) score 0.  Sums are in float32 in a
+ * fixed order.
+ * Limits: as fw_cache_attention's; 1 <= n < 2^31.
+ * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_DTYPE, FW_E_HIP.
+ * No workspace is used: the query returns 0 and ws may be NULL.
+ * ------------------------------------------------------------------------- */
+size_t fw_cache_scores_workspace_size(const fw_cache *cache, int64_t S, int64_t T, int64_t Hq, int64_t Hkv,
+                                      int64_t max_blocks);
+fw_status fw_cache_scores(const fw_cache *cache, int32_t dtype, const void *q, int64_t S, int64_t T, int64_t Hq,
+                          int64_t Hkv, int64_t q_seq, int64_t q_tok, int64_t q_head, const int32_t *table,
+                          int64_t max_blocks, const int32_t *lens, const float *scale, const float *lse,
+                          const float *earlier, float *scores, int64_t n, void *ws, size_t ws_bytes, fw_stream stream);
+
+/* ---------------------------------------------------------------------------
+ * fw_cache_select -- which tokens of every cell stay: its last `recent` ones
+ * and those of the highest scores before them, keep[c] in all (every token if
+ * the cell has no more; none if keep[c] <= 0).  Ties go to the lower position;
+ * NaN ranks highest.
+ *   scores    [C][n] float32 (fw_cache_scores, or its fw_maxpool_scores pooling)
+ *   lens, keep [C] int32 (a length is clamped to [0, n])
+ *   offsets   [C+1] int64 exclusive prefix of the kept counts (required)
+ *   kept_pos  [n_kept] int32 kept positions, ascending in each cell, cell after
+ *             cell; -1 behind the last one; those past n_kept are not listed
+ *             (required if n_kept > 0)
+ * The layout is fw_ragged_compact's, and fw_cache_compact's input.
+ * Limits: 1 <= C < 2^22; 1 <= n < 2^31 - 1024; recent >= 0; 0 <= n_kept < 2^40.
+ * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_WORKSPACE, FW_E_HIP.
+ * ------------------------------------------------------------------------- */
+size_t fw_cache_select_workspace_size(int64_t C, int64_t n);
+fw_status fw_cache_select(int64_t C, const float *scores, int64_t n, const int32_t *lens, const int32_t *keep,
+                          int64_t recent, int64_t n_kept, int64_t *offsets, int32_t *kept_pos, void *ws,
+                          size_t ws_bytes, fw_stream stream);
+
+/* Cells whose blocks may be held by several of them: fw_block_tables' arrays,
+ * and how often each block is shared.
+ *   table     [C][max_blocks] int32
+ *   lens      [C] int32 tokens of each cell
+ *   free_list [n_blocks] int32 stack of free blocks, n_free[0] int32 of them
+ *   shared    [n_blocks] int32: cells that hold the block besides its first;
+ *             all zero before the first fork, and changed by the calls below
+ *             alone.  fw_block_tables knows nothing of it: cells may grow with
+ *             it at any time, but cells that may share blocks are cut or ended
+ *             by fw_cache_release.
+ * All are in and out.  Blocks are taken from the top of the stack as it was
+ * before the call; blocks that their last cell leaves go back on it in
+ * ascending order, and are not taken again in the same call.
+ * Limits: 1 <= C < 2^22; max_blocks >= 1; max_blocks * block_size < 2^31. */
+typedef struct fw_cells {
+    int64_t C, max_blocks;
+    int32_t *table, *lens, *free_list, *n_free, *shared;
+} fw_cells;
+
+/* ---------------------------------------------------------------------------
+ * fw_cache_fork -- new cells that continue old ones: cell dst[p], which must
+ * be empty, gets the first length[p] tokens of cell src[p] (all of them if
+ * length is NULL or more).  The full blocks among these are shared; a block of
+ * which they fill a part is copied to a block of dst's own, so that both cells
+ * can go on.
+ *   P, src, dst [P] int32 cells; length [P] int32 or NULL
+ *   refused   [1] int32 pairs that were refused (required): cells out of range,
+ *             dst not empty or the dst of an earlier pair, or a copy for which,
+ *             with those of the pairs before it, too few blocks are free
+ * All pairs see the cells as they were before the call.
+ * Limits: 0 <= P < 2^22.
+ * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_WORKSPACE, FW_E_HIP.
+ * ------------------------------------------------------------------------- */
+size_t fw_cache_fork_workspace_size(const fw_cache *cache, const fw_cells *cells, int64_t P);
+fw_status fw_cache_fork(const fw_cache *cache, const fw_cells *cells, int64_t P, const int32_t *src,
+                        const int32_t *dst, const int32_t *length, int32_t *refused, void *ws, size_t ws_bytes,
+                        fw_stream stream);
+
+/* ---------------------------------------------------------------------------
+ * fw_cache_release -- cuts every cell to its first new_len tokens (0 ends it;
+ * a cell that is not longer keeps its length).  A cell whose last block is then
+ * part-filled and shared gets a copy of it, so that it can grow again.
+ *   new_len   [C] int32
+ *   refused   [1] int32 cells for whose copy, with those of the cells before
+ *             it, too few blocks are free (required); they stay as they were
+ * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_WORKSPACE, FW_E_HIP.
+ * ------------------------------------------------------------------------- */
+size_t fw_cache_release_workspace_size(const fw_cache *cache, const fw_cells *cells);
+fw_status fw_cache_release(const fw_cache *cache, const fw_cells *cells, const int32_t *new_len, int32_t *refused,
+                           void *ws, size_t ws_bytes, fw_stream stream);
+
+/* ---------------------------------------------------------------------------
+ * fw_cache_compact -- cells keep the listed tokens, moved to their front in
+ * order, and give back the blocks behind them.
+ *   P, which  [P] int32 cells, or NULL for cells 0 .. P - 1
+ *   offsets   [P+1] int64 ascending, kept_pos [n_kept] int32: cell which[p]
+ *             keeps the tokens at positions kept_pos[offsets[p]] ..
+ *             kept_pos[offsets[p+1] - 1], ascending (fw_cache_select,
+ *             fw_ragged_compact)
+ *   refused   [1] int32 cells that were refused (required) and stay as they
+ *             were: out of range or listed before; positions that do not ascend
+ *             or lie outside [0, length), or offsets outside [0, n_kept]; or
+ *             needs that, with those of the cells listed before, exceed the free
+ *             blocks.  If offsets do not ascend all are.
+ * A block whose tokens all stay where they are stays as it is.  Any other gets
+ * the least exponent that holds its tokens' finite values, as in
+ * fw_cache_store, and their codes are rounded to it (which changes a value only
+ * where it becomes subnormal; NaN stays NaN).  What lies behind a cell's last
+ * token in its block stays as it was.  No block that several cells hold is
+ * written: in its place the cell takes a free one, also for a part-filled last
+ * block whose tokens stay.
+ * Limits: 0 <= P < 2^22 (and <= C where which is NULL); 0 <= n_kept < 2^31;
+ * n_kept / block_size + 2 P < 2^23.
+ * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_WORKSPACE, FW_E_HIP.
+ * ------------------------------------------------------------------------- */
+size_t fw_cache_compact_workspace_size(const fw_cache *cache, const fw_cells *cells, int64_t P, int64_t n_kept);
+fw_status fw_cache_compact(const fw_cache *cache, const fw_cells *cells, int64_t P, const int32_t *which,
+                           const int64_t *offsets, int64_t n_kept, const int32_t *kept_pos, int32_t *refused,
+                           void *ws, size_t ws_bytes, fw_stream stream);
+
 /* Thread-local description of the calling thread's last error ("" if none). */
 const char *fw_last_error(void);
 /* Library version string. */

@@ -529,6 +529,75 @@ fw_status check_decode(int32_t block_size, int64_t S, int64_t T, int64_t Hq, int
     return FW_OK;
 }
 
+// rows [T][H][d] that a call writes: none may meet another
+bool rows_apart(int64_t T, int64_t H, int64_t d, int64_t row, int64_t head) {
+    if (T == 0 || H == 0) return true;
+    const bool heads_inside = (H == 1 || head >= d) && (T == 1 || row >= (H - 1) * head + d);
+    const bool rows_inside = (T == 1 || row >= d) && (H == 1 || head >= (T - 1) * row + d);
+    return heads_inside || rows_inside;
+}
+
+fw_status check_heads(const fw_heads *h) {
+    if (!h) return fail(FW_E_NULL, "heads is NULL");
+    if (h->dtype != FW_F32 && h->dtype != FW_BF16) return fail(FW_E_DTYPE, "unknown dtype %d", (int)h->dtype);
+    constexpr int64_t m31 = (int64_t)1 << 31, m30 = (int64_t)1 << 30;
+    if (h->T < 0 || h->Hq < 0 || h->Hkv < 0) return fail(FW_E_SHAPE, "T, Hq and Hkv must be >= 0");
+    // a workgroup of 256 threads for up to four tokens; a grid holds fewer than 2^32 threads
+    if (h->T > ((int64_t)1 << 25)) return fail(FW_E_SHAPE, "T must be <= 2^25, got %lld", (long long)h->T);
+    if (h->Hq >= m30 || h->Hkv >= m30 || (h->T > 0 && h->Hq + h->Hkv >= m30 / h->T))
+        return fail(FW_E_SHAPE, "T * (Hq + Hkv) must be < 2^30");
+    if (h->d < 1 || h->d > 256) return fail(FW_E_SHAPE, "d must be in [1, 256], got %lld", (long long)h->d);
+    if (h->rot < 0 || h->rot > h->d || h->rot % 2)
+        return fail(FW_E_SHAPE, "rot must be even and in [0, d], got %lld", (long long)h->rot);
+    const int64_t strides[] = {h->q_row, h->q_head, h->k_row, h->k_head};
+    for (int64_t s : strides)
+        if (s < 0 || s >= m31) return fail(FW_E_SHAPE, "strides must be in [0, 2^31)");
+    if (h->norm && !(h->eps >= 0.f)) return fail(FW_E_SHAPE, "eps must be >= 0");
+    if (h->norm && (h->q_weight || h->k_weight) && h->w_dtype != FW_F32 && h->w_dtype != FW_BF16)
+        return fail(FW_E_DTYPE, "unknown w_dtype %d", (int)h->w_dtype);
+    if (h->T == 0) return FW_OK;
+    if ((h->Hq > 0 && !h->q) || (h->Hkv > 0 && !h->k)) return fail(FW_E_NULL, "q or k is NULL");
+    if (h->rot > 0 && (!h->pos || !h->freq)) return fail(FW_E_NULL, "pos and freq are required");
+    return FW_OK;
+}
+
+fw_status check_cells(const fw_cache *cache, const fw_cells *t) {
+    fw_status s = check_cache(cache);
+    if (s != FW_OK) return s;
+    if (!t) return fail(FW_E_NULL, "cells is NULL");
+    if (t->C < 1 || t->C >= ((int64_t)1 << 22)) return fail(FW_E_SHAPE, "C must be in [1, 2^22), got %lld", (long long)t->C);
+    if (t->max_blocks < 1 || t->max_blocks >= ((int64_t)1 << 31) / cache->block_size)
+        return fail(FW_E_SHAPE, "need max_blocks >= 1 and max_blocks * block_size < 2^31");
+    if (!t->table || !t->lens || !t->free_list || !t->n_free || !t->shared)
+        return fail(FW_E_NULL, "cells->table, lens, free_list, n_free and shared are required");
+    return FW_OK;
+}
+
+fw_status check_fork(const fw_cache *cache, const fw_cells *cells, int64_t P) {
+    fw_status s = check_cells(cache, cells);
+    if (s != FW_OK) return s;
+    if (P < 0 || P >= ((int64_t)1 << 22)) return fail(FW_E_SHAPE, "P must be in [0, 2^22), got %lld", (long long)P);
+    return FW_OK;
+}
+
+fw_status check_cell_compact(const fw_cache *cache, const fw_cells *cells, int64_t P, int64_t n_kept) {
+    fw_status s = check_fork(cache, cells, P);
+    if (s != FW_OK) return s;
+    // a workgroup of 256 threads for each block of kept tokens and for each cell; a grid holds fewer than 2^32 threads
+    if (n_kept < 0 || n_kept >= ((int64_t)1 << 31) || n_kept / cache->block_size + 2 * P >= ((int64_t)1 << 23))
+        return fail(FW_E_SHAPE, "need 0 <= n_kept < 2^31 and n_kept / block_size + 2 P < 2^23");
+    return FW_OK;
+}
+
+fw_status check_select(int64_t C, int64_t n, int64_t recent, int64_t n_kept) {
+    if (C < 1 || C >= ((int64_t)1 << 22)) return fail(FW_E_SHAPE, "C must be in [1, 2^22), got %lld", (long long)C);
+    // a grid holds fewer than 2^32 threads: 1024 for a cell
+    if (n < 1 || n >= ((int64_t)1 << 31) - 1024) return fail(FW_E_SHAPE, "n must be in [1, 2^31 - 1024)");
+    if (recent < 0) return fail(FW_E_SHAPE, "recent must be >= 0");
+    if (n_kept < 0 || n_kept >= ((int64_t)1 << 40)) return fail(FW_E_SHAPE, "n_kept must be in [0, 2^40)");
+    return FW_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -628,6 +697,136 @@ fw_status fw_cache_attention(const fw_cache *cache, int32_t dtype, const void *q
     return hip_status(fw::launch_decode(*cache, dtype, q, S, T, Hq, Hkv, q_seq, q_tok, q_head, table, max_blocks, lens,
                                         scale, o, lse, ws, (hipStream_t)stream),
                       "fw_cache_attention");
+}
+
+// ---------------------------------------------------------------------------
+size_t fw_rotate_heads_workspace_size(const fw_heads *heads) {
+    (void)heads;
+    return 0;
+}
+
+fw_status fw_rotate_heads(const fw_heads *heads, void *q_out, int64_t qo_row, int64_t qo_head, void *k_out,
+                          int64_t ko_row, int64_t ko_head, void *ws, size_t ws_bytes, fw_stream stream) {
+    (void)ws;
+    (void)ws_bytes;
+    fw_status s = check_heads(heads);
+    if (s != FW_OK) return s;
+    constexpr int64_t m31 = (int64_t)1 << 31;
+    const int64_t strides[] = {qo_row, qo_head, ko_row, ko_head};
+    for (int64_t x : strides)
+        if (x < 0 || x >= m31) return fail(FW_E_SHAPE, "strides must be in [0, 2^31)");
+    if (!rows_apart(heads->T, heads->Hq, heads->d, qo_row, qo_head) || !rows_apart(heads->T, heads->Hkv, heads->d, ko_row, ko_head))
+        return fail(FW_E_SHAPE, "rows of an output meet each other");
+    if (heads->T == 0 || heads->Hq + heads->Hkv == 0) return FW_OK;
+    if ((heads->Hq > 0 && !q_out) || (heads->Hkv > 0 && !k_out)) return fail(FW_E_NULL, "q_out or k_out is NULL");
+    if ((heads->Hq > 0 && q_out == heads->q && (qo_row != heads->q_row || qo_head != heads->q_head)) ||
+        (heads->Hkv > 0 && k_out == heads->k && (ko_row != heads->k_row || ko_head != heads->k_head)))
+        return fail(FW_E_SHAPE, "an output in its input's place needs its strides");
+    return hip_status(fw::launch_rotate(*heads, q_out, qo_row, qo_head, k_out, ko_row, ko_head, (hipStream_t)stream),
+                      "fw_rotate_heads");
+}
+
+// ---------------------------------------------------------------------------
+size_t fw_cache_scores_workspace_size(const fw_cache *cache, int64_t S, int64_t T, int64_t Hq, int64_t Hkv,
+                                      int64_t max_blocks) {
+    (void)cache;
+    (void)S;
+    (void)T;
+    (void)Hq;
+    (void)Hkv;
+    (void)max_blocks;
+    return 0;
+}
+
+fw_status fw_cache_scores(const fw_cache *cache, int32_t dtype, const void *q, int64_t S, int64_t T, int64_t Hq,
+                          int64_t Hkv, int64_t q_seq, int64_t q_tok, int64_t q_head, const int32_t *table,
+                          int64_t max_blocks, const int32_t *lens, const float *scale, const float *lse,
+                          const float *earlier, float *scores, int64_t n, void *ws, size_t ws_bytes, fw_stream stream) {
+    (void)ws;
+    (void)ws_bytes;
+    fw_status s = check_cache(cache);
+    if (s != FW_OK) return s;
+    if (dtype != FW_F32 && dtype != FW_BF16) return fail(FW_E_DTYPE, "unknown dtype %d", (int)dtype);
+    if ((s = check_decode(cache->block_size, S, T, Hq, Hkv, max_blocks)) != FW_OK) return s;
+    constexpr int64_t m31 = (int64_t)1 << 31;
+    if (q_seq < 0 || q_tok < 0 || q_head < 0 || q_seq >= m31 || q_tok >= m31 || q_head >= m31)
+        return fail(FW_E_SHAPE, "strides must be in [0, 2^31)");
+    if (n < 1 || n >= m31) return fail(FW_E_SHAPE, "n must be in [1, 2^31)");
+    if (!q || !table || !lens || !lse || !scores) return fail(FW_E_NULL, "q, table, lens, lse and scores are required");
+    return hip_status(fw::launch_cache_scores(*cache, dtype, q, S, T, Hq, Hkv, q_seq, q_tok, q_head, table, max_blocks,
+                                              lens, scale, lse, earlier, scores, n, (hipStream_t)stream),
+                      "fw_cache_scores");
+}
+
+// ---------------------------------------------------------------------------
+size_t fw_cache_select_workspace_size(int64_t C, int64_t n) {
+    (void)C;
+    (void)n;
+    return 0;
+}
+
+fw_status fw_cache_select(int64_t C, const float *scores, int64_t n, const int32_t *lens, const int32_t *keep,
+                          int64_t recent, int64_t n_kept, int64_t *offsets, int32_t *kept_pos, void *ws,
+                          size_t ws_bytes, fw_stream stream) {
+    (void)ws;
+    (void)ws_bytes;
+    fw_status s = check_select(C, n, recent, n_kept);
+    if (s != FW_OK) return s;
+    if (!scores || !lens || !keep || !offsets) return fail(FW_E_NULL, "scores, lens, keep and offsets are required");
+    if (n_kept > 0 && !kept_pos) return fail(FW_E_NULL, "kept_pos is NULL");
+    return hip_status(fw::launch_select_cells(C, scores, n, lens, keep, recent, n_kept, offsets, kept_pos,
+                                              (hipStream_t)stream),
+                      "fw_cache_select");
+}
+
+// ---------------------------------------------------------------------------
+size_t fw_cache_fork_workspace_size(const fw_cache *cache, const fw_cells *cells, int64_t P) {
+    if (check_fork(cache, cells, P) != FW_OK) return 0;
+    return fw::pages_ws_bytes(*cache, *cells, 1, P, 0);
+}
+
+fw_status fw_cache_fork(const fw_cache *cache, const fw_cells *cells, int64_t P, const int32_t *src,
+                        const int32_t *dst, const int32_t *length, int32_t *refused, void *ws, size_t ws_bytes,
+                        fw_stream stream) {
+    fw_status s = check_fork(cache, cells, P);
+    if (s != FW_OK) return s;
+    if (!refused || (P > 0 && (!src || !dst))) return fail(FW_E_NULL, "src, dst and refused are required");
+    if ((s = check_ws(ws, ws_bytes, fw::pages_ws_bytes(*cache, *cells, 1, P, 0))) != FW_OK) return s;
+    return hip_status(fw::launch_fork(*cache, *cells, P, src, dst, length, refused, ws, (hipStream_t)stream),
+                      "fw_cache_fork");
+}
+
+size_t fw_cache_release_workspace_size(const fw_cache *cache, const fw_cells *cells) {
+    if (check_cells(cache, cells) != FW_OK) return 0;
+    return fw::pages_ws_bytes(*cache, *cells, 0, 0, 0);
+}
+
+fw_status fw_cache_release(const fw_cache *cache, const fw_cells *cells, const int32_t *new_len, int32_t *refused,
+                           void *ws, size_t ws_bytes, fw_stream stream) {
+    fw_status s = check_cells(cache, cells);
+    if (s != FW_OK) return s;
+    if (!new_len || !refused) return fail(FW_E_NULL, "new_len and refused are required");
+    if ((s = check_ws(ws, ws_bytes, fw::pages_ws_bytes(*cache, *cells, 0, 0, 0))) != FW_OK) return s;
+    return hip_status(fw::launch_release(*cache, *cells, new_len, refused, ws, (hipStream_t)stream), "fw_cache_release");
+}
+
+size_t fw_cache_compact_workspace_size(const fw_cache *cache, const fw_cells *cells, int64_t P, int64_t n_kept) {
+    if (check_cell_compact(cache, cells, P, n_kept) != FW_OK) return 0;
+    return fw::pages_ws_bytes(*cache, *cells, 2, P, n_kept);
+}
+
+fw_status fw_cache_compact(const fw_cache *cache, const fw_cells *cells, int64_t P, const int32_t *which,
+                           const int64_t *offsets, int64_t n_kept, const int32_t *kept_pos, int32_t *refused,
+                           void *ws, size_t ws_bytes, fw_stream stream) {
+    fw_status s = check_cell_compact(cache, cells, P, n_kept);
+    if (s != FW_OK) return s;
+    if (!which && P > cells->C) return fail(FW_E_SHAPE, "P = %lld cells of %lld", (long long)P, (long long)cells->C);
+    if (!refused || (P > 0 && !offsets)) return fail(FW_E_NULL, "offsets and refused are required");
+    if (n_kept > 0 && !kept_pos) return fail(FW_E_NULL, "kept_pos is NULL");
+    if ((s = check_ws(ws, ws_bytes, fw::pages_ws_bytes(*cache, *cells, 2, P, n_kept))) != FW_OK) return s;
+    return hip_status(fw::launch_cell_compact(*cache, *cells, P, which, offsets, n_kept, kept_pos, refused, ws,
+                                              (hipStream_t)stream),
+                      "fw_cache_compact");
 }
 
 }  // extern "C"

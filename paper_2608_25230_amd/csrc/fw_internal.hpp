@@ -114,4 +114,26 @@ hipError_t launch_decode(const fw_cache &cache, int dtype, const void *q, int64_
                          int64_t q_seq, int64_t q_tok, int64_t q_head, const int32_t *table, int64_t W,
                          const int32_t *lens, const float *scale, void *o, float *lse, void *ws, hipStream_t st);
 
+// k_rotate.hip -- norm and rotation of queries and keys
+hipError_t launch_rotate(const fw_heads &heads, void *q_out, int64_t qo_row, int64_t qo_head, void *k_out, int64_t ko_row,
+                         int64_t ko_head, hipStream_t st);
+
+// k_scores.hip -- scores of cached tokens and the choice among them
+hipError_t launch_cache_scores(const fw_cache &cache, int dtype, const void *q, int64_t S, int64_t T, int64_t Hq,
+                               int64_t Hkv, int64_t q_seq, int64_t q_tok, int64_t q_head, const int32_t *table,
+                               int64_t W, const int32_t *lens, const float *scale, const float *lse,
+                               const float *earlier, float *scores, int64_t n, hipStream_t st);
+hipError_t launch_select_cells(int64_t C, const float *scores, int64_t n, const int32_t *lens, const int32_t *keep,
+                               int64_t recent, int64_t n_kept, int64_t *offsets, int32_t *kept_pos, hipStream_t st);
+
+// k_pages.hip -- cells that share blocks (kind 0: release, 1: fork of P pairs, 2: compaction of P cells)
+size_t pages_ws_bytes(const fw_cache &cache, const fw_cells &cells, int kind, int64_t P, int64_t n_kept);
+hipError_t launch_release(const fw_cache &cache, const fw_cells &cells, const int32_t *new_len, int32_t *refused,
+                          void *ws, hipStream_t st);
+hipError_t launch_fork(const fw_cache &cache, const fw_cells &cells, int64_t P, const int32_t *src, const int32_t *dst,
+                       const int32_t *length, int32_t *refused, void *ws, hipStream_t st);
+hipError_t launch_cell_compact(const fw_cache &cache, const fw_cells &cells, int64_t P, const int32_t *which,
+                               const int64_t *offsets, int64_t n_kept, const int32_t *kept_pos, int32_t *refused,
+                               void *ws, hipStream_t st);
+
 }  // namespace fw

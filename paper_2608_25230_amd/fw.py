@@ -19,7 +19,9 @@ STATUS = {0: "FW_OK", 1: "FW_E_NULL", 2: "FW_E_SHAPE", 3: "FW_E_DTYPE", 4: "FW_E
           5: "FW_E_WORKSPACE", 6: "FW_E_HIP"}
 ENTRY_POINTS = ("fw_dense_topk", "fw_best_subset", "fw_swap", "fw_dropped_mass_curve",
                 "fw_ragged_compact", "fw_pool_subset", "fw_group_vote", "fw_maxpool_scores",
-                "fw_prompt_attention", "fw_block_tables", "fw_cache_store", "fw_cache_attention")
+                "fw_prompt_attention", "fw_block_tables", "fw_cache_store", "fw_cache_attention",
+                "fw_rotate_heads", "fw_cache_scores", "fw_cache_select", "fw_cache_fork", "fw_cache_release",
+                "fw_cache_compact")
 # entry points that take no workspace: their scratch is a static device array
 NOALLOC_ENTRY_POINTS = ("fw_dense_topk_noalloc",)
 # columns of fw_pool_subset's stats (FW_POOL_* in include/fw.h)
@@ -54,12 +56,29 @@ class Cache(ctypes.Structure):
                 ("n_blocks", ctypes.c_int64), ("d", ctypes.c_int64), ("block_size", ctypes.c_int32)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("T", ctypes.c_int64),
+                ("Hq", ctypes.c_int64), ("Hkv", ctypes.c_int64), ("d", ctypes.c_int64), ("q_row", ctypes.c_int64),
+                ("q_head", ctypes.c_int64), ("k_row", ctypes.c_int64), ("k_head", ctypes.c_int64),
+                ("rot", ctypes.c_int64), ("pos", ctypes.c_void_p), ("freq", ctypes.c_void_p),
+                ("interleaved", ctypes.c_int32), ("norm", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("w_dtype", ctypes.c_int32), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
+
+
+class Cells(ctypes.Structure):
+    _fields_ = [("C", ctypes.c_int64), ("max_blocks", ctypes.c_int64), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("free_list", ctypes.c_void_p), ("n_free", ctypes.c_void_p),
+                ("shared", ctypes.c_void_p)]
+
+
 _lib = None
 P = ctypes.c_void_p
 I32, I64, SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 RP = ctypes.POINTER(Rows)
 PP = ctypes.POINTER(Packed)
 CP = ctypes.POINTER(Cache)
+HP = ctypes.POINTER(Heads)
+LP = ctypes.POINTER(Cells)
 
 _SIGS = {
     "fw_dense_topk_workspace_size": (SZ, [RP, P, I32]),
@@ -88,6 +107,18 @@ _SIGS = {
     "fw_cache_store": (I32, [CP, I32, P, I64, P, I64, I64, P, P, SZ, P]),
     "fw_cache_attention_workspace_size": (SZ, [CP, I64, I64, I64, I64, I64]),
     "fw_cache_attention": (I32, [CP, I32, P, I64, I64, I64, I64, I64, I64, I64, P, I64, P, P, P, P, P, SZ, P]),
+    "fw_rotate_heads_workspace_size": (SZ, [HP]),
+    "fw_rotate_heads": (I32, [HP, P, I64, I64, P, I64, I64, P, SZ, P]),
+    "fw_cache_scores_workspace_size": (SZ, [CP, I64, I64, I64, I64, I64]),
+    "fw_cache_scores": (I32, [CP, I32, P, I64, I64, I64, I64, I64, I64, I64, P, I64, P, P, P, P, P, I64, P, SZ, P]),
+    "fw_cache_select_workspace_size": (SZ, [I64, I64]),
+    "fw_cache_select": (I32, [I64, P, I64, P, P, I64, I64, P, P, P, SZ, P]),
+    "fw_cache_fork_workspace_size": (SZ, [CP, LP, I64]),
+    "fw_cache_fork": (I32, [CP, LP, I64, P, P, P, P, P, SZ, P]),
+    "fw_cache_release_workspace_size": (SZ, [CP, LP]),
+    "fw_cache_release": (I32, [CP, LP, P, P, P, SZ, P]),
+    "fw_cache_compact_workspace_size": (SZ, [CP, LP, I64, I64]),
+    "fw_cache_compact": (I32, [CP, LP, I64, P, P, I64, P, P, P, SZ, P]),
     "fw_last_error": (ctypes.c_char_p, []),
     "fw_version": (ctypes.c_char_p, []),
 }
@@ -606,6 +637,265 @@ def cache_attention(q, cache: KvCache, table, lens, *, scale=None, want_lse=True
                                 lens.data_ptr(), _ptr(scale), o.data_ptr(), _ptr(lse), _ptr(ws),
                                 0 if ws is None else ws.numel(), _stream_of(q.get_device())))
     return {"o": o, "lse": lse, "_ws": ws}
+
+
+# ---------------------------------------------------------------------------
+# serving: positions, scores of cached tokens, cells that are compacted and share blocks
+# ---------------------------------------------------------------------------
+
+def rotate_heads(q, k, positions, freq, *, eps=None, q_weight=None, k_weight=None, interleaved: bool = False,
+                 out=None) -> Dict[str, object]:
+    """Queries q [T][Hq][d] and keys k [T][Hkv][d] (strided views of a fused projection are fine; k may be None)
+    normed, if eps is given, by the root of their mean square and the weights [d] (None: ones), and turned to their
+    positions [T] int64 by freq [rot/2] float32 radians a position (both None: not turned).  Pairs are columns i and
+    i + rot/2, or 2 i and 2 i + 1 if interleaved.  Returns q and k, new or in out = (q_out, k_out), which may be the
+    inputs."""
+    torch = _torch()
+    guard = _elsewhere("q", q)
+    if guard is not None:
+        with guard:
+            return rotate_heads(q, k, positions, freq, eps=eps, q_weight=q_weight, k_weight=k_weight,
+                                interleaved=interleaved, out=out)
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(q)
+    _rows_of("q", q, dt, 3, dev)
+    T, Hq, d = q.shape
+    Hkv = k_row = k_head = 0
+    if k is not None:
+        _rows_of("k", k, dt, 3, dev)
+        Hkv = k.shape[1]
+        if k.shape[0] != T or k.shape[2] != d:
+            raise FwError(2, f"k must be [{T}][Hkv][{d}], got {tuple(k.shape)}")
+        k_row, k_head, _ = k.stride()
+    rot = 0
+    if freq is not None:
+        _want("freq", freq, torch.float32, 1, dev)
+        _want("positions", positions, torch.int64, 1, dev)
+        rot = 2 * freq.shape[0]
+        if positions.shape[0] != T:
+            raise FwError(2, f"positions must be [{T}], got {tuple(positions.shape)}")
+    elif positions is not None:
+        raise FwError(2, "positions need freq")
+    w_code = 0
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is None:
+            continue
+        if eps is None:
+            raise FwError(2, f"{name} needs eps")
+        _want(name, w, w.dtype, 1, dev)
+        w_code = _dtype_code(w)
+        if w.shape[0] != d:
+            raise FwError(2, f"{name} must be [{d}], got {tuple(w.shape)}")
+    if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
+        raise FwError(2, "q_weight and k_weight must be of one type")
+    if out is None:
+        qo = q.new_empty((T, Hq, d))
+        ko = None if k is None else k.new_empty((T, Hkv, d))
+    else:
+        qo, ko = out
+        _rows_of("out q", qo, dt, 3, dev)
+        if qo.shape != q.shape or (ko is None) != (k is None):
+            raise FwError(2, "out must be (q_out, k_out) like q and k")
+        if ko is not None:
+            _rows_of("out k", ko, dt, 3, dev)
+            if ko.shape != k.shape:
+                raise FwError(2, "out must be (q_out, k_out) like q and k")
+    ko_row, ko_head = (0, 0) if ko is None else ko.stride()[:2]
+    q_row, q_head, _ = q.stride()
+    h = Heads(code, q.data_ptr(), _ptr(k), T, Hq, Hkv, d, q_row, q_head, k_row, k_head, rot,
+              _ptr(positions), _ptr(freq), 1 if interleaved else 0, 0 if eps is None else 1,
+              0.0 if eps is None else eps, w_code, _ptr(q_weight), _ptr(k_weight))
+    _check(lib().fw_rotate_heads(ctypes.byref(h), qo.data_ptr(), qo.stride(0), qo.stride(1), _ptr(ko), ko_row, ko_head,
+                                 None, 0, _stream_of(q.get_device())))
+    return {"q": qo, "k": ko}
+
+
+def cache_scores(q, cache: KvCache, table, lens, lse, *, scale=None, earlier=None, scores=None) -> Dict[str, object]:
+    """The mean softmax weight of every cached token over the rows of its cell: q [S][T][Hq][d], table, lens and scale
+    as in ``cache_attention``, lse [S][T][Hq] from it.  Returns scores [S*Hkv][n] float32: in `scores`, whose columns
+    from a cell's length on stay as they were, or new ones of n = max_blocks * block_size, zero there.  earlier: scores
+    of the same shape (or the same tensor) that are added."""
+    torch = _torch()
+    guard = _elsewhere("q", q)
+    if guard is not None:
+        with guard:
+            return cache_scores(q, cache, table, lens, lse, scale=scale, earlier=earlier, scores=scores)
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(q)
+    _rows_of("q", q, dt, 4, dev)
+    _want("table", table, torch.int32, 2, dev)
+    _want("lens", lens, torch.int32, 1, dev)
+    _want("lse", lse, torch.float32, 3, dev)
+    S, T, Hq, d = q.shape
+    C, W = table.shape
+    if S < 1 or C % S or lens.shape[0] != C or d != cache.d or lse.shape != (S, T, Hq):
+        raise FwError(2, f"table must be [S*Hkv][max_blocks], lens [S*Hkv], q [S][T][Hq][{cache.d}] and lse [S][T][Hq], got "
+                         f"{tuple(table.shape)}, {tuple(lens.shape)}, {tuple(q.shape)}, {tuple(lse.shape)}")
+    Hkv = C // S
+    if scale is not None:
+        _want("scale", scale, torch.float32, 1, dev)
+        if scale.shape[0] != Hkv:
+            raise FwError(2, f"scale must be [{Hkv}]")
+    c = _cache(cache, dev)
+    if scores is None:
+        shape = (C, W * cache.block_size) if earlier is None else earlier.shape
+        scores = q.new_zeros(shape, dtype=torch.float32)
+    for name, t in (("scores", scores), ("earlier", earlier)):
+        if t is not None:
+            _want(name, t, torch.float32, 2, dev)
+            if t.shape[0] != C or t.shape[1] != scores.shape[1]:
+                raise FwError(2, f"{name} must be [{C}][n], got {tuple(t.shape)}")
+    q_seq, q_tok, q_head, _ = q.stride()
+    _check(lib().fw_cache_scores(ctypes.byref(c), code, q.data_ptr(), S, T, Hq, Hkv, q_seq, q_tok, q_head,
+                                 table.data_ptr(), W, lens.data_ptr(), _ptr(scale), lse.data_ptr(), _ptr(earlier),
+                                 scores.data_ptr(), scores.shape[1], None, 0, _stream_of(q.get_device())))
+    return {"scores": scores}
+
+
+def cache_select(scores, lens, keep, *, recent: int = 0, n_kept: int) -> Dict[str, object]:
+    """Which tokens of every cell stay: keep [C] int32 of them, the last `recent` and the best of scores [C][n] before
+    those (ties to the lower position).  n_kept: the sum of what is kept, or an upper bound.  Returns offsets [C+1]
+    int64 and kept_pos [n_kept] int32, ascending in each cell, -1 behind the last one."""
+    torch = _torch()
+    guard = _elsewhere("scores", scores)
+    if guard is not None:
+        with guard:
+            return cache_select(scores, lens, keep, recent=recent, n_kept=n_kept)
+    dev = scores.device
+    _want("scores", scores, torch.float32, 2, dev)
+    _want("lens", lens, torch.int32, 1, dev)
+    _want("keep", keep, torch.int32, 1, dev)
+    C, n = scores.shape
+    if lens.shape[0] != C or keep.shape[0] != C:
+        raise FwError(2, f"lens and keep must be [{C}], got {tuple(lens.shape)}, {tuple(keep.shape)}")
+    if n_kept < 0:
+        raise FwError(2, "n_kept must be >= 0")
+    L = lib()
+    offsets = lens.new_empty(C + 1, dtype=torch.int64)
+    pos = lens.new_empty(n_kept)
+    need = L.fw_cache_select_workspace_size(C, n)
+    ws = lens.new_empty(need, dtype=torch.uint8) if need else None
+    _check(L.fw_cache_select(C, scores.data_ptr(), n, lens.data_ptr(), keep.data_ptr(), recent, n_kept,
+                             offsets.data_ptr(), pos.data_ptr(), _ptr(ws), need, _stream_of(scores.get_device())))
+    return {"offsets": offsets, "kept_pos": pos}
+
+
+class CacheCells(NamedTuple):
+    """Cells of a cache whose blocks several of them may hold (fw_cells in include/fw.h): table [C][max_blocks], lens
+    [C], free_list [n_blocks], n_free [1] and shared [n_blocks], all torch.int32, changed in place.  ``cache_cells``
+    makes empty ones; ``block_tables`` lets them grow."""
+    table: Any
+    lens: Any
+    free_list: Any
+    n_free: Any
+    shared: Any
+
+
+def cache_cells(C: int, max_blocks: int, n_blocks: int, device="cuda") -> CacheCells:
+    torch = _torch()
+    i32 = dict(dtype=torch.int32, device=device)
+    return CacheCells(torch.full((C, max_blocks), -1, **i32), torch.zeros(C, **i32),
+                      torch.arange(n_blocks - 1, -1, -1, **i32), torch.full((1,), n_blocks, **i32),
+                      torch.zeros(n_blocks, **i32))
+
+
+def _cells(t: CacheCells, cache: KvCache, device) -> Cells:
+    i32 = _torch().int32
+    _want("cells.table", t.table, i32, 2, device)
+    for name in ("lens", "free_list", "n_free", "shared"):
+        _want("cells." + name, getattr(t, name), i32, 1, device)
+    C, W = t.table.shape
+    n = cache.k.shape[0]
+    if t.lens.shape[0] != C or t.free_list.shape[0] != n or t.n_free.shape[0] != 1 or t.shared.shape[0] != n:
+        raise FwError(2, f"the cells' arrays do not fit together: table {tuple(t.table.shape)}, lens {tuple(t.lens.shape)}, "
+                         f"free_list {tuple(t.free_list.shape)}, n_free {tuple(t.n_free.shape)}, shared "
+                         f"{tuple(t.shared.shape)}, {n} blocks")
+    return Cells(C, W, t.table.data_ptr(), t.lens.data_ptr(), t.free_list.data_ptr(), t.n_free.data_ptr(),
+                 t.shared.data_ptr())
+
+
+def _space(need: int, ws, like):
+    """The caller's workspace if it is large enough, else a new one."""
+    torch = _torch()
+    if ws is not None:
+        _want("ws", ws, torch.uint8, 1, like.device)
+        if ws.numel() >= need:
+            return ws
+    return like.new_empty(need, dtype=torch.uint8)
+
+
+def cache_fork(cache: KvCache, cells: CacheCells, src, dst, *, length=None, ws=None) -> Dict[str, object]:
+    """Empty cells dst [P] int32 continue cells src [P] from their first length [P] tokens (None: all): full blocks are
+    shared, a part-filled one is copied.  Returns refused [1] int32."""
+    torch = _torch()
+    guard = _elsewhere("cells.table", cells.table)
+    if guard is not None:
+        with guard:
+            return cache_fork(cache, cells, src, dst, length=length, ws=ws)
+    dev = cells.table.device
+    c, t = _cache(cache, dev), _cells(cells, cache, dev)
+    for name, x in (("src", src), ("dst", dst), ("length", length)):
+        if x is not None:
+            _want(name, x, torch.int32, 1, dev)
+            if x.shape != src.shape:
+                raise FwError(2, f"{name} must be [{src.shape[0]}], got {tuple(x.shape)}")
+    L, P_ = lib(), src.shape[0]
+    refs = ctypes.byref(c), ctypes.byref(t)
+    refused = torch.empty_like(cells.n_free)
+    ws = _space(L.fw_cache_fork_workspace_size(*refs, P_), ws, cells.table)
+    _check(L.fw_cache_fork(*refs, P_, src.data_ptr(), dst.data_ptr(), _ptr(length), refused.data_ptr(), ws.data_ptr(),
+                           ws.numel(), _stream_of(cells.table.get_device())))
+    return {"refused": refused, "_ws": ws}
+
+
+def cache_release(cache: KvCache, cells: CacheCells, new_len, *, ws=None) -> Dict[str, object]:
+    """Cuts every cell to new_len [C] int32 tokens (0 ends it; a cell that is not longer stays); blocks that no other
+    cell holds go back.  Returns refused [1] int32."""
+    torch = _torch()
+    guard = _elsewhere("cells.table", cells.table)
+    if guard is not None:
+        with guard:
+            return cache_release(cache, cells, new_len, ws=ws)
+    dev = cells.table.device
+    c, t = _cache(cache, dev), _cells(cells, cache, dev)
+    _want("new_len", new_len, torch.int32, 1, dev)
+    if new_len.shape[0] != t.C:
+        raise FwError(2, f"new_len must be [{t.C}], got {tuple(new_len.shape)}")
+    L = lib()
+    refs = ctypes.byref(c), ctypes.byref(t)
+    refused = torch.empty_like(cells.n_free)
+    ws = _space(L.fw_cache_release_workspace_size(*refs), ws, cells.table)
+    _check(L.fw_cache_release(*refs, new_len.data_ptr(), refused.data_ptr(), ws.data_ptr(), ws.numel(),
+                              _stream_of(cells.table.get_device())))
+    return {"refused": refused, "_ws": ws}
+
+
+def cache_compact(cache: KvCache, cells: CacheCells, offsets, kept_pos, *, which=None, ws=None) -> Dict[str, object]:
+    """Cells which [P] int32 (None: all, or the first P) keep the tokens at kept_pos[offsets[p]:offsets[p + 1]]
+    (``cache_select``, ``ragged_compact``), moved to their front; the blocks behind go back.  Returns refused [1]
+    int32."""
+    torch = _torch()
+    guard = _elsewhere("cells.table", cells.table)
+    if guard is not None:
+        with guard:
+            return cache_compact(cache, cells, offsets, kept_pos, which=which, ws=ws)
+    dev = cells.table.device
+    c, t = _cache(cache, dev), _cells(cells, cache, dev)
+    _want("offsets", offsets, torch.int64, 1, dev)
+    _want("kept_pos", kept_pos, torch.int32, 1, dev)
+    P_ = offsets.shape[0] - 1
+    if which is not None:
+        _want("which", which, torch.int32, 1, dev)
+    if P_ < 0 or (which is not None and which.shape[0] != P_):
+        raise FwError(2, f"offsets must be [P+1] and which [P], got {tuple(offsets.shape)}, "
+                         f"{None if which is None else tuple(which.shape)}")
+    L, n = lib(), kept_pos.shape[0]
+    refs = ctypes.byref(c), ctypes.byref(t)
+    refused = torch.empty_like(cells.n_free)
+    ws = _space(L.fw_cache_compact_workspace_size(*refs, P_, n), ws, cells.table)
+    _check(L.fw_cache_compact(*refs, P_, _ptr(which), offsets.data_ptr(), n, kept_pos.data_ptr(), refused.data_ptr(),
+                              ws.data_ptr(), ws.numel(), _stream_of(cells.table.get_device())))
+    return {"refused": refused, "_ws": ws}
 
 
 # ---------------------------------------------------------------------------
