@@ -578,7 +578,8 @@ fw_status fw_cache_scores(const fw_cache *cache, int32_t dtype, const void *q, i
  *             cell; -1 behind the last one; those past n_kept are not listed
  *             (required if n_kept > 0)
  * The layout is fw_ragged_compact's, and fw_cache_compact's input.
- * Limits: 1 <= C < 2^22; 1 <= n < 2^31 - 1024; recent >= 0; 0 <= n_kept < 2^40.
+ * Limits: C >= 1; 1 <= n < 2^31 - 65536; C * (n / 8192 + 1) < 2^22; recent >= 0;
+ * 0 <= n_kept < 2^40.
  * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_WORKSPACE, FW_E_HIP.
  * ------------------------------------------------------------------------- */
 size_t fw_cache_select_workspace_size(int64_t C, int64_t n);
@@ -657,8 +658,8 @@ fw_status fw_cache_release(const fw_cache *cache, const fw_cells *cells, const i
  * token in its block stays as it was.  No block that several cells hold is
  * written: in its place the cell takes a free one, also for a part-filled last
  * block whose tokens stay.
- * Limits: 0 <= P < 2^22 (and <= C where which is NULL); 0 <= n_kept < 2^31;
- * n_kept / block_size + 2 P < 2^23.
+ * Limits: P >= 0 (and <= C where which is NULL); n_kept >= 0;
+ * n_kept / 256 + P < 2^22.
  * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_WORKSPACE, FW_E_HIP.
  * ------------------------------------------------------------------------- */
 size_t fw_cache_compact_workspace_size(const fw_cache *cache, const fw_cells *cells, int64_t P, int64_t n_kept);

@@ -583,16 +583,17 @@ fw_status check_fork(const fw_cache *cache, const fw_cells *cells, int64_t P) {
 fw_status check_cell_compact(const fw_cache *cache, const fw_cells *cells, int64_t P, int64_t n_kept) {
     fw_status s = check_fork(cache, cells, P);
     if (s != FW_OK) return s;
-    // a workgroup of 256 threads for each block of kept tokens and for each cell; a grid holds fewer than 2^32 threads
-    if (n_kept < 0 || n_kept >= ((int64_t)1 << 31) || n_kept / cache->block_size + 2 * P >= ((int64_t)1 << 23))
-        return fail(FW_E_SHAPE, "need 0 <= n_kept < 2^31 and n_kept / block_size + 2 P < 2^23");
+    // two workgroups of 512 threads for every 256 kept tokens of a cell; a grid holds fewer than 2^32 threads
+    if (n_kept < 0 || n_kept / 256 + P >= ((int64_t)1 << 22))
+        return fail(FW_E_SHAPE, "need n_kept >= 0 and n_kept / 256 + P < 2^22");
     return FW_OK;
 }
 
 fw_status check_select(int64_t C, int64_t n, int64_t recent, int64_t n_kept) {
     if (C < 1 || C >= ((int64_t)1 << 22)) return fail(FW_E_SHAPE, "C must be in [1, 2^22), got %lld", (long long)C);
-    // a grid holds fewer than 2^32 threads: 1024 for a cell
-    if (n < 1 || n >= ((int64_t)1 << 31) - 1024) return fail(FW_E_SHAPE, "n must be in [1, 2^31 - 1024)");
+    if (n < 1 || n >= ((int64_t)1 << 31) - 65536) return fail(FW_E_SHAPE, "n must be in [1, 2^31 - 65536)");
+    // a grid holds fewer than 2^32 threads: 1024 for a cell, and for 8192 of its tokens where rows are long
+    if (C * (n / 8192 + 1) >= ((int64_t)1 << 22)) return fail(FW_E_SHAPE, "C * (n / 8192 + 1) must be < 2^22");
     if (recent < 0) return fail(FW_E_SHAPE, "recent must be >= 0");
     if (n_kept < 0 || n_kept >= ((int64_t)1 << 40)) return fail(FW_E_SHAPE, "n_kept must be in [0, 2^40)");
     return FW_OK;
@@ -760,21 +761,19 @@ fw_status fw_cache_scores(const fw_cache *cache, int32_t dtype, const void *q, i
 
 // ---------------------------------------------------------------------------
 size_t fw_cache_select_workspace_size(int64_t C, int64_t n) {
-    (void)C;
-    (void)n;
-    return 0;
+    if (check_select(C, n, 0, 0) != FW_OK) return 0;
+    return fw::select_ws_bytes(C, n);
 }
 
 fw_status fw_cache_select(int64_t C, const float *scores, int64_t n, const int32_t *lens, const int32_t *keep,
                           int64_t recent, int64_t n_kept, int64_t *offsets, int32_t *kept_pos, void *ws,
                           size_t ws_bytes, fw_stream stream) {
-    (void)ws;
-    (void)ws_bytes;
     fw_status s = check_select(C, n, recent, n_kept);
     if (s != FW_OK) return s;
     if (!scores || !lens || !keep || !offsets) return fail(FW_E_NULL, "scores, lens, keep and offsets are required");
     if (n_kept > 0 && !kept_pos) return fail(FW_E_NULL, "kept_pos is NULL");
-    return hip_status(fw::launch_select_cells(C, scores, n, lens, keep, recent, n_kept, offsets, kept_pos,
+    if ((s = check_ws(ws, ws_bytes, fw::select_ws_bytes(C, n))) != FW_OK) return s;
+    return hip_status(fw::launch_select_cells(C, scores, n, lens, keep, recent, n_kept, offsets, kept_pos, ws,
                                               (hipStream_t)stream),
                       "fw_cache_select");
 }

@@ -124,7 +124,9 @@ hipError_t launch_cache_scores(const fw_cache &cache, int dtype, const void *q, 
                                int64_t W, const int32_t *lens, const float *scale, const float *lse,
                                const float *earlier, float *scores, int64_t n, hipStream_t st);
 hipError_t launch_select_cells(int64_t C, const float *scores, int64_t n, const int32_t *lens, const int32_t *keep,
-                               int64_t recent, int64_t n_kept, int64_t *offsets, int32_t *kept_pos, hipStream_t st);
+                               int64_t recent, int64_t n_kept, int64_t *offsets, int32_t *kept_pos, void *ws,
+                               hipStream_t st);
+size_t select_ws_bytes(int64_t C, int64_t n);
 
 // k_pages.hip -- cells that share blocks (kind 0: release, 1: fork of P pairs, 2: compaction of P cells)
 size_t pages_ws_bytes(const fw_cache &cache, const fw_cells &cells, int kind, int64_t P, int64_t n_kept);

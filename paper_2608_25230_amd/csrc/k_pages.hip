@@ -2,12 +2,11 @@
 // and fw_cache_compact.
 //
 // shared[b] counts the cells that hold block b besides its first.  A cell that
-// leaves a block takes one off; who finds 0 was the last, and marks the block
-// with -1.  The marked blocks go on the stack in ascending order, so the result
-// does not depend on who came last: collect_blocks finds their places from how
-// many each run of kRun blocks has (counted as they are marked).  Blocks that a
-// call takes come from the stack as it was before, so nothing that is still
-// read in a call is written in it.
+// leaves a block takes one off; who finds none was the last, and sets the
+// block's bit.  The marked blocks go on the stack in ascending order, so the
+// result does not depend on who came last: collect_blocks finds their places by
+// counting bits.  Blocks that a call takes come from the stack as it was
+// before, so no block that others hold is written.
 #include <algorithm>
 
 #include "fw_internal.hpp"
@@ -19,15 +18,14 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int PT = 1024;    // threads of the one workgroup that serves cells in order
 constexpr int WT = 256;     // threads of the others
-constexpr int kRun = 4096;  // blocks whose marks are counted together
+constexpr int kRun = 16 * WT;  // blocks that one workgroup puts back
 
 struct PageHead {
     int64_t top, left;  // free blocks before the call, and without those it takes
-    int32_t ok;
 };
 
 struct PageArgs {
-    int64_t C, W, n_blocks, P, n_kept, nruns;
+    int64_t C, W, n_blocks, P, n_kept, nruns, chunks;
     int shift, bs, d, dp;
     int32_t *table, *lens, *free_list, *n_free, *shared, *refused;
     uint8_t *kc, *vc, *k_exp, *v_exp;
@@ -35,11 +33,17 @@ struct PageArgs {
     const int64_t *offsets;
     // workspace
     PageHead *head;
-    int32_t *counts;      // [nruns] marked blocks of each run
+    uint16_t *marks;      // [nruns][WT] a bit for each block that its last cell left
+    int32_t *counts;      // [nruns] how many, where runs are many
     int32_t *claim;       // [C] the first pair or listed cell that names a cell
     int4 *plan;           // [max(C, P)] per cell, pair or listed cell
-    int32_t *rank;        // [tiles] compaction: rank among its cell's taken blocks, or -1
-    uint8_t *staged, *staged_exp;  // [tiles][2][bs * dp], [tiles][2]
+    // compaction
+    int32_t *rank;        // [blocks kept] rank among the blocks that the cell takes, or -1
+    int32_t *owner;       // [chunks] listed cell, or -1
+    int32_t *within;      // [chunks] of the cell's kept tokens, the first that lies in or behind the chunk's own positions
+    int32_t *read;        // [2][chunks] set once the chunk's keys, and values, have been read
+    int32_t *tickets;     // [2][kQueues][kApart] chunks handed out, of keys and of values
+    int32_t *starts;      // [kQueues + 1] first chunk of each queue; all equal if nothing moves
 };
 
 __device__ __forceinline__ int64_t length_of(const PageArgs &a, int64_t c) {
@@ -78,7 +82,10 @@ __device__ __forceinline__ int64_t sum_before(int64_t v, int64_t *red, int64_t *
 }
 
 __device__ __forceinline__ void leave_block(const PageArgs &a, int32_t b) {
-    if (is_block(a, b) && atomicSub(&a.shared[b], 1) == 0) atomicAdd(&a.counts[b / kRun], 1);
+    if (!is_block(a, b)) return;
+    if (atomicSub(&a.shared[b], 1) > 0) return;
+    __hip_atomic_store(&a.shared[b], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    atomicOr((uint32_t *)a.marks + (b >> 5), 1u << (b & 31));
 }
 
 // A block's codes and exponents, by a workgroup.
@@ -121,51 +128,55 @@ __device__ __forceinline__ void serve(const PageArgs &a, int64_t n, const Need &
     __syncthreads();
     if (threadIdx.x == 0) {
         a.refused[0] = refused;
-        a.head[0] = PageHead{top, top - (int64_t)taken, 1};
+        a.head[0] = PageHead{top, top - (int64_t)taken};
     }
 }
 __device__ __forceinline__ int32_t fresh_block(const PageArgs &a, int64_t top, int64_t rank) { return a.free_list[top - 1 - rank]; }
 
-__device__ __forceinline__ void clear_counts(const PageArgs &a) {
-    for (int64_t i = threadIdx.x; i < a.nruns; i += blockDim.x) a.counts[i] = 0;
+// by workgroup b of nb
+__device__ __forceinline__ void clear_marks(const PageArgs &a, int64_t b, int64_t nb) {
+    for (int64_t i = b * blockDim.x + threadIdx.x; i < a.nruns * (WT / 4); i += nb * blockDim.x) ((uint64_t *)a.marks)[i] = 0;
 }
 
-// Marked blocks of a run onto the stack.
+// Runs up to which collect_blocks counts the marks of those before its own from their bits; many have their numbers
+// counted first, and marks that many workgroups clear.
+constexpr int64_t kFewRuns = 64;
+
+__global__ void __launch_bounds__(WT) clear_all(PageArgs a) { clear_marks(a, blockIdx.x, gridDim.x); }
+
+__global__ void __launch_bounds__(WT) count_runs(PageArgs a) {
+    __shared__ int64_t red[WT / 64];
+    int64_t all;
+    sum_before<WT>(__popc(a.marks[(int64_t)blockIdx.x * WT + threadIdx.x]), red, &all);
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = (int32_t)all;
+}
+
+// A run's marked blocks onto the stack.
 __global__ void __launch_bounds__(WT) collect_blocks(PageArgs a) {
     __shared__ int64_t red[WT / 64];
     const int64_t run = blockIdx.x;
-    const bool last = run == a.nruns - 1;
-    const int mine = a.counts[run];
-    if (mine == 0 && !last) return;
-    int64_t before = 0, upto;
-    for (int64_t i = threadIdx.x; i < run; i += WT) before += a.counts[i];
+    int64_t before = 0, upto, here;
+    if (a.nruns <= kFewRuns)
+        for (int64_t i = threadIdx.x; i < run * (WT / 4); i += WT) before += __popcll(((const uint64_t *)a.marks)[i]);
+    else
+        for (int64_t i = threadIdx.x; i < run; i += WT) before += a.counts[i];
+    uint32_t m = a.marks[run * WT + threadIdx.x];
     sum_before<WT>(before, red, &upto);
-    int64_t at = a.head[0].left + upto;
-    if (last && threadIdx.x == 0) {
-        const int64_t n = at + mine;
+    int64_t at = a.head[0].left + upto + sum_before<WT>(__popc(m), red, &here);
+    if (run == a.nruns - 1 && threadIdx.x == 0) {
+        const int64_t n = a.head[0].left + upto + here;
         a.n_free[0] = (int32_t)(n < a.n_blocks ? n : a.n_blocks);
     }
-    if (mine == 0) return;
-    constexpr int E = kRun / WT;
-    const int64_t b0 = run * kRun + threadIdx.x * E;
-    int n = 0;
-    for (int i = 0; i < E; ++i) n += b0 + i < a.n_blocks && a.shared[b0 + i] < 0;
-    int64_t total;
-    at += sum_before<WT>(n, red, &total);
-    if (n == 0) return;
-    for (int i = 0; i < E; ++i)
-        if (b0 + i < a.n_blocks && a.shared[b0 + i] < 0) {
-            a.shared[b0 + i] = 0;
-            if (at < a.n_blocks) a.free_list[at] = (int32_t)(b0 + i);
-            ++at;
-        }
+    const int64_t b0 = 16 * (run * WT + threadIdx.x);
+    for (; m; m &= m - 1, ++at)
+        if (at < a.n_blocks) a.free_list[at] = (int32_t)(b0 + __builtin_ctz(m));
 }
 
 // ---------------------------------------------------------------------------
 // release: plan = (blocks kept, blocks held, block for the copy or -1, served)
 // ---------------------------------------------------------------------------
 __global__ void __launch_bounds__(PT) release_plan(PageArgs a) {
-    clear_counts(a);
+    if (a.nruns <= kFewRuns) clear_marks(a, 0, 1);
     const auto cut = [&](int64_t c, int64_t *old) {
         *old = length_of(a, c);
         const int64_t n = a.new_len[c] > 0 ? a.new_len[c] : 0;
@@ -272,35 +283,79 @@ __global__ void __launch_bounds__(WT) fork_apply(PageArgs a) {
 // ---------------------------------------------------------------------------
 // compaction
 //
-// The tokens that a listed cell keeps fall into tiles of one block each.  Tile j
-// of listed cell p is number offsets[p] / bs + p + j: ascending offsets leave
-// room for every cell's tiles, so none needs to be counted before.
-// plan = (tokens kept or -1, first tile that changes, blocks to take, first of them)
+// The tokens that a listed cell keeps fall into chunks of kChunk, one or more
+// blocks each.  Chunk j of listed cell p is number offsets[p] / kChunk + p + j
+// (and block j number offsets[p] / bs + p + j): ascending offsets leave room for
+// every cell's chunks, so none needs to be counted before.
+// plan = (tokens kept or -1, first block that changes, blocks to take, first of them)
+//
+// Tokens move inside their cell's own blocks, towards the front, so a chunk's
+// blocks may be written once the chunks that keep tokens of them, none of them
+// behind the chunk itself, have read theirs.  compact_move has a workgroup for
+// each chunk's keys and one for its values; each takes its chunk by ticket,
+// reads all it needs into LDS, says so, waits for the chunks before it that read
+// its blocks, and writes.  Tickets come from queues of whole cells, each in the
+// order of its chunks.  So who is waited for holds an earlier ticket of the same
+// queue, has started, and waits for nobody before it says that it has read:
+// every wait ends.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ int64_t cell_of(const PageArgs &a, int64_t p) { return a.which ? a.which[p] : p; }
-__device__ __forceinline__ int64_t tile0(const PageArgs &a, int64_t p) { return (a.offsets[p] >> a.shift) + p; }
+constexpr int CT = 1024;     // threads that look through a cell's list
+constexpr int MT = 512;      // threads that move a chunk
+constexpr int kChunk = 256;  // tokens
+constexpr int kChunkShift = 8;
+constexpr int kQueues = 32;  // of keys, and as many of values
+constexpr int kApart = 64;   // counters lie in lines of their own
 
-__global__ void __launch_bounds__(WT) compact_check(PageArgs a) {
-    __shared__ int64_t red[WT / 64];
+__device__ __forceinline__ int64_t cell_of(const PageArgs &a, int64_t p) { return a.which ? a.which[p] : p; }
+__device__ __forceinline__ int64_t block0(const PageArgs &a, int64_t p) { return (a.offsets[p] >> a.shift) + p; }
+__device__ __forceinline__ int64_t chunk0(const PageArgs &a, int64_t p) { return (a.offsets[p] >> kChunkShift) + p; }
+
+__global__ void __launch_bounds__(CT) compact_check(PageArgs a) {
+    __shared__ int64_t red[CT / 64];
     const int64_t p = blockIdx.x, c = cell_of(a, p);
     const int64_t o = a.offsets[p], e = a.offsets[p + 1], n = e - o;
+    const int tid = threadIdx.x;
+    clear_marks(a, p, a.P);
+    for (int64_t i = p * CT + tid; i < 2 * a.chunks; i += a.P * CT) a.read[i] = 0;
+    if (p == 0 && tid < 2 * kQueues) a.tickets[tid * kApart] = 0;
     bool bad = c < 0 || c >= a.C || o < 0 || e > a.n_kept || n < 0;
     const int64_t len = bad ? 0 : length_of(a, c);
     bad = bad || n > len;
+    // chunks of no cell before the first, behind this one's, and behind the last
+    const auto clamp = [&](int64_t t) { return t < 0 ? 0 : t > a.chunks ? a.chunks : t; };
+    const int64_t t0 = chunk0(a, p), t1 = bad ? t0 : t0 + ((n + kChunk - 1) >> kChunkShift);
+    const int64_t next = p + 1 < a.P ? chunk0(a, p + 1) : a.chunks;
+    if (p == 0)
+        for (int64_t t = tid; t < clamp(t0); t += CT) a.owner[t] = -1;
+    for (int64_t t = clamp(t0) + tid; t < clamp(next); t += CT) a.owner[t] = t < t1 ? (int32_t)p : -1;
     int64_t stay = 0;
-    if (!bad)
-        for (int64_t i = threadIdx.x; i < n; i += WT) {
-            const int64_t x = a.kept_pos[o + i], y = i > 0 ? a.kept_pos[o + i - 1] : -1;
-            bad = bad || x <= y || x >= len;
-            stay += x == i;
+    if (!bad) {
+        const int32_t *pos = a.kept_pos + o;
+        const int64_t last = ((n + kChunk - 1) >> kChunkShift) - 1;
+        for (int64_t i0 = 4 * tid; i0 < n; i0 += 4 * CT) {
+            int64_t z[5];
+#pragma unroll
+            for (int u = 0; u < 5; ++u) z[u] = i0 + u == 0 ? -1 : pos[i0 + u - 1 < n ? i0 + u - 1 : n - 1];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t i = i0 + u, x = z[u + 1], y = z[u];
+                if (i >= n) break;
+                bad = bad || x <= y || x >= len || x < i;
+                if (bad) break;
+                stay += x == i;
+                // chunks of positions that begin behind the token before and not behind this one
+                for (int64_t b = y < 0 ? 0 : (y >> kChunkShift) + 1; b <= x >> kChunkShift && b <= last; ++b)
+                    a.within[t0 + b] = (int32_t)i;
+            }
         }
+    }
     bad = __syncthreads_or(bad);
     if (bad) {
-        if (threadIdx.x == 0) a.plan[p] = make_int4(-1, 0, 0, 0);
+        if (tid == 0) a.plan[p] = make_int4(-1, 0, 0, 0);
         return;
     }
     int64_t fixed;
-    sum_before<WT>(stay, red, &fixed);  // positions ascend: the tokens that stay come first
+    sum_before<CT>(stay, red, &fixed);  // positions ascend: the tokens that stay come first
     const int32_t *row = a.table + c * a.W;
     int64_t first = fixed >> a.shift;
     if (fixed == n && (n & (a.bs - 1))) {
@@ -308,21 +363,20 @@ __global__ void __launch_bounds__(WT) compact_check(PageArgs a) {
         if (!is_block(a, b) || a.shared[b] <= 0) ++first;
     }
     int64_t take = 0;
-    const int64_t t0 = tile0(a, p);
-    for (int64_t j0 = first; j0 < nb(a, n); j0 += WT) {
-        const int64_t j = j0 + threadIdx.x;
+    const int64_t b0 = block0(a, p);
+    for (int64_t j0 = first; j0 < nb(a, n); j0 += CT) {
+        const int64_t j = j0 + tid;
         const int32_t b = j < nb(a, n) ? row[j] : -1;
         const bool other = is_block(a, b) && a.shared[b] > 0;
         int64_t all;
-        const int64_t before = sum_before<WT>(other, red, &all);
-        if (j < nb(a, n)) a.rank[t0 + j] = other ? (int32_t)(take + before) : -1;
+        const int64_t before = sum_before<CT>(other, red, &all);
+        if (j < nb(a, n)) a.rank[b0 + j] = other ? (int32_t)(take + before) : -1;
         take += all;
     }
-    if (threadIdx.x == 0) a.plan[p] = make_int4((int)n, (int)first, (int)take, 0);
+    if (tid == 0) a.plan[p] = make_int4((int)n, (int)first, (int)take, 0);
 }
 
 __global__ void __launch_bounds__(PT) compact_plan(PageArgs a) {
-    clear_counts(a);
     if (a.which) claim_cells(a, a.P, a.which);
     bool down = false;
     for (int64_t p = threadIdx.x; p < a.P; p += PT) down = down || a.offsets[p] > a.offsets[p + 1];
@@ -337,176 +391,321 @@ __global__ void __launch_bounds__(PT) compact_plan(PageArgs a) {
               if (!served) a.plan[p].x = -1;
               else a.plan[p].w = (int)first;
           });
-    if (threadIdx.x == 0) a.head[0].ok = !down;
+    // queue i begins with the first cell whose chunks begin at i / kQueues of all or behind; the first with chunk 0
+    if (down && threadIdx.x <= kQueues) a.starts[threadIdx.x] = 0;
+    for (int64_t p = threadIdx.x; p <= a.P && !down; p += PT) {
+        const int64_t t = p < a.P ? chunk0(a, p) : a.chunks, before = p > 0 ? chunk0(a, p - 1) : -1;
+        for (int64_t i = before < 0 ? 0 : before * kQueues / a.chunks; i <= kQueues; ++i) {
+            const int64_t at = i * a.chunks / kQueues;
+            if (at > t) break;
+            if (at > before) a.starts[i] = i == 0 ? 0 : (int32_t)t;
+        }
+    }
 }
 
-// The listed cell that a tile belongs to, and its number there.
-__device__ __forceinline__ bool find_tile(const PageArgs &a, int64_t t, int64_t *p, int64_t *j) {
-    int64_t lo = 0, hi = a.P - 1;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        if (tile0(a, mid) <= t) lo = mid;
-        else hi = mid - 1;
-    }
-    const int4 x = a.plan[lo];
-    *p = lo, *j = t - tile0(a, lo);
-    return x.x >= 0 && *j >= x.y && *j < nb(a, x.x);
-}
-
-// The largest finite magnitude of four codes, as a code.
-__device__ __forceinline__ int top_code(uint32_t x, int top) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = (x >> (8 * i)) & 0x7F;
-        top = c != 0x7F && c > top ? c : top;
-    }
-    return top;
-}
-// The least exponent byte for a magnitude `code` at exponent byte e; 0 for zero.
-__device__ __forceinline__ int least_exp(int code, int e) {
-    if (code == 0) return 0;
-    const float v = __builtin_amdgcn_cvt_pk_f32_fp8(code, false)[0];
+// A code's magnitude in an order with 0 below 1, NaN below all (four bytes at a time).
+__device__ __forceinline__ uint32_t magnitudes(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x7F7F7F7Fu; }
+// The least exponent byte for a magnitude (as above) at exponent byte e; 0 for zero.
+__device__ __forceinline__ int least_exp(int magnitude, int e) {
+    if (magnitude < 2) return 0;
+    const float v = __builtin_amdgcn_cvt_pk_f32_fp8(magnitude - 1, false)[0];
     int x;
     const float m = frexpf(v, &x);  // 448 = 7/8 2^9
     return x - 9 + (m > 0.875f) + e;
-}
-__device__ __forceinline__ uint32_t scale_codes(uint32_t c, float s) {
-    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
-    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(a[0] * s, a[1] * s, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b[0] * s, b[1] * s, r, true);
 }
 __device__ __forceinline__ float exp_ratio(int from, int to) {  // 2^(from - to): codes that are not 0 stay in range
     const int e = from - to;
     return __uint_as_float((uint32_t)(127 + (e < -126 ? -126 : e > 127 ? 127 : e)) << 23);
 }
+__device__ __forceinline__ uint32_t scale_codes(uint32_t c, float s0, float s1, float s2, float s3) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(a[0] * s0, a[1] * s1, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b[0] * s2, b[1] * s3, r, true);
+}
 __device__ __forceinline__ int exp_byte(uint8_t e) { return e < 1 ? 1 : e > 253 ? 253 : e; }
-
-// One tile's keys (blockIdx.y = 0) or values to the workspace, at their new exponent.
-__global__ void __launch_bounds__(WT) compact_gather(PageArgs a) {
-    extern __shared__ __align__(16) uint8_t lds[];
-    __shared__ int32_t blk[256];
-    __shared__ int16_t off[256];
-    __shared__ int16_t ex[256];
-    __shared__ int red[WT / 64];
-    int64_t p, j;
-    if (!a.head[0].ok || !find_tile(a, blockIdx.x, &p, &j)) return;
-    const bool values = blockIdx.y;
-    const int tid = threadIdx.x;
-    const int64_t n = a.plan[p].x, c = cell_of(a, p);
-    const int m = n - (j << a.shift) < a.bs ? (int)(n - (j << a.shift)) : a.bs;
-    const uint8_t *codes = values ? a.vc : a.kc, *exps = values ? a.v_exp : a.k_exp;
-    if (tid < a.bs) {
-        int32_t b = -1;
-        int x = 0, e = 1;
-        if (tid < m) {
-            x = a.kept_pos[a.offsets[p] + (j << a.shift) + tid];
-            b = a.table[c * a.W + (x >> a.shift)];
-            if (is_block(a, b)) e = exp_byte(exps[b]);
-            else b = -1;
-        }
-        blk[tid] = b, off[tid] = (int16_t)(x & (a.bs - 1)), ex[tid] = (int16_t)e;
-    }
-    __syncthreads();
-    const int64_t size = (int64_t)a.bs * a.dp;
-    int best = 0;
-    if (!values) {
-        const int per = a.dp / 16;
-        for (int i = tid; i < m * per; i += WT) {
-            const int t = i / per, x = i - t * per;
-            uint4 y = {0u, 0u, 0u, 0u};
-            if (blk[t] >= 0) y = *(const uint4 *)(codes + blk[t] * size + off[t] * a.dp + 16 * x);
-            *(uint4 *)(lds + 16 * i) = y;
-            best = max(best, least_exp(top_code(y.x, top_code(y.y, top_code(y.z, top_code(y.w, 0)))), ex[t]));
-        }
-    } else {
-        const int per = a.bs / 4;
-        for (int i = tid; i < a.dp * per; i += WT) {
-            const int r = i / per, t = 4 * (i - r * per);
-            uint32_t y = 0;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (t + u >= m || blk[t + u] < 0) continue;
-                const uint32_t z = codes[blk[t + u] * size + (int64_t)r * a.bs + off[t + u]];
-                y |= z << (8 * u);
-                best = max(best, least_exp(top_code(z, 0), ex[t + u]));
-            }
-            *(uint32_t *)(lds + 4 * i) = y;
-        }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) best = max(best, __shfl_xor(best, o));
-    if ((tid & 63) == 0) red[tid >> 6] = best;
-    __syncthreads();
-    best = 1;
-#pragma unroll
-    for (int i = 0; i < WT / 64; ++i) best = max(best, red[i]);
-    best = min(best, 253);
-    uint8_t *out = a.staged + (2 * (int64_t)blockIdx.x + values) * size;
-    if (tid == 0) a.staged_exp[2 * (int64_t)blockIdx.x + values] = (uint8_t)best;
-    if (!values) {
-        for (int i = tid; i < m * a.dp / 4; i += WT)
-            ((uint32_t *)out)[i] = scale_codes(((uint32_t *)lds)[i], exp_ratio(ex[4 * i / a.dp], best));
-    } else {
-        const int per = a.bs / 4;
-        for (int i = tid; i < a.dp * per; i += WT) {
-            const int t = 4 * (i % per);
-            const uint32_t x = ((uint32_t *)lds)[i];
-            uint32_t y = 0;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) y |= (scale_codes((x >> (8 * u)) & 0xFFu, exp_ratio(ex[t + u], best)) & 0xFFu) << (8 * u);
-            ((uint32_t *)out)[i] = y;
-        }
-    }
+__device__ __forceinline__ uint32_t max_bytes(uint32_t x, uint32_t y) {  // bytes below 0x80
+    const uint32_t more = ((x | 0x80808080u) - y) & 0x80808080u;          // where x >= y
+    const uint32_t keep = more - (more >> 7) | more;
+    return (x & keep) | (y & ~keep);
 }
 
-// Tiles from the workspace to their blocks; the workgroups behind them give back the blocks past the cells' ends.
-__global__ void __launch_bounds__(WT) compact_write(PageArgs a, int64_t tiles) {
-    const int tid = threadIdx.x;
-    if (!a.head[0].ok) return;
-    if (blockIdx.x >= tiles) {
-        if (blockIdx.y) return;
-        const int64_t p = blockIdx.x - tiles;
-        const int4 x = a.plan[p];
-        if (x.x < 0) return;
-        const int64_t c = cell_of(a, p), had = nb(a, length_of(a, c));
-        int32_t *row = a.table + c * a.W;
-        for (int64_t j = nb(a, x.x) + tid; j < had; j += WT) {
-            leave_block(a, row[j]);
-            row[j] = -1;
-        }
-        __syncthreads();  // everyone has read the length
-        if (tid == 0) a.lens[c] = x.x;
-        return;
-    }
-    int64_t p, j;
-    if (!find_tile(a, blockIdx.x, &p, &j)) return;
-    const bool values = blockIdx.y;
-    const int4 x = a.plan[p];
-    const int m = x.x - (j << a.shift) < a.bs ? (int)(x.x - (j << a.shift)) : a.bs;
-    int32_t *entry = a.table + cell_of(a, p) * a.W + j;
-    const int32_t r = a.rank[blockIdx.x];
-    // where a block is taken, the entry is this tile's keys' to change; its values do not need it
-    const int32_t b = r >= 0 ? fresh_block(a, a.head[0].top, x.w + r) : *entry;
-    if (!is_block(a, b)) return;
-    const int64_t size = (int64_t)a.bs * a.dp;
-    const uint8_t *in = a.staged + (2 * (int64_t)blockIdx.x + values) * size;
-    uint8_t *out = (values ? a.vc : a.kc) + b * size;
-    if (!values || m == a.bs) {
-        const int bytes = values ? (int)size : m * a.dp;
-        for (int i = tid; i < bytes / 16; i += WT) ((uint4 *)out)[i] = ((const uint4 *)in)[i];
-    } else {
-        for (int i = tid; i < a.dp * m; i += WT) {
-            const int y = i / m, t = i - y * m;
-            out[y * a.bs + t] = in[y * a.bs + t];
-        }
-    }
+// LDS: a chunk's codes, keys [token][dp] or values [dp][kChunk + 4] (the padding spreads a column over the banks).
+//
+// Values lie tokens innermost, so whole blocks are read for the tokens that
+// stay.  A wave takes 64 rows of a block, a lane each, and up to 64 tokens of a
+// row at a time, all in flight together: its line of memory is fetched once.
+// Which bytes of a word stay is the same for every row, so words are packed by
+// byte permutes whose selectors, made once, the whole wave shares.
+__global__ void __launch_bounds__(MT) compact_move(PageArgs a) {
+    extern __shared__ __align__(16) uint8_t lds[];
+    __shared__ int32_t blk[kChunk];      // keys: a token's block; values: the block of a group of up to 64 tokens
+    __shared__ int32_t info[kChunk];     // keys: its place there; values: words of the group that keep tokens, 16 its place
+    __shared__ __align__(16) uint32_t sel_a[kChunk];  // values: a word's bytes into the output word that it joins
+    __shared__ uint32_t sel_b[kChunk];   // its bytes for the word after, if it fills that one, else 0
+    __shared__ int16_t ex[kChunk];
+    __shared__ int32_t to[kChunk / 16];
+    __shared__ int least[kChunk / 16];
+    __shared__ int32_t s_ticket, s_count[2][kChunk / 64], s_first[2][8];
+    float *const ratio = (float *)sel_a;  // once the tokens are packed
+    uint32_t *const top = sel_b;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (tid == 0) {
-        (values ? a.v_exp : a.k_exp)[b] = a.staged_exp[2 * (int64_t)blockIdx.x + values];
-        if (!values && r >= 0) {
-            leave_block(a, *entry);
-            *entry = b;
+        s_ticket = -1;
+        for (int i = 0; i < 2 * kQueues && s_ticket < 0; ++i) {
+            const int q = (blockIdx.x + i) % (2 * kQueues), half = q >= kQueues, x = q - half * kQueues;
+            const int32_t first = a.starts[x], n = a.starts[x + 1] - first;
+            if (n <= 0) continue;
+            if (i > 0 && __hip_atomic_load(&a.tickets[q * kApart], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >= n) continue;
+            const int32_t got = atomicAdd(&a.tickets[q * kApart], 1);
+            if (got < n) s_ticket = 2 * (first + got) + half;
         }
     }
+    if (tid < kChunk / 16) least[tid] = 1;
+    __syncthreads();
+    if (s_ticket < 0) return;  // nothing moves: there are as many tickets as workgroups
+    const int64_t chunk = s_ticket >> 1;
+    const bool values = s_ticket & 1;
+    const int32_t p = a.owner[chunk];
+    if (p < 0) return;
+    const int4 x = a.plan[p];
+    const int64_t o = a.offsets[p], t0 = (o >> kChunkShift) + p, j = chunk - t0;
+    // this chunk's tokens in blocks that change
+    const int lo = (int)max((int64_t)x.y * a.bs - j * kChunk, (int64_t)0), hi = (int)min(x.x - j * kChunk, (int64_t)kChunk);
+    if (lo >= hi) return;
+    const int32_t *row = a.table + cell_of(a, p) * a.W;
+    const uint8_t *codes = values ? a.vc : a.kc, *exps = values ? a.v_exp : a.k_exp;
+    const int64_t size = (int64_t)a.bs * a.dp;
+    // where each token lies
+    const bool mine = tid >= lo && tid < hi;
+    int b = -1, off = 0, e = 1;
+    if (mine) {
+        const int y = a.kept_pos[o + j * kChunk + tid];
+        b = row[y >> a.shift];
+        off = y & (a.bs - 1);
+        if (is_block(a, b)) e = exp_byte(exps[b]);
+        else b = -1;
+    }
+    if (tid < kChunk) ex[tid] = (int16_t)e;
+    // where each block goes
+    if (tid >= MT - kChunk / 16 && ((tid - (MT - kChunk / 16)) << a.shift) < hi) {
+        const int y = tid - (MT - kChunk / 16);
+        const int64_t n = ((j << kChunkShift) >> a.shift) + y;
+        int32_t t = -1;
+        if (n >= x.y) {
+            const int32_t r = a.rank[(o >> a.shift) + p + n];
+            t = r >= 0 ? a.free_list[a.head[0].top - 1 - (x.w + r)] : row[n];
+        }
+        to[y] = is_block(a, t) ? t : -1;
+    }
+    constexpr int vrow = kChunk + 4;
+    if (!values) {
+        if (tid < kChunk) blk[tid] = b, info[tid] = off, top[tid] = 0;
+        __syncthreads();
+        const int per = a.dp / 16, n = hi * per;
+        for (int i0 = lo * per + tid; i0 < n; i0 += 4 * MT) {
+            uint4 z[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * MT, t = i < n ? i / per : lo;
+                z[u] = make_uint4(0u, 0u, 0u, 0u);
+                if (i < n && blk[t] >= 0) z[u] = *(const uint4 *)(codes + blk[t] * size + info[t] * a.dp + 16 * (i - t * per));
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * MT;
+                if (i >= n) break;
+                *(uint4 *)(lds + 16 * i) = z[u];
+                const uint32_t m = max_bytes(max_bytes(magnitudes(z[u].x), magnitudes(z[u].y)),
+                                             max_bytes(magnitudes(z[u].z), magnitudes(z[u].w)));
+                atomicMax(&top[i / per], max(max(m & 0xFFu, (m >> 8) & 0xFFu), max((m >> 16) & 0xFFu, m >> 24)));
+            }
+        }
+    } else {
+        // The tokens are cut into parts of at most 64; a part's tokens fall into words of four neighbours and groups of 64
+        // in their blocks.  The first token of a word or group stands for it.
+        const int groups = (a.dp + 63) / 64, parts = groups == 1 ? 8 : 4, per = kChunk / parts;
+        int2 *const place = (int2 *)lds;  // before any codes lie there
+        const int at = b < 0 ? 4 * tid : off;  // in a block that is none each token has a word of its own
+        if (tid < kChunk) place[tid] = make_int2(mine ? b : -2, at), info[tid] = 0;
+        __syncthreads();
+        const bool edge = tid == lo || (tid & (per - 1)) == 0;
+        const int2 prev = mine && !edge ? place[tid - 1] : make_int2(-3, 0);
+        const bool first_w = mine && (prev.x != b || prev.y >> 2 != at >> 2);
+        const bool first_g = mine && (prev.x != b || b < 0 || prev.y >> 6 != at >> 6);
+        const uint64_t bw = __ballot(first_w), bg = __ballot(first_g);
+        if (lane == 0 && w < kChunk / 64) s_count[0][w] = __popcll(bw), s_count[1][w] = __popcll(bg);
+        __syncthreads();
+        const uint64_t upto = (2ull << lane) - 1;
+        int nw = __popcll(bw & upto) - 1, ng = __popcll(bg & upto) - 1, words = 0, spans = 0;
+#pragma unroll
+        for (int i = 0; i < kChunk / 64; ++i) {
+            if (i < w) nw += s_count[0][i], ng += s_count[1][i];
+            words += s_count[0][i], spans += s_count[1][i];
+        }
+        if (first_g) blk[ng] = b;
+        if (mine) atomicOr(&info[ng], 1 << ((off >> 2) & 15) | (first_g ? off >> 6 << 16 : 0));
+        if (first_w) {
+            // the bytes of this word that stay, in order, and how many
+            uint32_t bytes = at & 3;
+            int k = 1;
+            for (int i = tid + 1; k < 4 && i < hi && (i & (per - 1)) && place[i].x == b && place[i].y >> 2 == at >> 2; ++i, ++k)
+                bytes |= (uint32_t)(place[i].y & 3) << (8 * k);
+            const int fill = tid & 3;  // bytes of the output word that are there already
+            uint32_t sa = 0, sb = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int on = i - fill, up = i + 4 - fill;
+                sa |= (i < fill ? 4u + i : on < k ? (bytes >> (8 * on)) & 0xFFu : 0x0Cu) << (8 * i);
+                sb |= (up < k ? (bytes >> (8 * up)) & 0xFFu : 0x0Cu) << (8 * i);
+            }
+            sel_a[nw] = sa, sel_b[nw] = fill + k >= 4 ? sb : 0u;
+        }
+        if (tid < kChunk && (tid & (per - 1)) == 0) {
+            // a part's first word and group: those of its first token, none before `lo`, all behind `hi`
+            s_first[0][tid / per] = tid < lo ? 0 : tid < hi ? nw : words;
+            s_first[1][tid / per] = tid < lo ? 0 : tid < hi ? ng : spans;
+        }
+        __syncthreads();
+        for (int y = w; y < groups * parts; y += MT / 64) {
+            const int gr = y / parts, part = y - gr * parts, r = 64 * gr + lane, start = max(part * per, lo);
+            const int stop = min((part + 1) * per, hi);
+            if (start >= stop) continue;
+            int word = __builtin_amdgcn_readfirstlane(s_first[0][part]);
+            const int q0 = __builtin_amdgcn_readfirstlane(s_first[1][part]);
+            const int q1 = __builtin_amdgcn_readfirstlane(part + 1 < parts ? s_first[1][part + 1] : spans);
+            // at most 64 words and groups: a lane each
+            const int li = min(word + lane, kChunk - 1), gi = min(q0 + lane, kChunk - 1);
+            const uint32_t wa = sel_a[li], wb = sel_b[li];
+            const int gb = blk[gi], gm = info[gi], word0 = word;
+            const uint8_t *base = codes + (int64_t)(r < a.dp ? r : 0) * a.bs;
+            uint32_t *out = (uint32_t *)(lds + (r < a.dp ? r : 0) * vrow + start);
+            struct Group {
+                uint4 z[4];
+            };
+            const auto fetch = [&](int q, Group &g) {
+                const int bq = __builtin_amdgcn_readlane(gb, q - q0), mq = __builtin_amdgcn_readlane(gm, q - q0);
+                const uint8_t *at = base + (bq < 0 ? 0 : bq * size + 64 * (mq >> 16));
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    g.z[u] = make_uint4(0u, 0u, 0u, 0u);
+                    if (bq >= 0 && (mq >> (4 * u) & 15)) g.z[u] = *(const uint4 *)(at + 16 * u);
+                }
+            };
+            uint32_t acc = 0;
+            const auto pack = [&](int q, const Group &g) {
+                const int mq = __builtin_amdgcn_readlane(gm, q - q0);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (!(mq >> (4 * u) & 15)) continue;
+                    const uint32_t v[4] = {g.z[u].x, g.z[u].y, g.z[u].z, g.z[u].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (!(mq >> (4 * u + i) & 1)) continue;
+                        acc = __builtin_amdgcn_perm(acc, v[i], __builtin_amdgcn_readlane(wa, word - word0));
+                        const uint32_t sb = __builtin_amdgcn_readlane(wb, word - word0);
+                        ++word;
+                        if (sb) {
+                            if (r < a.dp) *out = acc;
+                            ++out;
+                            acc = __builtin_amdgcn_perm(0u, v[i], sb);
+                        }
+                    }
+                }
+            };
+            Group g0, g1;
+            fetch(q0, g0);
+            for (int q = q0; q < q1; q += 2) {
+                if (q + 1 < q1) fetch(q + 1, g1);
+                pack(q, g0);
+                if (q + 1 >= q1) break;
+                if (q + 2 < q1) fetch(q + 2, g0);
+                pack(q + 1, g1);
+            }
+            if ((stop & 3) && r < a.dp) *out = acc;
+        }
+        __syncthreads();
+        // the largest magnitude of every token: four tokens and a share of the rows a thread
+        if (tid < kChunk) top[tid] = 0;
+        __syncthreads();
+        const int col = tid & (kChunk / 4 - 1);
+        if (4 * col >= lo && 4 * col < hi) {
+            uint32_t m = 0;
+            for (int y = tid / (kChunk / 4); y < a.dp; y += MT / (kChunk / 4))
+                m = max_bytes(m, magnitudes(*(const uint32_t *)(lds + y * vrow + 4 * col)));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) atomicMax(&top[4 * col + i], (m >> (8 * i)) & 0xFFu);
+        }
+    }
+    __syncthreads();  // everything has been read
+    if (tid == 0) __hip_atomic_store(&a.read[values * a.chunks + chunk], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (mine) atomicMax(&least[tid >> a.shift], least_exp((int)top[tid], e));
+    __syncthreads();
+    if (mine) ratio[tid] = exp_ratio(e, min(least[tid >> a.shift], 253));
+    // the chunks before this one that keep tokens of its positions
+    {
+        const int64_t r0 = a.within[chunk], r1 = (j + 1) * kChunk < x.x ? a.within[chunk + 1] : x.x;
+        const int64_t i0 = max(r0, (int64_t)x.y * a.bs) >> kChunkShift, i1 = min((r1 + kChunk - 1) >> kChunkShift, j);
+        for (int64_t i = i0 + tid; i < i1; i += MT)
+            while (!__hip_atomic_load(&a.read[values * a.chunks + t0 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
+                __builtin_amdgcn_s_sleep(1);
+    }
+    __syncthreads();
+    uint8_t *dst = values ? a.vc : a.kc;
+    if (!values) {
+        const int per = a.dp / 16;
+        for (int i = lo * per + tid; i < hi * per; i += MT) {
+            const int t = i / per, n = to[t >> a.shift];
+            if (n < 0) continue;
+            const float f = ratio[t];
+            uint4 z = *(const uint4 *)(lds + 16 * i);
+            z.x = scale_codes(z.x, f, f, f, f), z.y = scale_codes(z.y, f, f, f, f);
+            z.z = scale_codes(z.z, f, f, f, f), z.w = scale_codes(z.w, f, f, f, f);
+            *(uint4 *)(dst + n * size + 16 * (i - (t >> a.shift << a.shift) * per)) = z;
+        }
+    } else {
+        // a block's rows one after the other, 16 tokens a thread
+        const int per = a.bs / 16, each = a.dp * per;
+        for (int i = tid; i < each * (kChunk >> a.shift); i += MT) {
+            const int n = i / each, in = i - n * each, y = in / per, t = (n << a.shift) + 16 * (in - y * per);
+            if (t < lo || t >= hi || to[n] < 0) continue;
+            uint32_t z[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float4 f = *(const float4 *)(ratio + t + 4 * u);
+                z[u] = scale_codes(*(const uint32_t *)(lds + y * vrow + t + 4 * u), f.x, f.y, f.z, f.w);
+            }
+            uint8_t *q = dst + to[n] * size + 16 * in;
+            if (t + 16 <= hi) {
+                *(uint4 *)q = make_uint4(z[0], z[1], z[2], z[3]);
+            } else {
+                for (int u = 0; t + u < hi; ++u) q[u] = (uint8_t)(z[u / 4] >> (8 * (u % 4)));
+            }
+        }
+    }
+    if (tid < kChunk >> a.shift && (tid << a.shift) >= lo && (tid << a.shift) < hi && to[tid] >= 0)
+        (values ? a.v_exp : a.k_exp)[to[tid]] = (uint8_t)min(least[tid], 253);
+}
+
+// The listed cells' new tables and lengths.
+__global__ void __launch_bounds__(CT) compact_apply(PageArgs a) {
+    const int64_t p = blockIdx.x;
+    const int4 x = a.plan[p];
+    if (x.x < 0) return;
+    const int64_t c = cell_of(a, p), b0 = block0(a, p), now = nb(a, x.x), had = nb(a, length_of(a, c));
+    int32_t *row = a.table + c * a.W;
+    if (x.z > 0)
+        for (int64_t j = x.y + threadIdx.x; j < now; j += CT) {
+            const int32_t r = a.rank[b0 + j];
+            if (r < 0) continue;
+            leave_block(a, row[j]);
+            row[j] = a.free_list[a.head[0].top - 1 - (x.w + r)];
+        }
+    for (int64_t j = now + threadIdx.x; j < had; j += CT) {
+        leave_block(a, row[j]);
+        row[j] = -1;
+    }
+    __syncthreads();  // everyone has read the length
+    if (threadIdx.x == 0) a.lens[c] = x.x;
 }
 
 struct PageLayout {
@@ -519,21 +718,20 @@ struct PageLayout {
         return p;
     }
 };
-int64_t tiles_of(int64_t P, int64_t n_kept, int block_size) { return n_kept / block_size + P; }
-
 // kind 0: release, 1: fork, 2: compact
 size_t layout(PageArgs &a, int kind, void *ws) {
     PageLayout l{(char *)ws};
     a.nruns = (a.n_blocks + kRun - 1) / kRun;
     a.head = l.take<PageHead>(1);
-    if (kind != 1) a.counts = l.take<int32_t>(a.nruns);
+    if (kind != 1) a.marks = l.take<uint16_t>(a.nruns * WT), a.counts = l.take<int32_t>(a.nruns);
     if (kind != 0) a.claim = l.take<int32_t>(a.C);
     a.plan = l.take<int4>(kind == 0 ? a.C : a.P);
     if (kind == 2) {
-        const int64_t tiles = tiles_of(a.P, a.n_kept, a.bs);
-        a.rank = l.take<int32_t>(tiles);
-        a.staged_exp = l.take<uint8_t>(2 * tiles);
-        a.staged = l.take<uint8_t>(2 * tiles * a.bs * a.dp);
+        a.chunks = a.n_kept / kChunk + a.P;
+        a.rank = l.take<int32_t>(a.n_kept / a.bs + a.P), a.owner = l.take<int32_t>(a.chunks);
+        a.within = l.take<int32_t>(a.chunks), a.read = l.take<int32_t>(2 * a.chunks);
+        a.tickets = l.take<int32_t>(2 * kQueues * kApart);
+        a.starts = l.take<int32_t>(kQueues + 1);
     }
     return align_up(l.off, 256);
 }
@@ -546,6 +744,10 @@ PageArgs page_args(const fw_cache &cache, const fw_cells &cells) {
     a.shared = cells.shared;
     a.kc = cache.k, a.vc = cache.v, a.k_exp = cache.k_exp, a.v_exp = cache.v_exp;
     return a;
+}
+void launch_collect(const PageArgs &a, hipStream_t st) {
+    if (a.nruns > kFewRuns) hipLaunchKernelGGL(count_runs, dim3((unsigned)a.nruns), dim3(WT), 0, st, a);
+    hipLaunchKernelGGL(collect_blocks, dim3((unsigned)a.nruns), dim3(WT), 0, st, a);
 }
 }  // namespace
 
@@ -560,9 +762,10 @@ hipError_t launch_release(const fw_cache &cache, const fw_cells &cells, const in
     PageArgs a = page_args(cache, cells);
     a.new_len = new_len, a.refused = refused;
     layout(a, 0, ws);
+    if (a.nruns > kFewRuns) hipLaunchKernelGGL(clear_all, dim3((unsigned)std::min<int64_t>(a.nruns / 4 + 1, 1024)), dim3(WT), 0, st, a);
     hipLaunchKernelGGL(release_plan, dim3(1), dim3(PT), 0, st, a);
     hipLaunchKernelGGL(release_apply, dim3((unsigned)a.C), dim3(WT), 0, st, a);
-    hipLaunchKernelGGL(collect_blocks, dim3((unsigned)a.nruns), dim3(WT), 0, st, a);
+    launch_collect(a, st);
     return hipGetLastError();
 }
 
@@ -582,13 +785,12 @@ hipError_t launch_cell_compact(const fw_cache &cache, const fw_cells &cells, int
     PageArgs a = page_args(cache, cells);
     a.P = P, a.which = which, a.offsets = offsets, a.n_kept = n_kept, a.kept_pos = kept_pos, a.refused = refused;
     layout(a, 2, ws);
-    const int64_t tiles = tiles_of(P, n_kept, a.bs);
-    if (P > 0) hipLaunchKernelGGL(compact_check, dim3((unsigned)P), dim3(WT), 0, st, a);
+    if (P > 0) hipLaunchKernelGGL(compact_check, dim3((unsigned)P), dim3(CT), 0, st, a);
     hipLaunchKernelGGL(compact_plan, dim3(1), dim3(PT), 0, st, a);
     if (P == 0) return hipGetLastError();
-    hipLaunchKernelGGL(compact_gather, dim3((unsigned)tiles, 2), dim3(WT), a.bs * a.dp, st, a);
-    hipLaunchKernelGGL(compact_write, dim3((unsigned)(tiles + P), 2), dim3(WT), 0, st, a, tiles);
-    hipLaunchKernelGGL(collect_blocks, dim3((unsigned)a.nruns), dim3(WT), 0, st, a);
+    hipLaunchKernelGGL(compact_move, dim3((unsigned)(2 * a.chunks)), dim3(MT), a.dp * (kChunk + 4), st, a);
+    hipLaunchKernelGGL(compact_apply, dim3((unsigned)P), dim3(CT), 0, st, a);
+    launch_collect(a, st);
     return hipGetLastError();
 }
 

@@ -1,6 +1,7 @@
 // Scores of cached tokens and the choice among them (fw_cache_scores,
 // fw_cache_select).
 #include <algorithm>
+#include <type_traits>
 
 #include "fw_internal.hpp"
 
@@ -17,25 +18,34 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 //   s_j = 1/R sum_r [r sees j] exp(scale_h 2^ek(j) <q_r, code_j> - lse_r)
 //
 // over a cell's R rows (T positions x G heads).  A wave takes 64 tokens: their
-// codes become bf16 (exact) once, in registers, and meet the rows tile by tile
-// from LDS, S = Q K^T on 16x16x32 MFMA: a lane's four results are four rows of
-// one token, so the sum over rows stays in the lane.  lse is known, so nothing
-// is kept but the sums.  Float32 queries are taken apart into three bf16
-// parts, which hold all 24 bits.  More rows than the workgroup's LDS holds are
-// taken in turns, which add to what the turn before wrote.
+// codes become bf16 (exact) in registers and meet the rows 16 at a time, S = Q
+// K^T on 16x16x32 MFMA: a lane's four results are four rows of one token, so
+// the sum over rows stays in the lane.  lse is known, so nothing is kept but
+// the sums.  Float32 queries are taken apart into three bf16 parts, which hold
+// all 24 bits.
+//
+// Cells differ in length, so the work is cut by length, on the device: all
+// cells' tiles of 64 tokens in a row, the same number to each wave (few_rows) or
+// workgroup (many_rows).
+//
+// few_rows, up to 16 rows a cell: a wave holds them in registers and needs no
+// other wave; keys are loaded a tile ahead.
+// many_rows: a workgroup's waves share the rows in LDS; more rows than it holds
+// are taken in turns, which add to what the turn before wrote.
 // ---------------------------------------------------------------------------
-constexpr int SW = 4;          // waves of a workgroup
-constexpr int ST = 64 * SW;
-constexpr int TT = 64;         // tokens of a wave and step
-constexpr int kQBytes = 65536; // rows in LDS at a time
-constexpr int kShares = 512;   // workgroups that share the tokens
-constexpr int kLeast = 4;      // tiles of a workgroup at least
+constexpr int TT = 64;          // tokens of a wave and step
+constexpr int FT = 256;         // threads of few_rows
+constexpr int kFewGroups = 1024;  // its workgroups
+constexpr int kFewLeast = 1;    // tiles of a wave at least
+constexpr int kQBytes = 65536;  // many_rows: rows in LDS at a time
+constexpr int kManyGroups = 512;
+constexpr int kManyLeast = 2;   // tiles of a workgroup at least
 constexpr float SLOG2E = 1.4426950408889634f;
 
 struct ScoreArgs {
     const void *q;
     int64_t q_seq, q_tok, q_head;
-    int C, T, Hkv, G, W, R, d, turn;   // turn: rows in LDS at a time, a multiple of 16
+    int C, T, Hkv, G, W, R, d, turn;  // turn: rows in LDS at a time, a multiple of 16
     const uint8_t *kc, *k_exp;
     int64_t n_blocks;
     int shift;
@@ -43,17 +53,17 @@ struct ScoreArgs {
     const float *scale, *lse, *earlier;
     float *scores;
     int64_t n;
+    bool wide;  // 16-byte aligned queries of a multiple of 8 columns
 };
 
-__device__ __forceinline__ int scored(const ScoreArgs &a, int c) {  // tokens of a cell that are scored
-    const int64_t most = (int64_t)a.W << a.shift, cap = most < a.n ? most : a.n;
-    const int len = a.lens[c];
-    return len < 0 ? 0 : len > cap ? (int)cap : len;
-}
 __device__ __forceinline__ int cell_len(const ScoreArgs &a, int c) {
     const int64_t most = (int64_t)a.W << a.shift;
     const int len = a.lens[c];
     return len < 0 ? 0 : len > most ? (int)most : len;
+}
+__device__ __forceinline__ int scored(const ScoreArgs &a, int c) {  // tokens of a cell that are scored
+    const int len = cell_len(a, c);
+    return len > a.n ? (int)a.n : len;
 }
 __device__ __forceinline__ float exp2_of_byte(int b) { return __uint_as_float((uint32_t)(b < 1 ? 1 : b) << 23); }
 
@@ -65,20 +75,14 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
     return (bf16x8){a[0], a[1], b[0], b[1], c[0], c[1], e[0], e[1]};
 }
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(ST) cache_scores(ScoreArgs a) {
-    constexpr int NP = sizeof(T) == 4 ? 3 : 1;            // bf16 parts of a query
-    constexpr int KS = DP / 32, KB = DP / 4, KW = KB / 4;  // key steps; bytes and words of a lane's part of a key
-    extern __shared__ __align__(16) uint8_t lds[];
-    __shared__ int red[ST / 64], found[2];
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tl = lane & 15, g = lane >> 4;
-    bf16x8 *const qs = (bf16x8 *)lds;                          // [row tile][key step][part][lane]
-    float *const ls = (float *)(lds + (size_t)a.turn * KS * NP * 64);  // [row] lse, base 2
-    int *const back = (int *)(ls + a.turn);                    // [row] last tokens that it does not see
-
-    // this workgroup's tiles of all cells' in a row
-    const int run = (a.C + ST - 1) / ST, c0 = tid * run, c1 = c0 + run < a.C ? c0 + run : a.C;
+// Shares [g0, g1) of the cells' tiles, N to a workgroup, share i of workgroup b being number b N + i of `shares`: each
+// share's first cell and the first tile of that.  found[i] = (cell, its first tile), cell -1 where the share is empty.
+template <int NT, int N>
+__device__ __forceinline__ void find_shares(const ScoreArgs &a, int shares, int least, int2 (&found)[N], int *per) {
+    __shared__ int red[NT / 64];
+    __shared__ int2 got[N];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int run = (a.C + NT - 1) / NT, c0 = tid * run, c1 = c0 + run < a.C ? c0 + run : a.C;
     int mine = 0;
     for (int c = c0; c < c1; ++c) mine += (scored(a, c) + TT - 1) / TT;
     int x = mine;
@@ -88,133 +92,304 @@ __global__ void __launch_bounds__(ST) cache_scores(ScoreArgs a) {
         if (lane >= off) x += y;
     }
     if (lane == 63) red[w] = x;
+    if (tid < N) got[tid].x = -1;
     __syncthreads();
     int first = x - mine, all = 0;
 #pragma unroll
-    for (int i = 0; i < SW; ++i) {
+    for (int i = 0; i < NT / 64; ++i) {
         if (i < w) first += red[i];
         all += red[i];
     }
-    const int per = max((all + (int)gridDim.x - 1) / (int)gridDim.x, kLeast);
-    if ((int64_t)blockIdx.x * per >= all) return;
-    const int g0 = blockIdx.x * per, g1 = min(g0 + per, all);
-    if (g0 >= first && g0 < first + mine)
+    *per = max((int)(((int64_t)all + shares - 1) / shares), least);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int64_t g = ((int64_t)blockIdx.x * N + i) * *per;
+        if (g < first || g >= first + mine) continue;
+        int at = first;
         for (int c = c0; c < c1; ++c) {
             const int n = (scored(a, c) + TT - 1) / TT;
-            if (g0 < first + n) {
-                found[0] = c, found[1] = first;
+            if (g < at + n) {
+                got[i] = make_int2(c, at);
                 break;
             }
-            first += n;
+            at += n;
         }
+    }
     __syncthreads();
-    int c = __builtin_amdgcn_readfirstlane(found[0]), at = __builtin_amdgcn_readfirstlane(found[1]);
-    const float mean = 1.f / a.R;
-    const int bmask = (1 << a.shift) - 1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) found[i] = got[i];
+}
 
+// The 16 tokens of piece x of tile t lie in one block: its number, the same for the whole wave, or -1.
+__device__ __forceinline__ int page_of(const ScoreArgs &a, const int32_t *row, int len, int t, int x) {
+    const int tok = t * TT + 16 * x, b = tok < len ? row[tok >> a.shift] : -1;
+    return b >= 0 && b < a.n_blocks ? b : -1;
+}
+
+// A lane's part of a tile's keys: token 16 x + lane % 16, bytes KB (lane / 16) and on.
+template <int DP>
+struct Keys {
+    static constexpr int KW = DP / 16;  // words
+    uint32_t k[4][KW];
+    int e[4];
+    __device__ __forceinline__ void load(const ScoreArgs &a, int t, const int (&page)[4], int lane) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int64_t b = page[x] < 0 ? 0 : page[x];
+            const uint8_t *p = a.kc + ((b << a.shift) + ((t * TT + 16 * x) & ((1 << a.shift) - 1))) * DP + (lane & 15) * DP +
+                               DP / 4 * (lane >> 4);
+#pragma unroll
+            for (int y = 0; y < KW; y += (KW % 4 == 0 ? 4 : 2)) {
+                if constexpr (KW % 4 == 0) *(uint4 *)&k[x][y] = *(const uint4 *)(p + 4 * y);
+                else *(uint2 *)&k[x][y] = *(const uint2 *)(p + 4 * y);
+            }
+            e[x] = a.k_exp[b];
+        }
+    }
+};
+
+// Eight columns of row r of a cell as bf16 parts; zeros past the rows and columns there are.
+template <typename T, int NP>
+__device__ __forceinline__ void load_row(const ScoreArgs &a, const T *p, bool in, int col, bf16x8 (&z)[NP]) {
+    if (NP == 1 && a.wide) {
+        uint4 v = {0u, 0u, 0u, 0u};
+        if (in && col < a.d) v = *(const uint4 *)(p + col);
+        z[0] = __builtin_bit_cast(bf16x8, v);
+        return;
+    }
+    float v[8];
+    if (a.wide) {
+        f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+        if (in && col < a.d) lo = *(const f32x4 *)(p + col), hi = *(const f32x4 *)(p + col + 4);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = k < 4 ? lo[k & 3] : hi[k & 3];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = in && col + k < a.d ? Elem<T>::load(p, col + k) : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int s = 0; s < NP; ++s) {
+            z[s][k] = (__bf16)v[k];
+            v[k] -= (float)z[s][k];
+        }
+}
+
+// Adds e^(z - lse) of 16 rows to the lane's tokens' sums; hid: the first token that each of the lane's four rows does not see.
+template <bool MASKED>
+__device__ __forceinline__ void add_weights(const f32x4 (&s)[4], const f32x4 &l, const float (&f)[4], const int (&hid)[4], int tok,
+                                            float (&sum)[4]) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(s[x][i], f[x], -l[i]));
+            sum[x] += !MASKED || tok + 16 * x < hid[i] ? e : 0.f;
+        }
+}
+
+// A tile's scores: the sums of the lane groups together, times 1 / R, and what was there before.
+__device__ __forceinline__ void put_scores(const ScoreArgs &a, int64_t at, const float (&sum)[4], const int (&page)[4], int lane,
+                                           bool in, float mean, float old) {
+    float out = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        float y = page[x] >= 0 ? sum[x] : 0.f;
+        y += __shfl_xor(y, 16);
+        y += __shfl_xor(y, 32);
+        out = (lane >> 4) == x ? y : out;
+    }
+    if (in) a.scores[at] = fmaf(out, mean, old);
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(FT, DP <= (sizeof(T) == 2 ? 128 : 64) ? 4 : 2) few_rows(ScoreArgs a) {
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1, KS = DP / 32;  // bf16 parts of a query, key steps
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tl = lane & 15, g = lane >> 4;
+    int2 found[FT / 64];
+    int per;
+    find_shares<FT, FT / 64>(a, gridDim.x * (FT / 64), kFewLeast, found, &per);
+    int c = -1, at = 0;
+#pragma unroll
+    for (int i = 0; i < FT / 64; ++i)
+        if (i == w) c = __builtin_amdgcn_readfirstlane(found[i].x), at = __builtin_amdgcn_readfirstlane(found[i].y);
+    if (c < 0) return;
+    const int g0 = (blockIdx.x * (FT / 64) + w) * per, g1 = g0 + per;  // below 2^30 tiles
+    const float mean = 1.f / a.R;
     for (; c < a.C && at < g1; ++c) {
-        const int n = scored(a, c), nt = (n + TT - 1) / TT;
+        const int len = cell_len(a, c), n = scored(a, c), nt = (n + TT - 1) / TT;
         const int t0 = max(g0 - at, 0), t1 = min(g1 - at, nt);
         at += nt;
         if (t0 >= t1) continue;
-        const int len = cell_len(a, c), seq = c / a.Hkv, h = c % a.Hkv;
+        const int seq = c / a.Hkv, h = c % a.Hkv;
         const int32_t *row = a.table + (int64_t)c * a.W;
         const float sl2 = (a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d))) * SLOG2E;
+        const int full = len - (a.T - 1);  // tokens that every row sees
+        const int64_t out = c * a.n + lane;
+        int pg[4], pn[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) pg[x] = page_of(a, row, len, t0, x);
+        const auto old_score = [&](int t) { return a.earlier && t * TT + lane < n ? a.earlier[out + t * TT] : 0.f; };
+        float old = old_score(t0);
+        Keys<DP> kr;
+        kr.load(a, t0, pg, lane);
+        bf16x8 q[KS][NP];
+        f32x4 l;
+        int hid[4];
+        {
+            const T *p = (const T *)a.q + seq * a.q_seq + (tl / a.G) * a.q_tok + (h * a.G + tl % a.G) * a.q_head;
+#pragma unroll
+            for (int y = 0; y < KS; ++y) load_row<T, NP>(a, p, tl < a.R, DP / 4 * g + 8 * y, q[y]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 4 * g + i;
+                l[i] = r < a.R ? a.lse[((int64_t)seq * a.T + r / a.G) * a.Hkv * a.G + h * a.G + r % a.G] * SLOG2E : INFINITY;
+                hid[i] = r < a.R ? len - (a.T - 1 - r / a.G) : 0;
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) pn[x] = page_of(a, row, t0 + 1 < t1 ? len : 0, t0 + 1, x);
+        for (int t = t0; t < t1; ++t) {
+            float f[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) f[x] = sl2 * exp2_of_byte(kr.e[x]);
+            f32x4 s[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                s[x] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int y = 0; y < KS; ++y) {
+                    const bf16x8 kk = widen(kr.k[x][2 * y], kr.k[x][2 * y + 1]);
+#pragma unroll
+                    for (int z = NP - 1; z >= 0; --z) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[y][z], kk, s[x], 0, 0, 0);
+                }
+            }
+            // the next tile: what is added to before the keys, whose use waits for all loads before
+            const int now[4] = {pg[0], pg[1], pg[2], pg[3]};
+            const float was = old;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) pg[x] = pn[x];
+            if (t + 1 < t1) {
+                old = old_score(t + 1);
+                kr.load(a, t + 1, pg, lane);
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) pn[x] = page_of(a, row, t + 2 < t1 ? len : 0, t + 2, x);
+            if (t * TT + TT > full) add_weights<true>(s, l, f, hid, t * TT + tl, sum);
+            else add_weights<false>(s, l, f, hid, t * TT + tl, sum);
+            put_scores(a, out + t * TT, sum, now, lane, t * TT + lane < n, mean, was);
+        }
+    }
+}
+
+// NW waves; LDS: rows as MFMA operands [row tile][key step][part][lane], their lse (base 2), and how many of the last
+// tokens each does not see.
+template <typename T, int DP, int NW>
+__global__ void __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) many_rows(ScoreArgs a) {
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1, KS = DP / 32, NT = 64 * NW;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tl = lane & 15, g = lane >> 4;
+    bf16x8 *const qs = (bf16x8 *)lds;
+    float *const ls = (float *)(lds + (size_t)a.turn * KS * NP * 64);
+    int *const back = (int *)(ls + a.turn);
+    int2 found[1];
+    int per;
+    find_shares<NT, 1>(a, gridDim.x, kManyLeast, found, &per);
+    int c = __builtin_amdgcn_readfirstlane(found[0].x), at = __builtin_amdgcn_readfirstlane(found[0].y);
+    if (c < 0) return;
+    const int g0 = blockIdx.x * per, g1 = g0 + per;
+    const float mean = 1.f / a.R, inv_g = 1.f / a.G;
+
+    for (; c < a.C && at < g1; ++c) {
+        const int len = cell_len(a, c), n = scored(a, c), nt = (n + TT - 1) / TT;
+        const int t0 = max(g0 - at, 0), t1 = min(g1 - at, nt);
+        at += nt;
+        if (t0 >= t1) continue;
+        const int seq = c / a.Hkv, h = c % a.Hkv;
+        const int32_t *row = a.table + (int64_t)c * a.W;
+        const float sl2 = (a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d))) * SLOG2E;
+        const int full = len - (a.T - 1);  // tokens that every row sees
         for (int r0 = 0; r0 < a.R; r0 += a.turn) {
             const int rows = min(a.turn, a.R - r0), tiles = (rows + 15) / 16;
+            const float *before = r0 > 0 ? a.scores : a.earlier;
+            int pg[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) pg[x] = page_of(a, row, t0 + w < t1 ? len : 0, t0 + w, x);
             __syncthreads();  // the rows before are done with
-            for (int i = tid; i < tiles * KS * 64; i += ST) {
-                const int l = i & 63, y = (i >> 6) % KS, rt = (i >> 6) / KS;
-                const int r = r0 + 16 * rt + (l & 15), col = KB * (l >> 4) + 8 * y;
-                const T *p = (const T *)a.q + seq * a.q_seq + (r / a.G) * a.q_tok + (h * a.G + r % a.G) * a.q_head;
-                bf16x8 z[NP];
+            constexpr int FL = NP == 1 ? 4 : 2;  // pieces of eight columns in flight
+            for (int i0 = tid; i0 < tiles * KS * 64; i0 += FL * NT) {
+                bf16x8 z[FL][NP];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    float v = r < a.R && col + k < a.d ? Elem<T>::load(p, col + k) : 0.f;
-#pragma unroll
-                    for (int s = 0; s < NP; ++s) {
-                        z[s][k] = (__bf16)v;
-                        v -= (float)z[s][k];
-                    }
+                for (int u = 0; u < FL; ++u) {
+                    const int i = i0 + u * NT, y = (i >> 6) % KS, r = r0 + 16 * ((i >> 6) / KS) + tl;
+                    // row r is head r % G of position r / G; exact, since R <= 4096
+                    const int pos = (int)((r + 0.5f) * inv_g), head = h * a.G + r - pos * a.G;
+                    const T *p = (const T *)a.q + seq * a.q_seq + pos * a.q_tok + head * a.q_head;
+                    load_row<T, NP>(a, p, r < a.R && i < tiles * KS * 64, DP / 4 * g + 8 * y, z[u]);
                 }
 #pragma unroll
-                for (int s = 0; s < NP; ++s) qs[((rt * KS + y) * NP + s) * 64 + l] = z[s];
+                for (int u = 0; u < FL; ++u) {
+                    const int i = i0 + u * NT;
+                    if (i < tiles * KS * 64)
+#pragma unroll
+                        for (int s = 0; s < NP; ++s) qs[((i >> 6) * NP + s) * 64 + lane] = z[u][s];
+                }
             }
-            for (int i = tid; i < 16 * tiles; i += ST) {
-                const int r = r0 + i;
+            for (int i = tid; i < 16 * tiles; i += NT) {
+                const int r = r0 + i, pos = (int)((r + 0.5f) * inv_g);
                 const bool in = r < a.R;
-                ls[i] = in ? a.lse[((int64_t)seq * a.T + r / a.G) * a.Hkv * a.G + h * a.G + r % a.G] * SLOG2E : INFINITY;
-                back[i] = in ? a.T - 1 - r / a.G : len;
+                ls[i] = in ? a.lse[((int64_t)seq * a.T + pos) * a.Hkv * a.G + h * a.G + r - pos * a.G] * SLOG2E : INFINITY;
+                back[i] = in ? a.T - 1 - pos : len;
             }
             __syncthreads();
-            const int full = len - (a.T - 1);  // tokens that every row sees
-            for (int t = t0 + w; t < t1; t += SW) {
-                const int base = t * TT;
+            for (int t = t0 + w; t < t1; t += NW) {
+                const bool in = t * TT + lane < n;
+                const int64_t out = c * a.n + t * TT + lane;
+                const float old = before && in ? before[out] : 0.f;
                 bf16x8 kf[4][KS];
-                float f[4];
-                bool in[4];
+                float f[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+                {
+                    Keys<DP> kr;
+                    kr.load(a, t, pg, lane);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int tok = base + 16 * x + tl, b = tok < len ? row[tok >> a.shift] : -1;
-                    in[x] = b >= 0 && b < a.n_blocks;
-                    const int64_t bb = in[x] ? b : 0;
-                    const uint8_t *p = a.kc + ((bb << a.shift) + (tok & bmask)) * DP + KB * g;
-                    f[x] = sl2 * exp2_of_byte(a.k_exp[bb]);
-                    uint32_t kr[KW];
+                    for (int x = 0; x < 4; ++x) {
+                        f[x] = sl2 * exp2_of_byte(kr.e[x]);
 #pragma unroll
-                    for (int y = 0; y < KW; y += (KW % 4 == 0 ? 4 : 2)) {
-                        if constexpr (KW % 4 == 0) *(uint4 *)&kr[y] = *(const uint4 *)(p + 4 * y);
-                        else *(uint2 *)&kr[y] = *(const uint2 *)(p + 4 * y);
+                        for (int y = 0; y < KS; ++y) kf[x][y] = widen(kr.k[x][2 * y], kr.k[x][2 * y + 1]);
                     }
-#pragma unroll
-                    for (int y = 0; y < KS; ++y) kf[x][y] = widen(kr[2 * y], kr[2 * y + 1]);
                 }
-                const bool masked = base + TT > full;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                for (int rt = 0; rt < tiles; ++rt) {
-                    f32x4 s[4];
+                const int now[4] = {pg[0], pg[1], pg[2], pg[3]};
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) s[x] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                for (int x = 0; x < 4; ++x) pg[x] = page_of(a, row, t + NW < t1 ? len : 0, t + NW, x);
+                const auto all_rows = [&](auto masked) {
+#pragma unroll 1
+                    for (int rt = 0; rt < tiles; ++rt) {
+                        f32x4 s[4];
 #pragma unroll
-                    for (int y = 0; y < KS; ++y)
+                        for (int x = 0; x < 4; ++x) s[x] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int z = NP - 1; z >= 0; --z) {
-                            const bf16x8 qf = qs[((rt * KS + y) * NP + z) * 64 + lane];
+                        for (int y = 0; y < KS; ++y)
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf, kf[x][y], s[x], 0, 0, 0);
-                        }
-                    const f32x4 l = *(const f32x4 *)(ls + 16 * rt + 4 * g);
-                    if (masked) {
-                        const int4 bk = *(const int4 *)(back + 16 * rt + 4 * g);
-                        const int hid[4] = {len - bk.x, len - bk.y, len - bk.z, len - bk.w};
+                            for (int z = NP - 1; z >= 0; --z) {
+                                const bf16x8 qf = qs[((rt * KS + y) * NP + z) * 64 + lane];
 #pragma unroll
-                        for (int x = 0; x < 4; ++x)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float e = __builtin_amdgcn_exp2f(fmaf(s[x][i], f[x], -l[i]));
-                                sum[x] += base + 16 * x + tl < hid[i] ? e : 0.f;
+                                for (int x = 0; x < 4; ++x) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf, kf[x][y], s[x], 0, 0, 0);
                             }
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) sum[x] += __builtin_amdgcn_exp2f(fmaf(s[x][i], f[x], -l[i]));
+                        const f32x4 l = *(const f32x4 *)(ls + 16 * rt + 4 * g);
+                        int hid[4] = {0, 0, 0, 0};
+                        if constexpr (masked) {
+                            const int4 b = *(const int4 *)(back + 16 * rt + 4 * g);
+                            hid[0] = len - b.x, hid[1] = len - b.y, hid[2] = len - b.z, hid[3] = len - b.w;
+                        }
+                        add_weights<masked>(s, l, f, hid, t * TT + tl, sum);
                     }
-                }
-                float out = 0.f;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    float y = in[x] ? sum[x] : 0.f;
-                    y += __shfl_xor(y, 16);
-                    y += __shfl_xor(y, 32);
-                    out = g == x ? y : out;
-                }
-                const int tok = base + lane;  // 16 g + tl
-                if (tok < n) {
-                    const int64_t i = c * a.n + tok;
-                    const float old = r0 > 0 ? a.scores[i] : a.earlier ? a.earlier[i] : 0.f;
-                    a.scores[i] = fmaf(out, mean, old);
-                }
+                };
+                if (t * TT + TT > full) all_rows(std::true_type());
+                else all_rows(std::false_type());
+                put_scores(a, out, sum, now, lane, in, mean, old);
             }
         }
     }
@@ -222,13 +397,17 @@ __global__ void __launch_bounds__(ST) cache_scores(ScoreArgs a) {
 
 template <typename T, int DP>
 hipError_t launch_scores_width(ScoreArgs &a, hipStream_t st) {
-    constexpr int NP = sizeof(T) == 4 ? 3 : 1;
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1, NW = DP <= 128 ? 8 : 4;
+    const int64_t tiles = a.C * ((std::min<int64_t>((int64_t)a.W << a.shift, a.n) + TT - 1) / TT);
+    if (a.R <= 16) {
+        const int64_t groups = (tiles + FT / 64 * kFewLeast - 1) / (FT / 64 * kFewLeast);
+        hipLaunchKernelGGL((few_rows<T, DP>), dim3((unsigned)std::min<int64_t>(kFewGroups, groups)), dim3(FT), 0, st, a);
+        return hipGetLastError();
+    }
     const int row = 2 * DP * NP;
     a.turn = std::min((a.R + 15) / 16 * 16, kQBytes / row / 16 * 16);
-    const size_t lds = (size_t)a.turn * (row + 8);
-    const int64_t tiles = (int64_t)a.C * ((std::min<int64_t>((int64_t)a.W << a.shift, a.n) + TT - 1) / TT);
-    const unsigned grid = (unsigned)std::min<int64_t>(kShares, (tiles + kLeast - 1) / kLeast);
-    hipLaunchKernelGGL((cache_scores<T, DP>), dim3(grid), dim3(ST), lds, st, a);
+    hipLaunchKernelGGL((many_rows<T, DP, NW>), dim3((unsigned)std::min<int64_t>(kManyGroups, (tiles + kManyLeast - 1) / kManyLeast)),
+                       dim3(64 * NW), (size_t)a.turn * (row + 8), st, a);
     return hipGetLastError();
 }
 
@@ -237,10 +416,19 @@ hipError_t launch_scores_width(ScoreArgs &a, hipStream_t st) {
 //
 // The last `recent` kept tokens are certain; of those before them the rest of
 // keep[c] is chosen by the key of the score, found 11, 11 and 10 bits at a time
-// from a histogram, and then, among equal keys, by position.
+// from histograms, and then, among equal keys, by position.
+//
+// A workgroup holds its tokens' keys in registers, four neighbours at a time.
+// Rows of up to kAlone tokens take one workgroup a cell and one launch.  Longer
+// ones are cut into slices: a launch for each digit, whose histograms of all
+// slices meet in the cell's, and one that writes.  What a slice's tokens above
+// and at the key come to is read off its histogram of the last digit, so each
+// slice finds its place from those of the slices before it.
 // ---------------------------------------------------------------------------
-constexpr int LT = 1024;  // threads of a workgroup
+constexpr int LT = 1024;          // threads of a workgroup
 constexpr int kBins = 2048;
+constexpr int kAlone = 32 * LT;   // tokens of a cell that one workgroup takes alone
+constexpr int kSlice = 8 * LT;    // tokens of a slice otherwise
 
 struct SelectArgs {
     int64_t C, n, n_kept;
@@ -249,6 +437,11 @@ struct SelectArgs {
     int64_t recent;
     int64_t *offsets;
     int32_t *kept_pos;
+    // slices
+    int slices;
+    uint32_t *hist;   // [C][3][kBins]
+    uint32_t *last;   // [C][slices][kBins / 2] the last digit's, of a slice
+    uint32_t *above;  // [C][slices] tokens above the first two digits
 };
 
 __device__ __forceinline__ uint32_t rank_key(float x) { return x != x ? 0xFFFFFFFFu : ord_key(x); }
@@ -257,6 +450,17 @@ __device__ __forceinline__ int kept_of(const SelectArgs &a, int64_t c, int *len)
     const int n = l < 0 ? 0 : l > a.n ? (int)a.n : (int)l, k = a.keep[c];
     *len = n;
     return k < 0 ? 0 : k > n ? n : k;
+}
+struct CellChoice {
+    int nf, need, certain;  // tokens to choose from, how many of them, those kept in any case
+};
+__device__ __forceinline__ CellChoice choice_of(const SelectArgs &a, int64_t c) {
+    int len;
+    const int keep = kept_of(a, c, &len);
+    CellChoice x;
+    x.certain = (int)(a.recent < keep ? a.recent : keep);
+    x.nf = len - x.certain, x.need = keep - x.certain;
+    return x;
 }
 
 template <int NT, typename V>
@@ -282,6 +486,161 @@ __device__ __forceinline__ V scan_before(V v, V *red, V *total) {
     return before;
 }
 
+// The bin from the top that holds the rem-th entry, and the entries above it.
+__device__ __forceinline__ void pick_bin(const uint32_t *hist, uint32_t rem, uint32_t *red, uint32_t *found, uint32_t *bin,
+                                         uint32_t *above) {
+    const int t = kBins - 2 - 2 * threadIdx.x;  // two bins a thread
+    const uint2 h = *(const uint2 *)(hist + t);
+    uint32_t all;
+    const uint32_t before = scan_before<LT, uint32_t>(h.x + h.y, red, &all);
+    if (before < rem && rem <= before + h.y) found[0] = t + 1, found[1] = before;
+    else if (before + h.y < rem && rem <= before + h.y + h.x) found[0] = t, found[1] = before + h.y;
+    __syncthreads();
+    *bin = found[0], *above = found[1];
+}
+
+__device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ uint32_t digit_mask(int pass) { return pass == 2 ? 1023u : 2047u; }
+
+// Keys of tokens first + 4 LT k + 4 t + i; those at nf and past it are 0, below every score's key.
+template <int E>
+__device__ __forceinline__ void load_keys(const float *row, int first, int nf, uint32_t (&u)[E]) {
+    const bool wide = ((uintptr_t)row & 15) == 0;
+#pragma unroll
+    for (int k = 0; k < E / 4; ++k) {
+        const int j = first + 4 * LT * k + 4 * (int)threadIdx.x;
+        float4 x = {0.f, 0.f, 0.f, 0.f};
+        if (wide && j + 4 <= nf) {
+            x = *(const float4 *)(row + j);
+        } else {
+            if (j < nf) x.x = row[j];
+            if (j + 1 < nf) x.y = row[j + 1];
+            if (j + 2 < nf) x.z = row[j + 2];
+            if (j + 3 < nf) x.w = row[j + 3];
+        }
+        u[4 * k] = j < nf ? rank_key(x.x) : 0u, u[4 * k + 1] = j + 1 < nf ? rank_key(x.y) : 0u;
+        u[4 * k + 2] = j + 2 < nf ? rank_key(x.z) : 0u, u[4 * k + 3] = j + 3 < nf ? rank_key(x.w) : 0u;
+    }
+}
+
+template <int E>
+__device__ __forceinline__ void count_digit(const uint32_t (&u)[E], uint32_t key, uint32_t mask, int pass, uint32_t *hist) {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        if (u[i] && (u[i] & mask) == key) atomicAdd(&hist[(u[i] >> digit_shift(pass)) & digit_mask(pass)], 1u);
+}
+
+// Writes the positions above the key and the first rem - eq0 of those at it, from place `at` on; eq0: those at it before.
+template <int E>
+__device__ __forceinline__ void write_chosen(const SelectArgs &a, const uint32_t (&u)[E], int first, uint32_t key, uint32_t rem,
+                                             uint32_t eq0, int64_t at, uint32_t (*red)[LT / 64]) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    uint32_t before[E / 4];  // above the key in the low half, at it in the high one (at most 4096 each)
+#pragma unroll
+    for (int k = 0; k < E / 4; ++k) {
+        uint32_t v = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v += u[4 * k + i] > key ? 1u : u[4 * k + i] == key ? 0x10000u : 0u;
+        uint32_t x = v;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const uint32_t y = __shfl_up(x, off);
+            if (lane >= off) x += y;
+        }
+        if (lane == 63) red[k][w] = x;
+        before[k] = x - v;
+    }
+    __syncthreads();
+    uint32_t eq = eq0;
+#pragma unroll
+    for (int k = 0; k < E / 4; ++k) {
+        uint32_t all = 0, b = before[k];
+#pragma unroll
+        for (int i = 0; i < LT / 64; ++i) {
+            const uint32_t y = red[k][i];
+            if (i < w) b += y;
+            all += y;
+        }
+        uint32_t e = eq + (b >> 16);
+        int64_t o = at + (b & 0xFFFFu) + (min(e, rem) - min(eq, rem));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool same = u[4 * k + i] == key;
+            if (u[4 * k + i] > key || (same && e < rem)) {
+                if (o < a.n_kept) a.kept_pos[o] = first + 4 * LT * k + 4 * (int)threadIdx.x + i;
+                ++o;
+            }
+            e += same;
+        }
+        const uint32_t upto = eq + (all >> 16);
+        at += (all & 0xFFFFu) + (min(upto, rem) - min(eq, rem));
+        eq = upto;
+    }
+}
+
+// Kept tokens of the cells before c and of all.
+__device__ __forceinline__ int64_t kept_before(const SelectArgs &a, int64_t c, int64_t *red, int64_t *total) {
+    int64_t lo = 0, hi = 0;
+    int len;
+    for (int64_t i = threadIdx.x; i < a.C; i += LT) {
+        const int k = kept_of(a, i, &len);
+        if (i < c) lo += k;
+        else hi += k;
+    }
+    int64_t x, y;
+    scan_before<LT, int64_t>(lo, red, &x);
+    scan_before<LT, int64_t>(hi, red, &y);
+    *total = x + y;
+    return x;
+}
+__device__ __forceinline__ void write_certain(const SelectArgs &a, const CellChoice &x, int64_t o) {
+    for (int i = threadIdx.x; i < x.certain; i += LT)
+        if (o + x.need + i < a.n_kept) a.kept_pos[o + x.need + i] = x.nf + i;
+}
+// -1 behind the last kept token, by workgroup b of nb
+__device__ __forceinline__ void write_rest(const SelectArgs &a, int64_t total, int64_t b, int64_t nb) {
+    for (int64_t i = total + b * LT + threadIdx.x; i < a.n_kept; i += nb * LT) a.kept_pos[i] = -1;
+}
+
+// OWN: every workgroup sums the cells' counts for itself; else the offsets are there.
+template <int E, bool OWN>
+__global__ void __launch_bounds__(LT) select_cell(SelectArgs a) {
+    __shared__ __align__(8) uint32_t hist[kBins];
+    __shared__ uint32_t red[E / 4 > 1 ? E / 4 : 1][LT / 64], found[2];
+    __shared__ int64_t sums[LT / 64];
+    const int64_t c = blockIdx.x;
+    int64_t total, o;
+    if (OWN) {
+        o = kept_before(a, c, sums, &total);
+        if (threadIdx.x == 0) {
+            a.offsets[c] = o;
+            if (c == a.C - 1) a.offsets[a.C] = total;
+        }
+    } else {
+        o = a.offsets[c], total = a.offsets[a.C];
+    }
+    write_rest(a, total, c, gridDim.x);
+    const CellChoice x = choice_of(a, c);
+    write_certain(a, x, o);
+    if (x.need == 0) return;
+    uint32_t u[E];
+    load_keys<E>(a.scores + c * a.n, 0, x.nf, u);
+    uint32_t key = 0, mask = 0, rem = 0;  // all: every key is above 0
+    if (x.need < x.nf) {
+        rem = x.need;
+        for (int pass = 0; pass < 3; ++pass) {
+            *(uint2 *)(hist + 2 * threadIdx.x) = make_uint2(0u, 0u);
+            __syncthreads();
+            count_digit<E>(u, key, mask, pass, hist);
+            __syncthreads();
+            uint32_t bin, above;
+            pick_bin(hist, rem, red[0], found, &bin, &above);
+            key |= bin << digit_shift(pass), mask |= digit_mask(pass) << digit_shift(pass), rem -= above;
+        }
+    }
+    write_chosen<E>(a, u, 0, key, rem, 0, o, red);
+}
+
 __global__ void __launch_bounds__(LT) select_offsets(SelectArgs a) {
     __shared__ int64_t red[LT / 64];
     const int64_t run = (a.C + LT - 1) / LT, c0 = threadIdx.x * run, c1 = c0 + run < a.C ? c0 + run : a.C;
@@ -296,59 +655,82 @@ __global__ void __launch_bounds__(LT) select_offsets(SelectArgs a) {
     if (threadIdx.x == 0) a.offsets[a.C] = all;
 }
 
-__global__ void __launch_bounds__(LT) cache_select(SelectArgs a) {
-    __shared__ uint32_t hist[kBins];
-    __shared__ uint32_t red[LT / 64];
-    __shared__ uint32_t s_bin, s_above;
-    const int tid = threadIdx.x;
-    const int64_t c = blockIdx.x;
-    // behind the last kept token
-    for (int64_t i = a.offsets[a.C] + c * LT + tid; i < a.n_kept; i += (int64_t)gridDim.x * LT) a.kept_pos[i] = -1;
-    int len;
-    const int keep = kept_of(a, c, &len);
-    const int certain = (int)(a.recent < keep ? a.recent : keep), nf = len - certain, need = keep - certain;
-    const int64_t o = a.offsets[c];
-    for (int i = tid; i < certain; i += LT)
-        if (o + need + i < a.n_kept) a.kept_pos[o + need + i] = nf + i;
-    if (need == 0) return;
-    const float *row = a.scores + c * a.n;
-    uint32_t key = 0, mask = 0, rem = need;
-    if (need < nf) {
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-            const uint32_t dm = pass == 2 ? 1023u : 2047u;
-            for (int i = tid; i < kBins; i += LT) hist[i] = 0;
-            __syncthreads();
-            for (int j = tid; j < nf; j += LT) {
-                const uint32_t u = rank_key(row[j]);
-                if ((u & mask) == key) atomicAdd(&hist[(u >> shift) & dm], 1u);
-            }
-            __syncthreads();
-            // two bins a thread, from the top
-            const uint32_t h0 = hist[kBins - 1 - 2 * tid], h1 = hist[kBins - 2 - 2 * tid];
-            uint32_t all;
-            const uint32_t before = scan_before<LT, uint32_t>(h0 + h1, red, &all);
-            if (before < rem && rem <= before + h0) s_bin = kBins - 1 - 2 * tid, s_above = before;
-            else if (before + h0 < rem && rem <= before + h0 + h1) s_bin = kBins - 2 - 2 * tid, s_above = before + h0;
-            __syncthreads();
-            key |= s_bin << shift, mask |= dm << shift, rem -= s_above;
+// The key so far from the cell's histograms of the digits before `pass`.
+__device__ __forceinline__ void key_so_far(const SelectArgs &a, int64_t c, int pass, uint32_t need, uint32_t *red, uint32_t *found,
+                                           uint32_t *key, uint32_t *mask, uint32_t *rem) {
+    *key = 0, *mask = 0, *rem = need;
+    for (int p = 0; p < pass; ++p) {
+        uint32_t bin, above;
+        pick_bin(a.hist + (c * 3 + p) * kBins, *rem, red, found, &bin, &above);
+        *key |= bin << digit_shift(p), *mask |= digit_mask(p) << digit_shift(p), *rem -= above;
+        __syncthreads();
+    }
+}
+
+__global__ void __launch_bounds__(LT) select_clear(SelectArgs a) {
+    const int64_t n = a.C * 3 * kBins / 4;
+    for (int64_t i = (int64_t)blockIdx.x * LT + threadIdx.x; i < n; i += (int64_t)gridDim.x * LT)
+        ((uint4 *)a.hist)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+__global__ void __launch_bounds__(LT) select_digit(SelectArgs a, int pass) {
+    constexpr int E = kSlice / LT;
+    __shared__ __align__(8) uint32_t hist[kBins];
+    __shared__ uint32_t red[LT / 64], found[2];
+    const int64_t c = blockIdx.x / a.slices;
+    const int s = blockIdx.x % a.slices, first = s * kSlice;
+    const CellChoice x = choice_of(a, c);
+    if (first >= x.nf || x.need == 0 || x.need == x.nf) return;
+    uint32_t u[E], key, mask, rem;
+    load_keys<E>(a.scores + c * a.n, first, x.nf, u);
+    *(uint2 *)(hist + 2 * threadIdx.x) = make_uint2(0u, 0u);
+    key_so_far(a, c, pass, x.need, red, found, &key, &mask, &rem);
+    __syncthreads();
+    count_digit<E>(u, key, mask, pass, hist);
+    if (pass == 2) {
+        uint32_t more = 0, all;
+#pragma unroll
+        for (int i = 0; i < E; ++i) more += (u[i] & mask) > key;
+        scan_before<LT, uint32_t>(more, red, &all);
+        if (threadIdx.x == 0) a.above[c * a.slices + s] = all;
+    }
+    __syncthreads();
+    uint32_t *to = a.hist + (c * 3 + pass) * kBins;
+    for (int i = threadIdx.x; i < kBins; i += LT)
+        if (hist[i]) atomicAdd(&to[i], hist[i]);
+    if (pass == 2) a.last[(c * a.slices + s) * (kBins / 2) + threadIdx.x] = hist[threadIdx.x];
+}
+
+__global__ void __launch_bounds__(LT) select_write(SelectArgs a) {
+    constexpr int E = kSlice / LT;
+    __shared__ uint32_t red[E / 4][LT / 64], found[2];
+    const int64_t c = blockIdx.x / a.slices;
+    const int s = blockIdx.x % a.slices, first = s * kSlice;
+    int64_t o = a.offsets[c];
+    write_rest(a, a.offsets[a.C], blockIdx.x, gridDim.x);
+    const CellChoice x = choice_of(a, c);
+    if (s == 0) write_certain(a, x, o);
+    if (first >= x.nf || x.need == 0) return;
+    uint32_t u[E], key = 0, mask, rem = 0, eq = 0;
+    load_keys<E>(a.scores + c * a.n, first, x.nf, u);
+    if (x.need == x.nf) {
+        o += first;
+    } else {
+        key_so_far(a, c, 3, x.need, red[0], found, &key, &mask, &rem);
+        // tokens above and at the key in the slices before
+        const uint32_t bin = key & 1023u;
+        uint32_t more = 0, same = 0, all;
+        for (int i = 0; i < s; ++i) {
+            const uint32_t h = a.last[(c * a.slices + i) * (kBins / 2) + threadIdx.x];
+            more += threadIdx.x > bin ? h : 0u;
+            same += threadIdx.x == bin ? h : 0u;
+            if (threadIdx.x == 0) more += a.above[c * a.slices + i];
         }
+        scan_before<LT, uint32_t>(more, red[0], &all);
+        scan_before<LT, uint32_t>(same, red[0], &eq);
+        o += all + min(eq, rem);
     }
-    // those above the key, and the first rem of those at it
-    int64_t at = o;
-    uint32_t seen = 0;
-    for (int j0 = 0; j0 < nf; j0 += LT) {
-        const int j = j0 + tid;
-        const uint32_t u = j < nf ? rank_key(row[j]) : 0;
-        const bool more = j < nf && (need == nf || u > key), same = j < nf && need < nf && u == key;
-        uint32_t all;
-        const uint32_t before = scan_before<LT, uint32_t>((uint32_t)more | (uint32_t)same << 16, red, &all);
-        const uint32_t eq = seen + (before >> 16), taken = (before & 0xFFFFu) + (min(eq, rem) - min(seen, rem));
-        if ((more || (same && eq < rem)) && at + taken < a.n_kept) a.kept_pos[at + taken] = j;
-        const uint32_t upto = seen + (all >> 16);
-        at += (all & 0xFFFFu) + (min(upto, rem) - min(seen, rem));
-        seen = upto;
-    }
+    write_chosen<E>(a, u, first, key, rem, eq, o, red);
 }
 }  // namespace
 
@@ -362,6 +744,8 @@ hipError_t launch_cache_scores(const fw_cache &cache, int dtype, const void *q, 
     a.R = a.T * a.G, a.d = (int)cache.d;
     a.kc = cache.k, a.k_exp = cache.k_exp, a.n_blocks = cache.n_blocks, a.shift = __builtin_ctz(cache.block_size);
     a.table = table, a.lens = lens, a.scale = scale, a.lse = lse, a.earlier = earlier, a.scores = scores, a.n = n;
+    const int size = dtype == FW_F32 ? 4 : 2;
+    a.wide = a.d % 8 == 0 && (uintptr_t)q % 16 == 0 && q_seq * size % 16 == 0 && q_tok * size % 16 == 0 && q_head * size % 16 == 0;
     const auto width = [&](auto t) {
         using E = decltype(t);
         switch (cache_row(cache.d)) {
@@ -376,11 +760,44 @@ hipError_t launch_cache_scores(const fw_cache &cache, int dtype, const void *q, 
     return dtype == FW_F32 ? width(float()) : width(uint16_t());
 }
 
+// Cells whose counts every workgroup sums for itself, which saves a launch.
+constexpr int64_t kOwnSums = 4096;
+
+static int select_slices(int64_t n) { return n <= kAlone ? 0 : (int)((n + kSlice - 1) / kSlice); }
+
+size_t select_ws_bytes(int64_t C, int64_t n) {
+    const int64_t slices = select_slices(n);
+    if (!slices) return 0;
+    return align_up(C * 3 * kBins * 4, 256) + align_up(C * slices * (kBins / 2) * 4, 256) + align_up(C * slices * 4, 256);
+}
+
 hipError_t launch_select_cells(int64_t C, const float *scores, int64_t n, const int32_t *lens, const int32_t *keep,
-                               int64_t recent, int64_t n_kept, int64_t *offsets, int32_t *kept_pos, hipStream_t st) {
+                               int64_t recent, int64_t n_kept, int64_t *offsets, int32_t *kept_pos, void *ws,
+                               hipStream_t st) {
     SelectArgs a{C, n, n_kept, scores, lens, keep, recent, offsets, kept_pos};
-    hipLaunchKernelGGL(select_offsets, dim3(1), dim3(LT), 0, st, a);
-    hipLaunchKernelGGL(cache_select, dim3((unsigned)C), dim3(LT), 0, st, a);
+    a.slices = select_slices(n);
+    const bool own = !a.slices && C <= kOwnSums;
+    if (!own) hipLaunchKernelGGL(select_offsets, dim3(1), dim3(LT), 0, st, a);
+    if (a.slices) {
+        char *p = (char *)ws;
+        a.hist = (uint32_t *)p, p += align_up(C * 3 * kBins * 4, 256);
+        a.last = (uint32_t *)p, p += align_up(C * a.slices * (kBins / 2) * 4, 256);
+        a.above = (uint32_t *)p;
+        const dim3 grid((unsigned)(C * a.slices));
+        hipLaunchKernelGGL(select_clear, dim3((unsigned)std::min<int64_t>((C * 3 * kBins / 4 + LT - 1) / LT, 1024)), dim3(LT), 0, st, a);
+        for (int pass = 0; pass < 3; ++pass) hipLaunchKernelGGL(select_digit, grid, dim3(LT), 0, st, a, pass);
+        hipLaunchKernelGGL(select_write, grid, dim3(LT), 0, st, a);
+        return hipGetLastError();
+    }
+    const dim3 grid((unsigned)C);
+    const auto run = [&](auto k, auto o) {
+        if (own) hipLaunchKernelGGL(k, grid, dim3(LT), 0, st, a);
+        else hipLaunchKernelGGL(o, grid, dim3(LT), 0, st, a);
+    };
+    if (n <= 4 * LT) run(select_cell<4, true>, select_cell<4, false>);
+    else if (n <= 8 * LT) run(select_cell<8, true>, select_cell<8, false>);
+    else if (n <= 16 * LT) run(select_cell<16, true>, select_cell<16, false>);
+    else run(select_cell<32, true>, select_cell<32, false>);
     return hipGetLastError();
 }
 

@@ -67,7 +67,7 @@ def test_cache_select_validation(L):
     call = lambda **kw: L.fw_cache_select(*dict(base, **kw).values(), None)
     for null in ("scores", "lens", "keep", "offsets", "kept_pos"):
         assert call(**{null: None}) == 1, null
-    for bad in (dict(C=0), dict(C=1 << 22), dict(n=0), dict(n=(1 << 31) - 1024), dict(recent=-1), dict(n_kept=-1),
+    for bad in (dict(C=0), dict(C=1 << 22), dict(n=0), dict(n=(1 << 31) - 65536), dict(C=1 << 12, n=1 << 23), dict(recent=-1), dict(n_kept=-1),
                 dict(n_kept=1 << 40)):
         assert call(**bad) == 2, bad
     need = L.fw_cache_select_workspace_size(4, 100)
@@ -123,8 +123,8 @@ def test_cache_compact_validation(L):
     _common(L, call, lambda c, t: L.fw_cache_compact_workspace_size(c, t, 3, 100))
     for null in ("offsets", "kept_pos"):
         assert call(**{null: None}) == 1
-    for bad in (dict(P=-1), dict(P=1 << 22, which=16), dict(P=5), dict(n_kept=-1), dict(n_kept=1 << 31),
-                dict(n_kept=(1 << 29) - 1), dict(P=(1 << 22) - 1, which=16, n_kept=200)):
+    for bad in (dict(P=-1), dict(P=1 << 22, which=16), dict(P=5), dict(n_kept=-1), dict(n_kept=1 << 30),
+                dict(n_kept=(1 << 30) - 512), dict(P=(1 << 22) - 1, which=16, n_kept=256)):
         assert call(**bad) == 2, bad
 
 
