@@ -583,7 +583,7 @@ fw_status check_fork(const fw_cache *cache, const fw_cells *cells, int64_t P) {
 fw_status check_cell_compact(const fw_cache *cache, const fw_cells *cells, int64_t P, int64_t n_kept) {
     fw_status s = check_fork(cache, cells, P);
     if (s != FW_OK) return s;
-    // two workgroups of 512 threads for every 256 kept tokens of a cell; a grid holds fewer than 2^32 threads
+    // a workgroup of 1024 threads for each listed cell: a grid holds fewer than 2^32 threads
     if (n_kept < 0 || n_kept / 256 + P >= ((int64_t)1 << 22))
         return fail(FW_E_SHAPE, "need n_kept >= 0 and n_kept / 256 + P < 2^22");
     return FW_OK;

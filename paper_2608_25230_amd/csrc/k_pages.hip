@@ -39,10 +39,11 @@ struct PageArgs {
     int4 *plan;           // [max(C, P)] per cell, pair or listed cell
     // compaction
     int32_t *rank;        // [blocks kept] rank among the blocks that the cell takes, or -1
+    int32_t *taken;       // [blocks kept] the blocks taken, in their order
     int32_t *owner;       // [chunks] listed cell, or -1
     int32_t *within;      // [chunks] of the cell's kept tokens, the first that lies in or behind the chunk's own positions
     int32_t *read;        // [2][chunks] set once the chunk's keys, and values, have been read
-    int32_t *tickets;     // [2][kQueues][kApart] chunks handed out, of keys and of values
+    int32_t *tickets;     // [2 kQueues][kApart] chunks handed out, of keys and of values
     int32_t *starts;      // [kQueues + 1] first chunk of each queue; all equal if nothing moves
 };
 
@@ -98,7 +99,9 @@ __device__ __forceinline__ void copy_block(const PageArgs &a, int32_t from, int3
 }
 
 // Serves `n` requests in order, each thread a run of them: need(i) blocks (0 or more) for request i, -1 for one that is
-// refused in any case.  done(i, served, first): its first block's rank among those taken.  Returns how many are refused.
+// refused in any case.  done(i, served, first): its first block's rank among those taken.  Counts those refused, and
+// leaves the stack's heights in the head.  A run of up to kAsk is asked for once, a longer one twice.
+constexpr int kAsk = 4;
 template <typename Need, typename Done>
 __device__ __forceinline__ void serve(const PageArgs &a, int64_t n, const Need &need, const Done &done) {
     __shared__ int64_t red[PT / 64];
@@ -106,22 +109,37 @@ __device__ __forceinline__ void serve(const PageArgs &a, int64_t n, const Need &
     __shared__ unsigned long long taken;
     if (threadIdx.x == 0) refused = 0, taken = 0;
     const int64_t run = (n + PT - 1) / PT, i0 = threadIdx.x * run, i1 = i0 + run < n ? i0 + run : n;
-    int64_t mine = 0, all;
-    for (int64_t i = i0; i < i1; ++i) {
-        const int64_t x = need(i);
-        mine += x > 0 ? x : 0;
+    int64_t mine = 0, all, ask[kAsk];
+    const int64_t top = free_blocks(a);
+    if (run <= kAsk) {
+#pragma unroll
+        for (int u = 0; u < kAsk; ++u) {
+            ask[u] = i0 + u < i1 ? need(i0 + u) : 0;
+            mine += ask[u] > 0 ? ask[u] : 0;
+        }
+    } else {
+        for (int64_t i = i0; i < i1; ++i) {
+            const int64_t x = need(i);
+            mine += x > 0 ? x : 0;
+        }
     }
     int64_t at = sum_before<PT>(mine, red, &all);
-    const int64_t top = free_blocks(a);
     int64_t last = 0;
     int32_t out = 0;
-    for (int64_t i = i0; i < i1; ++i) {
-        const int64_t x = need(i), ask = x > 0 ? x : 0;
+    const auto one = [&](int64_t i, int64_t x) {
+        const int64_t want = x > 0 ? x : 0;
         const bool served = x == 0 || (x > 0 && at + x <= top);
-        if (served && ask) last = at + ask;
+        if (served && want) last = at + want;
         out += !served;
-        done(i, served, at);
-        at += ask;
+        done(i, served, x, at);
+        at += want;
+    };
+    if (run <= kAsk) {
+#pragma unroll
+        for (int u = 0; u < kAsk; ++u)
+            if (i0 + u < i1) one(i0 + u, ask[u]);
+    } else {
+        for (int64_t i = i0; i < i1; ++i) one(i, need(i));
     }
     if (out) atomicAdd(&refused, out);
     if (last) atomicMax(&taken, (unsigned long long)last);  // running sums only grow
@@ -151,10 +169,9 @@ __global__ void __launch_bounds__(WT) count_runs(PageArgs a) {
     if (threadIdx.x == 0) a.counts[blockIdx.x] = (int32_t)all;
 }
 
-// A run's marked blocks onto the stack.
-__global__ void __launch_bounds__(WT) collect_blocks(PageArgs a) {
+// A run's marked blocks onto the stack, by a workgroup.
+__device__ __forceinline__ void collect_run(const PageArgs &a, int64_t run) {
     __shared__ int64_t red[WT / 64];
-    const int64_t run = blockIdx.x;
     int64_t before = 0, upto, here;
     if (a.nruns <= kFewRuns)
         for (int64_t i = threadIdx.x; i < run * (WT / 4); i += WT) before += __popcll(((const uint64_t *)a.marks)[i]);
@@ -171,6 +188,7 @@ __global__ void __launch_bounds__(WT) collect_blocks(PageArgs a) {
     for (; m; m &= m - 1, ++at)
         if (at < a.n_blocks) a.free_list[at] = (int32_t)(b0 + __builtin_ctz(m));
 }
+__global__ void __launch_bounds__(WT) collect_blocks(PageArgs a) { collect_run(a, blockIdx.x); }
 
 // ---------------------------------------------------------------------------
 // release: plan = (blocks kept, blocks held, block for the copy or -1, served)
@@ -190,9 +208,9 @@ __global__ void __launch_bounds__(PT) release_plan(PageArgs a) {
         const int32_t b = a.table[c * a.W + (n >> a.shift)];
         return is_block(a, b) && a.shared[b] > 0;
     };
-    serve(a, a.C, need, [&](int64_t c, bool served, int64_t first) {
+    serve(a, a.C, need, [&](int64_t c, bool served, int64_t x, int64_t first) {
         int64_t old;
-        const int64_t n = cut(c, &old), x = need(c);
+        const int64_t n = cut(c, &old);
         a.plan[c] = make_int4((int)nb(a, n), (int)nb(a, old), served && x ? fresh_block(a, top, first) : -1, served);
         if (served) a.lens[c] = (int32_t)n;
     });
@@ -222,25 +240,36 @@ __global__ void __launch_bounds__(WT) release_apply(PageArgs a) {
 // fork: plan = (tokens or -1, block for the copy or -1)
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ bool in_range(const PageArgs &a, int32_t c) { return c >= 0 && c < a.C; }
-__device__ __forceinline__ int32_t claimed(const PageArgs &a, int32_t c) {
-    return __hip_atomic_load(&a.claim[c], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// Who is the first of `n` to name a cell: in LDS for up to kClaims cells, else in the workspace.
+constexpr int kClaims = 8192;
+__device__ __forceinline__ int32_t claimed(const PageArgs &a, const int32_t *lds, int32_t c) {
+    return a.C <= kClaims ? lds[c] : __hip_atomic_load(&a.claim[c], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// Who is the first of `n` to name a cell.
-__device__ __forceinline__ void claim_cells(const PageArgs &a, int64_t n, const int32_t *cells) {
-    for (int64_t p = threadIdx.x; p < n; p += PT)
-        if (in_range(a, cells[p])) __hip_atomic_store(&a.claim[cells[p]], INT32_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ void claim_cells(const PageArgs &a, int32_t *lds, int64_t n, const int32_t *cells) {
+    if (a.C <= kClaims) {
+        for (int64_t c = threadIdx.x; c < a.C; c += PT) lds[c] = INT32_MAX;
+    } else {
+        for (int64_t p = threadIdx.x; p < n; p += PT)
+            if (in_range(a, cells[p])) __hip_atomic_store(&a.claim[cells[p]], INT32_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     __syncthreads();
-    for (int64_t p = threadIdx.x; p < n; p += PT)
-        if (in_range(a, cells[p])) atomicMin(&a.claim[cells[p]], (int32_t)p);
+    for (int64_t p = threadIdx.x; p < n; p += PT) {
+        const int32_t c = cells[p];
+        if (!in_range(a, c)) continue;
+        if (a.C <= kClaims) atomicMin(&lds[c], (int32_t)p);
+        else atomicMin(&a.claim[c], (int32_t)p);
+    }
     __syncthreads();
 }
 
 __global__ void __launch_bounds__(PT) fork_plan(PageArgs a) {
-    claim_cells(a, a.P, a.dst);
-    for (int64_t p = threadIdx.x; p < a.P; p += PT) {  // lengths of before the call
+    __shared__ int32_t claims[kClaims];
+    claim_cells(a, claims, a.P, a.dst);
+    // lengths of before the call: all are read before any is written
+    for (int64_t p = threadIdx.x; p < a.P; p += PT) {
         const int32_t s = a.src[p], t = a.dst[p];
         int64_t n = -1;
-        if (in_range(a, s) && in_range(a, t) && claimed(a, t) == p && length_of(a, t) == 0) {
+        if (in_range(a, s) && in_range(a, t) && claimed(a, claims, t) == p && length_of(a, t) == 0) {
             n = length_of(a, s);
             if (a.length && a.length[p] < n) n = a.length[p] > 0 ? a.length[p] : 0;
         }
@@ -249,13 +278,12 @@ __global__ void __launch_bounds__(PT) fork_plan(PageArgs a) {
     __syncthreads();
     const int64_t top = free_blocks(a);
     serve(a, a.P, [&](int64_t p) -> int64_t { const int n = a.plan[p].x; return n < 0 ? -1 : (n & (a.bs - 1)) != 0; },
-          [&](int64_t p, bool served, int64_t first) {
-              const int n = a.plan[p].x;
+          [&](int64_t p, bool served, int64_t x, int64_t first) {
               if (!served) {
                   a.plan[p].x = -1;
               } else {
-                  if (n & (a.bs - 1)) a.plan[p].y = fresh_block(a, top, first);
-                  a.lens[a.dst[p]] = n;
+                  if (x) a.plan[p].y = fresh_block(a, top, first);
+                  a.lens[a.dst[p]] = a.plan[p].x;
               }
           });
     if (threadIdx.x == 0) a.n_free[0] = (int32_t)a.head[0].left;  // this thread wrote it
@@ -291,19 +319,21 @@ __global__ void __launch_bounds__(WT) fork_apply(PageArgs a) {
 //
 // Tokens move inside their cell's own blocks, towards the front, so a chunk's
 // blocks may be written once the chunks that keep tokens of them, none of them
-// behind the chunk itself, have read theirs.  compact_move has a workgroup for
-// each chunk's keys and one for its values; each takes its chunk by ticket,
-// reads all it needs into LDS, says so, waits for the chunks before it that read
-// its blocks, and writes.  Tickets come from queues of whole cells, each in the
-// order of its chunks.  So who is waited for holds an earlier ticket of the same
-// queue, has started, and waits for nobody before it says that it has read:
-// every wait ends.
+// behind the chunk itself, have read theirs.  compact_move's workgroups take
+// chunks, keys and values apart, by ticket: they read all they need into LDS,
+// say so, wait for the chunks before theirs that read their blocks, and write.
+// Tickets come from queues of whole cells, each in the order of its chunks, and
+// a workgroup takes its next one before it is done with the one at hand.  So a
+// chunk waits for chunks of earlier tickets of its queue, and is waited for at
+// most until its workgroup is done with that of its ticket before: always for
+// what was handed out earlier, so every wait ends.
 // ---------------------------------------------------------------------------
 constexpr int CT = 1024;     // threads that look through a cell's list
 constexpr int MT = 512;      // threads that move a chunk
+constexpr int kMovers = 768;  // workgroups of it, three to a compute unit
 constexpr int kChunk = 256;  // tokens
 constexpr int kChunkShift = 8;
-constexpr int kQueues = 32;  // of keys, and as many of values
+constexpr int kQueues = 64;  // of keys, and as many of values
 constexpr int kApart = 64;   // counters lie in lines of their own
 
 __device__ __forceinline__ int64_t cell_of(const PageArgs &a, int64_t p) { return a.which ? a.which[p] : p; }
@@ -328,6 +358,13 @@ __global__ void __launch_bounds__(CT) compact_check(PageArgs a) {
     if (p == 0)
         for (int64_t t = tid; t < clamp(t0); t += CT) a.owner[t] = -1;
     for (int64_t t = clamp(t0) + tid; t < clamp(next); t += CT) a.owner[t] = t < t1 ? (int32_t)p : -1;
+    // the first blocks' owners, beside the list
+    const int32_t *row = a.table + c * a.W;
+    bool early = false;
+    if (!bad && tid < nb(a, n)) {
+        const int32_t b = row[tid];
+        early = is_block(a, b) && a.shared[b] > 0;
+    }
     int64_t stay = 0;
     if (!bad) {
         const int32_t *pos = a.kept_pos + o;
@@ -356,7 +393,6 @@ __global__ void __launch_bounds__(CT) compact_check(PageArgs a) {
     }
     int64_t fixed;
     sum_before<CT>(stay, red, &fixed);  // positions ascend: the tokens that stay come first
-    const int32_t *row = a.table + c * a.W;
     int64_t first = fixed >> a.shift;
     if (fixed == n && (n & (a.bs - 1))) {
         const int32_t b = row[first];
@@ -364,10 +400,14 @@ __global__ void __launch_bounds__(CT) compact_check(PageArgs a) {
     }
     int64_t take = 0;
     const int64_t b0 = block0(a, p);
-    for (int64_t j0 = first; j0 < nb(a, n); j0 += CT) {
+    for (int64_t j0 = 0; j0 < nb(a, n); j0 += CT) {
         const int64_t j = j0 + tid;
-        const int32_t b = j < nb(a, n) ? row[j] : -1;
-        const bool other = is_block(a, b) && a.shared[b] > 0;
+        bool other = early;
+        if (j0 > 0) {
+            const int32_t b = j < nb(a, n) ? row[j] : -1;
+            other = is_block(a, b) && a.shared[b] > 0;
+        }
+        other = other && j >= first;
         int64_t all;
         const int64_t before = sum_before<CT>(other, red, &all);
         if (j < nb(a, n)) a.rank[b0 + j] = other ? (int32_t)(take + before) : -1;
@@ -377,17 +417,18 @@ __global__ void __launch_bounds__(CT) compact_check(PageArgs a) {
 }
 
 __global__ void __launch_bounds__(PT) compact_plan(PageArgs a) {
-    if (a.which) claim_cells(a, a.P, a.which);
+    __shared__ int32_t claims[kClaims];
+    if (a.which) claim_cells(a, claims, a.P, a.which);
     bool down = false;
     for (int64_t p = threadIdx.x; p < a.P; p += PT) down = down || a.offsets[p] > a.offsets[p + 1];
     down = __syncthreads_or(down);
     serve(a, a.P,
           [&](int64_t p) -> int64_t {
               const int4 x = a.plan[p];
-              if (down || x.x < 0 || (a.which && claimed(a, a.which[p]) != p)) return -1;
+              if (down || x.x < 0 || (a.which && claimed(a, claims, a.which[p]) != p)) return -1;
               return x.z;
           },
-          [&](int64_t p, bool served, int64_t first) {
+          [&](int64_t p, bool served, int64_t, int64_t first) {
               if (!served) a.plan[p].x = -1;
               else a.plan[p].w = (int)first;
           });
@@ -432,49 +473,94 @@ __device__ __forceinline__ uint32_t max_bytes(uint32_t x, uint32_t y) {  // byte
 // LDS: a chunk's codes, keys [token][dp] or values [dp][kChunk + 4] (the padding spreads a column over the banks).
 //
 // Values lie tokens innermost, so whole blocks are read for the tokens that
-// stay.  A wave takes 64 rows of a block, a lane each, and up to 64 tokens of a
-// row at a time, all in flight together: its line of memory is fetched once.
-// Which bytes of a word stay is the same for every row, so words are packed by
-// byte permutes whose selectors, made once, the whole wave shares.
-__global__ void __launch_bounds__(MT) compact_move(PageArgs a) {
-    extern __shared__ __align__(16) uint8_t lds[];
-    __shared__ int32_t blk[kChunk];      // keys: a token's block; values: the block of a group of up to 64 tokens
-    __shared__ int32_t info[kChunk];     // keys: its place there; values: words of the group that keep tokens, 16 its place
-    __shared__ __align__(16) uint32_t sel_a[kChunk];  // values: a word's bytes into the output word that it joins
-    __shared__ uint32_t sel_b[kChunk];   // its bytes for the word after, if it fills that one, else 0
-    __shared__ int16_t ex[kChunk];
-    __shared__ int32_t to[kChunk / 16];
-    __shared__ int least[kChunk / 16];
-    __shared__ int32_t s_ticket, s_count[2][kChunk / 64], s_first[2][8];
-    float *const ratio = (float *)sel_a;  // once the tokens are packed
-    uint32_t *const top = sel_b;
+// stay.  A load takes 16 tokens of a row in each lane, neighbouring lanes
+// neighbouring bytes (a line of memory that a second load asks for while it is
+// still on its way holds up the compute unit's cache), and a lane packs the
+// bytes that stay: byte permutes whose selectors a table has for every choice of
+// a word's bytes and every place in the output word.  Words that two lanes fill
+// together are joined by LDS atomics, each byte written once.
+struct MoveShared {
+    alignas(16) uint64_t stay[kChunk];  // values: tokens of the group that stay; then the tokens' ratios and magnitudes
+    uint2 pack[64];        // selectors for four bits of these and 0 .. 3 bytes that are there
+    int2 place[kChunk];
+    int32_t blk[kChunk];   // keys: a token's block; values: the block of a group of up to 64 neighbours
+    int32_t info[kChunk];  // keys: its place there; values: the group's first token, and 8 its place
+    int16_t ex[kChunk];
+    int32_t to[kChunk / 16];
+    int least[kChunk / 16];
+    int32_t ticket, count[kChunk / 64];
+};
+
+template <bool VALUES>
+__device__ __forceinline__ void move_chunks(const PageArgs &a, uint8_t *const lds, MoveShared &sh) {
+    auto &stay = sh.stay;
+    auto &pack = sh.pack;
+    auto &place = sh.place;
+    auto &blk = sh.blk, &info = sh.info;
+    auto &to = sh.to;
+    auto &ex = sh.ex;
+    auto &least = sh.least;
+    auto &s_count = sh.count;
+    int32_t &s_ticket = sh.ticket;
+    float *const ratio = (float *)stay;  // once the tokens are packed
+    uint32_t *const top = (uint32_t *)stay + kChunk;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    if (tid == 0) {
-        s_ticket = -1;
-        for (int i = 0; i < 2 * kQueues && s_ticket < 0; ++i) {
-            const int q = (blockIdx.x + i) % (2 * kQueues), half = q >= kQueues, x = q - half * kQueues;
-            const int32_t first = a.starts[x], n = a.starts[x + 1] - first;
-            if (n <= 0) continue;
-            if (i > 0 && __hip_atomic_load(&a.tickets[q * kApart], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >= n) continue;
-            const int32_t got = atomicAdd(&a.tickets[q * kApart], 1);
-            if (got < n) s_ticket = 2 * (first + got) + half;
+    const int64_t size = (int64_t)a.bs * a.dp;
+    constexpr int vrow = kChunk + 4;
+    // The last wave takes the tickets, a lane for each queue: the next one while the chunk at hand is waited for.
+    int32_t *const tickets = a.tickets + VALUES * kQueues * kApart, *const read = a.read + VALUES * a.chunks;
+    const int q_first = a.starts[lane], q_size = a.starts[lane + 1] - q_first;
+    uint64_t open = __ballot(q_size > 0);  // queues that may have tickets left
+    const auto take_ticket = [&]() {
+        int32_t got = -1;
+        while (open) {
+            const int from = blockIdx.x & 63;
+            const int q = (__builtin_ctzll(open >> from | open << (64 - from & 63)) + from) & 63;
+            int32_t n = 0;
+            if (lane == q) n = atomicAdd(&tickets[lane * kApart], 1);
+            n = __builtin_amdgcn_readlane(n, q);
+            if (n < __builtin_amdgcn_readlane(q_size, q)) {
+                got = __builtin_amdgcn_readlane(q_first, q) + n;
+                break;
+            }
+            // a look at all of them, only now: everyone reads the same few lines
+            open &= __ballot(__hip_atomic_load(&tickets[lane * kApart], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < q_size);
         }
-    }
-    if (tid < kChunk / 16) least[tid] = 1;
+        if (lane == 0) s_ticket = got;
+    };
     __syncthreads();
-    if (s_ticket < 0) return;  // nothing moves: there are as many tickets as workgroups
-    const int64_t chunk = s_ticket >> 1;
-    const bool values = s_ticket & 1;
+    if (VALUES && tid < 64) {
+        const int fill = tid & 3;
+        int k = 0;
+        uint32_t bytes = 0, join = 0, rest = 0;
+        for (int i = 0; i < 4; ++i)
+            if (tid >> (2 + i) & 1) bytes |= (uint32_t)i << (8 * k++);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // bytes 4 .. 7 are the output word's, 0 .. 3 the new ones, 0x0c is zero
+            const int on = i - fill, up = i + 4 - fill;
+            join |= (i < fill ? 4u + i : on < k ? (bytes >> (8 * on)) & 0xFFu : 0x0Cu) << (8 * i);
+            rest |= (up < k ? (bytes >> (8 * up)) & 0xFFu : 0x0Cu) << (8 * i);
+        }
+        pack[tid] = make_uint2(join, rest);
+    }
+    if (w == MT / 64 - 1) take_ticket();
+    for (;;) {
+    __syncthreads();  // the ticket is there, and what the chunk before left in LDS is done with
+    const int32_t chunk = __builtin_amdgcn_readfirstlane(s_ticket);
+    if (chunk < 0) return;
     const int32_t p = a.owner[chunk];
-    if (p < 0) return;
-    const int4 x = a.plan[p];
-    const int64_t o = a.offsets[p], t0 = (o >> kChunkShift) + p, j = chunk - t0;
+    const int4 x = p < 0 ? make_int4(-1, 0, 0, 0) : a.plan[p];
+    const int64_t o = p < 0 ? 0 : a.offsets[p], t0 = (o >> kChunkShift) + p, j = chunk - t0;
     // this chunk's tokens in blocks that change
     const int lo = (int)max((int64_t)x.y * a.bs - j * kChunk, (int64_t)0), hi = (int)min(x.x - j * kChunk, (int64_t)kChunk);
-    if (lo >= hi) return;
+    if (p < 0 || lo >= hi) {
+        __syncthreads();  // everyone has the ticket
+        if (w == MT / 64 - 1) take_ticket();
+        continue;
+    }
+    if (tid < kChunk / 16) least[tid] = 1;
     const int32_t *row = a.table + cell_of(a, p) * a.W;
-    const uint8_t *codes = values ? a.vc : a.kc, *exps = values ? a.v_exp : a.k_exp;
-    const int64_t size = (int64_t)a.bs * a.dp;
+    const uint8_t *codes = VALUES ? a.vc : a.kc, *exps = VALUES ? a.v_exp : a.k_exp;
     // where each token lies
     const bool mine = tid >= lo && tid < hi;
     int b = -1, off = 0, e = 1;
@@ -494,11 +580,11 @@ __global__ void __launch_bounds__(MT) compact_move(PageArgs a) {
         if (n >= x.y) {
             const int32_t r = a.rank[(o >> a.shift) + p + n];
             t = r >= 0 ? a.free_list[a.head[0].top - 1 - (x.w + r)] : row[n];
+            if (!VALUES && r >= 0) a.taken[x.w + r] = t;
         }
         to[y] = is_block(a, t) ? t : -1;
     }
-    constexpr int vrow = kChunk + 4;
-    if (!values) {
+    if constexpr (!VALUES) {
         if (tid < kChunk) blk[tid] = b, info[tid] = off, top[tid] = 0;
         __syncthreads();
         const int per = a.dp / 16, n = hi * per;
@@ -521,107 +607,71 @@ __global__ void __launch_bounds__(MT) compact_move(PageArgs a) {
             }
         }
     } else {
-        // The tokens are cut into parts of at most 64; a part's tokens fall into words of four neighbours and groups of 64
-        // in their blocks.  The first token of a word or group stands for it.
-        const int groups = (a.dp + 63) / 64, parts = groups == 1 ? 8 : 4, per = kChunk / parts;
-        int2 *const place = (int2 *)lds;  // before any codes lie there
-        const int at = b < 0 ? 4 * tid : off;  // in a block that is none each token has a word of its own
-        if (tid < kChunk) place[tid] = make_int2(mine ? b : -2, at), info[tid] = 0;
+        for (int i = tid; i < a.dp * vrow / 16; i += MT) ((uint4 *)lds)[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (tid < kChunk) place[tid] = make_int2(mine ? b : -2, off >> 6), stay[tid] = 0;
         __syncthreads();
-        const bool edge = tid == lo || (tid & (per - 1)) == 0;
-        const int2 prev = mine && !edge ? place[tid - 1] : make_int2(-3, 0);
-        const bool first_w = mine && (prev.x != b || prev.y >> 2 != at >> 2);
-        const bool first_g = mine && (prev.x != b || b < 0 || prev.y >> 6 != at >> 6);
-        const uint64_t bw = __ballot(first_w), bg = __ballot(first_g);
-        if (lane == 0 && w < kChunk / 64) s_count[0][w] = __popcll(bw), s_count[1][w] = __popcll(bg);
+        // the first token of a group stands for it
+        const bool first = mine && (tid == lo || place[tid - 1].x != b || place[tid - 1].y != off >> 6);
+        const uint64_t heads = __ballot(first);
+        if (lane == 0 && w < kChunk / 64) s_count[w] = __popcll(heads);
         __syncthreads();
-        const uint64_t upto = (2ull << lane) - 1;
-        int nw = __popcll(bw & upto) - 1, ng = __popcll(bg & upto) - 1, words = 0, spans = 0;
+        int n = __popcll(heads & ((2ull << lane) - 1)) - 1, spans = 0;
 #pragma unroll
         for (int i = 0; i < kChunk / 64; ++i) {
-            if (i < w) nw += s_count[0][i], ng += s_count[1][i];
-            words += s_count[0][i], spans += s_count[1][i];
+            if (i < w) n += s_count[i];
+            spans += s_count[i];
         }
-        if (first_g) blk[ng] = b;
-        if (mine) atomicOr(&info[ng], 1 << ((off >> 2) & 15) | (first_g ? off >> 6 << 16 : 0));
-        if (first_w) {
-            // the bytes of this word that stay, in order, and how many
-            uint32_t bytes = at & 3;
-            int k = 1;
-            for (int i = tid + 1; k < 4 && i < hi && (i & (per - 1)) && place[i].x == b && place[i].y >> 2 == at >> 2; ++i, ++k)
-                bytes |= (uint32_t)(place[i].y & 3) << (8 * k);
-            const int fill = tid & 3;  // bytes of the output word that are there already
-            uint32_t sa = 0, sb = 0;
+        if (first) blk[n] = b, info[n] = tid | off >> 6 << 8;
+        if (mine) atomicOr((uint32_t *)&stay[n] + (off >> 5 & 1), 1u << (off & 31));
+        __syncthreads();
+        // a wave takes 64 rows of a group: `ppr` loads of 64 / ppr rows
+        const int ppr = a.bs < 64 ? a.bs / 16 : 4, ps = __builtin_ctz(ppr), strips = (a.dp + 63) / 64;
+        const int piece = lane & (ppr - 1);
+        const uint32_t mine_at = (lane >> ps) * a.bs + 16 * piece;
+        for (int y = w; y < spans * strips; y += MT / 64) {
+            const int g = y / strips, r0 = 64 * (y - g * strips), bg = __builtin_amdgcn_readfirstlane(blk[g]);
+            if (bg < 0) continue;
+            const int in = __builtin_amdgcn_readfirstlane(info[g]);
+            const uint64_t st = (uint64_t)__builtin_amdgcn_readfirstlane((int)(stay[g] >> 32)) << 32 |
+                                (uint32_t)__builtin_amdgcn_readfirstlane((int)stay[g]);
+            const uint8_t *from = a.vc + bg * size + 64 * (in >> 8) + (int64_t)r0 * a.bs;
+            const uint32_t m = (uint32_t)(st >> (16 * piece)) & 0xFFFFu;
+            const int rows = m ? a.dp - r0 - (lane >> ps) : 0;  // of this lane's, from the strip's first on
+            uint4 z[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int on = i - fill, up = i + 4 - fill;
-                sa |= (i < fill ? 4u + i : on < k ? (bytes >> (8 * on)) & 0xFFu : 0x0Cu) << (8 * i);
-                sb |= (up < k ? (bytes >> (8 * up)) & 0xFFu : 0x0Cu) << (8 * i);
+                z[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (i < ppr && (i << (6 - ps)) < rows) z[i] = *(const uint4 *)(from + (i << (6 - ps)) * a.bs + mine_at);
             }
-            sel_a[nw] = sa, sel_b[nw] = fill + k >= 4 ? sb : 0u;
-        }
-        if (tid < kChunk && (tid & (per - 1)) == 0) {
-            // a part's first word and group: those of its first token, none before `lo`, all behind `hi`
-            s_first[0][tid / per] = tid < lo ? 0 : tid < hi ? nw : words;
-            s_first[1][tid / per] = tid < lo ? 0 : tid < hi ? ng : spans;
-        }
-        __syncthreads();
-        for (int y = w; y < groups * parts; y += MT / 64) {
-            const int gr = y / parts, part = y - gr * parts, r = 64 * gr + lane, start = max(part * per, lo);
-            const int stop = min((part + 1) * per, hi);
-            if (start >= stop) continue;
-            int word = __builtin_amdgcn_readfirstlane(s_first[0][part]);
-            const int q0 = __builtin_amdgcn_readfirstlane(s_first[1][part]);
-            const int q1 = __builtin_amdgcn_readfirstlane(part + 1 < parts ? s_first[1][part + 1] : spans);
-            // at most 64 words and groups: a lane each
-            const int li = min(word + lane, kChunk - 1), gi = min(q0 + lane, kChunk - 1);
-            const uint32_t wa = sel_a[li], wb = sel_b[li];
-            const int gb = blk[gi], gm = info[gi], word0 = word;
-            const uint8_t *base = codes + (int64_t)(r < a.dp ? r : 0) * a.bs;
-            uint32_t *out = (uint32_t *)(lds + (r < a.dp ? r : 0) * vrow + start);
-            struct Group {
-                uint4 z[4];
-            };
-            const auto fetch = [&](int q, Group &g) {
-                const int bq = __builtin_amdgcn_readlane(gb, q - q0), mq = __builtin_amdgcn_readlane(gm, q - q0);
-                const uint8_t *at = base + (bq < 0 ? 0 : bq * size + 64 * (mq >> 16));
+            const int at = (in & 0xFF) + __popcll(st & ((1ull << (16 * piece)) - 1));
+            uint2 sel[4];
+            bool full[4];
+            int fill = at & 3;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    g.z[u] = make_uint4(0u, 0u, 0u, 0u);
-                    if (bq >= 0 && (mq >> (4 * u) & 15)) g.z[u] = *(const uint4 *)(at + 16 * u);
-                }
-            };
-            uint32_t acc = 0;
-            const auto pack = [&](int q, const Group &g) {
-                const int mq = __builtin_amdgcn_readlane(gm, q - q0);
+            for (int v = 0; v < 4; ++v) {
+                const uint32_t nib = m >> (4 * v) & 15u;
+                sel[v] = pack[nib << 2 | fill];
+                fill += __popc(nib);
+                full[v] = fill >= 4;
+                fill &= 3;
+            }
+            const int out0 = (r0 + (lane >> ps)) * vrow + (at & ~3);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    if (!(mq >> (4 * u) & 15)) continue;
-                    const uint32_t v[4] = {g.z[u].x, g.z[u].y, g.z[u].z, g.z[u].w};
+            for (int i = 0; i < 4; ++i) {
+                if (i >= ppr || (i << (6 - ps)) >= rows) continue;
+                uint32_t *out = (uint32_t *)(lds + out0 + (i << (6 - ps)) * vrow), acc = 0;
+                const uint32_t word[4] = {z[i].x, z[i].y, z[i].z, z[i].w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (!(mq >> (4 * u + i) & 1)) continue;
-                        acc = __builtin_amdgcn_perm(acc, v[i], __builtin_amdgcn_readlane(wa, word - word0));
-                        const uint32_t sb = __builtin_amdgcn_readlane(wb, word - word0);
-                        ++word;
-                        if (sb) {
-                            if (r < a.dp) *out = acc;
-                            ++out;
-                            acc = __builtin_amdgcn_perm(0u, v[i], sb);
-                        }
+                for (int v = 0; v < 4; ++v) {
+                    acc = __builtin_amdgcn_perm(acc, word[v], sel[v].x);
+                    if (full[v]) {
+                        atomicOr(out, acc);
+                        ++out;
+                        acc = __builtin_amdgcn_perm(0u, word[v], sel[v].y);
                     }
                 }
-            };
-            Group g0, g1;
-            fetch(q0, g0);
-            for (int q = q0; q < q1; q += 2) {
-                if (q + 1 < q1) fetch(q + 1, g1);
-                pack(q, g0);
-                if (q + 1 >= q1) break;
-                if (q + 2 < q1) fetch(q + 2, g0);
-                pack(q + 1, g1);
+                if (fill) atomicOr(out, acc);
             }
-            if ((stop & 3) && r < a.dp) *out = acc;
         }
         __syncthreads();
         // the largest magnitude of every token: four tokens and a share of the rows a thread
@@ -637,21 +687,22 @@ __global__ void __launch_bounds__(MT) compact_move(PageArgs a) {
         }
     }
     __syncthreads();  // everything has been read
-    if (tid == 0) __hip_atomic_store(&a.read[values * a.chunks + chunk], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid == 0) __hip_atomic_store(&read[chunk], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (mine) atomicMax(&least[tid >> a.shift], least_exp((int)top[tid], e));
     __syncthreads();
     if (mine) ratio[tid] = exp_ratio(e, min(least[tid >> a.shift], 253));
+    if (w == MT / 64 - 1) take_ticket();  // everyone has the one at hand
     // the chunks before this one that keep tokens of its positions
     {
         const int64_t r0 = a.within[chunk], r1 = (j + 1) * kChunk < x.x ? a.within[chunk + 1] : x.x;
         const int64_t i0 = max(r0, (int64_t)x.y * a.bs) >> kChunkShift, i1 = min((r1 + kChunk - 1) >> kChunkShift, j);
         for (int64_t i = i0 + tid; i < i1; i += MT)
-            while (!__hip_atomic_load(&a.read[values * a.chunks + t0 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
+            while (!__hip_atomic_load(&read[t0 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
                 __builtin_amdgcn_s_sleep(1);
     }
     __syncthreads();
-    uint8_t *dst = values ? a.vc : a.kc;
-    if (!values) {
+    uint8_t *dst = VALUES ? a.vc : a.kc;
+    if constexpr (!VALUES) {
         const int per = a.dp / 16;
         for (int i = lo * per + tid; i < hi * per; i += MT) {
             const int t = i / per, n = to[t >> a.shift];
@@ -683,27 +734,46 @@ __global__ void __launch_bounds__(MT) compact_move(PageArgs a) {
         }
     }
     if (tid < kChunk >> a.shift && (tid << a.shift) >= lo && (tid << a.shift) < hi && to[tid] >= 0)
-        (values ? a.v_exp : a.k_exp)[to[tid]] = (uint8_t)min(least[tid], 253);
+        (VALUES ? a.v_exp : a.k_exp)[to[tid]] = (uint8_t)min(least[tid], 253);
+    }
 }
 
-// The listed cells' new tables and lengths.
-__global__ void __launch_bounds__(CT) compact_apply(PageArgs a) {
-    const int64_t p = blockIdx.x;
+// Two workgroups of three begin with values, which are twice the work, and end with keys.  Whoever is out of tickets
+// counts down the owners of the blocks that the listed cells leave.
+__global__ void __launch_bounds__(MT, 6) compact_move(PageArgs a) {
+    extern __shared__ __align__(16) uint8_t lds[];
+    __shared__ MoveShared sh;
+    for (int i = 0; i < 2; ++i) {
+        if ((blockIdx.x % 3 != 0) != (i == 1)) move_chunks<true>(a, lds, sh);
+        else move_chunks<false>(a, lds, sh);
+    }
+    for (int64_t p = blockIdx.x; p < a.P; p += gridDim.x) {
+        const int4 x = a.plan[p];
+        if (x.x < 0) continue;
+        const int64_t c = cell_of(a, p), b0 = block0(a, p), now = nb(a, x.x), had = nb(a, length_of(a, c));
+        const int32_t *row = a.table + c * a.W;
+        for (int64_t j = (x.z > 0 ? x.y : now) + threadIdx.x; j < had; j += MT)
+            if (j >= now || a.rank[b0 + j] >= 0) leave_block(a, row[j]);
+    }
+}
+
+// The blocks that were left onto the stack; the workgroups behind write the listed cells' new tables and lengths.
+__global__ void __launch_bounds__(WT) compact_finish(PageArgs a) {
+    if (blockIdx.x < a.nruns) {
+        collect_run(a, blockIdx.x);
+        return;
+    }
+    const int64_t p = blockIdx.x - a.nruns;
     const int4 x = a.plan[p];
     if (x.x < 0) return;
     const int64_t c = cell_of(a, p), b0 = block0(a, p), now = nb(a, x.x), had = nb(a, length_of(a, c));
     int32_t *row = a.table + c * a.W;
     if (x.z > 0)
-        for (int64_t j = x.y + threadIdx.x; j < now; j += CT) {
+        for (int64_t j = x.y + threadIdx.x; j < now; j += WT) {
             const int32_t r = a.rank[b0 + j];
-            if (r < 0) continue;
-            leave_block(a, row[j]);
-            row[j] = a.free_list[a.head[0].top - 1 - (x.w + r)];
+            if (r >= 0) row[j] = a.taken[x.w + r];
         }
-    for (int64_t j = now + threadIdx.x; j < had; j += CT) {
-        leave_block(a, row[j]);
-        row[j] = -1;
-    }
+    for (int64_t j = now + threadIdx.x; j < had; j += WT) row[j] = -1;
     __syncthreads();  // everyone has read the length
     if (threadIdx.x == 0) a.lens[c] = x.x;
 }
@@ -728,7 +798,8 @@ size_t layout(PageArgs &a, int kind, void *ws) {
     a.plan = l.take<int4>(kind == 0 ? a.C : a.P);
     if (kind == 2) {
         a.chunks = a.n_kept / kChunk + a.P;
-        a.rank = l.take<int32_t>(a.n_kept / a.bs + a.P), a.owner = l.take<int32_t>(a.chunks);
+        a.rank = l.take<int32_t>(a.n_kept / a.bs + a.P), a.taken = l.take<int32_t>(a.n_kept / a.bs + a.P);
+        a.owner = l.take<int32_t>(a.chunks);
         a.within = l.take<int32_t>(a.chunks), a.read = l.take<int32_t>(2 * a.chunks);
         a.tickets = l.take<int32_t>(2 * kQueues * kApart);
         a.starts = l.take<int32_t>(kQueues + 1);
@@ -744,10 +815,6 @@ PageArgs page_args(const fw_cache &cache, const fw_cells &cells) {
     a.shared = cells.shared;
     a.kc = cache.k, a.vc = cache.v, a.k_exp = cache.k_exp, a.v_exp = cache.v_exp;
     return a;
-}
-void launch_collect(const PageArgs &a, hipStream_t st) {
-    if (a.nruns > kFewRuns) hipLaunchKernelGGL(count_runs, dim3((unsigned)a.nruns), dim3(WT), 0, st, a);
-    hipLaunchKernelGGL(collect_blocks, dim3((unsigned)a.nruns), dim3(WT), 0, st, a);
 }
 }  // namespace
 
@@ -765,7 +832,8 @@ hipError_t launch_release(const fw_cache &cache, const fw_cells &cells, const in
     if (a.nruns > kFewRuns) hipLaunchKernelGGL(clear_all, dim3((unsigned)std::min<int64_t>(a.nruns / 4 + 1, 1024)), dim3(WT), 0, st, a);
     hipLaunchKernelGGL(release_plan, dim3(1), dim3(PT), 0, st, a);
     hipLaunchKernelGGL(release_apply, dim3((unsigned)a.C), dim3(WT), 0, st, a);
-    launch_collect(a, st);
+    if (a.nruns > kFewRuns) hipLaunchKernelGGL(count_runs, dim3((unsigned)a.nruns), dim3(WT), 0, st, a);
+    hipLaunchKernelGGL(collect_blocks, dim3((unsigned)a.nruns), dim3(WT), 0, st, a);
     return hipGetLastError();
 }
 
@@ -788,9 +856,9 @@ hipError_t launch_cell_compact(const fw_cache &cache, const fw_cells &cells, int
     if (P > 0) hipLaunchKernelGGL(compact_check, dim3((unsigned)P), dim3(CT), 0, st, a);
     hipLaunchKernelGGL(compact_plan, dim3(1), dim3(PT), 0, st, a);
     if (P == 0) return hipGetLastError();
-    hipLaunchKernelGGL(compact_move, dim3((unsigned)(2 * a.chunks)), dim3(MT), a.dp * (kChunk + 4), st, a);
-    hipLaunchKernelGGL(compact_apply, dim3((unsigned)P), dim3(CT), 0, st, a);
-    launch_collect(a, st);
+    hipLaunchKernelGGL(compact_move, dim3((unsigned)std::min<int64_t>(2 * a.chunks, kMovers)), dim3(MT), a.dp * (kChunk + 4), st, a);
+    if (a.nruns > kFewRuns) hipLaunchKernelGGL(count_runs, dim3((unsigned)a.nruns), dim3(WT), 0, st, a);
+    hipLaunchKernelGGL(compact_finish, dim3((unsigned)(a.nruns + P)), dim3(WT), 0, st, a);
     return hipGetLastError();
 }
 

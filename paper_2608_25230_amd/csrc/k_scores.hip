@@ -40,6 +40,7 @@ constexpr int kFewLeast = 1;    // tiles of a wave at least
 constexpr int kQBytes = 65536;  // many_rows: rows in LDS at a time
 constexpr int kManyGroups = 512;
 constexpr int kManyLeast = 2;   // tiles of a workgroup at least
+constexpr int kFill = 8;        // what a cell's rows cost there, in tiles
 constexpr float SLOG2E = 1.4426950408889634f;
 
 struct ScoreArgs {
@@ -75,16 +76,21 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
     return (bf16x8){a[0], a[1], b[0], b[1], c[0], c[1], e[0], e[1]};
 }
 
-// Shares [g0, g1) of the cells' tiles, N to a workgroup, share i of workgroup b being number b N + i of `shares`: each
-// share's first cell and the first tile of that.  found[i] = (cell, its first tile), cell -1 where the share is empty.
-template <int NT, int N>
+// Shares [g0, g1) of the cells' tiles, EXTRA more for what a cell costs besides them, N to a workgroup, share i of
+// workgroup b being number b N + i of `shares`: each share's first cell and the first tile of that.  found[i] = (cell, its
+// first tile), cell -1 where the share is empty.
+template <int NT, int N, int EXTRA>
 __device__ __forceinline__ void find_shares(const ScoreArgs &a, int shares, int least, int2 (&found)[N], int *per) {
     __shared__ int red[NT / 64];
     __shared__ int2 got[N];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int run = (a.C + NT - 1) / NT, c0 = tid * run, c1 = c0 + run < a.C ? c0 + run : a.C;
     int mine = 0;
-    for (int c = c0; c < c1; ++c) mine += (scored(a, c) + TT - 1) / TT;
+    const auto tiles_of = [&](int c) {
+        const int n = scored(a, c);
+        return n > 0 ? (n + TT - 1) / TT + EXTRA : 0;
+    };
+    for (int c = c0; c < c1; ++c) mine += tiles_of(c);
     int x = mine;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -107,7 +113,7 @@ __device__ __forceinline__ void find_shares(const ScoreArgs &a, int shares, int 
         if (g < first || g >= first + mine) continue;
         int at = first;
         for (int c = c0; c < c1; ++c) {
-            const int n = (scored(a, c) + TT - 1) / TT;
+            const int n = tiles_of(c);
             if (g < at + n) {
                 got[i] = make_int2(c, at);
                 break;
@@ -210,7 +216,7 @@ __global__ void __launch_bounds__(FT, DP <= (sizeof(T) == 2 ? 128 : 64) ? 4 : 2)
     const int tl = lane & 15, g = lane >> 4;
     int2 found[FT / 64];
     int per;
-    find_shares<FT, FT / 64>(a, gridDim.x * (FT / 64), kFewLeast, found, &per);
+    find_shares<FT, FT / 64, 0>(a, gridDim.x * (FT / 64), kFewLeast, found, &per);
     int c = -1, at = 0;
 #pragma unroll
     for (int i = 0; i < FT / 64; ++i)
@@ -297,7 +303,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) many_rows(ScoreArgs 
     int *const back = (int *)(ls + a.turn);
     int2 found[1];
     int per;
-    find_shares<NT, 1>(a, gridDim.x, kManyLeast, found, &per);
+    find_shares<NT, 1, kFill>(a, gridDim.x, kManyLeast, found, &per);
     int c = __builtin_amdgcn_readfirstlane(found[0].x), at = __builtin_amdgcn_readfirstlane(found[0].y);
     if (c < 0) return;
     const int g0 = blockIdx.x * per, g1 = g0 + per;
@@ -306,7 +312,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) many_rows(ScoreArgs 
     for (; c < a.C && at < g1; ++c) {
         const int len = cell_len(a, c), n = scored(a, c), nt = (n + TT - 1) / TT;
         const int t0 = max(g0 - at, 0), t1 = min(g1 - at, nt);
-        at += nt;
+        at += nt > 0 ? nt + kFill : 0;
         if (t0 >= t1) continue;
         const int seq = c / a.Hkv, h = c % a.Hkv;
         const int32_t *row = a.table + (int64_t)c * a.W;

@@ -6,6 +6,7 @@ no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Any, Dict, NamedTuple, Optional, Sequence
 
@@ -422,6 +423,7 @@ class KvCache(NamedTuple):
         return self.k.shape[1]
 
 
+@functools.lru_cache(maxsize=None)
 def cache_row(d: int) -> int:
     """Bytes of a cached key's row: d rounded up to 32, 64, 96, 128, 192 or 256."""
     return lib().fw_cache_row(d)
@@ -454,6 +456,14 @@ def _want(name: str, t, dtype, dim: int, device) -> None:
     if t.dtype is not dtype or t.dim() != dim or t.device != device or not t.is_contiguous():
         raise FwError(2, f"{name} must be a contiguous {dim}-dimensional {dtype} tensor on {device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _all_fit(tensors, dtype, index: int) -> bool:
+    """Whether these are contiguous tensors of this type on the device of this index (``_want`` says what is wrong)."""
+    for t in tensors:
+        if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+            return False
+    return True
 
 
 def _rows_of(name: str, t, dtype, dim: int, device) -> None:
@@ -567,10 +577,11 @@ def block_tables(old_len, new_len, table, free_list, n_free, block_size: int, *,
 def _cache(c: KvCache, device) -> Cache:
     k, v, k_exp, v_exp, d = c
     u8 = _torch().uint8
-    _want("cache.k", k, u8, 3, device)
-    _want("cache.v", v, u8, 3, device)
-    _want("cache.k_exp", k_exp, u8, 1, device)
-    _want("cache.v_exp", v_exp, u8, 1, device)
+    if not (_all_fit(c[:4], u8, device.index) and k.dim() == v.dim() == 3 and k_exp.dim() == v_exp.dim() == 1):
+        _want("cache.k", k, u8, 3, device)
+        _want("cache.v", v, u8, 3, device)
+        _want("cache.k_exp", k_exp, u8, 1, device)
+        _want("cache.v_exp", v_exp, u8, 1, device)
     n, bs, dp = k.shape
     if dp != cache_row(d) or v.shape != (n, dp, bs) or k_exp.shape[0] != n or v_exp.shape[0] != n:
         raise FwError(2, f"the cache's buffers do not fit together: k {tuple(k.shape)}, v {tuple(v.shape)}, "
@@ -801,17 +812,18 @@ def cache_cells(C: int, max_blocks: int, n_blocks: int, device="cuda") -> CacheC
 
 def _cells(t: CacheCells, cache: KvCache, device) -> Cells:
     i32 = _torch().int32
-    _want("cells.table", t.table, i32, 2, device)
-    for name in ("lens", "free_list", "n_free", "shared"):
-        _want("cells." + name, getattr(t, name), i32, 1, device)
-    C, W = t.table.shape
+    table, lens, free_list, n_free, shared = t
+    if not (_all_fit(t, i32, device.index) and table.dim() == 2 and lens.dim() == free_list.dim() == n_free.dim() == shared.dim() == 1):
+        _want("cells.table", table, i32, 2, device)
+        for name in ("lens", "free_list", "n_free", "shared"):
+            _want("cells." + name, getattr(t, name), i32, 1, device)
+    C, W = table.shape
     n = cache.k.shape[0]
-    if t.lens.shape[0] != C or t.free_list.shape[0] != n or t.n_free.shape[0] != 1 or t.shared.shape[0] != n:
-        raise FwError(2, f"the cells' arrays do not fit together: table {tuple(t.table.shape)}, lens {tuple(t.lens.shape)}, "
-                         f"free_list {tuple(t.free_list.shape)}, n_free {tuple(t.n_free.shape)}, shared "
-                         f"{tuple(t.shared.shape)}, {n} blocks")
-    return Cells(C, W, t.table.data_ptr(), t.lens.data_ptr(), t.free_list.data_ptr(), t.n_free.data_ptr(),
-                 t.shared.data_ptr())
+    if lens.shape[0] != C or free_list.shape[0] != n or n_free.shape[0] != 1 or shared.shape[0] != n:
+        raise FwError(2, f"the cells' arrays do not fit together: table {tuple(table.shape)}, lens {tuple(lens.shape)}, "
+                         f"free_list {tuple(free_list.shape)}, n_free {tuple(n_free.shape)}, shared {tuple(shared.shape)}, {n} "
+                         "blocks")
+    return Cells(C, W, table.data_ptr(), lens.data_ptr(), free_list.data_ptr(), n_free.data_ptr(), shared.data_ptr())
 
 
 def _space(need: int, ws, like):
