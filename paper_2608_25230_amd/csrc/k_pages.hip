@@ -89,12 +89,16 @@ __device__ __forceinline__ void leave_block(const PageArgs &a, int32_t b) {
     atomicOr((uint32_t *)a.marks + (b >> 5), 1u << (b & 31));
 }
 
-// A block's codes and exponents, by a workgroup.
+// A block's codes and exponents, by a workgroup of WT threads.
 __device__ __forceinline__ void copy_block(const PageArgs &a, int32_t from, int32_t to) {
     const int64_t n = (int64_t)a.bs * a.dp;
     const uint4 *k0 = (const uint4 *)(a.kc + from * n), *v0 = (const uint4 *)(a.vc + from * n);
     uint4 *k1 = (uint4 *)(a.kc + to * n), *v1 = (uint4 *)(a.vc + to * n);
-    for (int i = threadIdx.x; i < n / 16; i += blockDim.x) k1[i] = k0[i], v1[i] = v0[i];
+#pragma unroll 2
+    for (int i = threadIdx.x; i < n / 16; i += WT) {
+        const uint4 x = k0[i], y = v0[i];
+        k1[i] = x, v1[i] = y;
+    }
     if (threadIdx.x == 0) a.k_exp[to] = a.k_exp[from], a.v_exp[to] = a.v_exp[from];
 }
 
@@ -265,27 +269,30 @@ __device__ __forceinline__ void claim_cells(const PageArgs &a, int32_t *lds, int
 __global__ void __launch_bounds__(PT) fork_plan(PageArgs a) {
     __shared__ int32_t claims[kClaims];
     claim_cells(a, claims, a.P, a.dst);
-    // lengths of before the call: all are read before any is written
-    for (int64_t p = threadIdx.x; p < a.P; p += PT) {
+    const auto tokens = [&](int64_t p) -> int64_t {  // of pair p, or -1
         const int32_t s = a.src[p], t = a.dst[p];
-        int64_t n = -1;
-        if (in_range(a, s) && in_range(a, t) && claimed(a, claims, t) == p && length_of(a, t) == 0) {
-            n = length_of(a, s);
-            if (a.length && a.length[p] < n) n = a.length[p] > 0 ? a.length[p] : 0;
-        }
-        a.plan[p] = make_int4((int)n, -1, 0, 0);
-    }
-    __syncthreads();
+        if (!in_range(a, s) || !in_range(a, t) || claimed(a, claims, t) != p || length_of(a, t) != 0) return -1;
+        const int64_t n = length_of(a, s);
+        return !a.length || a.length[p] >= n ? n : a.length[p] > 0 ? a.length[p] : 0;
+    };
+    const auto blocks = [&](int64_t n) -> int64_t { return n < 0 ? -1 : (n & (a.bs - 1)) != 0; };
     const int64_t top = free_blocks(a);
-    serve(a, a.P, [&](int64_t p) -> int64_t { const int n = a.plan[p].x; return n < 0 ? -1 : (n & (a.bs - 1)) != 0; },
-          [&](int64_t p, bool served, int64_t x, int64_t first) {
-              if (!served) {
-                  a.plan[p].x = -1;
-              } else {
-                  if (x) a.plan[p].y = fresh_block(a, top, first);
-                  a.lens[a.dst[p]] = a.plan[p].x;
-              }
-          });
+    const auto done = [&](int64_t p, bool served, int64_t x, int64_t first, int64_t n) {
+        a.plan[p] = make_int4(served ? (int)n : -1, served && x ? fresh_block(a, top, first) : -1, 0, 0);
+        if (served) a.lens[a.dst[p]] = (int)n;
+    };
+    // lengths of before the call: all are read before any is written
+    const int64_t run = (a.P + PT - 1) / PT, i0 = threadIdx.x * run;
+    if (run <= kAsk) {  // read when serve asks, once, before it lets any thread go on
+        int64_t n[kAsk];
+        serve(a, a.P, [&](int64_t p) { return blocks(n[p - i0] = tokens(p)); },
+              [&](int64_t p, bool served, int64_t x, int64_t first) { done(p, served, x, first, n[p - i0]); });
+    } else {
+        for (int64_t p = threadIdx.x; p < a.P; p += PT) a.plan[p].x = (int)tokens(p);
+        __syncthreads();
+        serve(a, a.P, [&](int64_t p) { return blocks(a.plan[p].x); },
+              [&](int64_t p, bool served, int64_t x, int64_t first) { done(p, served, x, first, a.plan[p].x); });
+    }
     if (threadIdx.x == 0) a.n_free[0] = (int32_t)a.head[0].left;  // this thread wrote it
 }
 

@@ -431,7 +431,7 @@ hipError_t launch_scores_width(ScoreArgs &a, hipStream_t st) {
 // and at the key come to is read off its histogram of the last digit, so each
 // slice finds its place from those of the slices before it.
 // ---------------------------------------------------------------------------
-constexpr int LT = 1024;          // threads of a workgroup
+constexpr int LT = 1024;          // threads of a workgroup; fewer for short rows
 constexpr int kBins = 2048;
 constexpr int kAlone = 32 * LT;   // tokens of a cell that one workgroup takes alone
 constexpr int kSlice = 8 * LT;    // tokens of a slice otherwise
@@ -446,6 +446,7 @@ struct SelectArgs {
     // slices
     int slices;
     uint32_t *hist;   // [C][3][kBins]
+    uint2 *state;     // [C][3] the key's digits so far, and its rank among the tokens that share them
     uint32_t *last;   // [C][slices][kBins / 2] the last digit's, of a slice
     uint32_t *above;  // [C][slices] tokens above the first two digits
 };
@@ -492,15 +493,23 @@ __device__ __forceinline__ V scan_before(V v, V *red, V *total) {
     return before;
 }
 
-// The bin from the top that holds the rem-th entry, and the entries above it.
-__device__ __forceinline__ void pick_bin(const uint32_t *hist, uint32_t rem, uint32_t *red, uint32_t *found, uint32_t *bin,
+// The bin from the top that holds the rem-th entry, and the entries above it; `count` gives a bin's entries.
+template <int NT, typename Count>
+__device__ __forceinline__ void pick_bin(const Count &count, uint32_t rem, uint32_t *red, uint32_t *found, uint32_t *bin,
                                          uint32_t *above) {
-    const int t = kBins - 2 - 2 * threadIdx.x;  // two bins a thread
-    const uint2 h = *(const uint2 *)(hist + t);
-    uint32_t all;
-    const uint32_t before = scan_before<LT, uint32_t>(h.x + h.y, red, &all);
-    if (before < rem && rem <= before + h.y) found[0] = t + 1, found[1] = before;
-    else if (before + h.y < rem && rem <= before + h.y + h.x) found[0] = t, found[1] = before + h.y;
+    constexpr int N = kBins / NT;  // of a thread, from the top
+    uint32_t h[N], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        h[i] = count(kBins - 1 - N * (int)threadIdx.x - i);
+        sum += h[i];
+    }
+    uint32_t before = scan_before<NT, uint32_t>(sum, red, &all);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (before < rem && rem <= before + h[i]) found[0] = kBins - 1 - N * threadIdx.x - i, found[1] = before;
+        before += h[i];
+    }
     __syncthreads();
     *bin = found[0], *above = found[1];
 }
@@ -508,13 +517,13 @@ __device__ __forceinline__ void pick_bin(const uint32_t *hist, uint32_t rem, uin
 __device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
 __device__ __forceinline__ uint32_t digit_mask(int pass) { return pass == 2 ? 1023u : 2047u; }
 
-// Keys of tokens first + 4 LT k + 4 t + i; those at nf and past it are 0, below every score's key.
-template <int E>
+// Keys of tokens first + 4 NT k + 4 t + i; those at nf and past it are 0, below every score's key.
+template <int NT, int E>
 __device__ __forceinline__ void load_keys(const float *row, int first, int nf, uint32_t (&u)[E]) {
     const bool wide = ((uintptr_t)row & 15) == 0;
 #pragma unroll
     for (int k = 0; k < E / 4; ++k) {
-        const int j = first + 4 * LT * k + 4 * (int)threadIdx.x;
+        const int j = first + 4 * NT * k + 4 * (int)threadIdx.x;
         float4 x = {0.f, 0.f, 0.f, 0.f};
         if (wide && j + 4 <= nf) {
             x = *(const float4 *)(row + j);
@@ -529,18 +538,31 @@ __device__ __forceinline__ void load_keys(const float *row, int first, int nf, u
     }
 }
 
+// Scores have few exponents, so lanes meet in a bin: each bin has kCopies places, one for every kCopies-th lane.
+constexpr int kCopies = 4;
 template <int E>
 __device__ __forceinline__ void count_digit(const uint32_t (&u)[E], uint32_t key, uint32_t mask, int pass, uint32_t *hist) {
+    uint32_t *mine = hist + (threadIdx.x & (kCopies - 1));
 #pragma unroll
     for (int i = 0; i < E; ++i)
-        if (u[i] && (u[i] & mask) == key) atomicAdd(&hist[(u[i] >> digit_shift(pass)) & digit_mask(pass)], 1u);
+        if (u[i] && (u[i] & mask) == key) atomicAdd(&mine[((u[i] >> digit_shift(pass)) & digit_mask(pass)) * kCopies], 1u);
+}
+__device__ __forceinline__ uint32_t bin_of(const uint32_t *hist, int bin) {
+    const uint4 x = *(const uint4 *)(hist + bin * kCopies);
+    return x.x + x.y + x.z + x.w;
+}
+template <int NT>
+__device__ __forceinline__ void clear_bins(uint32_t *hist) {
+    for (int i = threadIdx.x; i < kBins; i += NT) *(uint4 *)(hist + i * kCopies) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // Writes the positions above the key and the first rem - eq0 of those at it, from place `at` on; eq0: those at it before.
-template <int E>
+template <int NT, int E>
 __device__ __forceinline__ void write_chosen(const SelectArgs &a, const uint32_t (&u)[E], int first, uint32_t key, uint32_t rem,
-                                             uint32_t eq0, int64_t at, uint32_t (*red)[LT / 64]) {
+                                             uint32_t eq0, int64_t at, uint32_t (*red)[NT / 64]) {
+    __shared__ uint32_t totals[E / 4];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    constexpr int NW = NT / 64, N = E / 4 * NW;
     uint32_t before[E / 4];  // above the key in the low half, at it in the high one (at most 4096 each)
 #pragma unroll
     for (int k = 0; k < E / 4; ++k) {
@@ -557,23 +579,31 @@ __device__ __forceinline__ void write_chosen(const SelectArgs &a, const uint32_t
         before[k] = x - v;
     }
     __syncthreads();
+    // the waves' sums of each k become what lies before each wave; the totals go behind
+    if (threadIdx.x < N) {
+        uint32_t *const p = &red[0][0] + threadIdx.x;
+        const uint32_t v = *p;
+        uint32_t x = v;
+#pragma unroll
+        for (int off = 1; off < NW; off <<= 1) {
+            const uint32_t y = __shfl_up(x, off, NW);
+            if ((lane & (NW - 1)) >= off) x += y;
+        }
+        *p = x - v;
+        if ((lane & (NW - 1)) == NW - 1) totals[threadIdx.x / NW] = x;
+    }
+    __syncthreads();
     uint32_t eq = eq0;
 #pragma unroll
     for (int k = 0; k < E / 4; ++k) {
-        uint32_t all = 0, b = before[k];
-#pragma unroll
-        for (int i = 0; i < LT / 64; ++i) {
-            const uint32_t y = red[k][i];
-            if (i < w) b += y;
-            all += y;
-        }
+        const uint32_t all = totals[k], b = before[k] + red[k][w];
         uint32_t e = eq + (b >> 16);
         int64_t o = at + (b & 0xFFFFu) + (min(e, rem) - min(eq, rem));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool same = u[4 * k + i] == key;
             if (u[4 * k + i] > key || (same && e < rem)) {
-                if (o < a.n_kept) a.kept_pos[o] = first + 4 * LT * k + 4 * (int)threadIdx.x + i;
+                if (o < a.n_kept) a.kept_pos[o] = first + 4 * NT * k + 4 * (int)threadIdx.x + i;
                 ++o;
             }
             e += same;
@@ -585,39 +615,42 @@ __device__ __forceinline__ void write_chosen(const SelectArgs &a, const uint32_t
 }
 
 // Kept tokens of the cells before c and of all.
+template <int NT>
 __device__ __forceinline__ int64_t kept_before(const SelectArgs &a, int64_t c, int64_t *red, int64_t *total) {
     int64_t lo = 0, hi = 0;
     int len;
-    for (int64_t i = threadIdx.x; i < a.C; i += LT) {
+    for (int64_t i = threadIdx.x; i < a.C; i += NT) {
         const int k = kept_of(a, i, &len);
         if (i < c) lo += k;
         else hi += k;
     }
     int64_t x, y;
-    scan_before<LT, int64_t>(lo, red, &x);
-    scan_before<LT, int64_t>(hi, red, &y);
+    scan_before<NT, int64_t>(lo, red, &x);
+    scan_before<NT, int64_t>(hi, red, &y);
     *total = x + y;
     return x;
 }
+template <int NT>
 __device__ __forceinline__ void write_certain(const SelectArgs &a, const CellChoice &x, int64_t o) {
-    for (int i = threadIdx.x; i < x.certain; i += LT)
+    for (int i = threadIdx.x; i < x.certain; i += NT)
         if (o + x.need + i < a.n_kept) a.kept_pos[o + x.need + i] = x.nf + i;
 }
 // -1 behind the last kept token, by workgroup b of nb
+template <int NT>
 __device__ __forceinline__ void write_rest(const SelectArgs &a, int64_t total, int64_t b, int64_t nb) {
-    for (int64_t i = total + b * LT + threadIdx.x; i < a.n_kept; i += nb * LT) a.kept_pos[i] = -1;
+    for (int64_t i = total + b * NT + threadIdx.x; i < a.n_kept; i += nb * NT) a.kept_pos[i] = -1;
 }
 
 // OWN: every workgroup sums the cells' counts for itself; else the offsets are there.
-template <int E, bool OWN>
-__global__ void __launch_bounds__(LT) select_cell(SelectArgs a) {
-    __shared__ __align__(8) uint32_t hist[kBins];
-    __shared__ uint32_t red[E / 4 > 1 ? E / 4 : 1][LT / 64], found[2];
-    __shared__ int64_t sums[LT / 64];
+template <int NT, int E, bool OWN>
+__global__ void __launch_bounds__(NT) select_cell(SelectArgs a) {
+    __shared__ __align__(16) uint32_t hist[kBins * kCopies];
+    __shared__ uint32_t red[E / 4 > 1 ? E / 4 : 1][NT / 64], found[2];
+    __shared__ int64_t sums[NT / 64];
     const int64_t c = blockIdx.x;
     int64_t total, o;
     if (OWN) {
-        o = kept_before(a, c, sums, &total);
+        o = kept_before<NT>(a, c, sums, &total);
         if (threadIdx.x == 0) {
             a.offsets[c] = o;
             if (c == a.C - 1) a.offsets[a.C] = total;
@@ -625,30 +658,29 @@ __global__ void __launch_bounds__(LT) select_cell(SelectArgs a) {
     } else {
         o = a.offsets[c], total = a.offsets[a.C];
     }
-    write_rest(a, total, c, gridDim.x);
+    write_rest<NT>(a, total, c, gridDim.x);
     const CellChoice x = choice_of(a, c);
-    write_certain(a, x, o);
+    write_certain<NT>(a, x, o);
     if (x.need == 0) return;
     uint32_t u[E];
-    load_keys<E>(a.scores + c * a.n, 0, x.nf, u);
+    load_keys<NT, E>(a.scores + c * a.n, 0, x.nf, u);
     uint32_t key = 0, mask = 0, rem = 0;  // all: every key is above 0
     if (x.need < x.nf) {
         rem = x.need;
         for (int pass = 0; pass < 3; ++pass) {
-            *(uint2 *)(hist + 2 * threadIdx.x) = make_uint2(0u, 0u);
+            clear_bins<NT>(hist);
             __syncthreads();
             count_digit<E>(u, key, mask, pass, hist);
             __syncthreads();
             uint32_t bin, above;
-            pick_bin(hist, rem, red[0], found, &bin, &above);
+            pick_bin<NT>([&](int i) { return bin_of(hist, i); }, rem, red[0], found, &bin, &above);
             key |= bin << digit_shift(pass), mask |= digit_mask(pass) << digit_shift(pass), rem -= above;
         }
     }
-    write_chosen<E>(a, u, 0, key, rem, 0, o, red);
+    write_chosen<NT, E>(a, u, 0, key, rem, 0, o, red);
 }
 
-__global__ void __launch_bounds__(LT) select_offsets(SelectArgs a) {
-    __shared__ int64_t red[LT / 64];
+__device__ __forceinline__ void write_offsets(const SelectArgs &a, int64_t *red) {
     const int64_t run = (a.C + LT - 1) / LT, c0 = threadIdx.x * run, c1 = c0 + run < a.C ? c0 + run : a.C;
     int64_t mine = 0, all;
     int len;
@@ -660,37 +692,53 @@ __global__ void __launch_bounds__(LT) select_offsets(SelectArgs a) {
     }
     if (threadIdx.x == 0) a.offsets[a.C] = all;
 }
-
-// The key so far from the cell's histograms of the digits before `pass`.
-__device__ __forceinline__ void key_so_far(const SelectArgs &a, int64_t c, int pass, uint32_t need, uint32_t *red, uint32_t *found,
-                                           uint32_t *key, uint32_t *mask, uint32_t *rem) {
-    *key = 0, *mask = 0, *rem = need;
-    for (int p = 0; p < pass; ++p) {
-        uint32_t bin, above;
-        pick_bin(a.hist + (c * 3 + p) * kBins, *rem, red, found, &bin, &above);
-        *key |= bin << digit_shift(p), *mask |= digit_mask(p) << digit_shift(p), *rem -= above;
-        __syncthreads();
+__global__ void __launch_bounds__(LT) select_offsets(SelectArgs a) {
+    __shared__ int64_t red[LT / 64];
+    write_offsets(a, red);
+}
+// The first workgroup writes the offsets, the others clear the histograms.
+__global__ void __launch_bounds__(LT) select_begin(SelectArgs a) {
+    __shared__ int64_t red[LT / 64];
+    if (blockIdx.x == 0) {
+        write_offsets(a, red);
+        return;
     }
+    const int64_t n = a.C * 3 * kBins / 4;
+    for (int64_t i = (int64_t)(blockIdx.x - 1) * LT + threadIdx.x; i < n; i += (int64_t)(gridDim.x - 1) * LT)
+        ((uint4 *)a.hist)[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-__global__ void __launch_bounds__(LT) select_clear(SelectArgs a) {
-    const int64_t n = a.C * 3 * kBins / 4;
-    for (int64_t i = (int64_t)blockIdx.x * LT + threadIdx.x; i < n; i += (int64_t)gridDim.x * LT)
-        ((uint4 *)a.hist)[i] = make_uint4(0u, 0u, 0u, 0u);
+// The key's digits before `pass`: those before the last of them as the launch before left them, that one from the cell's
+// histogram of it.  The cell's first slice leaves them for the launch after.
+__device__ __forceinline__ void key_so_far(const SelectArgs &a, int64_t c, int s, int pass, uint32_t need, uint32_t *red,
+                                           uint32_t *found, uint32_t *key, uint32_t *mask, uint32_t *rem) {
+    *key = 0, *mask = 0, *rem = need;
+    if (pass == 0) return;
+    const int p = pass - 1;
+    if (p > 0) {
+        const uint2 x = a.state[c * 3 + p - 1];
+        *key = x.x, *rem = x.y;
+        for (int i = 0; i < p; ++i) *mask |= digit_mask(i) << digit_shift(i);
+    }
+    uint32_t bin, above;
+    const uint32_t *hist = a.hist + (c * 3 + p) * kBins;
+    pick_bin<LT>([&](int i) { return hist[i]; }, *rem, red, found, &bin, &above);
+    *key |= bin << digit_shift(p), *mask |= digit_mask(p) << digit_shift(p), *rem -= above;
+    if (s == 0 && threadIdx.x == 0) a.state[c * 3 + p] = make_uint2(*key, *rem);
 }
 
 __global__ void __launch_bounds__(LT) select_digit(SelectArgs a, int pass) {
     constexpr int E = kSlice / LT;
-    __shared__ __align__(8) uint32_t hist[kBins];
+    __shared__ __align__(16) uint32_t hist[kBins * kCopies];
     __shared__ uint32_t red[LT / 64], found[2];
     const int64_t c = blockIdx.x / a.slices;
     const int s = blockIdx.x % a.slices, first = s * kSlice;
     const CellChoice x = choice_of(a, c);
     if (first >= x.nf || x.need == 0 || x.need == x.nf) return;
     uint32_t u[E], key, mask, rem;
-    load_keys<E>(a.scores + c * a.n, first, x.nf, u);
-    *(uint2 *)(hist + 2 * threadIdx.x) = make_uint2(0u, 0u);
-    key_so_far(a, c, pass, x.need, red, found, &key, &mask, &rem);
+    load_keys<LT, E>(a.scores + c * a.n, first, x.nf, u);
+    clear_bins<LT>(hist);
+    key_so_far(a, c, s, pass, x.need, red, found, &key, &mask, &rem);
     __syncthreads();
     count_digit<E>(u, key, mask, pass, hist);
     if (pass == 2) {
@@ -702,9 +750,11 @@ __global__ void __launch_bounds__(LT) select_digit(SelectArgs a, int pass) {
     }
     __syncthreads();
     uint32_t *to = a.hist + (c * 3 + pass) * kBins;
-    for (int i = threadIdx.x; i < kBins; i += LT)
-        if (hist[i]) atomicAdd(&to[i], hist[i]);
-    if (pass == 2) a.last[(c * a.slices + s) * (kBins / 2) + threadIdx.x] = hist[threadIdx.x];
+    for (int i = threadIdx.x; i < (pass == 2 ? kBins / 2 : kBins); i += LT) {
+        const uint32_t n = bin_of(hist, i);
+        if (n) atomicAdd(&to[i], n);
+        if (pass == 2) a.last[(c * a.slices + s) * (kBins / 2) + i] = n;
+    }
 }
 
 __global__ void __launch_bounds__(LT) select_write(SelectArgs a) {
@@ -713,30 +763,31 @@ __global__ void __launch_bounds__(LT) select_write(SelectArgs a) {
     const int64_t c = blockIdx.x / a.slices;
     const int s = blockIdx.x % a.slices, first = s * kSlice;
     int64_t o = a.offsets[c];
-    write_rest(a, a.offsets[a.C], blockIdx.x, gridDim.x);
+    write_rest<LT>(a, a.offsets[a.C], blockIdx.x, gridDim.x);
     const CellChoice x = choice_of(a, c);
-    if (s == 0) write_certain(a, x, o);
+    if (s == 0) write_certain<LT>(a, x, o);
     if (first >= x.nf || x.need == 0) return;
     uint32_t u[E], key = 0, mask, rem = 0, eq = 0;
-    load_keys<E>(a.scores + c * a.n, first, x.nf, u);
+    load_keys<LT, E>(a.scores + c * a.n, first, x.nf, u);
     if (x.need == x.nf) {
         o += first;
     } else {
-        key_so_far(a, c, 3, x.need, red[0], found, &key, &mask, &rem);
+        key_so_far(a, c, 1, 3, x.need, red[0], found, &key, &mask, &rem);
         // tokens above and at the key in the slices before
         const uint32_t bin = key & 1023u;
         uint32_t more = 0, same = 0, all;
+#pragma unroll 8
         for (int i = 0; i < s; ++i) {
             const uint32_t h = a.last[(c * a.slices + i) * (kBins / 2) + threadIdx.x];
             more += threadIdx.x > bin ? h : 0u;
             same += threadIdx.x == bin ? h : 0u;
-            if (threadIdx.x == 0) more += a.above[c * a.slices + i];
         }
+        for (int i = threadIdx.x; i < s; i += LT) more += a.above[c * a.slices + i];
         scan_before<LT, uint32_t>(more, red[0], &all);
         scan_before<LT, uint32_t>(same, red[0], &eq);
         o += all + min(eq, rem);
     }
-    write_chosen<E>(a, u, first, key, rem, eq, o, red);
+    write_chosen<LT, E>(a, u, first, key, rem, eq, o, red);
 }
 }  // namespace
 
@@ -774,7 +825,7 @@ static int select_slices(int64_t n) { return n <= kAlone ? 0 : (int)((n + kSlice
 size_t select_ws_bytes(int64_t C, int64_t n) {
     const int64_t slices = select_slices(n);
     if (!slices) return 0;
-    return align_up(C * 3 * kBins * 4, 256) + align_up(C * slices * (kBins / 2) * 4, 256) + align_up(C * slices * 4, 256);
+    return align_up(C * 3 * kBins * 4, 256) + align_up(C * 3 * sizeof(uint2), 256) + align_up(C * slices * (kBins / 2) * 4, 256) + align_up(C * slices * 4, 256);
 }
 
 hipError_t launch_select_cells(int64_t C, const float *scores, int64_t n, const int32_t *lens, const int32_t *keep,
@@ -782,28 +833,31 @@ hipError_t launch_select_cells(int64_t C, const float *scores, int64_t n, const 
                                hipStream_t st) {
     SelectArgs a{C, n, n_kept, scores, lens, keep, recent, offsets, kept_pos};
     a.slices = select_slices(n);
-    const bool own = !a.slices && C <= kOwnSums;
-    if (!own) hipLaunchKernelGGL(select_offsets, dim3(1), dim3(LT), 0, st, a);
+    const bool own = C <= kOwnSums;
     if (a.slices) {
         char *p = (char *)ws;
         a.hist = (uint32_t *)p, p += align_up(C * 3 * kBins * 4, 256);
+        a.state = (uint2 *)p, p += align_up(C * 3 * sizeof(uint2), 256);
         a.last = (uint32_t *)p, p += align_up(C * a.slices * (kBins / 2) * 4, 256);
         a.above = (uint32_t *)p;
         const dim3 grid((unsigned)(C * a.slices));
-        hipLaunchKernelGGL(select_clear, dim3((unsigned)std::min<int64_t>((C * 3 * kBins / 4 + LT - 1) / LT, 1024)), dim3(LT), 0, st, a);
+        const int64_t clears = (C * 3 * kBins / 4 + LT - 1) / LT;
+        hipLaunchKernelGGL(select_begin, dim3((unsigned)std::min<int64_t>(1 + clears, 1024)), dim3(LT), 0, st, a);
         for (int pass = 0; pass < 3; ++pass) hipLaunchKernelGGL(select_digit, grid, dim3(LT), 0, st, a, pass);
         hipLaunchKernelGGL(select_write, grid, dim3(LT), 0, st, a);
         return hipGetLastError();
     }
+    if (!own) hipLaunchKernelGGL(select_offsets, dim3(1), dim3(LT), 0, st, a);
     const dim3 grid((unsigned)C);
-    const auto run = [&](auto k, auto o) {
-        if (own) hipLaunchKernelGGL(k, grid, dim3(LT), 0, st, a);
-        else hipLaunchKernelGGL(o, grid, dim3(LT), 0, st, a);
+    const auto run = [&](auto k, auto o, int threads) {
+        if (own) hipLaunchKernelGGL(k, grid, dim3(threads), 0, st, a);
+        else hipLaunchKernelGGL(o, grid, dim3(threads), 0, st, a);
     };
-    if (n <= 4 * LT) run(select_cell<4, true>, select_cell<4, false>);
-    else if (n <= 8 * LT) run(select_cell<8, true>, select_cell<8, false>);
-    else if (n <= 16 * LT) run(select_cell<16, true>, select_cell<16, false>);
-    else run(select_cell<32, true>, select_cell<32, false>);
+    if (n <= 1024) run(select_cell<256, 4, true>, select_cell<256, 4, false>, 256);
+    else if (n <= 4096) run(select_cell<256, 16, true>, select_cell<256, 16, false>, 256);
+    else if (n <= 8 * LT) run(select_cell<LT, 8, true>, select_cell<LT, 8, false>, LT);
+    else if (n <= 16 * LT) run(select_cell<LT, 16, true>, select_cell<LT, 16, false>, LT);
+    else run(select_cell<LT, 32, true>, select_cell<LT, 32, false>, LT);
     return hipGetLastError();
 }
 
