@@ -534,8 +534,9 @@ typedef struct fw_heads {
  * reduced in float64 (less than 2^-50 of the angle is lost), rows computed in
  * float32 (their squares too) and rounded once.
  *   q_out, k_out  rows of the same type, strides qo_row .. ko_head; either may
- *                 be its own input with its strides (in place).  Rows of an
- *                 output must not meet each other.
+ *                 be its own input with its strides (in place), and meets
+ *                 nothing else that the call reads or writes.  Rows of an output
+ *                 must not meet each other.
  * No workspace is used: the query returns 0 and ws may be NULL.
  * Errors: FW_E_NULL, FW_E_SHAPE, FW_E_DTYPE, FW_E_HIP.
  * ------------------------------------------------------------------------- */
@@ -599,7 +600,8 @@ fw_status fw_cache_select(int64_t C, const float *scores, int64_t n, const int32
  *             by fw_cache_release.
  * All are in and out.  Blocks are taken from the top of the stack as it was
  * before the call; blocks that their last cell leaves go back on it in
- * ascending order, and are not taken again in the same call.
+ * ascending order, and are not taken again in the same call.  A call's workspace
+ * is its own until it is done: calls that may run at the same time need one each.
  * Limits: 1 <= C < 2^22; max_blocks >= 1; max_blocks * block_size < 2^31. */
 typedef struct fw_cells {
     int64_t C, max_blocks;

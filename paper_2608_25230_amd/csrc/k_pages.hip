@@ -342,10 +342,13 @@ constexpr int kChunk = 256;  // tokens
 constexpr int kChunkShift = 8;
 constexpr int kQueues = 64;  // of keys, and as many of values
 constexpr int kApart = 64;   // counters lie in lines of their own
+constexpr int kPolls = 1 << 22;  // seconds: a wait ends also if another call overwrites the workspace, which no caller may do
 
 __device__ __forceinline__ int64_t cell_of(const PageArgs &a, int64_t p) { return a.which ? a.which[p] : p; }
 __device__ __forceinline__ int64_t block0(const PageArgs &a, int64_t p) { return (a.offsets[p] >> a.shift) + p; }
 __device__ __forceinline__ int64_t chunk0(const PageArgs &a, int64_t p) { return (a.offsets[p] >> kChunkShift) + p; }
+// offsets of refused cells can be anything
+__device__ __forceinline__ int64_t clamp_chunk(const PageArgs &a, int64_t t) { return t < 0 ? 0 : t > a.chunks ? a.chunks : t; }
 
 __global__ void __launch_bounds__(CT) compact_check(PageArgs a) {
     __shared__ int64_t red[CT / 64];
@@ -359,12 +362,11 @@ __global__ void __launch_bounds__(CT) compact_check(PageArgs a) {
     const int64_t len = bad ? 0 : length_of(a, c);
     bad = bad || n > len;
     // chunks of no cell before the first, behind this one's, and behind the last
-    const auto clamp = [&](int64_t t) { return t < 0 ? 0 : t > a.chunks ? a.chunks : t; };
     const int64_t t0 = chunk0(a, p), t1 = bad ? t0 : t0 + ((n + kChunk - 1) >> kChunkShift);
     const int64_t next = p + 1 < a.P ? chunk0(a, p + 1) : a.chunks;
     if (p == 0)
-        for (int64_t t = tid; t < clamp(t0); t += CT) a.owner[t] = -1;
-    for (int64_t t = clamp(t0) + tid; t < clamp(next); t += CT) a.owner[t] = t < t1 ? (int32_t)p : -1;
+        for (int64_t t = tid; t < clamp_chunk(a, t0); t += CT) a.owner[t] = -1;
+    for (int64_t t = clamp_chunk(a, t0) + tid; t < clamp_chunk(a, next); t += CT) a.owner[t] = t < t1 ? (int32_t)p : -1;
     // the first blocks' owners, beside the list
     const int32_t *row = a.table + c * a.W;
     bool early = false;
@@ -442,7 +444,8 @@ __global__ void __launch_bounds__(PT) compact_plan(PageArgs a) {
     // queue i begins with the first cell whose chunks begin at i / kQueues of all or behind; the first with chunk 0
     if (down && threadIdx.x <= kQueues) a.starts[threadIdx.x] = 0;
     for (int64_t p = threadIdx.x; p <= a.P && !down; p += PT) {
-        const int64_t t = p < a.P ? chunk0(a, p) : a.chunks, before = p > 0 ? chunk0(a, p - 1) : -1;
+        const int64_t t = p < a.P ? clamp_chunk(a, chunk0(a, p)) : a.chunks;
+        const int64_t before = p > 0 ? clamp_chunk(a, chunk0(a, p - 1)) : -1;
         for (int64_t i = before < 0 ? 0 : before * kQueues / a.chunks; i <= kQueues; ++i) {
             const int64_t at = i * a.chunks / kQueues;
             if (at > t) break;
@@ -703,8 +706,9 @@ __device__ __forceinline__ void move_chunks(const PageArgs &a, uint8_t *const ld
     {
         const int64_t r0 = a.within[chunk], r1 = (j + 1) * kChunk < x.x ? a.within[chunk + 1] : x.x;
         const int64_t i0 = max(r0, (int64_t)x.y * a.bs) >> kChunkShift, i1 = min((r1 + kChunk - 1) >> kChunkShift, j);
+        int polls = 0;
         for (int64_t i = i0 + tid; i < i1; i += MT)
-            while (!__hip_atomic_load(&read[t0 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
+            while (!__hip_atomic_load(&read[t0 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) && ++polls < kPolls)
                 __builtin_amdgcn_s_sleep(1);
     }
     __syncthreads();

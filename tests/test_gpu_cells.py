@@ -346,6 +346,73 @@ def test_captured(tf):
         fw.cache_release(cache, cells, _i32(torch, [9999, 9999, 0, 0]))
 
 
+@pytest.mark.parametrize("off", [[0, 256 * 10 ** 6, 256 * 10 ** 6, 256 * 10 ** 6], [0, 2, 2 ** 33, 2 ** 40], [-2 ** 62, -2 ** 40, -7, -1],
+                                 [-2 ** 50, 0, 2, 4], [2 ** 62] * 4, [1, 2, 4, 4], [4, 4, 4, 4], [0, 1, 300000, 300001]])
+def test_offsets_out_of_range(tf, off):
+    """Ascending offsets that lie anywhere: their cells are refused, and the others served."""
+    print(f"compact offsets={off}", flush=True)
+    s = random_state(np.random.default_rng(13), [40, 64, 17], 16, 32, 20)
+    _compact(tf, s, off, [3, 9, 1, 2])
+
+
+def test_many_pairs_and_listed_cells(tf):
+    """More cells than claims fit LDS, and more pairs than are asked for once."""
+    rng = np.random.default_rng(14)
+    C = 10000
+    lens = np.zeros(C, int)
+    lens[:40] = rng.integers(0, 60, 40)
+    s = random_state(rng, lens, 16, 32, 4, n_blocks=6500)
+    dst = 40 + rng.permutation(C - 40)[:5000]
+    dst[[7, 4000, 4999]] = dst[6], dst[100], 3
+    s = _fork(tf, s, rng.integers(0, 40, 5000), dst, rng.integers(-1, 70, 5000))
+    which = rng.permutation(C)[:4500]
+    which[[4200, 4300]] = which[2], C
+    kept = [min(2, int(s["lens"][c])) if c < C else 1 for c in which]
+    pos = [x for c, n in zip(which, kept) for x in sorted(rng.permutation(max(1, int(s["lens"][c]) if c < C else 1))[:n].tolist())]
+    s = _compact(tf, s, np.cumsum([0] + kept).tolist(), pos, which)
+    s = _release(tf, s, rng.integers(0, 40, C))
+    _release(tf, s, [0] * C)
+
+
+def test_a_stack_of_many_runs(tf):
+    """Blocks whose numbers lie in more runs than are counted on the way."""
+    torch, fw = tf
+    rng = np.random.default_rng(15)
+    n, lens = 300000, [500, 320, 33, 0, 0]
+    s = random_state(rng, lens, 16, 32, 20)
+    few = len(s["shared"])
+    at = np.sort(rng.permutation(n)[:few])         # where the small cache's blocks lie in the large one
+    t = dict(s, n_free=n - few + s["n_free"], shared=np.zeros(n, np.int32))
+    for key in CACHE:
+        t[key] = np.zeros((n, *s[key].shape[1:]), np.uint8)
+        t[key][at] = s[key]
+    rest = np.setdiff1d(np.arange(n), at)
+    t["table"] = np.where(s["table"] >= 0, at[s["table"]], -1).astype(np.int32)
+    t["free_list"] = np.full(n, -7, np.int32)
+    t["free_list"][:t["n_free"]] = np.concatenate([rest, at[s["free_list"][:s["n_free"]]]])
+    cache, cells = _up(tf, t)
+    calls = (("fork", lambda: fw.cache_fork(cache, cells, _i32(torch, [0, 1]), _i32(torch, [3, 4])), lambda x: O.fork(x, [0, 1], [3, 4])),
+             ("compact", lambda: fw.cache_compact(cache, cells, _cuda(torch, [0, 60, 90], torch.int64),
+                                                  _i32(torch, [*range(2, 122, 2), *range(30)]), which=_i32(torch, [0, 2])),
+              lambda x: O.compact(x, [0, 60, 90], [*range(2, 122, 2), *range(30)], [0, 2])),
+             ("release", lambda: fw.cache_release(cache, cells, _i32(torch, [10, 300, 0, 123, 0])),
+              lambda x: O.release(x, [10, 300, 0, 123, 0])),
+             ("end", lambda: fw.cache_release(cache, cells, _i32(torch, [0] * 5)), lambda x: O.release(x, [0] * 5)))
+    for what, run, oracle in calls:
+        r = run()
+        torch.cuda.synchronize()
+        want, got = oracle(t), _down(cache, cells)
+        assert int(r["refused"]) == want["refused"] == 0
+        used = np.unique(np.concatenate([at, want["table"][want["table"] >= 0]]))
+        other = np.setdiff1d(np.arange(n), used)
+        for x in (got, want, t):
+            assert not x["k"][other].any() and not x["v"][other].any()
+        small = lambda x: dict(x, k=x["k"][used], v=x["v"][used], k_exp=x["k_exp"][used], v_exp=x["v_exp"][used])
+        compare(small(got), small(want), small(t), what)
+        O.invariants(want)
+        at, t = used, want
+
+
 def test_two_streams_with_workspaces_of_their_own(tf):
     torch, fw = tf
     rng = np.random.default_rng(11)

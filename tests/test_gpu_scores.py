@@ -227,6 +227,23 @@ def test_select(tf, C, n, what):
     _select(tf, x, np.zeros(C, int) - 1, keep, 1, extra=4)
 
 
+@pytest.mark.parametrize("C,n", [(5000, 70), (3, 4096), (3, 4097), (2, 8192), (2, 8193), (2, 16385), (2, 32768), (2, 32769), (3, 70001)])
+@pytest.mark.parametrize("what", ["normal", "ties"])
+def test_select_widths(tf, C, n, what):
+    """Every width of a row, rows in slices, and more cells than every workgroup sums for itself."""
+    print(f"select C={C} n={n} {what}", flush=True)
+    rng = np.random.default_rng(n)
+    x = rng.standard_normal((C, n)).astype(np.float32)
+    if what == "ties":
+        x = np.floor(x).astype(np.float32)
+    lens = rng.integers(0, n + 1, C)
+    lens[0], lens[-1] = n, n
+    keep = rng.integers(0, n + 1, C)
+    _select(tf, x, lens, keep, 40)
+    keep[0], keep[1], keep[-1] = n, 0, n - 1
+    _select(tf, x, lens, keep, 0, extra=5)
+
+
 def test_select_captured(tf):
     torch, fw = tf
     x = torch.rand(6, 3000, device="cuda")
