@@ -542,7 +542,7 @@ fw_status check_heads(const fw_heads *h) {
     if (h->dtype != FW_F32 && h->dtype != FW_BF16) return fail(FW_E_DTYPE, "unknown dtype %d", (int)h->dtype);
     constexpr int64_t m31 = (int64_t)1 << 31, m30 = (int64_t)1 << 30;
     if (h->T < 0 || h->Hq < 0 || h->Hkv < 0) return fail(FW_E_SHAPE, "T, Hq and Hkv must be >= 0");
-    // a workgroup of 256 threads for up to four tokens; a grid holds fewer than 2^32 threads
+    // a workgroup of 256 threads takes T / 2^23 tokens or more, at most eight; a grid holds fewer than 2^32 threads
     if (h->T > ((int64_t)1 << 25)) return fail(FW_E_SHAPE, "T must be <= 2^25, got %lld", (long long)h->T);
     if (h->Hq >= m30 || h->Hkv >= m30 || (h->T > 0 && h->Hq + h->Hkv >= m30 / h->T))
         return fail(FW_E_SHAPE, "T * (Hq + Hkv) must be < 2^30");

@@ -7,13 +7,15 @@
 // v sin a, v cos a + u sin a), a = pos freq.  The angle is taken in float64 as
 // a part of a full turn, so far positions lose nothing; what is left of it, at
 // most half a turn, goes to float32.
+#include <algorithm>
+
 #include "fw_internal.hpp"
 
 namespace fw {
 
 namespace {
 constexpr int RT = 256;      // threads of a workgroup
-constexpr int kTokens = 4;   // tokens of a workgroup at most
+constexpr int kTokens = 8;   // tokens of a workgroup at most
 constexpr int kPairs = 128;  // pairs of a row at most
 
 struct RotateArgs {
@@ -153,6 +155,11 @@ hipError_t launch_width(RotateArgs &a, int v, hipStream_t st) {
     const int pieces = (a.d + 2 * v - 1) / (2 * v);
     a.lanes = 1;
     while (a.lanes < pieces && a.lanes < 64) a.lanes *= 2;
+    // As many tokens as the threads hold rows of at once: a workgroup first waits for its tokens' angles, which few rows do
+    // not make up for (65536 tokens of 9 heads of 128: 60 us by four, 105 by one), and more rows than that only make it
+    // longer (16384 of 40 heads: 62 us by one, 64 by four; of 32 heads of 256: 93 and 106).  A grid holds 2^24 workgroups.
+    const int heads = a.H[0] + a.H[1], rows = RT / a.lanes;
+    a.tokens = std::max(std::min((rows + heads - 1) / heads, kTokens), (int)((a.T + (1 << 23) - 1) >> 23));
     const dim3 grid((unsigned)((a.T + a.tokens - 1) / a.tokens));
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(RT), 0, st, a); };
     if constexpr (sizeof(T) == 2) {
@@ -176,7 +183,6 @@ hipError_t launch_rotate(const fw_heads &h, void *q_out, int64_t qo_row, int64_t
     a.H[0] = (int)h.Hq, a.H[1] = (int)h.Hkv;
     a.T = h.T, a.d = (int)h.d, a.rot = (int)h.rot, a.pos = h.pos, a.freq = h.freq;
     a.interleaved = h.interleaved != 0, a.norm = h.norm != 0, a.eps = h.eps;
-    a.tokens = h.T >= 4096 ? kTokens : 1;
     // the widest pieces that columns, strides and addresses allow
     const int size = h.dtype == FW_F32 ? 4 : 2;
     int v = 16 / size;

@@ -36,7 +36,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int TT = 64;          // tokens of a wave and step
 constexpr int FT = 256;         // threads of few_rows
 constexpr int kFewGroups = 1024;  // its workgroups
-constexpr int kFewLeast = 1;    // tiles of a wave at least
 constexpr int kQBytes = 65536;  // many_rows: rows in LDS at a time
 constexpr int kManyGroups = 512;
 constexpr int kManyLeast = 2;   // tiles of a workgroup at least
@@ -216,7 +215,7 @@ __global__ void __launch_bounds__(FT, DP <= (sizeof(T) == 2 ? 128 : 64) ? 4 : 2)
     const int tl = lane & 15, g = lane >> 4;
     int2 found[FT / 64];
     int per;
-    find_shares<FT, FT / 64, 0>(a, gridDim.x * (FT / 64), kFewLeast, found, &per);
+    find_shares<FT, FT / 64, 0>(a, gridDim.x * (FT / 64), 1, found, &per);
     int c = -1, at = 0;
 #pragma unroll
     for (int i = 0; i < FT / 64; ++i)
@@ -406,7 +405,7 @@ hipError_t launch_scores_width(ScoreArgs &a, hipStream_t st) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, NW = DP <= 128 ? 8 : 4;
     const int64_t tiles = a.C * ((std::min<int64_t>((int64_t)a.W << a.shift, a.n) + TT - 1) / TT);
     if (a.R <= 16) {
-        const int64_t groups = (tiles + FT / 64 * kFewLeast - 1) / (FT / 64 * kFewLeast);
+        const int64_t groups = (tiles + FT / 64 - 1) / (FT / 64);
         hipLaunchKernelGGL((few_rows<T, DP>), dim3((unsigned)std::min<int64_t>(kFewGroups, groups)), dim3(FT), 0, st, a);
         return hipGetLastError();
     }
@@ -818,7 +817,7 @@ hipError_t launch_cache_scores(const fw_cache &cache, int dtype, const void *q, 
 }
 
 // Cells whose counts every workgroup sums for itself, which saves a launch.
-constexpr int64_t kOwnSums = 4096;
+constexpr int64_t kOwnSums = 2048;
 
 static int select_slices(int64_t n) { return n <= kAlone ? 0 : (int)((n + kSlice - 1) / kSlice); }
 
