@@ -7,6 +7,13 @@
 // v sin a, v cos a + u sin a), a = pos freq.  The angle is taken in float64 as
 // a part of a full turn, so far positions lose nothing; what is left of it, at
 // most half a turn, goes to float32.
+//
+// Memory bounds it: a row is read and written once, a dozen operations a
+// column.  A token's sines and cosines are taken once, into LDS, for all its
+// heads; a row lies in few lanes (8 for 128 columns of bf16), so that its sum of
+// squares takes few shuffles, and the next row is loaded before the one at hand
+// is done, the first one before the angles (16384 tokens of 40 heads of 128
+// columns, bf16 with norms: 77 us without, 65 with, 5.2 TB/s).
 #include <algorithm>
 
 #include "fw_internal.hpp"
@@ -16,6 +23,7 @@ namespace fw {
 namespace {
 constexpr int RT = 256;      // threads of a workgroup
 constexpr int kTokens = 8;   // tokens of a workgroup at most
+constexpr int kLong = 4096;  // tokens that are many
 constexpr int kPairs = 128;  // pairs of a row at most
 
 struct RotateArgs {
@@ -41,12 +49,6 @@ template <typename T, int V> struct alignas(V * sizeof(T)) Piece {
     T x[V];
 };
 template <typename T, int V>
-__device__ __forceinline__ void get(const T *p, float (&y)[V]) {
-    const Piece<T, V> z = *(const Piece<T, V> *)p;
-#pragma unroll
-    for (int i = 0; i < V; ++i) y[i] = Elem<T>::load(z.x, i);
-}
-template <typename T, int V>
 __device__ __forceinline__ void put(T *p, const float (&y)[V]) {
     Piece<T, V> z;
 #pragma unroll
@@ -65,19 +67,6 @@ __global__ void __launch_bounds__(RT) rotate_heads(RotateArgs a) {
     const int tid = threadIdx.x, half = a.rot / 2;
     const int64_t t0 = (int64_t)blockIdx.x * a.tokens;
     const int nt = a.T - t0 < a.tokens ? (int)(a.T - t0) : a.tokens;
-    for (int i = tid; i < nt * half; i += RT) {
-        const int t = i / half, j = i - t * half;
-        double turns = (double)a.pos[t0 + t] * (double)a.freq[j] * 0.15915494309189533577;
-        turns -= rint(turns);
-        sincospif((float)(2.0 * turns), &sn[t][j], &cs[t][j]);
-    }
-    if (a.norm)
-        for (int i = tid; i < 2 * a.d; i += RT) {
-            const int s = i >= a.d, c = i - s * a.d;
-            const void *w = a.weight[s];
-            wt[s][c] = !w ? 1.f : a.w32 ? ((const float *)w)[c] : bf16_bits_to_f32(((const uint16_t *)w)[c]);
-        }
-    __syncthreads();
     const int lane = tid & (a.lanes - 1), slot = tid / a.lanes, slots = RT / a.lanes;
     int c0[NC], c1[NC], pair[NC];  // columns of the two pieces, the first pair (-1: they do not turn)
     const int turning = half / V;
@@ -94,20 +83,43 @@ __global__ void __launch_bounds__(RT) rotate_heads(RotateArgs a) {
             pair[n] = -1;
         }
     }
-    const int heads = a.H[0] + a.H[1];
-    const float inv_d = 1.f / a.d;
-    for (int r = slot; r < nt * heads; r += slots) {
+    const int heads = a.H[0] + a.H[1], rows = nt * heads;
+    Piece<T, V> next[NC][2];  // a row ahead
+    const auto load = [&](int r) {
         const int t = r / heads, hh = r - t * heads, s = hh >= a.H[0], h = hh - (s ? a.H[0] : 0);
         const T *p = (const T *)a.in[s] + (t0 + t) * a.row[s] + h * a.head[s];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            next[n][0] = next[n][1] = Piece<T, V>{};
+            if (c0[n] < a.d) next[n][0] = *(const Piece<T, V> *)(p + c0[n]);
+            if (c1[n] < a.d) next[n][1] = *(const Piece<T, V> *)(p + c1[n]);
+        }
+    };
+    if (slot < rows) load(slot);
+    for (int i = tid; i < nt * half; i += RT) {
+        const int t = i / half, j = i - t * half;
+        double turns = (double)a.pos[t0 + t] * (double)a.freq[j] * 0.15915494309189533577;
+        turns -= rint(turns);
+        sincospif((float)(2.0 * turns), &sn[t][j], &cs[t][j]);
+    }
+    if (a.norm)
+        for (int i = tid; i < 2 * a.d; i += RT) {
+            const int s = i >= a.d, c = i - s * a.d;
+            const void *w = a.weight[s];
+            wt[s][c] = !w ? 1.f : a.w32 ? ((const float *)w)[c] : bf16_bits_to_f32(((const uint16_t *)w)[c]);
+        }
+    __syncthreads();
+    const float inv_d = 1.f / a.d;
+    for (int r = slot; r < rows; r += slots) {
+        const int t = r / heads, hh = r - t * heads, s = hh >= a.H[0], h = hh - (s ? a.H[0] : 0);
         T *o = (T *)a.out[s] + (t0 + t) * a.orow[s] + h * a.ohead[s];
         float x[NC][2][V];
 #pragma unroll
-        for (int n = 0; n < NC; ++n) {
+        for (int n = 0; n < NC; ++n)
 #pragma unroll
-            for (int i = 0; i < V; ++i) x[n][0][i] = x[n][1][i] = 0.f;
-            if (c0[n] < a.d) get<T, V>(p + c0[n], x[n][0]);
-            if (c1[n] < a.d) get<T, V>(p + c1[n], x[n][1]);
-        }
+            for (int i = 0; i < V; ++i)
+                x[n][0][i] = Elem<T>::load(next[n][0].x, i), x[n][1][i] = Elem<T>::load(next[n][1].x, i);
+        if (r + slots < rows) load(r + slots);
         if (a.norm) {
             float sum = 0.f;
 #pragma unroll
@@ -155,10 +167,11 @@ hipError_t launch_width(RotateArgs &a, int v, hipStream_t st) {
     const int pieces = (a.d + 2 * v - 1) / (2 * v);
     a.lanes = 1;
     while (a.lanes < pieces && a.lanes < 64) a.lanes *= 2;
-    // As many tokens as the threads hold rows of at once: a workgroup first waits for its tokens' angles, which few rows do
-    // not make up for (65536 tokens of 9 heads of 128: 60 us by four, 105 by one), and more rows than that only make it
-    // longer (16384 of 40 heads: 62 us by one, 64 by four; of 32 heads of 256: 93 and 106).  A grid holds 2^24 workgroups.
-    const int heads = a.H[0] + a.H[1], rows = RT / a.lanes;
+    // As many tokens as the threads take rows of at once, twice where tokens are many: a workgroup's first rows wait for
+    // its tokens' angles, which a few rows do not make up for, and too few workgroups leave the card idle.  bf16 with
+    // norms, by 1, 2, 4, 8 tokens: 1024 of 32 heads of 256 columns 12, 13, 21, 36 us; 4096 of 40 heads of 128 21, 19, 20,
+    // 27; 16384 of those 67, 65, 64, 68; 65536 of 9 heads of 128 128, 87, 70, 63.  A grid holds 2^24 workgroups.
+    const int heads = a.H[0] + a.H[1], rows = RT / a.lanes * (a.T >= kLong ? 2 : 1);
     a.tokens = std::max(std::min((rows + heads - 1) / heads, kTokens), (int)((a.T + (1 << 23) - 1) >> 23));
     const dim3 grid((unsigned)((a.T + a.tokens - 1) / a.tokens));
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(RT), 0, st, a); };
