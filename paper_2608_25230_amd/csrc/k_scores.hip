@@ -469,16 +469,31 @@ __device__ __forceinline__ CellChoice choice_of(const SelectArgs &a, int64_t c) 
     return x;
 }
 
-template <int NT, typename V>
-__device__ __forceinline__ V scan_before(V v, V *red, V *total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    V x = v;
+// Inclusive sum over the lanes up to this one: within rows of 16 by shifts, then the last lanes of the rows before.
+__device__ __forceinline__ uint32_t lanes_upto(uint32_t x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast 15 to rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // row_bcast 31 to rows 2 and 3
+    return x;
+}
+__device__ __forceinline__ int64_t lanes_upto(int64_t x) {
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
-        const V y = __shfl_up(x, off);
-        if (lane >= off) x += y;
+        const int64_t y = __shfl_up((long long)x, off);
+        if ((int)(threadIdx.x & 63) >= off) x += y;
     }
-    if (lane == 63) red[w] = x;
+    return x;
+}
+
+// Exclusive sum over the threads, and the total.
+template <int NT, typename V>
+__device__ __forceinline__ V scan_before(V v, V *red, V *total) {
+    const int w = threadIdx.x >> 6;
+    const V x = lanes_upto(v);
+    if ((threadIdx.x & 63) == 63) red[w] = x;
     __syncthreads();
     V before = x - v, all = 0;
 #pragma unroll
@@ -492,10 +507,12 @@ __device__ __forceinline__ V scan_before(V v, V *red, V *total) {
     return before;
 }
 
-// The bin from the top that holds the rem-th entry, and the entries above it; `count` gives a bin's entries.
+// The bin from the top that holds the rem-th entry, the entries above it and its own; `count` gives a bin's entries.
+struct Bin {
+    uint32_t bin, above, own;
+};
 template <int NT, typename Count>
-__device__ __forceinline__ void pick_bin(const Count &count, uint32_t rem, uint32_t *red, uint32_t *found, uint32_t *bin,
-                                         uint32_t *above) {
+__device__ __forceinline__ Bin pick_bin(const Count &count, uint32_t rem, uint32_t *red, Bin *found) {
     constexpr int N = kBins / NT;  // of a thread, from the top
     uint32_t h[N], sum = 0, all;
 #pragma unroll
@@ -506,35 +523,40 @@ __device__ __forceinline__ void pick_bin(const Count &count, uint32_t rem, uint3
     uint32_t before = scan_before<NT, uint32_t>(sum, red, &all);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if (before < rem && rem <= before + h[i]) found[0] = kBins - 1 - N * threadIdx.x - i, found[1] = before;
+        if (before < rem && rem <= before + h[i]) *found = Bin{kBins - 1 - N * threadIdx.x - i, before, h[i]};
         before += h[i];
     }
     __syncthreads();
-    *bin = found[0], *above = found[1];
+    return *found;
 }
 
 __device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
 __device__ __forceinline__ uint32_t digit_mask(int pass) { return pass == 2 ? 1023u : 2047u; }
 
-// Keys of tokens first + 4 NT k + 4 t + i; those at nf and past it are 0, below every score's key.
+// Scores of tokens first + 4 NT k + 4 t + i, and their keys in these scores' place; those at nf and past it get 0, which is
+// below every score's key.
 template <int NT, int E>
-__device__ __forceinline__ void load_keys(const float *row, int first, int nf, uint32_t (&u)[E]) {
+__device__ __forceinline__ void load_scores(const float *row, int first, int nf, float (&x)[E]) {
     const bool wide = ((uintptr_t)row & 15) == 0;
 #pragma unroll
     for (int k = 0; k < E / 4; ++k) {
         const int j = first + 4 * NT * k + 4 * (int)threadIdx.x;
-        float4 x = {0.f, 0.f, 0.f, 0.f};
+        float4 z = {0.f, 0.f, 0.f, 0.f};
         if (wide && j + 4 <= nf) {
-            x = *(const float4 *)(row + j);
+            z = *(const float4 *)(row + j);
         } else {
-            if (j < nf) x.x = row[j];
-            if (j + 1 < nf) x.y = row[j + 1];
-            if (j + 2 < nf) x.z = row[j + 2];
-            if (j + 3 < nf) x.w = row[j + 3];
+            if (j < nf) z.x = row[j];
+            if (j + 1 < nf) z.y = row[j + 1];
+            if (j + 2 < nf) z.z = row[j + 2];
+            if (j + 3 < nf) z.w = row[j + 3];
         }
-        u[4 * k] = j < nf ? rank_key(x.x) : 0u, u[4 * k + 1] = j + 1 < nf ? rank_key(x.y) : 0u;
-        u[4 * k + 2] = j + 2 < nf ? rank_key(x.z) : 0u, u[4 * k + 3] = j + 3 < nf ? rank_key(x.w) : 0u;
+        x[4 * k] = z.x, x[4 * k + 1] = z.y, x[4 * k + 2] = z.z, x[4 * k + 3] = z.w;
     }
+}
+template <int NT, int E>
+__device__ __forceinline__ void make_keys(const float (&x)[E], int first, int nf, uint32_t (&u)[E]) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) u[i] = first + 4 * NT * (i / 4) + 4 * (int)threadIdx.x + i % 4 < nf ? rank_key(x[i]) : 0u;
 }
 
 // Scores have few exponents, so lanes meet in a bin: each bin has kCopies places, one for every kCopies-th lane.
@@ -568,12 +590,7 @@ __device__ __forceinline__ void write_chosen(const SelectArgs &a, const uint32_t
         uint32_t v = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v += u[4 * k + i] > key ? 1u : u[4 * k + i] == key ? 0x10000u : 0u;
-        uint32_t x = v;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const uint32_t y = __shfl_up(x, off);
-            if (lane >= off) x += y;
-        }
+        const uint32_t x = lanes_upto(v);
         if (lane == 63) red[k][w] = x;
         before[k] = x - v;
     }
@@ -592,42 +609,50 @@ __device__ __forceinline__ void write_chosen(const SelectArgs &a, const uint32_t
         if ((lane & (NW - 1)) == NW - 1) totals[threadIdx.x / NW] = x;
     }
     __syncthreads();
+    // places from `at` on, in 32 bits: a cell's tokens
+    const int64_t left = a.n_kept - at;
+    const int room = left < 0 ? 0 : left > INT32_MAX ? INT32_MAX : (int)left;
+    int32_t *const out = a.kept_pos + at;
     uint32_t eq = eq0;
+    int done = 0;
 #pragma unroll
     for (int k = 0; k < E / 4; ++k) {
         const uint32_t all = totals[k], b = before[k] + red[k][w];
-        uint32_t e = eq + (b >> 16);
-        int64_t o = at + (b & 0xFFFFu) + (min(e, rem) - min(eq, rem));
+        if (all) {
+            uint32_t e = eq + (b >> 16);
+            int o = done + (int)(b & 0xFFFFu) + (int)(min(e, rem) - min(eq, rem));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool same = u[4 * k + i] == key;
-            if (u[4 * k + i] > key || (same && e < rem)) {
-                if (o < a.n_kept) a.kept_pos[o] = first + 4 * NT * k + 4 * (int)threadIdx.x + i;
-                ++o;
+            for (int i = 0; i < 4; ++i) {
+                const bool same = u[4 * k + i] == key, in = u[4 * k + i] > key || (same && e < rem);
+                if (in && o < room) out[o] = first + 4 * NT * k + 4 * (int)threadIdx.x + i;
+                o += in, e += same;
             }
-            e += same;
         }
         const uint32_t upto = eq + (all >> 16);
-        at += (all & 0xFFFFu) + (min(upto, rem) - min(eq, rem));
+        done += (int)(all & 0xFFFFu) + (int)(min(upto, rem) - min(eq, rem));
         eq = upto;
     }
 }
 
 // Kept tokens of the cells before c and of all.
 template <int NT>
-__device__ __forceinline__ int64_t kept_before(const SelectArgs &a, int64_t c, int64_t *red, int64_t *total) {
-    int64_t lo = 0, hi = 0;
+__device__ __forceinline__ int64_t kept_before(const SelectArgs &a, int64_t c, longlong2 *red, int64_t *total) {
+    long long lo = 0, all = 0;
     int len;
     for (int64_t i = threadIdx.x; i < a.C; i += NT) {
         const int k = kept_of(a, i, &len);
-        if (i < c) lo += k;
-        else hi += k;
+        all += k;
+        lo += i < c ? k : 0;
     }
-    int64_t x, y;
-    scan_before<NT, int64_t>(lo, red, &x);
-    scan_before<NT, int64_t>(hi, red, &y);
-    *total = x + y;
-    return x;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) lo += __shfl_xor(lo, off), all += __shfl_xor(all, off);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_longlong2(lo, all);
+    __syncthreads();
+    lo = all = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) lo += red[i].x, all += red[i].y;
+    *total = all;
+    return lo;
 }
 template <int NT>
 __device__ __forceinline__ void write_certain(const SelectArgs &a, const CellChoice &x, int64_t o) {
@@ -644,9 +669,13 @@ __device__ __forceinline__ void write_rest(const SelectArgs &a, int64_t total, i
 template <int NT, int E, bool OWN>
 __global__ void __launch_bounds__(NT) select_cell(SelectArgs a) {
     __shared__ __align__(16) uint32_t hist[kBins * kCopies];
-    __shared__ uint32_t red[E / 4 > 1 ? E / 4 : 1][NT / 64], found[2];
-    __shared__ int64_t sums[NT / 64];
+    __shared__ uint32_t red[E / 4][NT / 64];
+    __shared__ Bin found;
+    __shared__ longlong2 sums[NT / 64];
     const int64_t c = blockIdx.x;
+    const CellChoice x = choice_of(a, c);
+    float s[E];
+    load_scores<NT, E>(a.scores + c * a.n, 0, x.need ? x.nf : 0, s);
     int64_t total, o;
     if (OWN) {
         o = kept_before<NT>(a, c, sums, &total);
@@ -658,11 +687,10 @@ __global__ void __launch_bounds__(NT) select_cell(SelectArgs a) {
         o = a.offsets[c], total = a.offsets[a.C];
     }
     write_rest<NT>(a, total, c, gridDim.x);
-    const CellChoice x = choice_of(a, c);
     write_certain<NT>(a, x, o);
     if (x.need == 0) return;
     uint32_t u[E];
-    load_keys<NT, E>(a.scores + c * a.n, 0, x.nf, u);
+    make_keys<NT, E>(s, 0, x.nf, u);
     uint32_t key = 0, mask = 0, rem = 0;  // all: every key is above 0
     if (x.need < x.nf) {
         rem = x.need;
@@ -671,9 +699,12 @@ __global__ void __launch_bounds__(NT) select_cell(SelectArgs a) {
             __syncthreads();
             count_digit<E>(u, key, mask, pass, hist);
             __syncthreads();
-            uint32_t bin, above;
-            pick_bin<NT>([&](int i) { return bin_of(hist, i); }, rem, red[0], found, &bin, &above);
-            key |= bin << digit_shift(pass), mask |= digit_mask(pass) << digit_shift(pass), rem -= above;
+            const Bin b = pick_bin<NT>([&](int i) { return bin_of(hist, i); }, rem, red[0], &found);
+            key |= b.bin << digit_shift(pass), mask |= digit_mask(pass) << digit_shift(pass), rem -= b.above;
+            if (b.own == rem) {  // all of the bin: no need to part it
+                --key, rem = 0;  // some score's first digits, so above 0
+                break;
+            }
         }
     }
     write_chosen<NT, E>(a, u, 0, key, rem, 0, o, red);
@@ -710,7 +741,7 @@ __global__ void __launch_bounds__(LT) select_begin(SelectArgs a) {
 // The key's digits before `pass`: those before the last of them as the launch before left them, that one from the cell's
 // histogram of it.  The cell's first slice leaves them for the launch after.
 __device__ __forceinline__ void key_so_far(const SelectArgs &a, int64_t c, int s, int pass, uint32_t need, uint32_t *red,
-                                           uint32_t *found, uint32_t *key, uint32_t *mask, uint32_t *rem) {
+                                           Bin *found, uint32_t *key, uint32_t *mask, uint32_t *rem) {
     *key = 0, *mask = 0, *rem = need;
     if (pass == 0) return;
     const int p = pass - 1;
@@ -719,25 +750,27 @@ __device__ __forceinline__ void key_so_far(const SelectArgs &a, int64_t c, int s
         *key = x.x, *rem = x.y;
         for (int i = 0; i < p; ++i) *mask |= digit_mask(i) << digit_shift(i);
     }
-    uint32_t bin, above;
     const uint32_t *hist = a.hist + (c * 3 + p) * kBins;
-    pick_bin<LT>([&](int i) { return hist[i]; }, *rem, red, found, &bin, &above);
-    *key |= bin << digit_shift(p), *mask |= digit_mask(p) << digit_shift(p), *rem -= above;
+    const Bin b = pick_bin<LT>([&](int i) { return hist[i]; }, *rem, red, found);
+    *key |= b.bin << digit_shift(p), *mask |= digit_mask(p) << digit_shift(p), *rem -= b.above;
     if (s == 0 && threadIdx.x == 0) a.state[c * 3 + p] = make_uint2(*key, *rem);
 }
 
 __global__ void __launch_bounds__(LT) select_digit(SelectArgs a, int pass) {
     constexpr int E = kSlice / LT;
     __shared__ __align__(16) uint32_t hist[kBins * kCopies];
-    __shared__ uint32_t red[LT / 64], found[2];
+    __shared__ uint32_t red[LT / 64];
+    __shared__ Bin found;
     const int64_t c = blockIdx.x / a.slices;
     const int s = blockIdx.x % a.slices, first = s * kSlice;
     const CellChoice x = choice_of(a, c);
     if (first >= x.nf || x.need == 0 || x.need == x.nf) return;
+    float z[E];
     uint32_t u[E], key, mask, rem;
-    load_keys<LT, E>(a.scores + c * a.n, first, x.nf, u);
+    load_scores<LT, E>(a.scores + c * a.n, first, x.nf, z);
     clear_bins<LT>(hist);
-    key_so_far(a, c, s, pass, x.need, red, found, &key, &mask, &rem);
+    key_so_far(a, c, s, pass, x.need, red, &found, &key, &mask, &rem);
+    make_keys<LT, E>(z, first, x.nf, u);
     __syncthreads();
     count_digit<E>(u, key, mask, pass, hist);
     if (pass == 2) {
@@ -758,7 +791,8 @@ __global__ void __launch_bounds__(LT) select_digit(SelectArgs a, int pass) {
 
 __global__ void __launch_bounds__(LT) select_write(SelectArgs a) {
     constexpr int E = kSlice / LT;
-    __shared__ uint32_t red[E / 4][LT / 64], found[2];
+    __shared__ uint32_t red[E / 4][LT / 64];
+    __shared__ Bin found;
     const int64_t c = blockIdx.x / a.slices;
     const int s = blockIdx.x % a.slices, first = s * kSlice;
     int64_t o = a.offsets[c];
@@ -766,12 +800,13 @@ __global__ void __launch_bounds__(LT) select_write(SelectArgs a) {
     const CellChoice x = choice_of(a, c);
     if (s == 0) write_certain<LT>(a, x, o);
     if (first >= x.nf || x.need == 0) return;
+    float z[E];
     uint32_t u[E], key = 0, mask, rem = 0, eq = 0;
-    load_keys<LT, E>(a.scores + c * a.n, first, x.nf, u);
+    load_scores<LT, E>(a.scores + c * a.n, first, x.nf, z);
     if (x.need == x.nf) {
         o += first;
     } else {
-        key_so_far(a, c, 1, 3, x.need, red[0], found, &key, &mask, &rem);
+        key_so_far(a, c, 1, 3, x.need, red[0], &found, &key, &mask, &rem);
         // tokens above and at the key in the slices before
         const uint32_t bin = key & 1023u;
         uint32_t more = 0, same = 0, all;
@@ -786,6 +821,7 @@ __global__ void __launch_bounds__(LT) select_write(SelectArgs a) {
         scan_before<LT, uint32_t>(same, red[0], &eq);
         o += all + min(eq, rem);
     }
+    make_keys<LT, E>(z, first, x.nf, u);
     write_chosen<LT, E>(a, u, first, key, rem, eq, o, red);
 }
 }  // namespace
