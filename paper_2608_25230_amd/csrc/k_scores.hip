@@ -26,20 +26,35 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 //
 // Cells differ in length, so the work is cut by length, on the device: all
 // cells' tiles of 64 tokens in a row, the same number to each wave (few_rows) or
-// workgroup (many_rows).
+// workgroup (many_rows).  A cell's first share costs more than its tiles, which
+// many_rows counts in (kFill).
 //
 // few_rows, up to 16 rows a cell: a wave holds them in registers and needs no
-// other wave; keys are loaded a tile ahead.
+// other wave; keys are loaded a tile ahead.  Memory bounds it: 512 cells of 3000
+// to 30000 tokens of 128 columns, 4 rows, 438 MB in 98 us (4.5 TB/s; 5.6 once it
+// runs, after 15 us in which shares are found and the first keys come).  By
+// many_rows 128 cells of 8000 tokens and 1 to 16 rows take 32 us instead of 26 to
+// 27.
 // many_rows: a workgroup's waves share the rows in LDS; more rows than it holds
-// are taken in turns, which add to what the turn before wrote.
+// are taken in turns, which add to what the turn before wrote.  The vector units
+// bound it: a 16 x 16 tile of weights takes four products and adds, four
+// exponentials at half rate and four sums, about 85 cycles, beside 64 of the
+// matrix units at 128 columns (256 cells of 3000 to 30000 tokens, 256 rows: 102
+// GFLOP of products in 120 us; the loop's waves issue in 80 % of the cycles).
+// Keys staged in LDS for all waves instead of rows: 150 to 170 us.
 // ---------------------------------------------------------------------------
 constexpr int TT = 64;          // tokens of a wave and step
 constexpr int FT = 256;         // threads of few_rows
-constexpr int kFewGroups = 1024;  // its workgroups
-constexpr int kQBytes = 65536;  // many_rows: rows in LDS at a time
+// its workgroups: 4 to a compute unit, 98 us at the size above; 2 110, 3 100, 8 103, 16 106
+constexpr int kFewGroups = 1024;
+// many_rows: rows in LDS at a time, so that two workgroups fit a compute unit (64 cells of 4000 tokens, 512 rows: 59 us;
+// 32 KB 70, 96 KB 82)
+constexpr int kQBytes = 65536;
+// two to a compute unit: 138 us at the size above on one card; three in turns 152, four 160
 constexpr int kManyGroups = 512;
 constexpr int kManyLeast = 2;   // tiles of a workgroup at least
-constexpr int kFill = 8;        // what a cell's rows cost there, in tiles
+// what a cell's rows cost there, in tiles: 8 127 to 134 us at the size above; 0 136 to 151, 4 139 to 143, 16 134 to 143
+constexpr int kFill = 8;
 constexpr float SLOG2E = 1.4426950408889634f;
 
 struct ScoreArgs {
@@ -402,6 +417,8 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) many_rows(ScoreArgs 
 
 template <typename T, int DP>
 hipError_t launch_scores_width(ScoreArgs &a, hipStream_t st) {
+    // Eight waves share rows best (the size above: 135 us, by four 150), as long as a tile's keys fit their registers (64
+    // cells of 4000 tokens, 128 rows: 192 columns 26 us by four, 56 by eight; 256 columns 32 and 103).
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, NW = DP <= 128 ? 8 : 4;
     const int64_t tiles = a.C * ((std::min<int64_t>((int64_t)a.W << a.shift, a.n) + TT - 1) / TT);
     if (a.R <= 16) {
@@ -419,21 +436,36 @@ hipError_t launch_scores_width(ScoreArgs &a, hipStream_t st) {
 // ---------------------------------------------------------------------------
 // select
 //
-// The last `recent` kept tokens are certain; of those before them the rest of
-// keep[c] is chosen by the key of the score, found 11, 11 and 10 bits at a time
-// from histograms, and then, among equal keys, by position.
+// A cell's tokens by their scores' keys (an order of unsigned words): the key of
+// the last one that stays is found digit by digit, 11, 11 and 10 bits from the
+// top, by a histogram in LDS and the bin in which the rank falls; a bin that is
+// taken whole ends the search.  Then the tokens above it and the first of those
+// at it are written in their order, places from sums over lanes, waves and
+// fours.  Scores are read once, into registers.
 //
-// A workgroup holds its tokens' keys in registers, four neighbours at a time.
-// Rows of up to kAlone tokens take one workgroup a cell and one launch.  Longer
-// ones are cut into slices: a launch for each digit, whose histograms of all
-// slices meet in the cell's, and one that writes.  What a slice's tokens above
-// and at the key come to is read off its histogram of the last digit, so each
-// slice finds its place from those of the slices before it.
+// Nothing but latency bounds it: 256 cells of 3000 to 30000 tokens, 6.5 MB, take
+// 18 us, a chain of loads, six sums over a workgroup and three histograms.
+//
+// Rows of up to kAlone tokens: a workgroup to a cell, 256 threads where they
+// hold it (2000 cells of 1000: 13 us, by 1024 threads 39; of 4000: 22 and 41).
+// Longer ones in slices of 8192 tokens: a launch for each digit, in which the
+// slices' histograms meet in the cell's, and one that writes.  What a slice's
+// tokens above and at the key come to is read off its histogram of the last
+// digit, so each slice finds its place from those of the slices before it.  (8
+// cells of 131072: 27 us, by one workgroup each 187.  Slices for shorter rows too:
+// 8 cells of 30000 25 us instead of 17, 256 of them 57 instead of 20.)
 // ---------------------------------------------------------------------------
 constexpr int LT = 1024;          // threads of a workgroup; fewer for short rows
 constexpr int kBins = 2048;
 constexpr int kAlone = 32 * LT;   // tokens of a cell that one workgroup takes alone
-constexpr int kSlice = 8 * LT;    // tokens of a slice otherwise
+// tokens of a slice otherwise, and how many slices are many, so that each takes twice as many (256 cells of 131072: 176 us,
+// at 8192 193, at 32768 180; 8 of them 27 at 8192, 30 at 16384)
+constexpr int kSlice = 8 * LT;
+constexpr int kManySlices = 256;
+// Scores have few exponents, so lanes meet in a bin: each has four places (256 cells of 30000 equal scores 34 us, with one
+// place 89; different ones 20 and 19).  256 threads do with one, which leaves room for more workgroups (2000 cells of 1000
+// different scores 13 us, with four 22; equal ones 33 and 31).
+constexpr int kCopies = 4;
 
 struct SelectArgs {
     int64_t C, n, n_kept;
@@ -559,22 +591,25 @@ __device__ __forceinline__ void make_keys(const float (&x)[E], int first, int nf
     for (int i = 0; i < E; ++i) u[i] = first + 4 * NT * (i / 4) + 4 * (int)threadIdx.x + i % 4 < nf ? rank_key(x[i]) : 0u;
 }
 
-// Scores have few exponents, so lanes meet in a bin: each bin has kCopies places, one for every kCopies-th lane.
-constexpr int kCopies = 4;
-template <int E>
+// A histogram has CP places for each bin, one for every CP-th lane.
+template <int CP, int E>
 __device__ __forceinline__ void count_digit(const uint32_t (&u)[E], uint32_t key, uint32_t mask, int pass, uint32_t *hist) {
-    uint32_t *mine = hist + (threadIdx.x & (kCopies - 1));
+    uint32_t *mine = hist + (threadIdx.x & (CP - 1));
 #pragma unroll
     for (int i = 0; i < E; ++i)
-        if (u[i] && (u[i] & mask) == key) atomicAdd(&mine[((u[i] >> digit_shift(pass)) & digit_mask(pass)) * kCopies], 1u);
+        if (u[i] && (u[i] & mask) == key) atomicAdd(&mine[((u[i] >> digit_shift(pass)) & digit_mask(pass)) * CP], 1u);
 }
+template <int CP>
 __device__ __forceinline__ uint32_t bin_of(const uint32_t *hist, int bin) {
-    const uint4 x = *(const uint4 *)(hist + bin * kCopies);
-    return x.x + x.y + x.z + x.w;
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < CP; ++i) n += hist[bin * CP + i];
+    return n;
 }
-template <int NT>
+template <int NT, int CP>
 __device__ __forceinline__ void clear_bins(uint32_t *hist) {
-    for (int i = threadIdx.x; i < kBins; i += NT) *(uint4 *)(hist + i * kCopies) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < kBins * CP / 4; i += NT) *(uint4 *)(hist + 4 * (i + threadIdx.x)) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // Writes the positions above the key and the first rem - eq0 of those at it, from place `at` on; eq0: those at it before.
@@ -668,7 +703,8 @@ __device__ __forceinline__ void write_rest(const SelectArgs &a, int64_t total, i
 // OWN: every workgroup sums the cells' counts for itself; else the offsets are there.
 template <int NT, int E, bool OWN>
 __global__ void __launch_bounds__(NT) select_cell(SelectArgs a) {
-    __shared__ __align__(16) uint32_t hist[kBins * kCopies];
+    constexpr int CP = NT == LT ? kCopies : 1;
+    __shared__ __align__(16) uint32_t hist[kBins * CP];
     __shared__ uint32_t red[E / 4][NT / 64];
     __shared__ Bin found;
     __shared__ longlong2 sums[NT / 64];
@@ -695,11 +731,11 @@ __global__ void __launch_bounds__(NT) select_cell(SelectArgs a) {
     if (x.need < x.nf) {
         rem = x.need;
         for (int pass = 0; pass < 3; ++pass) {
-            clear_bins<NT>(hist);
+            clear_bins<NT, CP>(hist);
             __syncthreads();
-            count_digit<E>(u, key, mask, pass, hist);
+            count_digit<CP>(u, key, mask, pass, hist);
             __syncthreads();
-            const Bin b = pick_bin<NT>([&](int i) { return bin_of(hist, i); }, rem, red[0], &found);
+            const Bin b = pick_bin<NT>([&](int i) { return bin_of<CP>(hist, i); }, rem, red[0], &found);
             key |= b.bin << digit_shift(pass), mask |= digit_mask(pass) << digit_shift(pass), rem -= b.above;
             if (b.own == rem) {  // all of the bin: no need to part it
                 --key, rem = 0;  // some score's first digits, so above 0
@@ -756,23 +792,23 @@ __device__ __forceinline__ void key_so_far(const SelectArgs &a, int64_t c, int s
     if (s == 0 && threadIdx.x == 0) a.state[c * 3 + p] = make_uint2(*key, *rem);
 }
 
+template <int E>
 __global__ void __launch_bounds__(LT) select_digit(SelectArgs a, int pass) {
-    constexpr int E = kSlice / LT;
     __shared__ __align__(16) uint32_t hist[kBins * kCopies];
     __shared__ uint32_t red[LT / 64];
     __shared__ Bin found;
     const int64_t c = blockIdx.x / a.slices;
-    const int s = blockIdx.x % a.slices, first = s * kSlice;
+    const int s = blockIdx.x % a.slices, first = s * E * LT;
     const CellChoice x = choice_of(a, c);
     if (first >= x.nf || x.need == 0 || x.need == x.nf) return;
     float z[E];
     uint32_t u[E], key, mask, rem;
     load_scores<LT, E>(a.scores + c * a.n, first, x.nf, z);
-    clear_bins<LT>(hist);
+    clear_bins<LT, kCopies>(hist);
     key_so_far(a, c, s, pass, x.need, red, &found, &key, &mask, &rem);
     make_keys<LT, E>(z, first, x.nf, u);
     __syncthreads();
-    count_digit<E>(u, key, mask, pass, hist);
+    count_digit<kCopies>(u, key, mask, pass, hist);
     if (pass == 2) {
         uint32_t more = 0, all;
 #pragma unroll
@@ -783,18 +819,18 @@ __global__ void __launch_bounds__(LT) select_digit(SelectArgs a, int pass) {
     __syncthreads();
     uint32_t *to = a.hist + (c * 3 + pass) * kBins;
     for (int i = threadIdx.x; i < (pass == 2 ? kBins / 2 : kBins); i += LT) {
-        const uint32_t n = bin_of(hist, i);
+        const uint32_t n = bin_of<kCopies>(hist, i);
         if (n) atomicAdd(&to[i], n);
         if (pass == 2) a.last[(c * a.slices + s) * (kBins / 2) + i] = n;
     }
 }
 
+template <int E>
 __global__ void __launch_bounds__(LT) select_write(SelectArgs a) {
-    constexpr int E = kSlice / LT;
     __shared__ uint32_t red[E / 4][LT / 64];
     __shared__ Bin found;
     const int64_t c = blockIdx.x / a.slices;
-    const int s = blockIdx.x % a.slices, first = s * kSlice;
+    const int s = blockIdx.x % a.slices, first = s * E * LT;
     int64_t o = a.offsets[c];
     write_rest<LT>(a, a.offsets[a.C], blockIdx.x, gridDim.x);
     const CellChoice x = choice_of(a, c);
@@ -852,13 +888,19 @@ hipError_t launch_cache_scores(const fw_cache &cache, int dtype, const void *q, 
     return dtype == FW_F32 ? width(float()) : width(uint16_t());
 }
 
-// Cells whose counts every workgroup sums for itself, which saves a launch.
+// Cells whose counts every workgroup sums for itself, which saves a launch (300 scores each: 2000 cells 9 us, with a launch
+// 11.5; 4000 cells 18 and 12.5).
 constexpr int64_t kOwnSums = 2048;
 
-static int select_slices(int64_t n) { return n <= kAlone ? 0 : (int)((n + kSlice - 1) / kSlice); }
+static int select_slices(int64_t C, int64_t n, int *size = nullptr) {
+    if (n <= kAlone) return 0;
+    const int tokens = C * ((n + kSlice - 1) / kSlice) > kManySlices ? 2 * kSlice : kSlice;
+    if (size) *size = tokens;
+    return (int)((n + tokens - 1) / tokens);
+}
 
 size_t select_ws_bytes(int64_t C, int64_t n) {
-    const int64_t slices = select_slices(n);
+    const int64_t slices = select_slices(C, n);
     if (!slices) return 0;
     return align_up(C * 3 * kBins * 4, 256) + align_up(C * 3 * sizeof(uint2), 256) + align_up(C * slices * (kBins / 2) * 4, 256) + align_up(C * slices * 4, 256);
 }
@@ -867,7 +909,8 @@ hipError_t launch_select_cells(int64_t C, const float *scores, int64_t n, const 
                                int64_t recent, int64_t n_kept, int64_t *offsets, int32_t *kept_pos, void *ws,
                                hipStream_t st) {
     SelectArgs a{C, n, n_kept, scores, lens, keep, recent, offsets, kept_pos};
-    a.slices = select_slices(n);
+    int size = 0;
+    a.slices = select_slices(C, n, &size);
     const bool own = C <= kOwnSums;
     if (a.slices) {
         char *p = (char *)ws;
@@ -878,8 +921,12 @@ hipError_t launch_select_cells(int64_t C, const float *scores, int64_t n, const 
         const dim3 grid((unsigned)(C * a.slices));
         const int64_t clears = (C * 3 * kBins / 4 + LT - 1) / LT;
         hipLaunchKernelGGL(select_begin, dim3((unsigned)std::min<int64_t>(1 + clears, 1024)), dim3(LT), 0, st, a);
-        for (int pass = 0; pass < 3; ++pass) hipLaunchKernelGGL(select_digit, grid, dim3(LT), 0, st, a, pass);
-        hipLaunchKernelGGL(select_write, grid, dim3(LT), 0, st, a);
+        const auto run = [&](auto digit, auto write) {
+            for (int pass = 0; pass < 3; ++pass) hipLaunchKernelGGL(digit, grid, dim3(LT), 0, st, a, pass);
+            hipLaunchKernelGGL(write, grid, dim3(LT), 0, st, a);
+        };
+        if (size == kSlice) run(select_digit<kSlice / LT>, select_write<kSlice / LT>);
+        else run(select_digit<2 * kSlice / LT>, select_write<2 * kSlice / LT>);
         return hipGetLastError();
     }
     if (!own) hipLaunchKernelGGL(select_offsets, dim3(1), dim3(LT), 0, st, a);

@@ -227,7 +227,7 @@ def test_select(tf, C, n, what):
     _select(tf, x, np.zeros(C, int) - 1, keep, 1, extra=4)
 
 
-@pytest.mark.parametrize("C,n", [(5000, 70), (3, 4096), (3, 4097), (2, 8192), (2, 8193), (2, 16385), (2, 32768), (2, 32769), (3, 70001)])
+@pytest.mark.parametrize("C,n", [(5000, 70), (3, 4096), (3, 4097), (2, 8192), (2, 8193), (2, 16385), (2, 32768), (2, 32769), (3, 70001), (60, 34000)])
 @pytest.mark.parametrize("what", ["normal", "ties"])
 def test_select_widths(tf, C, n, what):
     """Every width of a row, rows in slices, and more cells than every workgroup sums for itself."""
