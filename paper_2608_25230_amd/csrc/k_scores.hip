@@ -36,12 +36,14 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // many_rows 128 cells of 8000 tokens and 1 to 16 rows take 32 us instead of 26 to
 // 27.
 // many_rows: a workgroup's waves share the rows in LDS; more rows than it holds
-// are taken in turns, which add to what the turn before wrote.  The vector units
-// bound it: a 16 x 16 tile of weights takes four products and adds, four
-// exponentials at half rate and four sums, about 85 cycles, beside 64 of the
-// matrix units at 128 columns (256 cells of 3000 to 30000 tokens, 256 rows: 102
-// GFLOP of products in 120 us; the loop's waves issue in 80 % of the cycles).
-// Keys staged in LDS for all waves instead of rows: 150 to 170 us.
+// are taken in turns, which add to what the turn before wrote.  Matrix and vector
+// units bound it together, which run side by side only in part: 64 tokens x 16
+// rows of 128 columns take 16 matrix instructions and as many products with the
+// scale, exponentials and sums, in a bare loop on registers about 200 ns a SIMD,
+// here 228 (256 cells of 3000 to 30000 tokens, 256 rows: 102 GFLOP of products in
+// 120 us).  Slower were: the next tile's keys loaded ahead by waves of twice the
+// registers (132), a tile's products between the weights of the one before (125
+// to 133), keys staged in LDS for all waves instead of rows (150 to 170).
 // ---------------------------------------------------------------------------
 constexpr int TT = 64;          // tokens of a wave and step
 constexpr int FT = 256;         // threads of few_rows
