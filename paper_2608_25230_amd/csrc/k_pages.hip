@@ -7,6 +7,13 @@
 // result does not depend on who came last: collect_blocks finds their places by
 // counting bits.  Blocks that a call takes come from the stack as it was
 // before, so no block that others hold is written.
+//
+// What bounds them: a fork of 2048 cells from 256 cells of 3000 to 30000 tokens,
+// after they were ended, takes 55 us: 7 and 13 in which one workgroup serves the
+// requests in order (a chain of a dozen loads), 13 for the counters of 300000
+// blocks down, 4 for the stack, 17 for them up and 2048 part-filled blocks (67
+// MB, 13 at the rate of a copy).  A counter for each run of blocks instead of the
+// bits took 480: atomics at one address come one by one, 10 ns each.
 #include <algorithm>
 
 #include "fw_internal.hpp"
@@ -104,7 +111,8 @@ __device__ __forceinline__ void copy_block(const PageArgs &a, int32_t from, int3
 
 // Serves `n` requests in order, each thread a run of them: need(i) blocks (0 or more) for request i, -1 for one that is
 // refused in any case.  done(i, served, first): its first block's rank among those taken.  Counts those refused, and
-// leaves the stack's heights in the head.  A run of up to kAsk is asked for once, a longer one twice.
+// leaves the stack's heights in the head.  A run of up to kAsk is asked for once, a longer one twice (the fork above 55 us,
+// with two askings 57).
 constexpr int kAsk = 4;
 template <typename Need, typename Done>
 __device__ __forceinline__ void serve(const PageArgs &a, int64_t n, const Need &need, const Done &done) {
@@ -161,7 +169,8 @@ __device__ __forceinline__ void clear_marks(const PageArgs &a, int64_t b, int64_
 }
 
 // Runs up to which collect_blocks counts the marks of those before its own from their bits; many have their numbers
-// counted first, and marks that many workgroups clear.
+// counted first, and marks that many workgroups clear (a release of nothing among 260000 blocks, 64 runs: 19 us, with the
+// two launches 25; among 1000000, 245 runs: 25 either way).
 constexpr int64_t kFewRuns = 64;
 
 __global__ void __launch_bounds__(WT) clear_all(PageArgs a) { clear_marks(a, blockIdx.x, gridDim.x); }
@@ -324,10 +333,17 @@ __global__ void __launch_bounds__(WT) fork_apply(PageArgs a) {
 // chunk waits for chunks of earlier tickets of its queue, and is waited for at
 // most until its workgroup is done with that of its ticket before: always for
 // what was handed out earlier, so every wait ends.
+//
+// Memory bounds it: 256 cells of 6000 to 60000 tokens of 128 columns of which
+// 0.3 stay, 443 MB of kept tokens, for which 700 MB are read and written in whole
+// lines (values lie tokens innermost), take 193 us in compact_move (4 TB/s of
+// what its counters see), 227 in all.  Two passes through buffers of their own
+// took 273 for the reads alone.  Keys and values in launches of their own: 275 in
+// all.  One queue for all: 26000 tickets at one address, 10 ns each.
 // ---------------------------------------------------------------------------
 constexpr int CT = 1024;     // threads that look through a cell's list
 constexpr int MT = 512;      // threads that move a chunk
-constexpr int kMovers = 768;  // workgroups of it, three to a compute unit
+constexpr int kMovers = 768;  // workgroups of it, three to a compute unit (the size above: 247 us, two 254, four 264)
 constexpr int kChunk = 256;  // tokens
 constexpr int kChunkShift = 8;
 constexpr int kQueues = 64;  // of keys, and as many of values
@@ -368,10 +384,17 @@ __global__ void __launch_bounds__(CT) compact_check(PageArgs a) {
     if (!bad) {
         const int32_t *pos = a.kept_pos + o;
         const int64_t last = ((n + kChunk - 1) >> kChunkShift) - 1;
+        int32_t ahead[5];  // positions i0 - 1 .. i0 + 3, a step ahead
+        const auto load = [&](int64_t i0) {
+#pragma unroll
+            for (int u = 0; u < 5; ++u) ahead[u] = i0 + u == 0 ? -1 : pos[i0 + u - 1 < n ? i0 + u - 1 : n - 1];
+        };
+        if (4 * tid < n) load(4 * tid);
         for (int64_t i0 = 4 * tid; i0 < n; i0 += 4 * CT) {
             int64_t z[5];
 #pragma unroll
-            for (int u = 0; u < 5; ++u) z[u] = i0 + u == 0 ? -1 : pos[i0 + u - 1 < n ? i0 + u - 1 : n - 1];
+            for (int u = 0; u < 5; ++u) z[u] = ahead[u];
+            if (i0 + 4 * CT < n) load(i0 + 4 * CT);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int64_t i = i0 + u, x = z[u + 1], y = z[u];
@@ -738,8 +761,8 @@ __device__ __forceinline__ void move_chunks(const PageArgs &a, uint8_t *const ld
     }
 }
 
-// Every other workgroup begins with values and ends with keys.  Whoever is out of tickets
-// counts down the owners of the blocks that the listed cells leave.
+// Every other workgroup begins with values, the rest with keys (at the size above 5 us less than two of three).
+// Whoever is out of tickets counts down the owners of the blocks that the listed cells leave.
 __global__ void __launch_bounds__(MT, 6) compact_move(PageArgs a) {
     extern __shared__ __align__(16) uint8_t lds[];
     __shared__ MoveShared sh;
