@@ -406,7 +406,8 @@ fw_status fw_prompt_attention(const fw_packed *packed, void *o, float *lse, void
  *   free_list [n_blocks] int32 stack of free blocks, n_free[0] int32 of them
  *             (both in and out).  Growing cells, in order, take from the top;
  *             shrinking cells give back so that the same growth would get the
- *             same blocks again.
+ *             same blocks again.  (Cells that may share blocks do not
+ *             shrink here, but by fw_cache_release.)
  *   slots     [n_slots] int64: for each token that comes (cells in order,
  *             positions ascending) block * block_size + position % block_size,
  *             or -1 for a refused cell; entries past the last such token stay
