@@ -46,9 +46,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // to 133), keys staged in LDS for all waves instead of rows (150 to 170).
 // ---------------------------------------------------------------------------
 constexpr int TT = 64;          // tokens of a wave and step
-constexpr int FT = 256;         // threads of few_rows
 // its workgroups: 4 to a compute unit, 98 us at the size above; 2 110, 3 100, 8 103, 16 106
-constexpr int kFewGroups = 1024;
+constexpr int kFewGroups = 256;
 // many_rows: rows in LDS at a time, so that two workgroups fit a compute unit (64 cells of 4000 tokens, 512 rows: 59 us;
 // 32 KB 70, 96 KB 82)
 constexpr int kQBytes = 65536;
@@ -148,22 +147,26 @@ __device__ __forceinline__ int page_of(const ScoreArgs &a, const int32_t *row, i
     return b >= 0 && b < a.n_blocks ? b : -1;
 }
 
-// A lane's part of a tile's keys: token 16 x + lane % 16, bytes KB (lane / 16) and on.
+// A lane's part of a tile's keys: token 16 x + lane % 16, and of its columns those that a load of 16 bytes (8 where rows are
+// no multiple of 64) gives to lane group lane / 16: neighbouring groups load neighbouring bytes.
 template <int DP>
 struct Keys {
-    static constexpr int KW = DP / 16;  // words
+    static constexpr int KW = DP / 16;                // words
+    static constexpr int LW = KW % 4 == 0 ? 4 : 2;    // words of a load
     uint32_t k[4][KW];
     int e[4];
+    // first column of key step y
+    static __device__ __forceinline__ int column(int y, int g) { return 16 * LW * (2 * y / LW) + 4 * LW * g + 8 * y % (4 * LW); }
     __device__ __forceinline__ void load(const ScoreArgs &a, int t, const int (&page)[4], int lane) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const int64_t b = page[x] < 0 ? 0 : page[x];
             const uint8_t *p = a.kc + ((b << a.shift) + ((t * TT + 16 * x) & ((1 << a.shift) - 1))) * DP + (lane & 15) * DP +
-                               DP / 4 * (lane >> 4);
+                               4 * LW * (lane >> 4);
 #pragma unroll
-            for (int y = 0; y < KW; y += (KW % 4 == 0 ? 4 : 2)) {
-                if constexpr (KW % 4 == 0) *(uint4 *)&k[x][y] = *(const uint4 *)(p + 4 * y);
-                else *(uint2 *)&k[x][y] = *(const uint2 *)(p + 4 * y);
+            for (int y = 0; y < KW; y += LW) {
+                if constexpr (LW == 4) *(uint4 *)&k[x][y] = *(const uint4 *)(p + 16 * y);
+                else *(uint2 *)&k[x][y] = *(const uint2 *)(p + 16 * y);
             }
             e[x] = a.k_exp[b];
         }
@@ -225,84 +228,104 @@ __device__ __forceinline__ void put_scores(const ScoreArgs &a, int64_t at, const
     if (in) a.scores[at] = fmaf(out, mean, old);
 }
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(FT, DP <= (sizeof(T) == 2 ? 128 : 64) ? 4 : 2) few_rows(ScoreArgs a) {
+// NW waves, which take their workgroup's tiles one by one.
+struct Tile {
+    int c, t, len;  // cell (-1: none), tile of it, its length
+};
+template <typename T, int DP, int NW>
+__global__ void __launch_bounds__(64 * NW, NW / 4) few_rows(ScoreArgs a) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, KS = DP / 32;  // bf16 parts of a query, key steps
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tl = lane & 15, g = lane >> 4;
-    int2 found[FT / 64];
+    __shared__ int taken;
+    const int lane = threadIdx.x & 63, tl = lane & 15, g = lane >> 4;
+    if (threadIdx.x == 0) taken = 0;
+    int2 found[1];
     int per;
-    find_shares<FT, FT / 64, 0>(a, gridDim.x * (FT / 64), 1, found, &per);
-    int c = -1, at = 0;
-#pragma unroll
-    for (int i = 0; i < FT / 64; ++i)
-        if (i == w) c = __builtin_amdgcn_readfirstlane(found[i].x), at = __builtin_amdgcn_readfirstlane(found[i].y);
+    find_shares<64 * NW, 1, 0>(a, gridDim.x, 1, found, &per);
+    int c = __builtin_amdgcn_readfirstlane(found[0].x), at = __builtin_amdgcn_readfirstlane(found[0].y);
     if (c < 0) return;
-    const int g0 = (blockIdx.x * (FT / 64) + w) * per, g1 = g0 + per;  // below 2^30 tiles
+    const int g0 = blockIdx.x * per;  // below 2^30 tiles
     const float mean = 1.f / a.R;
-    for (; c < a.C && at < g1; ++c) {
-        const int len = cell_len(a, c), n = scored(a, c), nt = (n + TT - 1) / TT;
-        const int t0 = max(g0 - at, 0), t1 = min(g1 - at, nt);
-        at += nt;
-        if (t0 >= t1) continue;
-        const int seq = c / a.Hkv, h = c % a.Hkv;
-        const int32_t *row = a.table + (int64_t)c * a.W;
-        const float sl2 = (a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d))) * SLOG2E;
-        const int full = len - (a.T - 1);  // tokens that every row sees
-        const int64_t out = c * a.n + lane;
-        int pg[4], pn[4];
+    int len = cell_len(a, c), nt = (scored(a, c) + TT - 1) / TT;  // of cell c, whose first tile is number `at`
+    const auto take = [&]() -> Tile {
+        int k = 0;
+        if (lane == 0) k = atomicAdd(&taken, 1);
+        k = __builtin_amdgcn_readfirstlane(k);
+        if (k >= per) return Tile{-1, 0, 0};
+        while (g0 + k >= at + nt) {
+            at += nt;
+            if (++c >= a.C) return Tile{-1, 0, 0};
+            len = cell_len(a, c), nt = (scored(a, c) + TT - 1) / TT;
+        }
+        return Tile{c, g0 + k - at, len};
+    };
+    const auto pages = [&](const Tile &z, int (&pg)[4]) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) pg[x] = page_of(a, row, len, t0, x);
-        const auto old_score = [&](int t) { return a.earlier && t * TT + lane < n ? a.earlier[out + t * TT] : 0.f; };
-        float old = old_score(t0);
-        Keys<DP> kr;
-        kr.load(a, t0, pg, lane);
-        bf16x8 q[KS][NP];
-        f32x4 l;
-        int hid[4];
-        {
+        for (int x = 0; x < 4; ++x) pg[x] = page_of(a, a.table + (int64_t)z.c * a.W, z.c >= 0 ? z.len : 0, z.t, x);
+    };
+    const auto old_score = [&](const Tile &z) {
+        const int j = z.t * TT + lane;
+        return a.earlier && j < z.len && j < a.n ? a.earlier[z.c * a.n + j] : 0.f;
+    };
+    Tile z = take();
+    if (z.c < 0) return;
+    int pg[4], pn[4];
+    pages(z, pg);
+    float old = old_score(z);
+    Keys<DP> kr;
+    kr.load(a, z.t, pg, lane);
+    Tile next = take();
+    pages(next, pn);
+    int cell = -1;  // whose rows these are
+    bf16x8 q[KS][NP];
+    f32x4 l;
+    int hid[4];
+    float sl2 = 0.f;
+    while (z.c >= 0) {
+        if (z.c != cell) {
+            cell = z.c;
+            const int seq = cell / a.Hkv, h = cell % a.Hkv;
+            sl2 = (a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d))) * SLOG2E;
             const T *p = (const T *)a.q + seq * a.q_seq + (tl / a.G) * a.q_tok + (h * a.G + tl % a.G) * a.q_head;
 #pragma unroll
-            for (int y = 0; y < KS; ++y) load_row<T, NP>(a, p, tl < a.R, DP / 4 * g + 8 * y, q[y]);
+            for (int y = 0; y < KS; ++y) load_row<T, NP>(a, p, tl < a.R, Keys<DP>::column(y, g), q[y]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = 4 * g + i;
                 l[i] = r < a.R ? a.lse[((int64_t)seq * a.T + r / a.G) * a.Hkv * a.G + h * a.G + r % a.G] * SLOG2E : INFINITY;
-                hid[i] = r < a.R ? len - (a.T - 1 - r / a.G) : 0;
+                hid[i] = r < a.R ? z.len - (a.T - 1 - r / a.G) : 0;
             }
         }
+        float f[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int x = 0; x < 4; ++x) pn[x] = page_of(a, row, t0 + 1 < t1 ? len : 0, t0 + 1, x);
-        for (int t = t0; t < t1; ++t) {
-            float f[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < 4; ++x) f[x] = sl2 * exp2_of_byte(kr.e[x]);
+        f32x4 s[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) f[x] = sl2 * exp2_of_byte(kr.e[x]);
-            f32x4 s[4];
+        for (int x = 0; x < 4; ++x) {
+            s[x] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                s[x] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            for (int y = 0; y < KS; ++y) {
+                const bf16x8 kk = widen(kr.k[x][2 * y], kr.k[x][2 * y + 1]);
 #pragma unroll
-                for (int y = 0; y < KS; ++y) {
-                    const bf16x8 kk = widen(kr.k[x][2 * y], kr.k[x][2 * y + 1]);
-#pragma unroll
-                    for (int z = NP - 1; z >= 0; --z) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[y][z], kk, s[x], 0, 0, 0);
-                }
+                for (int u = NP - 1; u >= 0; --u) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[y][u], kk, s[x], 0, 0, 0);
             }
-            // the next tile: what is added to before the keys, whose use waits for all loads before
-            const int now[4] = {pg[0], pg[1], pg[2], pg[3]};
-            const float was = old;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) pg[x] = pn[x];
-            if (t + 1 < t1) {
-                old = old_score(t + 1);
-                kr.load(a, t + 1, pg, lane);
-            }
-#pragma unroll
-            for (int x = 0; x < 4; ++x) pn[x] = page_of(a, row, t + 2 < t1 ? len : 0, t + 2, x);
-            if (t * TT + TT > full) add_weights<true>(s, l, f, hid, t * TT + tl, sum);
-            else add_weights<false>(s, l, f, hid, t * TT + tl, sum);
-            put_scores(a, out + t * TT, sum, now, lane, t * TT + lane < n, mean, was);
         }
+        // the next tile: what is added to before the keys, whose use waits for all loads before
+        const Tile now = z;
+        const int from[4] = {pg[0], pg[1], pg[2], pg[3]};
+        const float was = old;
+        z = next;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) pg[x] = pn[x];
+        if (z.c >= 0) {
+            old = old_score(z);
+            kr.load(a, z.t, pg, lane);
+            next = take();
+            pages(next, pn);
+        }
+        const int tok = now.t * TT;
+        if (tok + TT > now.len - (a.T - 1)) add_weights<true>(s, l, f, hid, tok + tl, sum);
+        else add_weights<false>(s, l, f, hid, tok + tl, sum);
+        put_scores(a, now.c * a.n + tok + lane, sum, from, lane, tok + lane < now.len && tok + lane < a.n, mean, was);
     }
 }
 
@@ -350,7 +373,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) many_rows(ScoreArgs 
                     // row r is head r % G of position r / G; exact, since R <= 4096
                     const int pos = (int)((r + 0.5f) * inv_g), head = h * a.G + r - pos * a.G;
                     const T *p = (const T *)a.q + seq * a.q_seq + pos * a.q_tok + head * a.q_head;
-                    load_row<T, NP>(a, p, r < a.R && i < tiles * KS * 64, DP / 4 * g + 8 * y, z[u]);
+                    load_row<T, NP>(a, p, r < a.R && i < tiles * KS * 64, Keys<DP>::column(y, g), z[u]);
                 }
 #pragma unroll
                 for (int u = 0; u < FL; ++u) {
@@ -424,8 +447,8 @@ hipError_t launch_scores_width(ScoreArgs &a, hipStream_t st) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, NW = DP <= 128 ? 8 : 4;
     const int64_t tiles = a.C * ((std::min<int64_t>((int64_t)a.W << a.shift, a.n) + TT - 1) / TT);
     if (a.R <= 16) {
-        const int64_t groups = (tiles + FT / 64 - 1) / (FT / 64);
-        hipLaunchKernelGGL((few_rows<T, DP>), dim3((unsigned)std::min<int64_t>(kFewGroups, groups)), dim3(FT), 0, st, a);
+        constexpr int FW = DP <= (sizeof(T) == 2 ? 128 : 64) ? 16 : 8;
+        hipLaunchKernelGGL((few_rows<T, DP, FW>), dim3((unsigned)std::min<int64_t>(kFewGroups, tiles)), dim3(64 * FW), 0, st, a);
         return hipGetLastError();
     }
     const int row = 2 * DP * NP;
