@@ -25,16 +25,19 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // all 24 bits.
 //
 // Cells differ in length, so the work is cut by length, on the device: all
-// cells' tiles of 64 tokens in a row, the same number to each wave (few_rows) or
-// workgroup (many_rows).  A cell's first share costs more than its tiles, which
-// many_rows counts in (kFill).
+// cells' tiles of 64 tokens in a row, the same number to each workgroup.  A
+// cell's first share costs more than its tiles, which many_rows counts in
+// (kFill).
 //
-// few_rows, up to 16 rows a cell: a wave holds them in registers and needs no
-// other wave; keys are loaded a tile ahead.  Memory bounds it: 512 cells of 3000
-// to 30000 tokens of 128 columns, 4 rows, 438 MB in 98 us (4.5 TB/s; 5.6 once it
-// runs, after 15 us in which shares are found and the first keys come).  By
-// many_rows 128 cells of 8000 tokens and 1 to 16 rows take 32 us instead of 26 to
-// 27.
+// few_rows, up to 16 rows a cell: a wave holds them in registers; keys are loaded
+// a tile ahead.  Memory bounds it: 512 cells of 3000 to 30000 tokens of 128
+// columns, 4 rows, 438 MB in 95.5 us (4.6 TB/s; 5.8 once it runs, after 15 us in
+// which shares are found and the first keys come).  The older waves of a compute
+// unit are served first, so a workgroup takes all of it and its waves take tiles
+// one by one: with a fixed share each the first were done at two thirds of the
+// time (98 us; 16384 cells of 200 tokens 113 instead of 64).  By many_rows 128
+// cells of 8000 tokens and 1 to 16 rows take 32 us instead of 25 to 28.
+//
 // many_rows: a workgroup's waves share the rows in LDS; more rows than it holds
 // are taken in turns, which add to what the turn before wrote.  Matrix and vector
 // units bound it together, which run side by side only in part: 64 tokens x 16
@@ -46,10 +49,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // to 133), keys staged in LDS for all waves instead of rows (150 to 170).
 // ---------------------------------------------------------------------------
 constexpr int TT = 64;          // tokens of a wave and step
-// its workgroups: 4 to a compute unit, 98 us at the size above; 2 110, 3 100, 8 103, 16 106
+// its workgroups: one to a compute unit, whose registers its waves fill; twice as many take 98 us at the size above, and
+// 128 cells of 8000 tokens 33 us instead of 27
 constexpr int kFewGroups = 256;
-// many_rows: rows in LDS at a time, so that two workgroups fit a compute unit (64 cells of 4000 tokens, 512 rows: 59 us;
-// 32 KB 70, 96 KB 82)
+// many_rows: rows in LDS at a time, so that two workgroups fit a compute unit and one loads rows while the other computes.
+// Where they do not hold all rows, one workgroup of twice the waves holds twice as many and takes fewer turns (64 cells of
+// 4000 tokens, 512 / 2048 rows: 60 / 207 us, by two 64 / 220; float32, 128 rows: 36 and 40; 256 columns, 512 rows: 94 and
+// 108).  Where they do, two are better (2048 cells of 500 tokens, 20 rows: 48 us, by one 61).
 constexpr int kQBytes = 65536;
 // two to a compute unit: 138 us at the size above on one card; three in turns 152, four 160
 constexpr int kManyGroups = 512;
@@ -147,26 +153,30 @@ __device__ __forceinline__ int page_of(const ScoreArgs &a, const int32_t *row, i
     return b >= 0 && b < a.n_blocks ? b : -1;
 }
 
-// A lane's part of a tile's keys: token 16 x + lane % 16, and of its columns those that a load of 16 bytes (8 where rows are
-// no multiple of 64) gives to lane group lane / 16: neighbouring groups load neighbouring bytes.
-template <int DP>
+// A lane's part of a tile's keys: token 16 x + lane % 16, and a quarter of its columns, by loads of 16 bytes (8 where rows
+// are no multiple of 64).  NEAR: a lane's bytes are neighbours, which many_rows does better with (64 cells of 4000 tokens,
+// 2048 rows of 128 columns: 216 us, else 222); otherwise the lane groups' bytes of a load are (512 cells of 8000 tokens of
+// 256 columns, 4 rows: 212 us, else 230; of 128 columns the same).
+template <int DP, bool NEAR>
 struct Keys {
     static constexpr int KW = DP / 16;                // words
     static constexpr int LW = KW % 4 == 0 ? 4 : 2;    // words of a load
+    static constexpr int STEP = NEAR ? 4 : 16;        // bytes from a load to the next, for each of its words
+    static constexpr int GROUP = NEAR ? DP / 4 : 4 * LW;  // and from a lane group to the next
     uint32_t k[4][KW];
     int e[4];
     // first column of key step y
-    static __device__ __forceinline__ int column(int y, int g) { return 16 * LW * (2 * y / LW) + 4 * LW * g + 8 * y % (4 * LW); }
+    static __device__ __forceinline__ int column(int y, int g) { return STEP * (2 * y / LW * LW) + GROUP * g + 8 * y % (4 * LW); }
     __device__ __forceinline__ void load(const ScoreArgs &a, int t, const int (&page)[4], int lane) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const int64_t b = page[x] < 0 ? 0 : page[x];
             const uint8_t *p = a.kc + ((b << a.shift) + ((t * TT + 16 * x) & ((1 << a.shift) - 1))) * DP + (lane & 15) * DP +
-                               4 * LW * (lane >> 4);
+                               GROUP * (lane >> 4);
 #pragma unroll
             for (int y = 0; y < KW; y += LW) {
-                if constexpr (LW == 4) *(uint4 *)&k[x][y] = *(const uint4 *)(p + 16 * y);
-                else *(uint2 *)&k[x][y] = *(const uint2 *)(p + 16 * y);
+                if constexpr (LW == 4) *(uint4 *)&k[x][y] = *(const uint4 *)(p + STEP * y);
+                else *(uint2 *)&k[x][y] = *(const uint2 *)(p + STEP * y);
             }
             e[x] = a.k_exp[b];
         }
@@ -271,7 +281,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) few_rows(ScoreArgs a) {
     int pg[4], pn[4];
     pages(z, pg);
     float old = old_score(z);
-    Keys<DP> kr;
+    Keys<DP, false> kr;
     kr.load(a, z.t, pg, lane);
     Tile next = take();
     pages(next, pn);
@@ -287,7 +297,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) few_rows(ScoreArgs a) {
             sl2 = (a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d))) * SLOG2E;
             const T *p = (const T *)a.q + seq * a.q_seq + (tl / a.G) * a.q_tok + (h * a.G + tl % a.G) * a.q_head;
 #pragma unroll
-            for (int y = 0; y < KS; ++y) load_row<T, NP>(a, p, tl < a.R, Keys<DP>::column(y, g), q[y]);
+            for (int y = 0; y < KS; ++y) load_row<T, NP>(a, p, tl < a.R, Keys<DP, false>::column(y, g), q[y]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = 4 * g + i;
@@ -332,7 +342,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) few_rows(ScoreArgs a) {
 // NW waves; LDS: rows as MFMA operands [row tile][key step][part][lane], their lse (base 2), and how many of the last
 // tokens each does not see.
 template <typename T, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) many_rows(ScoreArgs a) {
+__global__ void __launch_bounds__(64 * NW, DP <= 128 ? 4 : NW / 4) many_rows(ScoreArgs a) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, KS = DP / 32, NT = 64 * NW;
     extern __shared__ __align__(16) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -373,7 +383,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) many_rows(ScoreArgs 
                     // row r is head r % G of position r / G; exact, since R <= 4096
                     const int pos = (int)((r + 0.5f) * inv_g), head = h * a.G + r - pos * a.G;
                     const T *p = (const T *)a.q + seq * a.q_seq + pos * a.q_tok + head * a.q_head;
-                    load_row<T, NP>(a, p, r < a.R && i < tiles * KS * 64, Keys<DP>::column(y, g), z[u]);
+                    load_row<T, NP>(a, p, r < a.R && i < tiles * KS * 64, Keys<DP, true>::column(y, g), z[u]);
                 }
 #pragma unroll
                 for (int u = 0; u < FL; ++u) {
@@ -397,7 +407,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) many_rows(ScoreArgs 
                 bf16x8 kf[4][KS];
                 float f[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
                 {
-                    Keys<DP> kr;
+                    Keys<DP, true> kr;
                     kr.load(a, t, pg, lane);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
@@ -442,9 +452,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) many_rows(ScoreArgs 
 
 template <typename T, int DP>
 hipError_t launch_scores_width(ScoreArgs &a, hipStream_t st) {
-    // Eight waves share rows best (the size above: 135 us, by four 150), as long as a tile's keys fit their registers (64
-    // cells of 4000 tokens, 128 rows: 192 columns 26 us by four, 56 by eight; 256 columns 32 and 103).
-    constexpr int NP = sizeof(T) == 4 ? 3 : 1, NW = DP <= 128 ? 8 : 4;
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1;
     const int64_t tiles = a.C * ((std::min<int64_t>((int64_t)a.W << a.shift, a.n) + TT - 1) / TT);
     if (a.R <= 16) {
         constexpr int FW = DP <= (sizeof(T) == 2 ? 128 : 64) ? 16 : 8;
@@ -452,9 +460,16 @@ hipError_t launch_scores_width(ScoreArgs &a, hipStream_t st) {
         return hipGetLastError();
     }
     const int row = 2 * DP * NP;
-    a.turn = std::min((a.R + 15) / 16 * 16, kQBytes / row / 16 * 16);
-    hipLaunchKernelGGL((many_rows<T, DP, NW>), dim3((unsigned)std::min<int64_t>(kManyGroups, (tiles + kManyLeast - 1) / kManyLeast)),
-                       dim3(64 * NW), (size_t)a.turn * (row + 8), st, a);
+    const auto many = [&](auto kernel, int waves, int groups, int bytes) {
+        a.turn = std::min((a.R + 15) / 16 * 16, bytes / row / 16 * 16);
+        const int64_t most = (tiles + kManyLeast - 1) / kManyLeast;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(groups, most)), dim3(64 * waves), (size_t)a.turn * (row + 8), st, a);
+    };
+    // Eight waves share rows best (256 cells of 3000 to 30000 tokens, 256 rows: 135 us, by four 150), as long as a tile's keys
+    // fit their registers (64 cells of 4000 tokens, 128 rows: 192 columns 26 us by four, 56 by eight; 256 columns 32 and 103).
+    constexpr int NW = DP <= 128 ? 8 : 4;
+    if ((a.R + 15) / 16 * 16 * row <= kQBytes) many(many_rows<T, DP, NW>, NW, kManyGroups, kQBytes);
+    else many(many_rows<T, DP, 2 * NW>, 2 * NW, kManyGroups / 2, 2 * kQBytes);
     return hipGetLastError();
 }
 

@@ -89,6 +89,14 @@ def test_rows(tf, dtype, T, G):
     _run(tf, dtype, 128, 64, [5, 400], 1, T, G)
 
 
+@pytest.mark.parametrize("dtype,d,T,G", [("bf16", 20, 1100, 2), ("bf16", 20, 520, 2), ("f32", 20, 350, 2), ("f32", 80, 60, 3),
+                                         ("bf16", 160, 100, 2), ("bf16", 256, 65, 2), ("bf16", 256, 300, 1), ("f32", 256, 23, 2),
+                                         ("f32", 256, 100, 1)])
+def test_rows_past_what_is_held(tf, dtype, d, T, G):
+    """Rows that a workgroup of twice the waves holds, in one turn and in several, at every kind of width."""
+    _run(tf, dtype, d, 16, [90, 0, 700, 3], 1, T, G)
+
+
 @pytest.mark.parametrize("C,top", [(1, 5000), (64, 700), (300, 60), (1500, 20)])
 def test_many_and_long_cells(tf, C, top):
     rng = np.random.default_rng(C)
