@@ -285,57 +285,54 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) few_rows(ScoreArgs a) {
     kr.load(a, z.t, pg, lane);
     Tile next = take();
     pages(next, pn);
-    int cell = -1;  // whose rows these are
-    bf16x8 q[KS][NP];
-    f32x4 l;
-    int hid[4];
-    float sl2 = 0.f;
     while (z.c >= 0) {
-        if (z.c != cell) {
-            cell = z.c;
-            const int seq = cell / a.Hkv, h = cell % a.Hkv;
-            sl2 = (a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d))) * SLOG2E;
-            const T *p = (const T *)a.q + seq * a.q_seq + (tl / a.G) * a.q_tok + (h * a.G + tl % a.G) * a.q_head;
+        const int cell = z.c, seq = cell / a.Hkv, h = cell % a.Hkv;
+        const float sl2 = (a.scale ? a.scale[h] : (float)(1.0 / sqrt((double)a.d))) * SLOG2E;
+        bf16x8 q[KS][NP];
+        f32x4 l;
+        int hid[4];
+        const T *p = (const T *)a.q + seq * a.q_seq + (tl / a.G) * a.q_tok + (h * a.G + tl % a.G) * a.q_head;
 #pragma unroll
-            for (int y = 0; y < KS; ++y) load_row<T, NP>(a, p, tl < a.R, Keys<DP, false>::column(y, g), q[y]);
+        for (int y = 0; y < KS; ++y) load_row<T, NP>(a, p, tl < a.R, Keys<DP, false>::column(y, g), q[y]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 4 * g + i;
-                l[i] = r < a.R ? a.lse[((int64_t)seq * a.T + r / a.G) * a.Hkv * a.G + h * a.G + r % a.G] * SLOG2E : INFINITY;
-                hid[i] = r < a.R ? z.len - (a.T - 1 - r / a.G) : 0;
+        for (int i = 0; i < 4; ++i) {
+            const int r = 4 * g + i;
+            l[i] = r < a.R ? a.lse[((int64_t)seq * a.T + r / a.G) * a.Hkv * a.G + h * a.G + r % a.G] * SLOG2E : INFINITY;
+            hid[i] = r < a.R ? z.len - (a.T - 1 - r / a.G) : 0;
+        }
+        do {
+            float f[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) f[x] = sl2 * exp2_of_byte(kr.e[x]);
+            f32x4 s[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                s[x] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int y = 0; y < KS; ++y) {
+                    const bf16x8 kk = widen(kr.k[x][2 * y], kr.k[x][2 * y + 1]);
+#pragma unroll
+                    for (int u = NP - 1; u >= 0; --u) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[y][u], kk, s[x], 0, 0, 0);
+                }
             }
-        }
-        float f[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+            // the next tile: what is added to before the keys, whose use waits for all loads before
+            const Tile now = z;
+            const int from[4] = {pg[0], pg[1], pg[2], pg[3]};
+            const float was = old;
+            z = next;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) f[x] = sl2 * exp2_of_byte(kr.e[x]);
-        f32x4 s[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            s[x] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int y = 0; y < KS; ++y) {
-                const bf16x8 kk = widen(kr.k[x][2 * y], kr.k[x][2 * y + 1]);
-#pragma unroll
-                for (int u = NP - 1; u >= 0; --u) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[y][u], kk, s[x], 0, 0, 0);
+            for (int x = 0; x < 4; ++x) pg[x] = pn[x];
+            if (z.c >= 0) {
+                old = old_score(z);
+                kr.load(a, z.t, pg, lane);
+                next = take();
+                pages(next, pn);
             }
-        }
-        // the next tile: what is added to before the keys, whose use waits for all loads before
-        const Tile now = z;
-        const int from[4] = {pg[0], pg[1], pg[2], pg[3]};
-        const float was = old;
-        z = next;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) pg[x] = pn[x];
-        if (z.c >= 0) {
-            old = old_score(z);
-            kr.load(a, z.t, pg, lane);
-            next = take();
-            pages(next, pn);
-        }
-        const int tok = now.t * TT;
-        if (tok + TT > now.len - (a.T - 1)) add_weights<true>(s, l, f, hid, tok + tl, sum);
-        else add_weights<false>(s, l, f, hid, tok + tl, sum);
-        put_scores(a, now.c * a.n + tok + lane, sum, from, lane, tok + lane < now.len && tok + lane < a.n, mean, was);
+            const int tok = now.t * TT;
+            if (tok + TT > now.len - (a.T - 1)) add_weights<true>(s, l, f, hid, tok + tl, sum);
+            else add_weights<false>(s, l, f, hid, tok + tl, sum);
+            put_scores(a, now.c * a.n + tok + lane, sum, from, lane, tok + lane < now.len && tok + lane < a.n, mean, was);
+        } while (z.c == cell);
     }
 }
 
