@@ -101,6 +101,13 @@ def test_many_tokens(tf, T):
     _run(tf, "bf16", T, 3, 1, 32, 32, False, 1e-6, "bf16")
 
 
+@pytest.mark.parametrize("T,Hq,Hkv,d", [(4101, 1, 0, 128), (37, 1, 1, 16), (4999, 2, 1, 256), (13, 3, 0, 20), (8193, 1, 1, 20), (3, 70, 3, 64)])
+@pytest.mark.parametrize("eps", [None, 1e-6])
+def test_tokens_of_a_workgroup(tf, T, Hq, Hkv, d, eps):
+    """Few heads, so that a workgroup takes up to eight tokens, the last one fewer; many heads."""
+    _run(tf, "bf16", T, Hq, Hkv, d, d, False, eps, eps is not None)
+
+
 @pytest.mark.parametrize("far", [131072, 1 << 24, (1 << 31) - 1, 1 << 40])
 def test_far_positions(tf, far):
     _run(tf, "f32", 40, 2, 1, 64, 64, False, None, None, far=far)
