@@ -513,7 +513,7 @@ struct MoveShared {
     int32_t ticket, count[kChunk / 64];
 };
 
-template <bool VALUES>
+template <bool VALUES, bool ONCE>
 __device__ __forceinline__ void move_chunks(const PageArgs &a, uint8_t *const lds, MoveShared &sh) {
     auto &stay = sh.stay;
     auto &pack = sh.pack;
@@ -575,6 +575,7 @@ __device__ __forceinline__ void move_chunks(const PageArgs &a, uint8_t *const ld
     const int64_t o = p < 0 ? 0 : a.offsets[p], t0 = (o >> kChunkShift) + p, j = chunk - t0;
     // this chunk's tokens in blocks that change
     const int lo = (int)max((int64_t)x.y * a.bs - j * kChunk, (int64_t)0), hi = (int)min(x.x - j * kChunk, (int64_t)kChunk);
+    if (ONCE) open = 0;
     if (p < 0 || lo >= hi) {
         __syncthreads();  // everyone has the ticket
         if (w == MT / 64 - 1) take_ticket();
@@ -763,12 +764,15 @@ __device__ __forceinline__ void move_chunks(const PageArgs &a, uint8_t *const ld
 
 // Every other workgroup begins with values, the rest with keys (at the size above 5 us less than two of three).
 // Whoever is out of tickets counts down the owners of the blocks that the listed cells leave.
+// ONCE: there is a workgroup for every chunk's keys and one for its values, so none asks for a second ticket (16 cells of
+// 4000 tokens that grow and are compacted: 38 us, with second tickets 42).
+template <bool ONCE>
 __global__ void __launch_bounds__(MT, 6) compact_move(PageArgs a) {
     extern __shared__ __align__(16) uint8_t lds[];
     __shared__ MoveShared sh;
-    for (int i = 0; i < 2; ++i) {
-        if ((blockIdx.x % 2 != 0) != (i == 1)) move_chunks<true>(a, lds, sh);
-        else move_chunks<false>(a, lds, sh);
+    for (int i = 0; i < (ONCE ? 1 : 2); ++i) {
+        if ((blockIdx.x % 2 != 0) != (i == 1)) move_chunks<true, ONCE>(a, lds, sh);
+        else move_chunks<false, ONCE>(a, lds, sh);
     }
     for (int64_t p = blockIdx.x; p < a.P; p += gridDim.x) {
         const int4 x = a.plan[p];
@@ -879,7 +883,9 @@ hipError_t launch_cell_compact(const fw_cache &cache, const fw_cells &cells, int
     if (P > 0) hipLaunchKernelGGL(compact_check, dim3((unsigned)P), dim3(CT), 0, st, a);
     hipLaunchKernelGGL(compact_plan, dim3(1), dim3(PT), 0, st, a);
     if (P == 0) return hipGetLastError();
-    hipLaunchKernelGGL(compact_move, dim3((unsigned)std::min<int64_t>(2 * a.chunks, kMovers)), dim3(MT), a.dp * (kChunk + 4), st, a);
+    const unsigned lds = a.dp * (kChunk + 4);
+    if (2 * a.chunks <= kMovers) hipLaunchKernelGGL(compact_move<true>, dim3((unsigned)(2 * a.chunks)), dim3(MT), lds, st, a);
+    else hipLaunchKernelGGL(compact_move<false>, dim3(kMovers), dim3(MT), lds, st, a);
     if (a.nruns > kFewRuns) hipLaunchKernelGGL(count_runs, dim3((unsigned)a.nruns), dim3(WT), 0, st, a);
     hipLaunchKernelGGL(compact_finish, dim3((unsigned)(a.nruns + P)), dim3(WT), 0, st, a);
     return hipGetLastError();
