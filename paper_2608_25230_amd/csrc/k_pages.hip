@@ -9,8 +9,8 @@
 // before, so no block that others hold is written.
 //
 // What bounds them: a fork of 2048 cells from 256 cells of 3000 to 30000 tokens,
-// after they were ended, takes 55 us: 7 and 13 in which one workgroup serves the
-// requests in order (a chain of a dozen loads), 13 for the counters of 300000
+// after they were ended, takes 51 us: 7 and 9 in which one workgroup serves the
+// requests in order (a chain of loads), 14 for the counters of 300000
 // blocks down, 4 for the stack, 17 for them up and 2048 part-filled blocks (67
 // MB, 13 at the rate of a copy).  A counter for each run of blocks instead of the
 // bits took 480: atomics at one address come one by one, 10 ns each.
@@ -111,8 +111,8 @@ __device__ __forceinline__ void copy_block(const PageArgs &a, int32_t from, int3
 
 // Serves `n` requests in order, each thread a run of them: need(i) blocks (0 or more) for request i, -1 for one that is
 // refused in any case.  done(i, served, first): its first block's rank among those taken.  Counts those refused, and
-// leaves the stack's heights in the head.  A run of up to kAsk is asked for once, a longer one twice (the fork above 55 us,
-// with two askings 57).
+// leaves the stack's heights in the head.  A run of up to kAsk is asked for once, a longer one twice (the fork above
+// 2 us less than with two askings).
 constexpr int kAsk = 4;
 template <typename Need, typename Done>
 __device__ __forceinline__ void serve(const PageArgs &a, int64_t n, const Need &need, const Done &done) {
@@ -154,7 +154,12 @@ __device__ __forceinline__ void serve(const PageArgs &a, int64_t n, const Need &
         for (int64_t i = i0; i < i1; ++i) one(i, need(i));
     }
     if (out) atomicAdd(&refused, out);
-    if (last) atomicMax(&taken, (unsigned long long)last);  // running sums only grow
+    // running sums only grow: a wave's last one is its highest lane's
+    const uint64_t any = __ballot(last > 0);
+    if (any) {
+        const int hi = 63 - __builtin_clzll(any);
+        if ((int)(threadIdx.x & 63) == hi) atomicMax(&taken, (unsigned long long)last);
+    }
     __syncthreads();
     if (threadIdx.x == 0) {
         a.refused[0] = refused;
@@ -267,13 +272,13 @@ __device__ __forceinline__ void claim_cells(const PageArgs &a, int64_t n, const 
 }
 
 __global__ void __launch_bounds__(PT) fork_plan(PageArgs a) {
-    claim_cells(a, a.P, a.dst);
-    const auto tokens = [&](int64_t p) -> int64_t {  // of pair p, or -1
+    const auto tokens = [&](int64_t p) -> int64_t {  // of pair p, or -1; whether it is the first to name its cell aside
         const int32_t s = a.src[p], t = a.dst[p];
-        if (!in_range(a, s) || !in_range(a, t) || claimed(a, t) != p || length_of(a, t) != 0) return -1;
-        const int64_t n = length_of(a, s);
-        return !a.length || a.length[p] >= n ? n : a.length[p] > 0 ? a.length[p] : 0;
+        const bool ok = in_range(a, s) && in_range(a, t);
+        const int64_t n = length_of(a, ok ? s : 0), is = length_of(a, ok ? t : 0), most = a.length ? a.length[p] : n;
+        return !ok || is != 0 ? -1 : most >= n ? n : most > 0 ? most : 0;
     };
+    const auto if_first = [&](int64_t p, int64_t n) { return n >= 0 && claimed(a, a.dst[p]) == p ? n : -1; };
     const auto blocks = [&](int64_t n) -> int64_t { return n < 0 ? -1 : (n & (a.bs - 1)) != 0; };
     const int64_t top = free_blocks(a);
     const auto done = [&](int64_t p, bool served, int64_t x, int64_t first, int64_t n) {
@@ -282,12 +287,16 @@ __global__ void __launch_bounds__(PT) fork_plan(PageArgs a) {
     };
     // lengths of before the call: all are read before any is written
     const int64_t run = (a.P + PT - 1) / PT, i0 = threadIdx.x * run;
-    if (run <= kAsk) {  // read when serve asks, once, before it lets any thread go on
+    if (run <= kAsk) {
         int64_t n[kAsk];
-        serve(a, a.P, [&](int64_t p) { return blocks(n[p - i0] = tokens(p)); },
+#pragma unroll
+        for (int u = 0; u < kAsk; ++u) n[u] = u < run && i0 + u < a.P ? tokens(i0 + u) : -1;
+        claim_cells(a, a.P, a.dst);
+        serve(a, a.P, [&](int64_t p) { return blocks(n[p - i0] = if_first(p, n[p - i0])); },
               [&](int64_t p, bool served, int64_t x, int64_t first) { done(p, served, x, first, n[p - i0]); });
     } else {
-        for (int64_t p = threadIdx.x; p < a.P; p += PT) a.plan[p].x = (int)tokens(p);
+        claim_cells(a, a.P, a.dst);
+        for (int64_t p = threadIdx.x; p < a.P; p += PT) a.plan[p].x = (int)if_first(p, tokens(p));
         __syncthreads();
         serve(a, a.P, [&](int64_t p) { return blocks(a.plan[p].x); },
               [&](int64_t p, bool served, int64_t x, int64_t first) { done(p, served, x, first, a.plan[p].x); });
