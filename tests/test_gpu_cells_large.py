@@ -214,3 +214,30 @@ def test_graphs_that_share_a_workspace(tf):
             got = _rows(torch, cache, cells.table[2 + c], torch.arange(p.numel(), device="cuda", dtype=torch.int32), 16)
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (i, c)
         assert int(stop()) == 0 and int(cells.n_free) == free and not cells.shared.any()
+
+
+def test_two_compactions_at_once(tf):
+    """On two streams, each with more chunks than workgroups fit the card."""
+    torch, fw = tf
+    gen = _gen(torch, 5)
+    bs, dp, lens = 64, 128, [9000 + 31 * i for i in range(60)]
+    sides = []
+    for _ in range(2):
+        cells, n_blocks = _grown(tf, gen, lens, bs)
+        cache = _cache(tf, gen, n_blocks, bs, dp)
+        pos = [torch.nonzero(torch.rand(n, generator=gen, device="cuda") < 0.6).flatten().int() for n in lens]
+        off = torch.tensor([0] + [p.numel() for p in pos], device="cuda").cumsum(0)
+        was = cache._replace(k=cache.k.clone(), v=cache.v.clone())
+        sides.append((torch.cuda.Stream(), cells, cache, pos, torch.cat(pos), off, was, cells.table.clone()))
+    torch.cuda.synchronize()
+    out = []
+    for st, cells, cache, _, flat, off, _, _ in sides:
+        with torch.cuda.stream(st):
+            out.append(fw.cache_compact(cache, cells, off, flat))
+    torch.cuda.synchronize()
+    for (_, cells, cache, pos, _, _, was, table), r in zip(sides, out):
+        assert int(r["refused"]) == 0
+        for c in range(0, len(lens), 7):
+            want = _rows(torch, was, table[c], pos[c], bs)
+            got = _rows(torch, cache, cells.table[c], torch.arange(pos[c].numel(), device="cuda", dtype=torch.int32), bs)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), c
