@@ -88,6 +88,9 @@ __device__ __forceinline__ int scored(const ScoreArgs &a, int c) {  // tokens of
     const int len = cell_len(a, c);
     return len > a.n ? (int)a.n : len;
 }
+// Tiles of n tokens.  A cell may hold 2^31 - 1 of them: counts that round up are unsigned, and no token number goes past
+// the last tile's.
+__device__ __forceinline__ int tile_count(int n) { return (int)(((uint32_t)n + TT - 1) / TT); }
 __device__ __forceinline__ float exp2_of_byte(int b) { return __uint_as_float((uint32_t)(b < 1 ? 1 : b) << 23); }
 
 __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
@@ -109,8 +112,8 @@ __device__ __forceinline__ void find_shares(const ScoreArgs &a, int shares, int 
     const int run = (a.C + NT - 1) / NT, c0 = tid * run, c1 = c0 + run < a.C ? c0 + run : a.C;
     int mine = 0;
     const auto tiles_of = [&](int c) {
-        const int n = scored(a, c);
-        return n > 0 ? (n + TT - 1) / TT + EXTRA : 0;
+        const int n = tile_count(scored(a, c));
+        return n > 0 ? n + EXTRA : 0;
     };
     for (int c = c0; c < c1; ++c) mine += tiles_of(c);
     int x = mine;
@@ -150,7 +153,8 @@ __device__ __forceinline__ void find_shares(const ScoreArgs &a, int shares, int 
 
 // The 16 tokens of piece x of tile t lie in one block: its number, the same for the whole wave, or -1.
 __device__ __forceinline__ int page_of(const ScoreArgs &a, const int32_t *row, int len, int t, int x) {
-    const int tok = t * TT + 16 * x, b = tok < len ? row[tok >> a.shift] : -1;
+    const uint32_t tok = (uint32_t)t * TT + 16 * x;  // of a tile that a wave looks ahead to, maybe past 2^31
+    const int b = tok < (uint32_t)len ? row[tok >> a.shift] : -1;
     return b >= 0 && b < a.n_blocks ? b : -1;
 }
 
@@ -256,7 +260,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) few_rows(ScoreArgs a) {
     if (c < 0) return;
     const int g0 = blockIdx.x * per;  // below 2^30 tiles
     const float mean = 1.f / a.R;
-    int len = cell_len(a, c), nt = (scored(a, c) + TT - 1) / TT;  // of cell c, whose first tile is number `at`
+    int len = cell_len(a, c), nt = tile_count(scored(a, c));  // of cell c, whose first tile is number `at`
     const auto take = [&]() -> Tile {
         int k = 0;
         if (lane == 0) k = atomicAdd(&taken, 1);
@@ -265,7 +269,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) few_rows(ScoreArgs a) {
         while (g0 + k >= at + nt) {
             at += nt;
             if (++c >= a.C) return Tile{-1, 0, 0};
-            len = cell_len(a, c), nt = (scored(a, c) + TT - 1) / TT;
+            len = cell_len(a, c), nt = tile_count(scored(a, c));
         }
         return Tile{c, g0 + k - at, len};
     };
@@ -330,7 +334,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) few_rows(ScoreArgs a) {
                 pages(next, pn);
             }
             const int tok = now.t * TT;
-            if (tok + TT > now.len - (a.T - 1)) add_weights<true>(s, l, f, hid, tok + tl, sum);
+            if (tok > now.len - (a.T - 1) - TT) add_weights<true>(s, l, f, hid, tok + tl, sum);
             else add_weights<false>(s, l, f, hid, tok + tl, sum);
             put_scores(a, now.c * a.n + tok + lane, sum, from, lane, tok + lane < now.len && tok + lane < a.n, mean, was);
         } while (z.c == cell);
@@ -357,7 +361,7 @@ __global__ void __launch_bounds__(64 * NW, DP <= 128 ? 4 : NW / 4) many_rows(Sco
     const float mean = 1.f / a.R, inv_g = 1.f / a.G;
 
     for (; c < a.C && at < g1; ++c) {
-        const int len = cell_len(a, c), n = scored(a, c), nt = (n + TT - 1) / TT;
+        const int len = cell_len(a, c), n = scored(a, c), nt = tile_count(n);
         const int t0 = max(g0 - at, 0), t1 = min(g1 - at, nt);
         at += nt > 0 ? nt + kFill : 0;
         if (t0 >= t1) continue;
@@ -440,7 +444,7 @@ __global__ void __launch_bounds__(64 * NW, DP <= 128 ? 4 : NW / 4) many_rows(Sco
                         add_weights<masked>(s, l, f, hid, t * TT + tl, sum);
                     }
                 };
-                if (t * TT + TT > full) all_rows(std::true_type());
+                if (t * TT > full - TT) all_rows(std::true_type());
                 else all_rows(std::false_type());
                 put_scores(a, out, sum, now, lane, in, mean, old);
             }
