@@ -112,8 +112,9 @@ __device__ __forceinline__ int sum_before(int v, int *red, int *total) {
     return x - v + before;
 }
 
-// Tiles of a cell; an empty one has a tile too, in which nothing is seen.
-__device__ __forceinline__ int tiles_of(int len) { return len > 0 ? (len + DT - 1) / DT : 1; }
+// Tiles of a cell; an empty one has a tile too, in which nothing is seen.  A cell may hold 2^31 - 1 tokens: the count
+// rounds up unsigned, and no token number goes past the last tile's.
+__device__ __forceinline__ int tiles_of(int len) { return len > 0 ? (int)(((uint32_t)len + DT - 1) / DT) : 1; }
 
 // This workgroup's share of the tiles [g0, g1), the cell that holds the first and that cell's first tile; false if
 // nothing is left for it.
@@ -330,7 +331,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 && DP <= (sizeof(T) == 4 ? 96
         }
         const bool more = AHEAD && t + NW < t1;
         if (more) load_keys(base + NW * DT, kpn, vpn);
-        const bool masked = base + DT > fewest || __any(vp < 0);
+        const bool masked = base > fewest - DT || __any(vp < 0);
         if (masked) {
             const int valid = vp < 0 ? 0 : len - vtok;
 #pragma unroll
@@ -420,9 +421,11 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 && DP <= (sizeof(T) == 4 ? 96
         }
         if (more) load_values(base + NW * DT, vpn);
         kp = kpn, vp = vpn;
-        const int ahead = base + 2 * NW * DT;
         kpn = vpn = -1;
-        if (AHEAD && t + 2 * NW < t1) kpn = page(ahead + 16 * (rl / 4)), vpn = page(ahead + 16 * g);
+        if (AHEAD && t + 2 * NW < t1) {
+            const int ahead = base + 2 * NW * DT;
+            kpn = page(ahead + 16 * (rl / 4)), vpn = page(ahead + 16 * g);
+        }
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {

@@ -87,3 +87,43 @@ def test_scores(tf, dtype, T, G):
             x, y = e[at].sum() / R, err[at].sum() / R
             assert abs(float(got[c, j]) - x) <= tol(x, y), (c, j)
         assert not got[c, n:].any(), c
+
+
+@pytest.mark.parametrize("dtype,T,G", [("bf16", 2, 4), ("f32", 3, 2), ("bf16", 2, 9)])
+def test_attention(tf, dtype, T, G):
+    """Two cells' weights and values, summed over each kind of token with its count.
+
+    256 workgroups of four waves share 2^25 + 2 tiles and four more for each cell, so a wave sums at most N = 2^15 + 1 of
+    them: a row's weights of a tile one by one in a lane group (16) and then to the sum, its products with the values in
+    2 MFMA for each of two (bf16) or three (float32) parts of the weights.  Each step is off by 2^-23 at most, also where
+    a product's sum is cut, not rounded.  64 more steps hold the sums inside an MFMA, over lane groups, waves and
+    workgroups, and the scalings.  A weight's argument is off as in test_gpu_scores._check; parts leave 2^-15 at most of
+    a weight in bf16."""
+    torch, fw = tf
+    print(f"attention over {LENS[0]} tokens {dtype} T={T} G={G}", flush=True)
+    cache, table, lens, K, V = _state(tf, T + G)
+    q = _queries(tf, dtype, T, G, T + G)
+    f, u = 6.0, 2.0 ** -24
+    got = fw.cache_attention(q.cuda(), cache, table, lens, scale=torch.full((len(LENS),), f, device="cuda"))
+    o, lse = (got[x].double().cpu().numpy()[0] for x in ("o", "lse"))
+    count = [torch.bincount(table[c, :n // BS], minlength=BLOCKS).cpu().numpy() for c, n in enumerate(LENS)]
+    N, parts = 2 ** 15 + 1, 2 if dtype == "bf16" else 3
+    half_step = 2.0 ** -8 if dtype == "bf16" else u
+    for c, n in enumerate(LENS):
+        for t in range(T):
+            seen = n - (T - 1 - t)
+            w = np.zeros((BLOCKS, BS)) + count[c][:, None]
+            for j in range(min(seen, n // BS * BS), max(seen, n // BS * BS)):   # the last block's, and full blocks' hidden ones
+                w[int(table[c, j // BS]), j % BS] += 1 if seen > n // BS * BS else -1
+            here = w > 0
+            k, v, w = K[here], V[here], w[here]
+            for g in range(G):
+                row = q[0, t, c * G + g].double().numpy()
+                z = f * (k @ row)
+                p = w * np.exp(z)
+                want = math.log(p.sum())
+                off = 2 * u * ((D + 4) * f * (np.abs(k) @ np.abs(row)).max() + abs(want) + 2)
+                assert abs(lse[t, c * G + g] - want) <= (N + 64) * 2.0 ** -23 + off, (c, t, g)
+                x, a = p @ v / p.sum(), p @ np.abs(v) / p.sum()
+                tol = a * (((2 * parts + 1) * N + 64) * 2.0 ** -23 + 2 * off + 2.0 ** -15)
+                assert np.all(np.abs(o[t, c * G + g] - x) <= tol + half_step * (np.abs(x) + tol)), (c, t, g)
