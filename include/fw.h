@@ -653,7 +653,10 @@ fw_status fw_cache_release(const fw_cache *cache, const fw_cells *cells, const i
  *             were: out of range or listed before; positions that do not ascend
  *             or lie outside [0, length), or offsets outside [0, n_kept]; or
  *             needs that, with those of the cells listed before, exceed the free
- *             blocks.  If offsets do not ascend all are.
+ *             blocks.  If offsets do not ascend all are.  -1: something else
+ *             wrote into the workspace during the call, parts of which waited
+ *             for others in vain; what the listed cells hold is lost, and they
+ *             are best ended (their tables, lengths and blocks are as if served)
  * A block whose tokens all stay where they are stays as it is.  Any other gets
  * the least exponent that holds its tokens' finite values, as in
  * fw_cache_store, and their codes are rounded to it (which changes a value only

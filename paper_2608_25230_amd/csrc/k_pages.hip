@@ -33,7 +33,7 @@ struct PageHead {
 
 struct PageArgs {
     int64_t C, W, n_blocks, P, n_kept, nruns, chunks;
-    int shift, bs, d, dp;
+    int shift, bs, polls, dp;
     int32_t *table, *lens, *free_list, *n_free, *shared, *refused;
     uint8_t *kc, *vc, *k_exp, *v_exp;
     const int32_t *new_len, *src, *dst, *length, *which, *kept_pos;
@@ -357,7 +357,9 @@ constexpr int kChunk = 256;  // tokens
 constexpr int kChunkShift = 8;
 constexpr int kQueues = 64;  // of keys, and as many of values
 constexpr int kApart = 64;   // counters lie in lines of their own
-constexpr int kPolls = 1 << 22;  // seconds: a wait ends also if another call overwrites the workspace, which no caller may do
+// Looks at flags before a wait is given up, seconds: a wait ends also if another call overwrites the workspace, which
+// no caller may do.  The chunk is then left unwritten and `refused` becomes -1.
+constexpr int kPolls = 1 << 22;
 
 __device__ __forceinline__ int64_t cell_of(const PageArgs &a, int64_t p) { return a.which ? a.which[p] : p; }
 __device__ __forceinline__ int64_t block0(const PageArgs &a, int64_t p) { return (a.offsets[p] >> a.shift) + p; }
@@ -730,8 +732,12 @@ __device__ __forceinline__ void move_chunks(const PageArgs &a, uint8_t *const ld
         const int64_t i0 = max(r0, (int64_t)x.y * a.bs) >> kChunkShift, i1 = min((r1 + kChunk - 1) >> kChunkShift, j);
         int polls = 0;
         for (int64_t i = i0 + tid; i < i1; i += MT)
-            while (!__hip_atomic_load(&read[t0 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) && ++polls < kPolls)
+            while (!__hip_atomic_load(&read[t0 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) && ++polls < a.polls)
                 __builtin_amdgcn_s_sleep(1);
+        if (polls >= a.polls && i0 + tid < i1) {  // in vain: what lies there may not have been read, so nothing is written
+            for (int y = 0; y < kChunk / 16; ++y) to[y] = -1;
+            a.refused[0] = -1;
+        }
     }
     __syncthreads();
     uint8_t *dst = VALUES ? a.vc : a.kc;
@@ -846,7 +852,7 @@ size_t layout(PageArgs &a, int kind, void *ws) {
 PageArgs page_args(const fw_cache &cache, const fw_cells &cells) {
     PageArgs a{};
     a.C = cells.C, a.W = cells.max_blocks, a.n_blocks = cache.n_blocks;
-    a.bs = cache.block_size, a.shift = __builtin_ctz(cache.block_size), a.d = (int)cache.d, a.dp = cache_row(cache.d);
+    a.bs = cache.block_size, a.shift = __builtin_ctz(cache.block_size), a.dp = cache_row(cache.d);
     a.table = cells.table, a.lens = cells.lens, a.free_list = cells.free_list, a.n_free = cells.n_free;
     a.shared = cells.shared;
     a.kc = cache.k, a.vc = cache.v, a.k_exp = cache.k_exp, a.v_exp = cache.v_exp;
@@ -883,11 +889,17 @@ hipError_t launch_fork(const fw_cache &cache, const fw_cells &cells, int64_t P, 
     return hipGetLastError();
 }
 
+// kPolls, but for the test that sets 0: then every wait is given up.  No part of the interface.
+extern "C" {
+int32_t fw_compact_polls = kPolls;
+}
+
 hipError_t launch_cell_compact(const fw_cache &cache, const fw_cells &cells, int64_t P, const int32_t *which,
                                const int64_t *offsets, int64_t n_kept, const int32_t *kept_pos, int32_t *refused,
                                void *ws, hipStream_t st) {
     PageArgs a = page_args(cache, cells);
     a.P = P, a.which = which, a.offsets = offsets, a.n_kept = n_kept, a.kept_pos = kept_pos, a.refused = refused;
+    a.polls = fw_compact_polls;
     layout(a, 2, ws);
     if (P > 0) hipLaunchKernelGGL(compact_check, dim3((unsigned)P), dim3(CT), 0, st, a);
     hipLaunchKernelGGL(compact_plan, dim3(1), dim3(PT), 0, st, a);

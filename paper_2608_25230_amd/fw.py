@@ -885,7 +885,7 @@ def cache_release(cache: KvCache, cells: CacheCells, new_len, *, ws=None) -> Dic
 def cache_compact(cache: KvCache, cells: CacheCells, offsets, kept_pos, *, which=None, ws=None) -> Dict[str, object]:
     """Cells which [P] int32 (None: all, or the first P) keep the tokens at kept_pos[offsets[p]:offsets[p + 1]]
     (``cache_select``, ``ragged_compact``), moved to their front; the blocks behind go back.  Returns refused [1]
-    int32."""
+    int32, -1 if something else wrote into the workspace meanwhile (the listed cells' tokens are lost then)."""
     torch = _torch()
     guard = _elsewhere("cells.table", cells.table)
     if guard is not None:
