@@ -149,6 +149,34 @@ def test_hidden_and_missing_tokens(tf):
     _check(keep, ref, 10)
 
 
+@pytest.mark.parametrize("dtype,T,G", [("bf16", 5, 2), ("f32", 5, 3), ("bf16", 5, 8), ("f32", 17, 2)])
+def test_nan_keys_reach_only_rows_that_see_them(tf, dtype, T, G):
+    """Keys of NaN among the last tokens, which some rows see and others do not: they alone score NaN.  The log-sum-exps
+    are those of the cache before, and NaN for rows that see nothing, which are not looked at."""
+    torch, fw = tf
+    rng = np.random.default_rng(T + G)
+    lens = [40, 3, 100, 20, 200, 64]
+    s = _state(rng, lens, 16, 64)
+    q, scale, lse = _inputs(tf, rng, s, dtype, 2, T, G)
+    lse[np.isneginf(lse)] = np.nan
+    assert np.isnan(lse).any()
+    bad = [(0, 37), (2, 97), (3, 19), (4, 199), (4, 196), (5, 63)]
+    for c, j in bad:
+        s["k"][s["table"][c, j // 16], j % 16, 5] = 0x7F
+    ref = O.cache_scores(q.double().numpy(), s, s["table"], s["lens"], lse, scale, 208)
+    want = np.full((6, 208), False)
+    for c, j in bad:
+        want[c, j] = True
+    for c, n in enumerate(lens):
+        assert np.array_equal(np.isnan(ref["scores"][c, :n]), want[c, :n])
+    got = fw.cache_scores(q.cuda(), _cache(tf, s), _cuda(torch, s["table"]), _cuda(torch, s["lens"]), _cuda(torch, lse),
+                          scale=_cuda(torch, scale))["scores"].cpu().numpy()
+    assert np.array_equal(np.isnan(got), want)
+    ref["err"][want] = 0
+    inside = _check(got, ref, T * G)
+    assert inside.sum() == sum(lens) - len(bad)
+
+
 def test_they_are_the_weights_of_cache_attention(tf):
     """Scores with cache_attention's lse sum to the share of rows that see something, at the sizes of a window."""
     torch, fw = tf
