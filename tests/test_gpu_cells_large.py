@@ -83,6 +83,14 @@ def test_compaction_of_long_and_many_cells(tf, lens, bs, dp):
         assert torch.equal(both.sort().values, torch.arange(n_blocks, device="cuda", dtype=torch.int32))
 
 
+@pytest.mark.parametrize("bs,dp", [(64, 192), (16, 256), (256, 256)])
+def test_compaction_of_many_wide_chunks(tf, bs, dp):
+    """More chunks than workgroups, at widths of which fewer workgroups fit the card than are launched."""
+    lens = [40000 + 77 * i for i in range(8)] + [100, 0, 1]
+    assert all(2 * (part * sum(lens) / 256) > 800 for part in (0.7, 0.7 * 0.5, 0.7 * 0.5 * 0.97))
+    test_compaction_of_long_and_many_cells(tf, lens, bs, dp)
+
+
 def test_blocks_past_32_bits(tf):
     """A cache of more than 2^32 bytes: the same scores, the same compaction, fork and release as in a small copy."""
     torch, fw = tf
