@@ -260,6 +260,56 @@ def test_blocks_that_are_none_do_no_harm(tf):
     assert len(set(free.tolist())) == len(free) and free.min() >= 0 and free.max() < len(s["shared"])
 
 
+@pytest.mark.parametrize("seed", range(4))
+def test_what_entries_out_of_range_stand_for(tf, seed):
+    """Tokens of such a block are zeros, what goes to one is lost, and it is never copied, counted or freed: as if each
+    were a block of its own, of zeros, that nobody looks at afterwards.  All other blocks hold what they then would."""
+    torch, fw = tf
+    rng = np.random.default_rng(300 + seed)
+    s = random_state(rng, [60, 60, 60, 0, 75], 16, 32, 20, W=5)
+    n = len(s["shared"])
+    bad = (0, 1, -1), (1, 2, 10 ** 8), (2, 3, -9), (4, 0, n), (4, 4, 2 ** 31 - 1)
+    t = dict(s, table=s["table"].copy())
+    more = lambda x, fill: np.concatenate([x, np.full((len(bad), *x.shape[1:]), fill, x.dtype)])
+    for key, fill in (("k", 0), ("v", 0), ("k_exp", 1), ("v_exp", 1), ("shared", 0), ("free_list", -7)):
+        t[key] = more(s[key], fill)
+    for i, (c, j, b) in enumerate(bad):
+        s["table"][c, j], t["table"][c, j] = b, n + i
+    cache, cells = _up(tf, s)
+
+    def check(want, was, r, what):
+        torch.cuda.synchronize()
+        got = _down(cache, cells)
+        assert int(r["refused"]) == want["refused"] == 0, what
+        cut = lambda x: dict(x, **{key: x[key][:n] for key in (*CACHE, "shared")})
+        free = [b for b in want["free_list"][:want["n_free"]] if b < n]
+        table = want["table"].copy()
+        for i, (_, _, b) in enumerate(bad):
+            table[table == n + i] = b
+        compare(got, dict(cut(want), table=table, free_list=np.array(free), n_free=len(free)), cut(was), what)
+
+    def again(x):
+        """The stand-ins as the next call would read them: zeros, none of them free or shared."""
+        free = [b for b in x["free_list"][:x["n_free"]] if b < n]
+        x = dict(x, free_list=np.array(free + [-7] * (n + len(bad) - len(free)), np.int32), n_free=len(free))
+        for key, fill in (("k", 0), ("v", 0), ("k_exp", 1), ("v_exp", 1), ("shared", 0)):
+            x[key][n:] = fill
+        return x
+
+    off, pos = _some(rng, s, [0, 2, 4], 0.5, 0.0)
+    r = fw.cache_compact(cache, cells, _cuda(torch, off, torch.int64), _i32(torch, pos), which=_i32(torch, [0, 2, 4]))
+    a = O.compact(t, off, pos, [0, 2, 4])
+    check(a, t, r, "compact")
+    r = fw.cache_fork(cache, cells, _i32(torch, [1]), _i32(torch, [3]))
+    a = again(a)
+    b = O.fork(a, [1], [3])
+    check(b, a, r, "fork")
+    end = [3, 20, 50, 33, 17]
+    r = fw.cache_release(cache, cells, _i32(torch, end))
+    b = again(b)
+    check(O.release(b, end), b, r, "release")
+
+
 def test_the_loop_as_it_is_used(tf):
     """A prompt's keys turn, are stored, attended and scored; the cells are compacted, forked, grow and end."""
     torch, fw = tf
