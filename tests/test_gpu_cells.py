@@ -396,6 +396,55 @@ def test_captured(tf):
         fw.cache_release(cache, cells, _i32(torch, [9999, 9999, 0, 0]))
 
 
+def test_captured_and_replayed_on_other_states(tf):
+    """A step that forks, compacts and releases, captured once and replayed on other lengths, tables, codes, exponents,
+    pairs and positions, some of which are refused."""
+    torch, fw = tf
+    rng = np.random.default_rng(16)
+    dims = dict(bs=16, dp=32, d=20, W=8, n_blocks=30)
+    plan = [([100, 80, 0, 0], [0, 1], [2, 3], [2, 3], [9999, 9999, 0, 0]),
+            ([64, 17, 0, 0], [1, 0], [2, 3], [3, 2], [20, 9999, 5, 16]),
+            ([120, 128, 0, 9], [0, 1], [2, 3], [2, 0], [64, 33, 9999, 0]),       # the second pair's cell holds tokens
+            ([31, 100, 0, 0], [0, 0], [2, 2], [1, 2], [0, 48, 9999, 7]),         # one cell twice
+            ([100, 80, 0, 0], [1, 5], [3, 2], [3, 3], [99, 80, 0, 11])]          # a cell that is none, a cell listed twice
+    make = lambda lens: random_state(rng, lens, dims["bs"], dims["dp"], dims["d"], W=dims["W"], n_blocks=dims["n_blocks"])
+    s = make(plan[0][0])
+    cache, cells = _up(tf, s)
+    arrays = dict(zip(CACHE, cache[:4]), table=cells.table, lens=cells.lens, free_list=cells.free_list, shared=cells.shared)
+    src, dst, which, end = (_i32(torch, x) for x in plan[0][1:])
+    off, pos = _cuda(torch, [0, 30, 55], torch.int64), _i32(torch, [*range(3, 93, 3), *range(0, 75, 3)])
+
+    def step():
+        return (fw.cache_fork(cache, cells, src, dst), fw.cache_compact(cache, cells, off, pos, which=which),
+                fw.cache_release(cache, cells, end))
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    refusals = 0
+    for i, (lens, *now) in enumerate(plan + plan[::-1]):
+        s = make(lens)
+        for key, x in arrays.items():
+            x.copy_(_cuda(torch, s[key]))
+        cells.n_free.fill_(s["n_free"])
+        for x, y in zip((src, dst, which, end), now):
+            x.copy_(_i32(torch, y))
+        a = O.fork(s, *now[:2])
+        cut = int(rng.integers(20, 36))
+        kept = [sorted(rng.permutation(max(m, int(a["lens"][c])))[:m].tolist()) for c, m in zip(now[2], (cut, 55 - cut))]
+        off.copy_(_cuda(torch, [0, cut, 55]))
+        pos.copy_(_i32(torch, kept[0] + kept[1]))
+        g.replay()
+        torch.cuda.synchronize()
+        b = O.compact(a, [0, cut, 55], kept[0] + kept[1], now[2])
+        c = O.release(b, now[3])
+        compare(_down(cache, cells), c, s, f"replay {i}")
+        assert [int(x["refused"]) for x in out] == [x["refused"] for x in (a, b, c)], i
+        refusals += a["refused"] + b["refused"] + c["refused"]
+    assert refusals
+
+
 @pytest.mark.parametrize("off", [[0, 256 * 10 ** 6, 256 * 10 ** 6, 256 * 10 ** 6], [0, 2, 2 ** 33, 2 ** 40], [-2 ** 62, -2 ** 40, -7, -1],
                                  [-2 ** 50, 0, 2, 4], [2 ** 62] * 4, [1, 2, 4, 4], [4, 4, 4, 4], [0, 1, 300000, 300001]])
 def test_offsets_out_of_range(tf, off):
