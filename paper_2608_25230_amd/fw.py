@@ -679,14 +679,14 @@ def rotate_heads(q, k, positions, freq, *, eps=None, q_weight=None, k_weight=Non
             raise FwError(2, f"k must be [{T}][Hkv][{d}], got {tuple(k.shape)}")
         k_row, k_head, _ = k.stride()
     rot = 0
+    if (freq is None) != (positions is None):
+        raise FwError(2, "positions and freq go together")
     if freq is not None:
         _want("freq", freq, torch.float32, 1, dev)
         _want("positions", positions, torch.int64, 1, dev)
         rot = 2 * freq.shape[0]
         if positions.shape[0] != T:
             raise FwError(2, f"positions must be [{T}], got {tuple(positions.shape)}")
-    elif positions is not None:
-        raise FwError(2, "positions need freq")
     w_code = 0
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is None:

@@ -203,3 +203,14 @@ def test_refusals(tf):
               lambda: fw.rotate_heads(q, None, pos.cpu(), freq)):
         with pytest.raises(fw.FwError):
             f()
+
+
+def test_positions_and_freq_go_together(tf):
+    torch, fw = tf
+    q = torch.randn(6, 3, 64, device="cuda")
+    pos, freq = torch.arange(6, device="cuda"), torch.rand(32, device="cuda")
+    for given in ((pos, None), (None, freq)):
+        with pytest.raises(fw.FwError) as e:
+            fw.rotate_heads(q, None, *given)
+        assert e.value.status == 2
+    assert torch.equal(fw.rotate_heads(q, None, None, None)["q"], q)
