@@ -532,8 +532,9 @@ typedef struct fw_heads {
 /* ---------------------------------------------------------------------------
  * fw_rotate_heads -- norms and turns every head's row: pair (x, y) of angle
  * a = pos * freq becomes (x cos a - y sin a, y cos a + x sin a).  Angles are
- * reduced in float64 (less than 2^-50 of the angle is lost), rows computed in
- * float32 (their squares too) and rounded once.
+ * reduced in float64 (less than 2^-50 of the angle is lost), what is left of them,
+ * at most half a turn, rounded to float32, rows computed in float32 (their squares
+ * too) and rounded once.
  *   q_out, k_out  rows of the same type, strides qo_row .. ko_head; either may
  *                 be its own input with its strides (in place), and meets
  *                 nothing else that the call reads or writes.  Rows of an output
