@@ -396,6 +396,21 @@ def test_captured(tf):
         fw.cache_release(cache, cells, _i32(torch, [9999, 9999, 0, 0]))
 
 
+@pytest.mark.parametrize("more", [1, 300, 200000])
+def test_more_room_than_is_kept(tf, more):
+    """kept_pos as cache_select leaves it where n_kept is an upper bound: -1 behind the last cell's, here also before the
+    first one's."""
+    rng = np.random.default_rng(17)
+    s = random_state(rng, [600, 0, 33, 280, 0], 16, 32, 20, n_blocks=70)
+    s = _fork(tf, s, [0], [4])
+    off, pos = _some(rng, s, range(5), 0.6, 0.0)
+    for before in (0, more):
+        _compact(tf, s, [before + x for x in off], [-1] * before + pos + [-1] * more)
+    which = [4, 2]
+    off, pos = _some(rng, s, which, 0.6, 0.0)
+    _compact(tf, s, off, pos + [-1] * more, which)
+
+
 def test_captured_and_replayed_on_other_states(tf):
     """A step that forks, compacts and releases, captured once and replayed on other lengths, tables, codes, exponents,
     pairs and positions, some of which are refused."""
