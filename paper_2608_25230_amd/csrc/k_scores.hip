@@ -27,7 +27,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // Cells differ in length, so the work is cut by length, on the device: all
 // cells' tiles of 64 tokens in a row, the same number to each workgroup.  A
 // cell's first share costs more than its tiles, which many_rows counts in
-// (kFill).
+// (kFill).  Its time goes by rounds of a tile for each wave, not by tiles, which
+// cells of a few thousand tokens feel: 64 of 4000, 128 rows, are shares of 9 tiles
+// for 8 waves (26 us; its products alone 6).
 //
 // few_rows, up to 16 rows a cell: a wave holds them in registers; keys are loaded
 // a tile ahead.  Memory bounds it: 512 cells of 3000 to 30000 tokens of 128
@@ -495,7 +497,9 @@ hipError_t launch_scores_width(ScoreArgs &a, hipStream_t st) {
 // tokens above and at the key come to is read off its histogram of the last
 // digit, so each slice finds its place from those of the slices before it.  (8
 // cells of 131072: 27 us, by one workgroup each 187.  Slices for shorter rows too:
-// 8 cells of 30000 25 us instead of 17, 256 of them 57 instead of 20.)
+// 8 cells of 30000 25 us instead of 17, 256 of them 57 instead of 20.)  The row's
+// width decides, since lengths are on the device: 256 cells of 3000 tokens take 135
+// us in rows of 131072 and 11 in rows of 3000.
 // ---------------------------------------------------------------------------
 constexpr int LT = 1024;          // threads of a workgroup; fewer for short rows
 constexpr int kBins = 2048;
